@@ -27,6 +27,11 @@
  *     before that kernel has completed, so stream order holds as for a plain launch.  The
  *     environment variable PATCONV_PDL=0 (read once) makes every launch a plain one.
  *
+ * The training side (pp_group_norm, pp_tensors_*, pp_grad_norm, pp_adamw_step) serves the masked
+ * retraining of a pruned network between its convolutions and after its backward pass; its
+ * activations are channels last, as training libraries keep them for convolutions, and its kernels
+ * are plain launches.
+ *
  * Thread safety: a handle is immutable after pp_pack/pp_bind_device, so pp_conv on one handle
  * may be called from several host threads and streams at once.
  */
@@ -61,7 +66,8 @@ typedef enum {
     PP_ERR_PATH = -14         /* the layer's kernel does not offer the requested fusion        */
 } pp_status;
 
-typedef enum { PP_F32 = 0, PP_F16 = 1 } pp_dtype;
+/* PP_BF16: the training side only; pp_conv and its variants answer PP_ERR_DTYPE. */
+typedef enum { PP_F32 = 0, PP_F16 = 1, PP_BF16 = 2 } pp_dtype;
 
 /* Sections of a packed layer (pp_export).  Byte layouts:
  *   HEADER u32[16]: 'PPK1' (0x314B5050), version 1, Cout, Cin_g, groups, stride, n_patterns,
@@ -320,6 +326,121 @@ int pp_debug_inject_timeout(void);
 
 /* Release the handle's host memory (the bound device image stays the caller's).  NULL is OK. */
 int pp_destroy(pp_handle h);
+
+/* ------------------------------------------------------------------------------------------------
+ * Group norm with its activation, channels last (the paper's networks are trained with normalisation
+ * between their convolutions; which one is left open there). */
+
+typedef enum { PP_ACT_NONE = 0, PP_ACT_RELU = 1, PP_ACT_SILU = 2 } pp_act;
+
+/* y = act(gamma_c (x - mean) rstd + beta_c): mean and variance over the C / G channels of a group and
+ * all pixels of a sample, rstd = 1 / sqrt(variance + eps), the variance that of the values themselves
+ * (divided by their count); act the identity, max(z, 0) or z / (1 + exp(-z)).
+ *   x          DEVICE [N][pixels][C] of `dtype` (PP_F32, PP_F16, PP_BF16): channels adjacent, pixels
+ *              x_pixel >= C elements apart, samples x_sample elements (0: the same sample again);
+ *   gamma, beta  DEVICE fp32 [C], or NULL (ones, zeros);   eps >= 0;
+ *   y          DEVICE, dense [N][pixels][C]; may be x itself where that is dense, else must not overlap;
+ *   mean, rstd DEVICE fp32 [N][G], kept for the backward pass, or NULL;
+ *   workspace  DEVICE, 16-byte aligned, pp_group_norm_workspace_size bytes (backward 0).
+ * Sums are fp32, joined as means and squared distances, in a fixed order: the same inputs and strides
+ * give the same bits.  A NaN or an infinity makes its own group NaN.  Pointers need element alignment
+ * only; 16-byte aligned addresses and strides are fastest.  N == 0 or pixels == 0 is a no-op.  Never
+ * synchronises.  Errors: PP_ERR_NULL, _SHAPE (C not a multiple of G, N above 65534, strides), _ALIGN,
+ * _DTYPE, _BUFFER (workspace too small, overlap), _ARG (act, eps), _CUDA. */
+int pp_group_norm(const void* x, int64_t x_pixel, int64_t x_sample, int dtype, int N, int64_t pixels, int C, int G,
+                  const float* gamma, const float* beta, float eps, int act, void* y, float* mean, float* rstd,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gradients of pp_group_norm: with dz = dy act'(z), dbeta = sum of dz and dgamma = sum of dz xh over
+ * samples and pixels (fp32 [C], either may be NULL), and dx, dense [N][pixels][C] of `dtype` (may be dy
+ * itself where that is dense).  dy has strides of its own, as x; mean and rstd are the forward pass's.
+ * At z = 0 the ReLU's slope is 0.  Workspace with backward 1.  N == 0 or pixels == 0: dgamma and dbeta
+ * become zero.  Otherwise as pp_group_norm. */
+int pp_group_norm_backward(const void* dy, int64_t dy_pixel, int64_t dy_sample, const void* x, int64_t x_pixel,
+                           int64_t x_sample, int dtype, int N, int64_t pixels, int C, int G, const float* gamma,
+                           const float* beta, const float* mean, const float* rstd, int act, void* dx, float* dgamma,
+                           float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of pp_group_norm (backward 0) or pp_group_norm_backward (1).  Host-only. */
+int pp_group_norm_workspace_size(int dtype, int N, int64_t pixels, int C, int G, int backward, size_t* bytes);
+
+/* ------------------------------------------------------------------------------------------------
+ * Many tensors at once: the gradients' norm and AdamW steps of masked retraining (the paper's
+ * retraining updates the kept weights alone; which optimiser does is left open there). */
+
+typedef struct pp_tensors* pp_tensors_handle;
+
+typedef enum {
+    PP_TQ_COUNT = 0,            /* tensors                                                        */
+    PP_TQ_TABLE_BYTES = 1,      /* device bytes pp_tensors_bind needs                             */
+    PP_TQ_STATE_ELEMENTS = 2,   /* elements of each of the states m and v                         */
+    PP_TQ_STATE_OFFSET = 16     /* + tensor: its first element in the states                      */
+} pp_tensors_key;
+
+#define PP_STATE_BLOCK 256      /* elements that share a scale; a tensor's states start at a multiple */
+
+/* Describe n tensors.  All arrays are HOST arrays of n values, read during the call only; the
+ * addresses in them are DEVICE memory that the caller keeps alive while the handle is used.
+ *   numel        elements of each tensor, 0 and up;
+ *   grad_dtypes  pp_dtype of each tensor's gradient;
+ *   taps         NULL, or per tensor NULL (every element is kept) or 9-bit masks (int16 or uint16)
+ *                of the taps kept of each consecutive group of nine elements -- a contiguous
+ *                [Cout][Cin/groups][3][3] tensor's kernels, bit t = raster tap t, 0 a kernel that is
+ *                pruned away; numel must be a multiple of 9;
+ *   params       NULL (a handle for pp_grad_norm only) or fp32 parameters;
+ *   copies       NULL, or per tensor NULL or a copy of the parameters in copy_dtype (PP_F16,
+ *                PP_BF16) that each step writes beside them, rounded to nearest;
+ *   decay        NULL (zeros) or the weight decay of each tensor.
+ * Host-only.  Errors: PP_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _ARG (decay not finite), _ALLOC. */
+int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const uint16_t* const* taps,
+                      float* const* params, void* const* copies, int copy_dtype, const float* decay,
+                      pp_tensors_handle* out);
+
+/* Read one property (pp_tensors_key).  Errors: PP_ERR_NULL, PP_ERR_ARG. */
+int pp_tensors_query(pp_tensors_handle h, int key, int64_t* value);
+
+/* Copy the handle's tables (and the norm's scratch, zeroed) into caller-owned DEVICE memory (256-byte
+ * aligned, >= PP_TQ_TABLE_BYTES bytes) on `stream`.  The caller keeps it alive while the handle is
+ * used and orders the copy before the first call.
+ * Errors: PP_ERR_NULL, _BUFFER (too small), _ALIGN, _CUDA. */
+int pp_tensors_bind(pp_tensors_handle h, void* dev, size_t bytes, void* stream);
+
+/* Release the handle.  NULL is OK. */
+int pp_tensors_destroy(pp_tensors_handle h);
+
+/* out[0] = the root of the sum of squares of all kept gradients, out[1] = min(1, max_norm / (out[0] +
+ * 1e-6)), the factor that clips them; NaN where a kept gradient is NaN.
+ *   grads     HOST array of the gradients' DEVICE addresses (element aligned, of the handle's types);
+ *             NULL: that tensor has none this time;
+ *   max_norm  above 0 (infinity: no clipping);   out  DEVICE fp32[2].
+ * Sums are fp32 over a few hundred squares and 64 bits from there, in a fixed order: the same inputs
+ * give the same bits.  The scratch is the handle's: order calls on one handle.  Never synchronises.
+ * Errors: PP_ERR_NULL, _NOT_BOUND, _ALIGN, _ARG, _CUDA. */
+int pp_grad_norm(pp_tensors_handle h, const void* const* grads, double max_norm, float* out, void* stream);
+
+/* One AdamW step (decoupled weight decay) on all tensors: for every kept element, with g its gradient
+ * times *grad_scale,
+ *     m = beta1 m + (1 - beta1) g,    v = beta2 v + (1 - beta2) g^2,
+ *     p = p (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
+ * An element that the masks leave out keeps its parameter, whatever its gradient holds, NaN included.
+ *   grads       as for pp_grad_norm; a tensor without a gradient is left alone, states and all;
+ *   state_bits  32: m and v are DEVICE fp32, PP_TQ_STATE_ELEMENTS each, a tensor's from
+ *               PP_TQ_STATE_OFFSET + tensor on;  8: they are 8-bit floats (1 sign, 4 exponent, 3
+ *               mantissa bits; 448 the largest, 0x7F NaN), and m_scale and v_scale DEVICE fp32 hold a
+ *               power of two for every PP_STATE_BLOCK of them.  Both 32-byte aligned; zeros to begin
+ *               with (scales any), and zero wherever an element is left out or beyond its tensor;
+ *   step        1 for the first step;   grad_scale  DEVICE fp32[1] or NULL (1);
+ *   seed        8-bit states only.  A new state is rounded to one of its two neighbours, up with a
+ *               probability equal to its distance from the lower one: to the nearest, a second moment
+ *               that shrinks by a thousandth a step would never move, codes being a sixteenth to an
+ *               eighth apart.  The dither is a hash of seed, step and the element's place: the same
+ *               arguments give the same bits.  A v above zero is never stored as zero, what is not
+ *               finite is stored as NaN, and the parameter's step uses m and v before the rounding.
+ * Never synchronises; a captured step replays with the captured step number and addresses.
+ * Errors: PP_ERR_NULL, _NOT_BOUND (no table, or no params), _ALIGN, _ARG, _CUDA. */
+int pp_adamw_step(pp_tensors_handle h, const void* const* grads, int state_bits, void* m, void* v, float* m_scale,
+                  float* v_scale, double lr, double beta1, double beta2, double eps, int64_t step, uint32_t seed,
+                  const float* grad_scale, void* stream);
 
 /* Static English text for a status code. */
 const char* pp_status_string(int status);

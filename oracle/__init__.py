@@ -16,6 +16,8 @@ Plain, slow, obviously-correct numpy in IEEE float64:
                    the projected weights with the zeros in place, and the normalised error metric.
 * ``admm``      -- the layer-wise ADMM pruning of Algorithm 1 (§4.3-4.5, Eq. 4-7) with a hand-written
                    gradient, for the training-side module of the library.
+* ``train``     -- group norm with its activation, the gradients' norm and AdamW steps with fp32 and
+                   8-bit states, for the kernels of masked retraining, with bounds of fp32 errors.
 
 Every function is pinned by ``tests/test_oracle_*.py`` against something other than itself:
 brute-force enumeration, torch's CPU convolution, hand-computed fixtures under
@@ -25,4 +27,4 @@ weights from the sections; its byte-level encoding itself is a specification of 
 not a result the paper prints ("parity unpinned" against the paper for the byte encoding).
 """
 
-from . import admm, conv, layout, patterns, project  # noqa: F401
+from . import admm, conv, layout, patterns, project, train  # noqa: F401

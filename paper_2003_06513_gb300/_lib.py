@@ -12,6 +12,7 @@ import threading
 from . import build as _build
 
 _c_int, _c_void_p, _c_size_t = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+_c_i64, _c_double, _c_float = ctypes.c_int64, ctypes.c_double, ctypes.c_float
 
 # name -> (restype, argtypes); the exported symbols of include/patconv.h
 SIGNATURES = {
@@ -48,6 +49,26 @@ SIGNATURES = {
     "pp_maxpool2x2": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, _c_int, _c_int, _c_void_p,
                                _c_void_p]),
     "pp_device_status": (_c_int, [_c_int, ctypes.POINTER(ctypes.c_uint)]),
+    "pp_group_norm": (_c_int, [_c_void_p, _c_i64, _c_i64, _c_int, _c_int, _c_i64, _c_int, _c_int,
+                               _c_void_p, _c_void_p, _c_float, _c_int, _c_void_p, _c_void_p, _c_void_p,
+                               _c_void_p, _c_size_t, _c_void_p]),
+    "pp_group_norm_backward": (_c_int, [_c_void_p, _c_i64, _c_i64, _c_void_p, _c_i64, _c_i64, _c_int,
+                                        _c_int, _c_i64, _c_int, _c_int, _c_void_p, _c_void_p, _c_void_p,
+                                        _c_void_p, _c_int, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+                                        _c_size_t, _c_void_p]),
+    "pp_group_norm_workspace_size": (_c_int, [_c_int, _c_int, _c_i64, _c_int, _c_int, _c_int,
+                                              ctypes.POINTER(_c_size_t)]),
+    "pp_tensors_create": (_c_int, [_c_int, ctypes.POINTER(_c_i64), ctypes.POINTER(_c_int),
+                                   ctypes.POINTER(_c_void_p), ctypes.POINTER(_c_void_p),
+                                   ctypes.POINTER(_c_void_p), _c_int, ctypes.POINTER(_c_float),
+                                   ctypes.POINTER(_c_void_p)]),
+    "pp_tensors_query": (_c_int, [_c_void_p, _c_int, ctypes.POINTER(_c_i64)]),
+    "pp_tensors_bind": (_c_int, [_c_void_p, _c_void_p, _c_size_t, _c_void_p]),
+    "pp_tensors_destroy": (_c_int, [_c_void_p]),
+    "pp_grad_norm": (_c_int, [_c_void_p, ctypes.POINTER(_c_void_p), _c_double, _c_void_p, _c_void_p]),
+    "pp_adamw_step": (_c_int, [_c_void_p, ctypes.POINTER(_c_void_p), _c_int, _c_void_p, _c_void_p,
+                               _c_void_p, _c_void_p, _c_double, _c_double, _c_double, _c_double,
+                               _c_i64, ctypes.c_uint32, _c_void_p, _c_void_p]),
     "pp_destroy": (_c_int, [_c_void_p]),
     "pp_status_string": (ctypes.c_char_p, [_c_int]),
 }

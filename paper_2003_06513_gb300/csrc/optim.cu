@@ -1,0 +1,625 @@
+// Operators over many tensors at once, for masked retraining: the gradients' norm and AdamW steps.
+//
+// The tensors are cut into chunks of kChunk elements; a table in device memory, built once, says which
+// tensor a chunk belongs to and where that tensor's parameters, states and tap masks are.  The
+// gradients' addresses change from step to step and travel as kernel arguments, so that a step is one
+// launch however many tensors there are (of up to kMaxGrads; a launch for each kMaxGrads beyond).
+//
+// A tap mask is the packer's own form: nine bits for each 3x3 kernel.  An element that its mask leaves
+// out takes no part: its gradient is not used, whatever it is, and its parameter stays.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "patconv.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlock = 256;               // elements that share a scale: a warp's, eight a lane
+constexpr int kChunk = kThreads * 8;      // elements of a chunk: a CTA's, eight a thread
+constexpr int kFewGrads = 64, kMaxGrads = 448;   // 448 addresses and the rest are below 4 KB of arguments
+constexpr int64_t kMaxNumel = int64_t(1) << 40;
+
+struct TensorEntry {                      // of the device table
+    float* param;
+    void* copy;
+    const uint16_t* taps;
+    int64_t numel;
+    int64_t state;                        // first element in the states
+    float decay;
+    int grad_dtype;
+};
+
+struct ChunkEntry {
+    uint32_t tensor, index;
+};
+
+template <int N>
+struct Grads {
+    const void* at[N];
+};
+
+}  // namespace
+
+struct pp_tensors {
+    std::vector<TensorEntry> tensors;
+    std::vector<uint32_t> first_chunk;    // per tensor, and the number of all chunks
+    std::vector<uint8_t> image;           // tensors | chunks | counter and partial sums (zero)
+    size_t off_chunks = 0, off_sums = 0;
+    int64_t state_elements = 0;
+    int copy_dtype = PP_F16;
+    bool has_params = false;
+    unsigned char* dev = nullptr;
+};
+
+namespace {
+
+constexpr int kSumCtas = 1024;            // most CTAs of the norm's kernel: partial sums
+
+struct Vec8 {
+    float v[8];
+};
+
+__device__ __forceinline__ Vec8 load8(const float* p) {
+    Vec8 r;
+    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(r.v[0]), "=f"(r.v[1]), "=f"(r.v[2]), "=f"(r.v[3]), "=f"(r.v[4]), "=f"(r.v[5]), "=f"(r.v[6]),
+                   "=f"(r.v[7])
+                 : "l"(p)
+                 : "memory");
+    return r;
+}
+__device__ __forceinline__ void store8(float* p, const Vec8& r) {
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(r.v[0]), "f"(r.v[1]), "f"(r.v[2]),
+                 "f"(r.v[3]), "f"(r.v[4]), "f"(r.v[5]), "f"(r.v[6]), "f"(r.v[7])
+                 : "memory");
+}
+__device__ __forceinline__ float2 widen(uint32_t w, int dtype) {
+    if (dtype == PP_F16) {
+        __half2 h;
+        memcpy(&h, &w, 4);
+        return __half22float2(h);
+    }
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ float widen1(const void* p, int64_t i, int dtype) {
+    if (dtype == PP_F32) return static_cast<const float*>(p)[i];
+    const uint16_t w = static_cast<const uint16_t*>(p)[i];
+    return widen(w, dtype).x;
+}
+__device__ __forceinline__ uint16_t narrow1(float f, int dtype) {
+    if (dtype == PP_F16) return __half_as_ushort(__float2half_rn(f));
+    return __bfloat16_as_ushort(__float2bfloat16_rn(f));
+}
+
+// eight gradients from element e; n of them are in the tensor (the others read as zero)
+__device__ __forceinline__ Vec8 load_grad(const void* g, int dtype, int64_t e, int n, bool wide) {
+    Vec8 r;
+    if (wide && n == 8) {
+        if (dtype == PP_F32) return load8(static_cast<const float*>(g) + e);
+        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(g) + e));
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = widen(u[i], dtype);
+            r.v[2 * i] = f.x;
+            r.v[2 * i + 1] = f.y;
+        }
+        return r;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = i < n ? widen1(g, e + i, dtype) : 0.0f;
+    return r;
+}
+// whether eight-element accesses from a tensor's start are aligned
+__device__ __forceinline__ bool wide_grad(const void* g, int dtype) {
+    return (reinterpret_cast<uintptr_t>(g) & (dtype == PP_F32 ? 31 : 15)) == 0;
+}
+
+// Which of the eight elements from `lane_e` elements past the chunk's start take part: in the tensor
+// (n of them) and kept by its mask.  Eight elements touch two 3x3 kernels at most.
+__device__ __forceinline__ uint32_t kept8(const TensorEntry& t, int64_t chunk_e, int lane_e, int n) {
+    if (n <= 0) return 0;
+    const uint32_t in = n >= 8 ? 0xFFu : (1u << n) - 1;
+    if (!t.taps) return in;
+    const int64_t k0 = chunk_e / 9;
+    const uint32_t local = (uint32_t)(chunk_e - 9 * k0) + (uint32_t)lane_e;
+    const int64_t k = k0 + local / 9;
+    const uint32_t r = local % 9;
+    const uint32_t a = t.taps[k] & 0x1FFu;
+    const uint32_t b = 9 * (k + 1) < t.numel ? t.taps[k + 1] & 0x1FFu : 0;
+    return ((a | b << 9) >> r) & in;
+}
+
+// ------------------------------------------------------------------------------------- the norm
+
+// Sum over a CTA's chunks of (g f)^2 for one of three factors f; per thread in fp32 over at most a few
+// hundred squares, then over the CTA.
+template <int N>
+__device__ float chunk_squares(const TensorEntry* tensors, const ChunkEntry* chunks, uint32_t begin, uint32_t end,
+                               uint32_t t0, const Grads<N>& grads, float factor, float* smem) {
+    float sum = 0.0f;
+    for (uint32_t c = begin + blockIdx.x; c < end; c += gridDim.x) {
+        const ChunkEntry ce = chunks[c];
+        const void* g = grads.at[ce.tensor - t0];
+        if (!g) continue;
+        const TensorEntry t = tensors[ce.tensor];
+        const int64_t e0 = (int64_t)ce.index * kChunk;
+        const int le = threadIdx.x * 8;
+        const int64_t left = t.numel - e0 - le;
+        const int n = left < 8 ? (int)(left > 0 ? left : 0) : 8;
+        const uint32_t keep = kept8(t, e0, le, n);
+        if (!keep) continue;
+        const Vec8 v = load_grad(g, t.grad_dtype, e0 + le, n, wide_grad(g, t.grad_dtype));
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = keep >> i & 1 ? v.v[i] * factor : 0.0f;
+            s = fmaf(x, x, s);
+        }
+        sum += s;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) smem[threadIdx.x / 32] = sum;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) sum += smem[i];
+    return sum;
+}
+
+// Partial sums of squares, one a CTA, and in the last CTA to finish of the call's last launch their sum
+// in 64 bits, the norm and the clip factor.  Squares that leave fp32's range (a sum below 2^-80, where
+// they may have been rounded away, or above 2^120) are summed again with the gradients times 2^64 or
+// 2^-64, so that the norm holds over fp32's whole range of gradients.
+template <int N>
+__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
+                                                             uint32_t begin, uint32_t end, uint32_t t0, Grads<N> grads,
+                                                             double* sums, unsigned* counter, unsigned first_sum,
+                                                             unsigned all_sums, float max_norm, float* out) {
+    __shared__ float smem[kThreads / 32];
+    __shared__ double dsum[kThreads];
+    __shared__ bool last;
+    float s = chunk_squares(tensors, chunks, begin, end, t0, grads, 1.0f, smem);
+    double total = s;
+    if (!(s >= 0x1p-80f && s <= 0x1p120f)) {      // uniform over the CTA
+        const bool small = s < 0x1p-80f;
+        s = chunk_squares(tensors, chunks, begin, end, t0, grads, small ? 0x1p64f : 0x1p-64f, smem);
+        total = (double)s * (small ? 0x1p-128 : 0x1p128);
+    }
+    if (threadIdx.x == 0) {
+        sums[first_sum + blockIdx.x] = total;
+        __threadfence();
+        last = atomicAdd(counter, 1) == all_sums - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double d = 0.0;
+    for (unsigned i = threadIdx.x; i < all_sums; i += kThreads) d += __ldcg(sums + i);
+    dsum[threadIdx.x] = d;
+    __syncthreads();
+    for (int o = kThreads / 2; o; o >>= 1) {
+        if (threadIdx.x < o) dsum[threadIdx.x] += dsum[threadIdx.x + o];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        const float norm = (float)sqrt(dsum[0]);
+        const float f = max_norm / (norm + 1e-6f);
+        out[0] = norm;
+        out[1] = f > 1.0f ? 1.0f : f;             // NaN stays NaN
+        *counter = 0;                             // for the next call
+    }
+}
+
+// ------------------------------------------------------------------------------------- AdamW
+
+struct AdamArgs {
+    float lr, step_size, b1, b2, c1, c2, inv_bc2, eps;   // step_size = lr / (1 - b1^t), c = 1 - b
+    uint32_t key;
+    int copy_dtype;
+    const float* grad_scale;
+    void *m, *v;
+    float *m_scale, *v_scale;
+};
+
+__device__ __forceinline__ float approx_sqrt(float x) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// The states' arithmetic rounds every product and sum by itself: an 8-bit state then depends on the
+// formula alone and not on how a compiler contracts it.
+__device__ __forceinline__ void moments(float g, float& m, float& v, const AdamArgs& a) {
+    m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.c1));
+    v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.c2));
+}
+__device__ __forceinline__ float stepped(float p, float m, float v, float shrink, const AdamArgs& a) {
+    const float den = approx_sqrt(v * a.inv_bc2) + a.eps;
+    return fmaf(-a.step_size, __fdividef(m, den), p * shrink);
+}
+
+__host__ __device__ inline uint32_t mix(uint32_t x) {
+    x ^= x >> 16;
+    x *= 0xCBBB9D5Du;
+    x ^= x >> 15;
+    x *= 0x629A292Bu;
+    return x ^ x >> 16;
+}
+
+// A block's scale: the power of two that brings its largest magnitude into (224, 448], e4m3's top.
+__device__ __forceinline__ float block_scale(uint32_t largest) {
+    if (!largest) return 1.0f;
+    const int field = (int)((largest + 0x1FFFFFu) >> 23) - 8;    // 1.75 2^k and below have exponent k
+    return __uint_as_float((uint32_t)(field < 1 ? 1 : field) << 23);
+}
+
+// A value over its block's scale, rounded to one of its two neighbours in e4m3 by the dither r (16
+// bits): the bits below the format's three are filled up by the dither and cut off.  Below 2^-6 the
+// format's grid is that of [2^-6, 2^-5), so 2^-6 is added for the cut.
+template <bool POSITIVE>
+__device__ __forceinline__ float rounded(float t, uint32_t r) {
+    const float a = fabsf(t);
+    const float small = a < 0x1p-6f ? 0x1p-6f : 0.0f;
+    float w = __uint_as_float((__float_as_uint(__fadd_rn(a, small)) + (r << 4) + 8) & 0xFFF00000u) - small;
+    if (POSITIVE && a > 0.0f) w = fmaxf(w, 0x1p-9f);              // a second moment is not lost
+    if (!(a < INFINITY)) w = NAN;
+    return copysignf(w, t);
+}
+
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+}
+__device__ __forceinline__ void unpack4(uint32_t w, float scale, float* out) {
+    const __half2 a = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3));
+    const __half2 b = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3));
+    const float2 x = __half22float2(a), y = __half22float2(b);
+    out[0] = x.x * scale;
+    out[1] = x.y * scale;
+    out[2] = y.x * scale;
+    out[3] = y.y * scale;
+}
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
+    return b < 0x7F800000u ? b : 0;
+}
+
+// One chunk a CTA, one block of 256 elements a warp, eight consecutive elements a lane: what a lane
+// reads and writes of an fp32 tensor is one 32-byte sector, which is skipped where the mask keeps none
+// of its eight elements.
+template <int BITS, int N>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
+                                                         uint32_t begin, uint32_t t0, Grads<N> grads, AdamArgs a) {
+    const ChunkEntry ce = chunks[begin + blockIdx.x];
+    const void* gp = grads.at[ce.tensor - t0];
+    if (!gp) return;                               // a tensor without a gradient is left alone
+    const TensorEntry t = tensors[ce.tensor];
+    const int64_t e0 = (int64_t)ce.index * kChunk;
+    const int le = threadIdx.x * 8;
+    if (BITS == 8 && e0 + (le & ~(kBlock - 1)) >= t.numel) return;   // whole warps
+    const int64_t e = e0 + le, left = t.numel - e;
+    const int n = left < 8 ? (int)(left > 0 ? left : 0) : 8;
+    const uint32_t keep = kept8(t, e0, le, n);
+    const int64_t s = t.state + e;                 // of the states; they are padded to whole blocks
+    const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
+    const float shrink = fmaf(-a.lr, t.decay, 1.0f);
+    const bool wide_p = n == 8 && (reinterpret_cast<uintptr_t>(t.param) & 31) == 0;
+
+    Vec8 g, p, m, v;
+    float ms = 1.0f, vs = 1.0f;
+    if (keep) {
+        if (BITS == 8) {
+            ms = a.m_scale[s / kBlock];
+            vs = a.v_scale[s / kBlock];
+            const uint2 mc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + s);
+            const uint2 vc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + s);
+            unpack4(mc.x, ms, m.v);
+            unpack4(mc.y, ms, m.v + 4);
+            unpack4(vc.x, vs, v.v);
+            unpack4(vc.y, vs, v.v + 4);
+        } else {
+            m = load8(static_cast<const float*>(a.m) + s);
+            v = load8(static_cast<const float*>(a.v) + s);
+        }
+        g = load_grad(gp, t.grad_dtype, e, n, wide_grad(gp, t.grad_dtype));
+        if (wide_p) {
+            p = load8(t.param + e);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p.v[i] = i < n ? t.param[e + i] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool k = keep >> i & 1;
+            float mi = m.v[i], vi = v.v[i];
+            moments(__fmul_rn(g.v[i], gs), mi, vi, a);
+            const float pi = stepped(p.v[i], mi, vi, shrink, a);
+            m.v[i] = k ? mi : BITS == 8 ? 0.0f : m.v[i];
+            v.v[i] = k ? vi : BITS == 8 ? 0.0f : v.v[i];
+            p.v[i] = k ? pi : p.v[i];
+        }
+        if (wide_p) {
+            store8(t.param + e, p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (keep >> i & 1) t.param[e + i] = p.v[i];
+        }
+        if (t.copy) {
+            uint16_t* c = static_cast<uint16_t*>(t.copy) + e;
+            if (n == 8 && (reinterpret_cast<uintptr_t>(t.copy) & 15) == 0) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = narrow1(p.v[2 * i], a.copy_dtype) | (uint32_t)narrow1(p.v[2 * i + 1], a.copy_dtype) << 16;
+                *reinterpret_cast<uint4*>(c) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < n) c[i] = narrow1(p.v[i], a.copy_dtype);
+            }
+        }
+        if (BITS == 32) {
+            store8(static_cast<float*>(a.m) + s, m);
+            store8(static_cast<float*>(a.v) + s, v);
+        }
+    }
+    if (BITS == 8) {
+        uint32_t largest_m = 0, largest_v = 0;
+        if (keep) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                largest_m = max(largest_m, finite_bits(m.v[i]));
+                largest_v = max(largest_v, finite_bits(v.v[i]));
+            }
+        }
+        ms = block_scale(__reduce_max_sync(0xffffffffu, largest_m));
+        vs = block_scale(__reduce_max_sync(0xffffffffu, largest_v));
+        if (threadIdx.x % 32 == 0) {
+            a.m_scale[s / kBlock] = ms;
+            a.v_scale[s / kBlock] = vs;
+        }
+        if (!keep) return;
+        const float im = 1.0f / ms, iv = 1.0f / vs;
+        // one hash for the lane's eight elements, times an odd constant for each: the first 32 bits of
+        // the fractions of the square roots of 2 to 19, made odd (mix has those of 23 and 29)
+        constexpr uint32_t odd[8] = {0x6A09E667u, 0xBB67AE85u, 0x3C6EF373u, 0xA54FF53Bu,
+                                     0x510E527Fu, 0x9B05688Du, 0x1F83D9ABu, 0x5BE0CD19u};
+        const uint32_t h = mix((uint32_t)(s >> 3) * 0x9E3779B1u ^ a.key);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t y = h * odd[i];
+            y ^= y >> 15;
+            m.v[i] = rounded<false>(m.v[i] * im, y & 0xFFFFu);
+            v.v[i] = rounded<true>(v.v[i] * iv, y >> 16);
+        }
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s) =
+            make_uint2(pack4(m.v[0], m.v[1], m.v[2], m.v[3]), pack4(m.v[4], m.v[5], m.v[6], m.v[7]));
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s) =
+            make_uint2(pack4(v.v[0], v.v[1], v.v[2], v.v[3]), pack4(v.v[4], v.v[5], v.v[6], v.v[7]));
+    }
+}
+
+template <int N>
+Grads<N> take(const void* const* grads, int first, int count) {
+    Grads<N> g;
+    for (int i = 0; i < N; ++i) g.at[i] = i < count ? grads[first + i] : nullptr;
+    return g;
+}
+
+bool known(int dtype) { return dtype == PP_F32 || dtype == PP_F16 || dtype == PP_BF16; }
+
+int check_grads(const pp_tensors* h, const void* const* grads) {
+    if (!h) return PP_ERR_NULL;
+    if (!h->tensors.empty() && !grads) return PP_ERR_NULL;
+    if (!h->dev) return PP_ERR_NOT_BOUND;
+    for (size_t i = 0; i < h->tensors.size(); ++i)
+        if (reinterpret_cast<uintptr_t>(grads[i]) % (h->tensors[i].grad_dtype == PP_F32 ? 4 : 2)) return PP_ERR_ALIGN;
+    return PP_OK;
+}
+
+int launched() { return cudaGetLastError() == cudaSuccess ? PP_OK : PP_ERR_CUDA; }
+
+}  // namespace
+
+extern "C" {
+
+int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const uint16_t* const* taps,
+                      float* const* params, void* const* copies, int copy_dtype, const float* decay,
+                      pp_tensors_handle* out) {
+    if (n < 0 || n > (1 << 20)) return PP_ERR_SHAPE;
+    if (!out || (n && (!numel || !grad_dtypes))) return PP_ERR_NULL;
+    if (copies && copy_dtype != PP_F16 && copy_dtype != PP_BF16) return PP_ERR_DTYPE;
+    for (int i = 0; i < n; ++i) {
+        if (numel[i] < 0 || numel[i] > kMaxNumel) return PP_ERR_SHAPE;
+        if (!known(grad_dtypes[i])) return PP_ERR_DTYPE;
+        if (taps && taps[i] && numel[i] % 9) return PP_ERR_SHAPE;
+        if (taps && reinterpret_cast<uintptr_t>(taps[i]) % 2) return PP_ERR_ALIGN;
+        if (params && numel[i] && !params[i]) return PP_ERR_NULL;
+        if (params && reinterpret_cast<uintptr_t>(params[i]) % 4) return PP_ERR_ALIGN;
+        if (copies && reinterpret_cast<uintptr_t>(copies[i]) % 2) return PP_ERR_ALIGN;
+        if (decay && !std::isfinite(decay[i])) return PP_ERR_ARG;
+    }
+    try {
+        pp_tensors* h = new pp_tensors;
+        struct Guard {
+            pp_tensors* h;
+            ~Guard() { delete h; }
+        } guard{h};
+        uint64_t chunks = 0;
+        for (int i = 0; i < n; ++i) {
+            TensorEntry t{};
+            t.param = params ? params[i] : nullptr;
+            t.copy = copies ? copies[i] : nullptr;
+            t.taps = taps ? taps[i] : nullptr;
+            t.numel = numel[i];
+            t.state = h->state_elements;
+            t.decay = decay ? decay[i] : 0.0f;
+            t.grad_dtype = grad_dtypes[i];
+            h->tensors.push_back(t);
+            h->first_chunk.push_back((uint32_t)chunks);
+            h->state_elements += (numel[i] + kBlock - 1) / kBlock * kBlock;
+            chunks += (uint64_t)((numel[i] + kChunk - 1) / kChunk);
+            if (chunks > 0x7FFFFFFFu) return PP_ERR_SHAPE;
+        }
+        h->first_chunk.push_back((uint32_t)chunks);
+        h->copy_dtype = copy_dtype;
+        h->has_params = params != nullptr;
+        h->off_chunks = ((size_t)n * sizeof(TensorEntry) + 255) / 256 * 256;
+        h->off_sums = (h->off_chunks + chunks * sizeof(ChunkEntry) + 255) / 256 * 256;
+        const size_t launches = ((size_t)n + kMaxGrads - 1) / kMaxGrads;
+        h->image.assign(h->off_sums + 256 + std::max<size_t>(1, launches) * kSumCtas * sizeof(double), 0);
+        if (n) memcpy(h->image.data(), h->tensors.data(), (size_t)n * sizeof(TensorEntry));
+        ChunkEntry* c = reinterpret_cast<ChunkEntry*>(h->image.data() + h->off_chunks);
+        for (int i = 0; i < n; ++i)
+            for (uint32_t k = h->first_chunk[i]; k < h->first_chunk[i + 1]; ++k) *c++ = {(uint32_t)i, k - h->first_chunk[i]};
+        guard.h = nullptr;
+        *out = h;
+        return PP_OK;
+    } catch (const std::bad_alloc&) {
+        return PP_ERR_ALLOC;
+    }
+}
+
+int pp_tensors_query(pp_tensors_handle h, int key, int64_t* value) {
+    if (!h || !value) return PP_ERR_NULL;
+    switch (key) {
+        case PP_TQ_COUNT: *value = (int64_t)h->tensors.size(); return PP_OK;
+        case PP_TQ_TABLE_BYTES: *value = (int64_t)h->image.size(); return PP_OK;
+        case PP_TQ_STATE_ELEMENTS: *value = h->state_elements; return PP_OK;
+    }
+    if (key >= PP_TQ_STATE_OFFSET && (size_t)(key - PP_TQ_STATE_OFFSET) < h->tensors.size()) {
+        *value = h->tensors[key - PP_TQ_STATE_OFFSET].state;
+        return PP_OK;
+    }
+    return PP_ERR_ARG;
+}
+
+int pp_tensors_bind(pp_tensors_handle h, void* dev, size_t bytes, void* stream) {
+    if (!h || !dev) return PP_ERR_NULL;
+    if (bytes < h->image.size()) return PP_ERR_BUFFER;
+    if (reinterpret_cast<uintptr_t>(dev) % 256) return PP_ERR_ALIGN;
+    if (cudaMemcpyAsync(dev, h->image.data(), h->image.size(), cudaMemcpyHostToDevice,
+                        static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        cudaGetLastError();
+        return PP_ERR_CUDA;
+    }
+    h->dev = static_cast<unsigned char*>(dev);
+    return PP_OK;
+}
+
+int pp_tensors_destroy(pp_tensors_handle h) {
+    delete h;
+    return PP_OK;
+}
+
+int pp_grad_norm(pp_tensors_handle h, const void* const* grads, double max_norm, float* out, void* stream) {
+    if (const int e = check_grads(h, grads)) return e;
+    if (!out) return PP_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(out) % 4) return PP_ERR_ALIGN;
+    if (!(max_norm > 0)) return PP_ERR_ARG;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const TensorEntry* tensors = reinterpret_cast<const TensorEntry*>(h->dev);
+    const ChunkEntry* chunks = reinterpret_cast<const ChunkEntry*>(h->dev + h->off_chunks);
+    unsigned* counter = reinterpret_cast<unsigned*>(h->dev + h->off_sums);
+    double* sums = reinterpret_cast<double*>(h->dev + h->off_sums + 256);
+    const int n = (int)h->tensors.size();
+    unsigned all = 0;
+    for (int pass = 0; pass < 2; ++pass) {        // count the partial sums, then launch
+        unsigned done = 0;
+        int i = 0;
+        do {
+            const int count = std::min(n - i, kMaxGrads);
+            const uint32_t begin = h->first_chunk[i], end = h->first_chunk[i + count];
+            const unsigned grid = std::max(1u, std::min<uint32_t>(end - begin, kSumCtas));
+            if (pass) {
+                const float mx = (float)max_norm;
+                if (count <= kFewGrads)
+                    grad_norm_kernel<kFewGrads><<<grid, kThreads, 0, st>>>(
+                        tensors, chunks, begin, end, (uint32_t)i, take<kFewGrads>(grads, i, count), sums, counter, done,
+                        all, mx, out);
+                else
+                    grad_norm_kernel<kMaxGrads><<<grid, kThreads, 0, st>>>(
+                        tensors, chunks, begin, end, (uint32_t)i, take<kMaxGrads>(grads, i, count), sums, counter, done,
+                        all, mx, out);
+                if (const int e = launched()) return e;
+            }
+            done += grid;
+            i += count;
+        } while (i < n);
+        all = done;
+    }
+    return PP_OK;
+}
+
+int pp_adamw_step(pp_tensors_handle h, const void* const* grads, int state_bits, void* m, void* v, float* m_scale,
+                  float* v_scale, double lr, double beta1, double beta2, double eps, int64_t step, uint32_t seed,
+                  const float* grad_scale, void* stream) {
+    if (const int e = check_grads(h, grads)) return e;
+    if (!h->has_params) return PP_ERR_NOT_BOUND;
+    if (state_bits != 32 && state_bits != 8) return PP_ERR_ARG;
+    if (!std::isfinite(lr) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) ||
+        !std::isfinite(eps) || step < 1)
+        return PP_ERR_ARG;
+    const uint32_t all = h->first_chunk.back();
+    if (!all) return PP_OK;
+    if (!m || !v || (state_bits == 8 && (!m_scale || !v_scale))) return PP_ERR_NULL;
+    const auto off = [](const void* p, size_t k) { return reinterpret_cast<uintptr_t>(p) % k != 0; };
+    if (off(m, 32) || off(v, 32) || off(m_scale, 4) || off(v_scale, 4) || off(grad_scale, 4)) return PP_ERR_ALIGN;
+    AdamArgs a{};
+    a.lr = (float)lr;
+    a.step_size = (float)(lr / (1 - std::pow(beta1, (double)step)));
+    a.b1 = (float)beta1;
+    a.b2 = (float)beta2;
+    a.c1 = (float)(1 - beta1);
+    a.c2 = (float)(1 - beta2);
+    a.inv_bc2 = (float)(1 / (1 - std::pow(beta2, (double)step)));
+    a.eps = (float)eps;
+    a.key = mix(seed + (uint32_t)step * 0x9E3779B1u);
+    a.copy_dtype = h->copy_dtype;
+    a.grad_scale = grad_scale;
+    a.m = m;
+    a.v = v;
+    a.m_scale = m_scale;
+    a.v_scale = v_scale;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const TensorEntry* tensors = reinterpret_cast<const TensorEntry*>(h->dev);
+    const ChunkEntry* chunks = reinterpret_cast<const ChunkEntry*>(h->dev + h->off_chunks);
+    const int n = (int)h->tensors.size();
+    for (int i = 0; i < n; i += kMaxGrads) {
+        const int count = std::min(n - i, kMaxGrads);
+        const uint32_t begin = h->first_chunk[i], grid = h->first_chunk[i + count] - begin;
+        if (!grid) continue;
+        const bool few = count <= kFewGrads;
+        if (state_bits == 8 && few)
+            adamw_kernel<8, kFewGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
+                                                                 take<kFewGrads>(grads, i, count), a);
+        else if (state_bits == 8)
+            adamw_kernel<8, kMaxGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
+                                                                 take<kMaxGrads>(grads, i, count), a);
+        else if (few)
+            adamw_kernel<32, kFewGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
+                                                                  take<kFewGrads>(grads, i, count), a);
+        else
+            adamw_kernel<32, kMaxGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
+                                                                  take<kMaxGrads>(grads, i, count), a);
+        if (const int e = launched()) return e;
+    }
+    return PP_OK;
+}
+
+}  // extern "C"
