@@ -1,4 +1,5 @@
-"""ctypes loader for libpatconv.so (the C ABI declared in include/patconv.h).
+"""Loader for libpatconv.so (the C ABI declared in include/patconv.h, by ctypes) and for the native
+binding of its training side.
 
 Argument marshalling only.  There is no fallback: if the library is missing or fails to load,
 ``load`` raises, and nothing in this package computes a convolution any other way.
@@ -6,6 +7,8 @@ Argument marshalling only.  There is no fallback: if the library is missing or f
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 import threading
 
@@ -75,6 +78,7 @@ SIGNATURES = {
 
 _lock = threading.Lock()
 _lib = None
+_binding = None
 
 
 def load(build_if_missing: bool = True) -> ctypes.CDLL:
@@ -98,6 +102,21 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
             fn.argtypes = args
         _lib = lib
         return lib
+
+
+def binding():
+    """The native binding of the training side (csrc/binding.cpp), beside the library."""
+    global _binding
+    if _binding is None:
+        import torch  # noqa: F401  (the binding links against its libraries)
+        load()
+        with _lock:
+            if _binding is None:
+                loader = importlib.machinery.ExtensionFileLoader("_patconv", _build.BINDING)
+                module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_patconv", loader))
+                loader.exec_module(module)
+                _binding = module
+    return _binding
 
 
 class PatconvError(RuntimeError):

@@ -1,16 +1,19 @@
-"""Build libpatconv.so in-tree: nvcc for the sm_103a kernels, g++ for the host packer.
+"""Build libpatconv.so in-tree: nvcc for the sm_103a kernels, g++ for the host packer; and beside it
+_patconv.so, the native binding of the training side, which links against torch and the library.
 
-The library is written to ``paper_2003_06513_gb300/_build/libpatconv.so`` (git-ignored) and is
-rebuilt whenever a source file or a flag changes.  No CMake: five translation units compiled in
-parallel and one link, so a fresh build takes well under a minute.
+Both are written to ``paper_2003_06513_gb300/_build/`` (git-ignored) and are rebuilt whenever a source
+file, a flag or the torch version changes.  No CMake: six translation units compiled in parallel and
+two links, so a fresh build takes a minute or so, the largest unit's time.
 """
 from __future__ import annotations
 
 import hashlib
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +21,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libpatconv.so")
+BINDING = os.path.join(BUILD, "_patconv.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC",
@@ -25,7 +29,7 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--expt-relaxed-constexpr", "-Xc
 GXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-I",
              os.path.join(ROOT, "include")]
 SOURCES = ["conv.cu", "tensor.cu", "tensor.h", "norm.cu", "optim.cu",
-            "pack.cpp", "layer.h", "gen_dispatch.py"]
+           "pack.cpp", "layer.h", "gen_dispatch.py", "binding.cpp"]
 
 
 def _nvcc() -> str:
@@ -35,8 +39,21 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libpatconv")
 
 
+def _torch_dir() -> str:
+    """torch's folder, without the time that importing it takes."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None or not spec.submodule_search_locations:
+        raise RuntimeError("torch not found: the package's binding is built against it")
+    return spec.submodule_search_locations[0]
+
+
+def _torch_version(torch_dir: str) -> str:
+    with open(os.path.join(torch_dir, "version.py")) as f:
+        return f.read()
+
+
 def _digest(extra) -> str:
-    h = hashlib.sha256()
+    h = hashlib.sha256(_torch_version(_torch_dir()).encode())
     for name in SOURCES + [os.path.join("..", "..", "include", "patconv.h")]:
         with open(os.path.join(CSRC, name), "rb") as f:
             h.update(f.read())
@@ -49,7 +66,7 @@ def build(force: bool = False, verbose: bool = False, extra_nvcc=()) -> str:
     os.makedirs(BUILD, exist_ok=True)
     stamp = os.path.join(BUILD, "stamp")
     digest = _digest(tuple(extra_nvcc))
-    if not force and os.path.exists(LIB) and os.path.exists(stamp):
+    if not force and all(os.path.exists(f) for f in (LIB, BINDING, stamp)):
         with open(stamp) as f:
             if f.read().strip() == digest:
                 return LIB
@@ -61,12 +78,19 @@ def build(force: bool = False, verbose: bool = False, extra_nvcc=()) -> str:
     norm_o = os.path.join(BUILD, "norm.o")
     optim_o = os.path.join(BUILD, "optim.o")
     pack_o = os.path.join(BUILD, "pack.o")
+    binding_o = os.path.join(BUILD, "binding.o")
+    torch_dir = _torch_dir()
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
+    includes = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     cmds = [
         [nvcc, "-c", os.path.join(CSRC, "conv.cu"), "-o", conv_o, "-I", BUILD] + NVCC_FLAGS + list(extra_nvcc),
         [nvcc, "-c", os.path.join(CSRC, "tensor.cu"), "-o", tensor_o] + NVCC_FLAGS + list(extra_nvcc),
         [nvcc, "-c", os.path.join(CSRC, "norm.cu"), "-o", norm_o] + NVCC_FLAGS + list(extra_nvcc),
         [nvcc, "-c", os.path.join(CSRC, "optim.cu"), "-o", optim_o] + NVCC_FLAGS + list(extra_nvcc),
         ["g++", "-c", os.path.join(CSRC, "pack.cpp"), "-o", pack_o] + GXX_FLAGS,
+        ["g++", "-c", os.path.join(CSRC, "binding.cpp"), "-o", binding_o] + GXX_FLAGS
+        + [f for d in includes for f in ("-isystem", d)],
     ]
 
     def run(cmd):
@@ -82,6 +106,10 @@ def build(force: bool = False, verbose: bool = False, extra_nvcc=()) -> str:
     tmp = LIB + ".tmp"
     run([nvcc, "-shared", "-o", tmp, conv_o, tensor_o, norm_o, optim_o, pack_o] + ARCH + ["-cudart", "static"])
     os.replace(tmp, LIB)
+    tmp, lib = BINDING + ".tmp", os.path.join(torch_dir, "lib")
+    run(["g++", "-shared", "-o", tmp, binding_o, "-L", BUILD, "-l:libpatconv.so", "-L", lib, "-lc10", "-lc10_cuda",
+         "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN:" + lib])
+    os.replace(tmp, BINDING)
     with open(stamp, "w") as f:
         f.write(digest)
     return LIB

@@ -17,12 +17,12 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
-from typing import List, Optional, Sequence, Union
+from typing import Optional, Sequence, Union
 
 import torch
 
 from . import _lib
-from .api import _raw_stream, _stream_ptr
+from .api import _stream_ptr
 
 PP_F32, PP_F16, PP_BF16 = 0, 1, 2
 _DT = {torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16}
@@ -89,7 +89,6 @@ class _Tensors:
                 raise ValueError("taps go with a [Cout, Cin/groups, 3, 3] tensor, one mask a kernel")
             if t.dtype != torch.int16 or not t.is_contiguous() or t.get_device() != index:
                 raise ValueError("taps must be contiguous int16 tensors on the tensors' device")
-        self._expect = [(tuple(shape), tuple(stride), dt) for shape, stride, dt in zip(shapes, strides, dtypes)]
         self._keep_alive = (taps, params, copies)
         copy_dtype = next((_DT[c.dtype] for c in copies or [] if c is not None), PP_F16)
 
@@ -104,7 +103,9 @@ class _Tensors:
             addresses(copies) if copies is not None else None, copy_dtype,
             (ctypes.c_float * max(1, n))(*decay) if decay is not None else None, ctypes.byref(h)))
         self._h = h
-        self._pointers_t = ctypes.c_void_p * max(1, n)
+        self.native = _lib.binding()
+        self.list = self.native.tensors(h.value, index, [(tuple(shape), tuple(stride), _DT[d])
+                                                         for shape, stride, d in zip(shapes, strides, dtypes)])
         with torch.cuda.device(index), self._on(stream):
             self._table = torch.empty(self.query(_TABLE_BYTES), dtype=torch.uint8, device=self._device)
             _lib.check("pp_tensors_bind", lib.pp_tensors_bind(h, ctypes.c_void_p(self._table.data_ptr()),
@@ -120,39 +121,11 @@ class _Tensors:
     def _on(self, stream):
         return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
-    def _guard(self):
-        if torch.cuda.current_device() == self._index:
-            return contextlib.nullcontext()
-        return torch.cuda.device(self._index)
-
-    def _pointers(self, grads):
-        """The gradients' addresses, each checked against its tensor: type, shape, order, device."""
-        if len(grads) != len(self._expect):
-            raise ValueError(f"{len(grads)} gradients for {len(self._expect)} tensors")
-        index, found = self._index, []
-        for g, (shape, stride, dtype) in zip(grads, self._expect):
-            if g is None:
-                found.append(None)
-                continue
-            if g.dtype is not dtype or g.get_device() != index or g.shape != shape:
-                raise ValueError(f"a gradient is {tuple(g.shape)} {g.dtype} on {g.device}, "
-                                 f"expected {shape} {dtype} on {self._device}")
-            if g.stride() != stride and any(a != b for a, b, k in zip(g.stride(), stride, shape) if k > 1) and g.numel():
-                raise ValueError(f"a gradient's strides are {g.stride()}, its tensor's {stride}")
-            found.append(g.data_ptr())
-        return self._pointers_t(*found)
-
     def norm(self, grads, max_norm, out, stream):
-        pointers = self._pointers(grads)
-        with self._guard():
-            if out is None:
-                with self._on(stream):
-                    out = torch.empty(2, dtype=torch.float32, device=self._device)
-            elif out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous() or out.get_device() != self._index:
-                raise ValueError("out must be a contiguous float32 tensor of two values on the tensors' device")
-            _lib.check("pp_grad_norm", _lib.load().pp_grad_norm(self._h, pointers, float(max_norm), out.data_ptr(),
-                                                                _raw_stream(stream, self._device)))
-        return out[0:1], out[1:2]
+        got = self.native.grad_norm(self.list, grads, max_norm, out, None if stream is None else stream.cuda_stream)
+        if type(got) is int:
+            raise _lib.PatconvError("pp_grad_norm", got)
+        return got
 
     def __del__(self):
         h, self._h = getattr(self, "_h", None), None
@@ -269,19 +242,12 @@ class AdamW:
         """One step with the gradients (default: the parameters' ``grad``; None: that tensor is left
         alone), each times ``grad_scale`` (one float32 on the device) if given, at rate ``lr`` (default:
         the object's).  Calls on one object must be ordered."""
-        pointers = self._t._pointers(self._grads(grads))
-        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
-                                       or grad_scale.get_device() != self._t._index):
-            raise ValueError("grad_scale must be one float32 on the parameters' device")
-        eight = self.state_bits == 8
-        with self._t._guard():
-            _lib.check("pp_adamw_step", _lib.load().pp_adamw_step(
-                self._t._h, pointers, self.state_bits, self.m.data_ptr(), self.v.data_ptr(),
-                self.m_scale.data_ptr() if eight else None, self.v_scale.data_ptr() if eight else None,
-                self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.steps + 1, self.seed,
-                grad_scale.data_ptr() if grad_scale is not None else None, _raw_stream(stream, self._t._device)))
+        t = self._t
+        _lib.check("pp_adamw_step", t.native.adamw_step(
+            t.list, self._grads(grads), self.params, self.state_bits, self.m, self.v, self.m_scale, self.v_scale,
+            self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.steps + 1, self.seed,
+            grad_scale, None if stream is None else stream.cuda_stream))
         self.steps += 1
-        torch.autograd.graph.increment_version(self.params)     # they changed behind torch's back
 
-    def _grads(self, grads) -> List[Optional[torch.Tensor]]:
+    def _grads(self, grads) -> Sequence:
         return [p.grad for p in self.params] if grads is None else grads
