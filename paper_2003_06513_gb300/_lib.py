@@ -61,6 +61,8 @@ SIGNATURES = {
                                         _c_size_t, _c_void_p]),
     "pp_group_norm_workspace_size": (_c_int, [_c_int, _c_int, _c_i64, _c_int, _c_int, _c_int,
                                               ctypes.POINTER(_c_size_t)]),
+    "pp_group_norm_plan": (_c_int, [_c_int, _c_int, _c_i64, _c_int, _c_int, _c_int, _c_int,
+                                    ctypes.POINTER(_c_i64), _c_int]),
     "pp_tensors_create": (_c_int, [_c_int, ctypes.POINTER(_c_i64), ctypes.POINTER(_c_int),
                                    ctypes.POINTER(_c_void_p), ctypes.POINTER(_c_void_p),
                                    ctypes.POINTER(_c_void_p), _c_int, ctypes.POINTER(_c_float),

@@ -2,7 +2,7 @@
 _patconv.so, the native binding of the training side, which links against torch and the library.
 
 Both are written to ``paper_2003_06513_gb300/_build/`` (git-ignored) and are rebuilt whenever a source
-file, a flag or the torch version changes.  No CMake: six translation units compiled in parallel and
+file, a flag or the torch version changes.  No CMake: nine translation units compiled in parallel and
 two links, so a fresh build takes a minute or so, the largest unit's time.
 """
 from __future__ import annotations
@@ -28,8 +28,8 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--expt-relaxed-constexpr", "-Xc
               "-Xcompiler", "-ffp-contract=off", "-I", os.path.join(ROOT, "include")] + ARCH
 GXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-I",
              os.path.join(ROOT, "include")]
-SOURCES = ["conv.cu", "tensor.cu", "tensor.h", "norm.cu", "optim.cu",
-           "pack.cpp", "layer.h", "gen_dispatch.py", "binding.cpp"]
+KERNELS = ["conv.cu", "tensor.cu", "norm.cu", "norm_f32.cu", "norm_f16.cu", "norm_bf16.cu", "optim.cu"]
+SOURCES = KERNELS + ["tensor.h", "norm.h", "norm.cuh", "pack.cpp", "layer.h", "gen_dispatch.py", "binding.cpp"]
 
 
 def _nvcc() -> str:
@@ -73,25 +73,19 @@ def build(force: bool = False, verbose: bool = False, extra_nvcc=()) -> str:
     nvcc = _nvcc()
     subprocess.run([sys.executable, os.path.join(CSRC, "gen_dispatch.py"),
                     os.path.join(BUILD, "pattern_dispatch.h")], check=True)
-    conv_o = os.path.join(BUILD, "conv.o")
-    tensor_o = os.path.join(BUILD, "tensor.o")
-    norm_o = os.path.join(BUILD, "norm.o")
-    optim_o = os.path.join(BUILD, "optim.o")
-    pack_o = os.path.join(BUILD, "pack.o")
-    binding_o = os.path.join(BUILD, "binding.o")
     torch_dir = _torch_dir()
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
     includes = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
                 os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
-    cmds = [
-        [nvcc, "-c", os.path.join(CSRC, "conv.cu"), "-o", conv_o, "-I", BUILD] + NVCC_FLAGS + list(extra_nvcc),
-        [nvcc, "-c", os.path.join(CSRC, "tensor.cu"), "-o", tensor_o] + NVCC_FLAGS + list(extra_nvcc),
-        [nvcc, "-c", os.path.join(CSRC, "norm.cu"), "-o", norm_o] + NVCC_FLAGS + list(extra_nvcc),
-        [nvcc, "-c", os.path.join(CSRC, "optim.cu"), "-o", optim_o] + NVCC_FLAGS + list(extra_nvcc),
-        ["g++", "-c", os.path.join(CSRC, "pack.cpp"), "-o", pack_o] + GXX_FLAGS,
-        ["g++", "-c", os.path.join(CSRC, "binding.cpp"), "-o", binding_o] + GXX_FLAGS
-        + [f for d in includes for f in ("-isystem", d)],
-    ]
+
+    def obj(name):
+        return os.path.join(BUILD, name.split(".")[0] + ".o")
+
+    cmds = [[nvcc, "-c", os.path.join(CSRC, name), "-o", obj(name), "-I", BUILD] + NVCC_FLAGS + list(extra_nvcc)
+            for name in KERNELS]
+    cmds += [["g++", "-c", os.path.join(CSRC, "pack.cpp"), "-o", obj("pack.cpp")] + GXX_FLAGS,
+             ["g++", "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj("binding.cpp")] + GXX_FLAGS
+             + [f for d in includes for f in ("-isystem", d)]]
 
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
@@ -104,10 +98,10 @@ def build(force: bool = False, verbose: bool = False, extra_nvcc=()) -> str:
     with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
         list(ex.map(run, cmds))
     tmp = LIB + ".tmp"
-    run([nvcc, "-shared", "-o", tmp, conv_o, tensor_o, norm_o, optim_o, pack_o] + ARCH + ["-cudart", "static"])
+    run([nvcc, "-shared", "-o", tmp] + [obj(name) for name in KERNELS + ["pack.cpp"]] + ARCH + ["-cudart", "static"])
     os.replace(tmp, LIB)
     tmp, lib = BINDING + ".tmp", os.path.join(torch_dir, "lib")
-    run(["g++", "-shared", "-o", tmp, binding_o, "-L", BUILD, "-l:libpatconv.so", "-L", lib, "-lc10", "-lc10_cuda",
+    run(["g++", "-shared", "-o", tmp, obj("binding.cpp"), "-L", BUILD, "-l:libpatconv.so", "-L", lib, "-lc10", "-lc10_cuda",
          "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN:" + lib])
     os.replace(tmp, BINDING)
     with open(stamp, "w") as f:

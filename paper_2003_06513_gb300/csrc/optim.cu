@@ -25,7 +25,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBlock = 256;               // elements that share a scale: a warp's, eight a lane
-constexpr int kChunk = kThreads * 8;      // elements of a chunk: a CTA's, eight a thread
+constexpr int kGroups = 2;                // blocks of a warp, and eights of a thread, in a chunk
+constexpr int kChunk = kThreads * 8 * kGroups;   // elements of a CTA's chunk; 4096 = 455 * 9 + 1
 constexpr int kFewGrads = 64, kMaxGrads = 448;   // 448 addresses and the rest are below 4 KB of arguments
 constexpr int64_t kMaxNumel = int64_t(1) << 40;
 
@@ -63,7 +64,7 @@ struct pp_tensors {
 
 namespace {
 
-constexpr int kSumCtas = 1024;            // most CTAs of the norm's kernel: partial sums
+constexpr int kSumCtas = 152 * 8;           // most CTAs of the norm's kernel: partial sums
 
 struct Vec8 {
     float v[8];
@@ -125,25 +126,30 @@ __device__ __forceinline__ bool wide_grad(const void* g, int dtype) {
     return (reinterpret_cast<uintptr_t>(g) & (dtype == PP_F32 ? 31 : 15)) == 0;
 }
 
-// Which of the eight elements from `lane_e` elements past the chunk's start take part: in the tensor
-// (n of them) and kept by its mask.  Eight elements touch two 3x3 kernels at most.
-__device__ __forceinline__ uint32_t kept8(const TensorEntry& t, int64_t chunk_e, int lane_e, int n) {
+// Which of the eight elements from element `le` of chunk `index` on take part: in the tensor (n of
+// them) and kept by its mask.  Eight elements touch two 3x3 kernels at most.
+__device__ __forceinline__ uint32_t kept8(const TensorEntry& t, uint32_t index, uint32_t le, int n) {
     if (n <= 0) return 0;
     const uint32_t in = n >= 8 ? 0xFFu : (1u << n) - 1;
     if (!t.taps) return in;
-    const int64_t k0 = chunk_e / 9;
-    const uint32_t local = (uint32_t)(chunk_e - 9 * k0) + (uint32_t)lane_e;
-    const int64_t k = k0 + local / 9;
-    const uint32_t r = local % 9;
+    static_assert(kChunk % 9 == 1, "a chunk starts at element index % 9 of a kernel");
+    const uint32_t local = index % 9 + le, r = local % 9;
+    const int64_t k = (int64_t)index * (kChunk / 9) + index / 9 + local / 9;
     const uint32_t a = t.taps[k] & 0x1FFu;
     const uint32_t b = 9 * (k + 1) < t.numel ? t.taps[k + 1] & 0x1FFu : 0;
     return ((a | b << 9) >> r) & in;
 }
+// elements of the tensor among the eight from element `le` of chunk `index` on
+__device__ __forceinline__ int in_tensor(const TensorEntry& t, uint32_t index, uint32_t le) {
+    const int64_t left = t.numel - (int64_t)index * kChunk - le;
+    return left < 8 ? (int)(left > 0 ? left : 0) : 8;
+}
 
 // ------------------------------------------------------------------------------------- the norm
 
-// Sum over a CTA's chunks of (g f)^2 for one of three factors f; per thread in fp32 over at most a few
-// hundred squares, then over the CTA.
+// Sum over a CTA's chunks of (g f)^2 for a factor f: per thread in fp32 over at most a few hundred
+// squares, then over the CTA.  A thread's masks and gradients of a chunk are all asked for before the
+// first is used.
 template <int N>
 __device__ float chunk_squares(const TensorEntry* tensors, const ChunkEntry* chunks, uint32_t begin, uint32_t end,
                                uint32_t t0, const Grads<N>& grads, float factor, float* smem) {
@@ -153,20 +159,29 @@ __device__ float chunk_squares(const TensorEntry* tensors, const ChunkEntry* chu
         const void* g = grads.at[ce.tensor - t0];
         if (!g) continue;
         const TensorEntry t = tensors[ce.tensor];
-        const int64_t e0 = (int64_t)ce.index * kChunk;
-        const int le = threadIdx.x * 8;
-        const int64_t left = t.numel - e0 - le;
-        const int n = left < 8 ? (int)(left > 0 ? left : 0) : 8;
-        const uint32_t keep = kept8(t, e0, le, n);
-        if (!keep) continue;
-        const Vec8 v = load_grad(g, t.grad_dtype, e0 + le, n, wide_grad(g, t.grad_dtype));
-        float s = 0.0f;
+        const bool wide = wide_grad(g, t.grad_dtype);
+        uint32_t keep[kGroups];
+        Vec8 v[kGroups];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float x = keep >> i & 1 ? v.v[i] * factor : 0.0f;
-            s = fmaf(x, x, s);
+        for (int k = 0; k < kGroups; ++k) {
+            const uint32_t le = (k * kThreads + threadIdx.x) * 8;
+            keep[k] = kept8(t, ce.index, le, in_tensor(t, ce.index, le));
         }
-        sum += s;
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            const uint32_t le = (k * kThreads + threadIdx.x) * 8;
+            if (keep[k]) v[k] = load_grad(g, t.grad_dtype, (int64_t)ce.index * kChunk + le, in_tensor(t, ce.index, le), wide);
+        }
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = keep[k] >> i & 1 ? v[k].v[i] * factor : 0.0f;
+                s = fmaf(x, x, s);
+            }
+            sum += s;
+        }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -236,19 +251,27 @@ struct AdamArgs {
 
 __device__ __forceinline__ float approx_sqrt(float x) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float approx_rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 
 // The states' arithmetic rounds every product and sum by itself: an 8-bit state then depends on the
-// formula alone and not on how a compiler contracts it.
-__device__ __forceinline__ void moments(float g, float& m, float& v, const AdamArgs& a) {
-    m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.c1));
-    v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.c2));
+// formula alone and not on how a compiler contracts it.  m and v come as values times m_unit and
+// v_unit: an 8-bit state's code and its scale times b, a product by a power of two being exact.
+__device__ __forceinline__ void moments(float g, float& m, float& v, float mb, float vb, const AdamArgs& a) {
+    m = __fadd_rn(__fmul_rn(m, mb), __fmul_rn(g, a.c1));
+    v = __fadd_rn(__fmul_rn(v, vb), __fmul_rn(__fmul_rn(g, g), a.c2));
 }
+// 2^-126 keeps the root in fp32's normal range, where the approximations flush nothing: a root below
+// 2^-63 is far below any eps in use, and with eps = 0 it makes 0 / 0 zero.
 __device__ __forceinline__ float stepped(float p, float m, float v, float shrink, const AdamArgs& a) {
-    const float den = approx_sqrt(v * a.inv_bc2) + a.eps;
-    return fmaf(-a.step_size, __fdividef(m, den), p * shrink);
+    const float den = approx_sqrt(fmaf(v, a.inv_bc2, 0x1p-126f)) + a.eps;
+    return fmaf(-a.step_size, m * approx_rcp(den), p * shrink);
 }
 
 __host__ __device__ inline uint32_t mix(uint32_t x) {
@@ -266,17 +289,41 @@ __device__ __forceinline__ float block_scale(uint32_t largest) {
     return __uint_as_float((uint32_t)(field < 1 ? 1 : field) << 23);
 }
 
-// A value over its block's scale, rounded to one of its two neighbours in e4m3 by the dither r (16
-// bits): the bits below the format's three are filled up by the dither and cut off.  Below 2^-6 the
-// format's grid is that of [2^-6, 2^-5), so 2^-6 is added for the cut.
-template <bool POSITIVE>
-__device__ __forceinline__ float rounded(float t, uint32_t r) {
-    const float a = fabsf(t);
-    const float small = a < 0x1p-6f ? 0x1p-6f : 0.0f;
-    float w = __uint_as_float((__float_as_uint(__fadd_rn(a, small)) + (r << 4) + 8) & 0xFFF00000u) - small;
-    if (POSITIVE && a > 0.0f) w = fmaxf(w, 0x1p-9f);              // a second moment is not lost
-    if (!(a < INFINITY)) w = NAN;
-    return copysignf(w, t);
+// A finite value over its block's scale, rounded to one of its two neighbours in e4m3 by the dither: 16
+// random bits, then a half, in the place of the bits below the format's three, which are filled up by it
+// and cut off.  Below 2^-6 the format's grid is that of [2^-6, 2^-5), so 2^-6 is added for the cut.
+__device__ __forceinline__ float rounded(float t, uint32_t dither) {      // either sign
+    const float small = fabsf(t) < 0x1p-6f ? copysignf(0x1p-6f, t) : 0.0f;
+    return __uint_as_float((__float_as_uint(__fadd_rn(t, small)) + dither) & 0xFFF00000u) - small;
+}
+__device__ __forceinline__ float rounded_up(float t, uint32_t dither) {   // not negative; above zero stays so
+    const float small = t < 0x1p-6f ? 0x1p-6f : 0.0f;
+    const float w = __uint_as_float((__float_as_uint(__fadd_rn(t, small)) + dither) & 0xFFF00000u) - small;
+    return t > 0.0f ? fmaxf(w, 0x1p-9f) : w;
+}
+__device__ __forceinline__ uint32_t dither_m(uint32_t y) { return (y << 4 & 0xFFFF0u) | 8; }
+__device__ __forceinline__ uint32_t dither_v(uint32_t y) { return (y >> 12 & 0xFFFF0u) | 8; }
+
+// One hash for eight consecutive elements, times an odd constant for each: the first 32 bits of the
+// fractions of the square roots of 2 to 19, made odd (mix has those of 23 and 29).
+__device__ __forceinline__ uint32_t hash8(int64_t state, uint32_t key) {
+    return mix((uint32_t)(state >> 3) * 0x9E3779B1u ^ key);
+}
+__device__ __forceinline__ uint32_t odd(int i) {
+    constexpr uint32_t c[8] = {0x6A09E667u, 0xBB67AE85u, 0x3C6EF373u, 0xA54FF53Bu,
+                               0x510E527Fu, 0x9B05688Du, 0x1F83D9ABu, 0x5BE0CD19u};
+    return c[i];
+}
+__device__ __forceinline__ uint32_t own_bits(uint32_t h, uint32_t factor) {
+    const uint32_t y = h * factor;
+    return y ^ y >> 15;
+}
+
+// larger magnitude; NaN if either is NaN
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
 }
 
 __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
@@ -284,133 +331,246 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
     return lo | hi << 16;
 }
-__device__ __forceinline__ void unpack4(uint32_t w, float scale, float* out) {
+__device__ __forceinline__ void unpack4(uint32_t w, float* out) {
     const __half2 a = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3));
     const __half2 b = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3));
     const float2 x = __half22float2(a), y = __half22float2(b);
-    out[0] = x.x * scale;
-    out[1] = x.y * scale;
-    out[2] = y.x * scale;
-    out[3] = y.y * scale;
+    out[0] = x.x;
+    out[1] = x.y;
+    out[2] = y.x;
+    out[3] = y.y;
 }
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-    return b < 0x7F800000u ? b : 0;
+__device__ __forceinline__ float unpack1(uint8_t w) {
+    return __half2float(__half(__nv_cvt_fp8_to_halfraw(w, __NV_E4M3)));
+}
+__device__ __forceinline__ uint8_t pack1(float x) { return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3); }
+
+// The block's scale from each lane's values.  Where one of them is not finite (a warp's rare case) the
+// scale is the others', and `spoilt` says which of the lane's those are: they are stored as NaN.
+template <int K>
+__device__ __forceinline__ float warp_scale(const float (&x)[K], uint32_t& spoilt) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < K; ++i) top = larger(top, x[i]);
+    uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+    spoilt = 0;
+    if (bits >= 0x7F800000u) {
+        uint32_t fine = 0;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const uint32_t b = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+            if (b < 0x7F800000u)
+                fine = max(fine, b);
+            else
+                spoilt |= 1u << i;
+        }
+        bits = __reduce_max_sync(0xffffffffu, fine);
+    }
+    return block_scale(bits);
+}
+template <int K>
+__device__ __forceinline__ void spoil(float (&x)[K], uint32_t spoilt) {
+    if (!spoilt) return;
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+        if (spoilt >> i & 1) x[i] = NAN;
 }
 
-// One chunk a CTA, one block of 256 elements a warp, eight consecutive elements a lane: what a lane
-// reads and writes of an fp32 tensor is one 32-byte sector, which is skipped where the mask keeps none
-// of its eight elements.
+__device__ __forceinline__ void store_copy(const TensorEntry& t, int64_t e, float p, int dtype) {
+    static_cast<uint16_t*>(t.copy)[e] = narrow1(p, dtype);
+}
+
+// A block of a tensor without a mask: eight consecutive elements a lane, n of them in the tensor.
+template <int BITS>
+__device__ __forceinline__ void dense_block(const TensorEntry& t, const void* gp, int64_t e, int n, float gs, float shrink,
+                                            bool wide_g, bool wide_p, const AdamArgs& a) {
+    const int64_t s = t.state + e;
+    Vec8 g, p, m, v;
+    float mb = a.b1, vb = a.b2;
+    if (BITS == 8) {
+        mb *= a.m_scale[s / kBlock];
+        vb *= a.v_scale[s / kBlock];
+        const uint2 mc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + s);
+        const uint2 vc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + s);
+        g = load_grad(gp, t.grad_dtype, e, n, wide_g);
+        unpack4(mc.x, m.v);
+        unpack4(mc.y, m.v + 4);
+        unpack4(vc.x, v.v);
+        unpack4(vc.y, v.v + 4);
+    } else if (n > 0) {
+        m = load8(static_cast<const float*>(a.m) + s);
+        v = load8(static_cast<const float*>(a.v) + s);
+        g = load_grad(gp, t.grad_dtype, e, n, wide_g);
+    } else {
+        return;
+    }
+    if (wide_p && n == 8) {
+        p = load8(t.param + e);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p.v[i] = i < n ? t.param[e + i] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        moments(__fmul_rn(g.v[i], gs), m.v[i], v.v[i], mb, vb, a);
+        p.v[i] = stepped(p.v[i], m.v[i], v.v[i], shrink, a);
+    }
+    if (wide_p && n == 8) {
+        store8(t.param + e, p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) t.param[e + i] = p.v[i];
+    }
+    if (t.copy) {
+        if (n == 8 && (reinterpret_cast<uintptr_t>(t.copy) & 15) == 0) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = narrow1(p.v[2 * i], a.copy_dtype) | (uint32_t)narrow1(p.v[2 * i + 1], a.copy_dtype) << 16;
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(t.copy) + e) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) store_copy(t, e + i, p.v[i], a.copy_dtype);
+        }
+    }
+    if (BITS == 32) {
+        store8(static_cast<float*>(a.m) + s, m);
+        store8(static_cast<float*>(a.v) + s, v);
+        return;
+    }
+    uint32_t spoilt_m, spoilt_v;
+    const float ms = warp_scale(m.v, spoilt_m), vs = warp_scale(v.v, spoilt_v), im = 1.0f / ms, iv = 1.0f / vs;
+    const uint32_t h = hash8(s, a.key);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t y = own_bits(h, odd(i));
+        m.v[i] = rounded(m.v[i] * im, dither_m(y));
+        v.v[i] = rounded_up(v.v[i] * iv, dither_v(y));
+    }
+    spoil(m.v, spoilt_m);
+    spoil(v.v, spoilt_v);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s) =
+        make_uint2(pack4(m.v[0], m.v[1], m.v[2], m.v[3]), pack4(m.v[4], m.v[5], m.v[6], m.v[7]));
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s) =
+        make_uint2(pack4(v.v[0], v.v[1], v.v[2], v.v[3]), pack4(v.v[4], v.v[5], v.v[6], v.v[7]));
+    if (threadIdx.x % 32 == 0) {
+        a.m_scale[s / kBlock] = ms;
+        a.v_scale[s / kBlock] = vs;
+    }
+}
+
+// A block of a tensor with a mask.  A pruned layer keeps a tenth to a half of its elements, all over the
+// block: the warp lists them, and its lanes take the listed ones in turn, so that the arithmetic is done
+// for kept elements only.  The others' states are zero and stay so.
+template <int BITS>
+__device__ __forceinline__ void masked_block(const TensorEntry& t, const void* gp, uint32_t index, uint32_t le, float gs,
+                                             float shrink, uint8_t* list, const AdamArgs& a) {
+    const int lane = threadIdx.x % 32;
+    const uint32_t keep = kept8(t, index, le, in_tensor(t, index, le));
+    uint32_t upto = __popc(keep);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t below = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += below;
+    }
+    const int count = __shfl_sync(0xffffffffu, upto, 31);
+    uint32_t at = upto - __popc(keep);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (keep >> i & 1) list[at++] = (uint8_t)(lane * 8 + i);
+    __syncwarp();
+    const int64_t e0 = (int64_t)index * kChunk + (le - lane * 8), s0 = t.state + e0;
+    float mb = a.b1, vb = a.b2;
+    if (BITS == 8) {
+        mb *= a.m_scale[s0 / kBlock];
+        vb *= a.v_scale[s0 / kBlock];
+    }
+    constexpr int R = 8;                  // of 32 elements: a block's 256 at most
+    const auto element = [&](int r) { return (uint32_t)list[min(r * 32 + lane, count - 1)]; };
+    float g[R], p[R], m[R], v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = v[r] = 0.0f;
+        if (r * 32 >= count) continue;    // the whole warp
+        const uint32_t el = element(r);
+        g[r] = widen1(gp, e0 + el, t.grad_dtype);
+        p[r] = t.param[e0 + el];
+        if (BITS == 8) {
+            m[r] = unpack1(static_cast<const uint8_t*>(a.m)[s0 + el]);
+            v[r] = unpack1(static_cast<const uint8_t*>(a.v)[s0 + el]);
+        } else {
+            m[r] = static_cast<const float*>(a.m)[s0 + el];
+            v[r] = static_cast<const float*>(a.v)[s0 + el];
+        }
+    }
+    __syncwarp();                         // lanes past the last element have read it again, for the scale
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r * 32 >= count) continue;
+        moments(__fmul_rn(g[r], gs), m[r], v[r], mb, vb, a);
+        const float stepped_p = stepped(p[r], m[r], v[r], shrink, a);
+        if (r * 32 + lane < count) {
+            const uint32_t el = element(r);
+            t.param[e0 + el] = stepped_p;
+            if (t.copy) store_copy(t, e0 + el, stepped_p, a.copy_dtype);
+            if (BITS == 32) {
+                static_cast<float*>(a.m)[s0 + el] = m[r];
+                static_cast<float*>(a.v)[s0 + el] = v[r];
+            }
+        }
+    }
+    if (BITS == 32) return;
+    uint32_t spoilt_m, spoilt_v;
+    const float ms = warp_scale(m, spoilt_m), vs = warp_scale(v, spoilt_v), im = 1.0f / ms, iv = 1.0f / vs;
+    uint32_t factor = 0;                  // lane i < 8: odd(i)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) factor = lane == i ? odd(i) : factor;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r * 32 >= count) continue;
+        const uint32_t el = element(r);
+        const uint32_t y = own_bits(hash8(s0 + el, a.key), __shfl_sync(0xffffffffu, factor, el & 7));
+        m[r] = rounded(m[r] * im, dither_m(y));
+        v[r] = rounded_up(v[r] * iv, dither_v(y));
+    }
+    spoil(m, spoilt_m);
+    spoil(v, spoilt_v);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r * 32 + lane >= count) continue;
+        static_cast<uint8_t*>(a.m)[s0 + element(r)] = pack1(m[r]);
+        static_cast<uint8_t*>(a.v)[s0 + element(r)] = pack1(v[r]);
+    }
+    if (lane == 0) {
+        a.m_scale[s0 / kBlock] = ms;
+        a.v_scale[s0 / kBlock] = vs;
+    }
+}
+
+// One chunk a CTA, kGroups blocks of 256 elements a warp.
 template <int BITS, int N>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
-                                                         uint32_t begin, uint32_t t0, Grads<N> grads, AdamArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
+                                                            uint32_t begin, uint32_t t0, Grads<N> grads, AdamArgs a) {
+    __shared__ uint8_t lists[kThreads / 32][kBlock];
     const ChunkEntry ce = chunks[begin + blockIdx.x];
     const void* gp = grads.at[ce.tensor - t0];
     if (!gp) return;                               // a tensor without a gradient is left alone
     const TensorEntry t = tensors[ce.tensor];
-    const int64_t e0 = (int64_t)ce.index * kChunk;
-    const int le = threadIdx.x * 8;
-    if (BITS == 8 && e0 + (le & ~(kBlock - 1)) >= t.numel) return;   // whole warps
-    const int64_t e = e0 + le, left = t.numel - e;
-    const int n = left < 8 ? (int)(left > 0 ? left : 0) : 8;
-    const uint32_t keep = kept8(t, e0, le, n);
-    const int64_t s = t.state + e;                 // of the states; they are padded to whole blocks
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
     const float shrink = fmaf(-a.lr, t.decay, 1.0f);
-    const bool wide_p = n == 8 && (reinterpret_cast<uintptr_t>(t.param) & 31) == 0;
-
-    Vec8 g, p, m, v;
-    float ms = 1.0f, vs = 1.0f;
-    if (keep) {
-        if (BITS == 8) {
-            ms = a.m_scale[s / kBlock];
-            vs = a.v_scale[s / kBlock];
-            const uint2 mc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + s);
-            const uint2 vc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + s);
-            unpack4(mc.x, ms, m.v);
-            unpack4(mc.y, ms, m.v + 4);
-            unpack4(vc.x, vs, v.v);
-            unpack4(vc.y, vs, v.v + 4);
-        } else {
-            m = load8(static_cast<const float*>(a.m) + s);
-            v = load8(static_cast<const float*>(a.v) + s);
-        }
-        g = load_grad(gp, t.grad_dtype, e, n, wide_grad(gp, t.grad_dtype));
-        if (wide_p) {
-            p = load8(t.param + e);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p.v[i] = i < n ? t.param[e + i] : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool k = keep >> i & 1;
-            float mi = m.v[i], vi = v.v[i];
-            moments(__fmul_rn(g.v[i], gs), mi, vi, a);
-            const float pi = stepped(p.v[i], mi, vi, shrink, a);
-            m.v[i] = k ? mi : BITS == 8 ? 0.0f : m.v[i];
-            v.v[i] = k ? vi : BITS == 8 ? 0.0f : v.v[i];
-            p.v[i] = k ? pi : p.v[i];
-        }
-        if (wide_p) {
-            store8(t.param + e, p);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (keep >> i & 1) t.param[e + i] = p.v[i];
-        }
-        if (t.copy) {
-            uint16_t* c = static_cast<uint16_t*>(t.copy) + e;
-            if (n == 8 && (reinterpret_cast<uintptr_t>(t.copy) & 15) == 0) {
-                uint32_t w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    w[i] = narrow1(p.v[2 * i], a.copy_dtype) | (uint32_t)narrow1(p.v[2 * i + 1], a.copy_dtype) << 16;
-                *reinterpret_cast<uint4*>(c) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < n) c[i] = narrow1(p.v[i], a.copy_dtype);
-            }
-        }
-        if (BITS == 32) {
-            store8(static_cast<float*>(a.m) + s, m);
-            store8(static_cast<float*>(a.v) + s, v);
-        }
-    }
-    if (BITS == 8) {
-        uint32_t largest_m = 0, largest_v = 0;
-        if (keep) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                largest_m = max(largest_m, finite_bits(m.v[i]));
-                largest_v = max(largest_v, finite_bits(v.v[i]));
-            }
-        }
-        ms = block_scale(__reduce_max_sync(0xffffffffu, largest_m));
-        vs = block_scale(__reduce_max_sync(0xffffffffu, largest_v));
-        if (threadIdx.x % 32 == 0) {
-            a.m_scale[s / kBlock] = ms;
-            a.v_scale[s / kBlock] = vs;
-        }
-        if (!keep) return;
-        const float im = 1.0f / ms, iv = 1.0f / vs;
-        // one hash for the lane's eight elements, times an odd constant for each: the first 32 bits of
-        // the fractions of the square roots of 2 to 19, made odd (mix has those of 23 and 29)
-        constexpr uint32_t odd[8] = {0x6A09E667u, 0xBB67AE85u, 0x3C6EF373u, 0xA54FF53Bu,
-                                     0x510E527Fu, 0x9B05688Du, 0x1F83D9ABu, 0x5BE0CD19u};
-        const uint32_t h = mix((uint32_t)(s >> 3) * 0x9E3779B1u ^ a.key);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t y = h * odd[i];
-            y ^= y >> 15;
-            m.v[i] = rounded<false>(m.v[i] * im, y & 0xFFFFu);
-            v.v[i] = rounded<true>(v.v[i] * iv, y >> 16);
-        }
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s) =
-            make_uint2(pack4(m.v[0], m.v[1], m.v[2], m.v[3]), pack4(m.v[4], m.v[5], m.v[6], m.v[7]));
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s) =
-            make_uint2(pack4(v.v[0], v.v[1], v.v[2], v.v[3]), pack4(v.v[4], v.v[5], v.v[6], v.v[7]));
+    const bool wide_g = wide_grad(gp, t.grad_dtype), wide_p = (reinterpret_cast<uintptr_t>(t.param) & 31) == 0;
+    const int64_t e0 = (int64_t)ce.index * kChunk;
+#pragma unroll 1
+    for (int k = 0; k < kGroups; ++k) {
+        const uint32_t le = (k * kThreads + threadIdx.x) * 8;
+        if (e0 + (le & ~(kBlock - 1)) >= t.numel) return;       // whole warps
+        if (t.taps)
+            masked_block<BITS>(t, gp, ce.index, le, gs, shrink, lists[threadIdx.x / 32], a);
+        else
+            dense_block<BITS>(t, gp, e0 + le, in_tensor(t, ce.index, le), gs, shrink, wide_g, wide_p, a);
     }
 }
 

@@ -33,6 +33,19 @@ def workspace_bytes(x_shape, groups: int, dtype=torch.float32, backward: bool = 
     return int(v.value)
 
 
+PLAN_KEYS = ("path", "channels", "columns", "pixels", "held", "cluster", "ctas", "sets")
+
+
+def plan(x_shape, groups: int, dtype=torch.float32, backward: bool = False, align: int = 16) -> dict:
+    """How a call on activations of this shape and type runs (pp_group_norm_plan): ``path`` 2 resident, 1
+    streamed.  ``align``: the largest power of two that divides all addresses and strides in bytes."""
+    n, c, h, w = x_shape
+    info = (ctypes.c_int64 * len(PLAN_KEYS))()
+    _lib.check("pp_group_norm_plan", _lib.load().pp_group_norm_plan(
+        _DT[dtype], n, h * w, c, groups, 1 if backward else 0, align, info, len(PLAN_KEYS)))
+    return dict(zip(PLAN_KEYS, (int(v) for v in info)))
+
+
 def _act(act: str) -> int:
     if act not in ACTS:
         raise ValueError(f"act must be one of {', '.join(ACTS)}")
