@@ -17,6 +17,7 @@
 #include <cstdint>
 #include <cstring>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "patconv.h"
@@ -25,8 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBlock = 256;               // elements that share a scale: a warp's, eight a lane
-constexpr int kGroups = 2;                // blocks of a warp, and eights of a thread, in a chunk
-constexpr int kChunk = kThreads * 8 * kGroups;   // elements of a CTA's chunk; 4096 = 455 * 9 + 1
+constexpr int kChunk = kThreads * 8;      // elements of a CTA's chunk: a block a warp, eight a lane
 constexpr int kFewGrads = 64, kMaxGrads = 448;   // 448 addresses and the rest are below 4 KB of arguments
 constexpr int64_t kMaxNumel = int64_t(1) << 40;
 
@@ -53,7 +53,8 @@ struct Grads {
 
 struct pp_tensors {
     std::vector<TensorEntry> tensors;
-    std::vector<uint32_t> first_chunk;    // per tensor, and the number of all chunks
+    std::vector<uint32_t> first_chunk;    // chunks of the tensors before each (whole launches matter), and of all
+    std::vector<uint32_t> masked_end;     // per launch: the end of its chunks of tensors with masks, which come first
     std::vector<uint8_t> image;           // tensors | chunks | counter and partial sums (zero)
     size_t off_chunks = 0, off_sums = 0;
     int64_t state_elements = 0;
@@ -64,7 +65,8 @@ struct pp_tensors {
 
 namespace {
 
-constexpr int kSumCtas = 152 * 8;           // most CTAs of the norm's kernel: partial sums
+constexpr int kSMs = 152;
+constexpr int kSumCtas = kSMs * 8;           // most CTAs of the norm's kernel: partial sums
 
 struct Vec8 {
     float v[8];
@@ -102,25 +104,6 @@ __device__ __forceinline__ uint16_t narrow1(float f, int dtype) {
     return __bfloat16_as_ushort(__float2bfloat16_rn(f));
 }
 
-// eight gradients from element e; n of them are in the tensor (the others read as zero)
-__device__ __forceinline__ Vec8 load_grad(const void* g, int dtype, int64_t e, int n, bool wide) {
-    Vec8 r;
-    if (wide && n == 8) {
-        if (dtype == PP_F32) return load8(static_cast<const float*>(g) + e);
-        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(g) + e));
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = widen(u[i], dtype);
-            r.v[2 * i] = f.x;
-            r.v[2 * i + 1] = f.y;
-        }
-        return r;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = i < n ? widen1(g, e + i, dtype) : 0.0f;
-    return r;
-}
 // whether eight-element accesses from a tensor's start are aligned
 __device__ __forceinline__ bool wide_grad(const void* g, int dtype) {
     return (reinterpret_cast<uintptr_t>(g) & (dtype == PP_F32 ? 31 : 15)) == 0;
@@ -132,9 +115,9 @@ __device__ __forceinline__ uint32_t kept8(const TensorEntry& t, uint32_t index, 
     if (n <= 0) return 0;
     const uint32_t in = n >= 8 ? 0xFFu : (1u << n) - 1;
     if (!t.taps) return in;
-    static_assert(kChunk % 9 == 1, "a chunk starts at element index % 9 of a kernel");
-    const uint32_t local = index % 9 + le, r = local % 9;
-    const int64_t k = (int64_t)index * (kChunk / 9) + index / 9 + local / 9;
+    const uint32_t past = index * (kChunk % 9);     // of whole kernels, by the chunks before this one
+    const uint32_t local = past % 9 + le, r = local % 9;
+    const int64_t k = (int64_t)index * (kChunk / 9) + past / 9 + local / 9;
     const uint32_t a = t.taps[k] & 0x1FFu;
     const uint32_t b = 9 * (k + 1) < t.numel ? t.taps[k + 1] & 0x1FFu : 0;
     return ((a | b << 9) >> r) & in;
@@ -147,41 +130,74 @@ __device__ __forceinline__ int in_tensor(const TensorEntry& t, uint32_t index, u
 
 // ------------------------------------------------------------------------------------- the norm
 
+// Eight gradients as they lie in memory.
+template <int GRAD>
+struct RawGrad {
+    uint4 w[GRAD == PP_F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const void* g, int64_t e) {
+        if constexpr (GRAD == PP_F32) {
+            const Vec8 x = load8(static_cast<const float*>(g) + e);
+            memcpy(w, &x, 32);
+        } else {
+            w[0] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(g) + e));
+        }
+    }
+    __device__ __forceinline__ float2 pair(int i) const {
+        const uint4 q = w[GRAD == PP_F32 ? i / 2 : 0];
+        if constexpr (GRAD == PP_F32)
+            return i % 2 ? make_float2(__uint_as_float(q.z), __uint_as_float(q.w)) : make_float2(__uint_as_float(q.x), __uint_as_float(q.y));
+        return widen(i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w, GRAD);
+    }
+};
 // Sum over a CTA's chunks of (g f)^2 for a factor f: per thread in fp32 over at most a few hundred
-// squares, then over the CTA.  A thread's masks and gradients of a chunk are all asked for before the
-// first is used.
+// squares, then over the CTA.
 template <int N>
-__device__ float chunk_squares(const TensorEntry* tensors, const ChunkEntry* chunks, uint32_t begin, uint32_t end,
-                               uint32_t t0, const Grads<N>& grads, float factor, float* smem) {
+__device__ __forceinline__ float chunk_squares(const TensorEntry* tensors, const ChunkEntry* chunks, uint32_t begin, uint32_t end,
+                                               uint32_t t0, const Grads<N>& grads, float factor, float* smem) {
     float sum = 0.0f;
-    for (uint32_t c = begin + blockIdx.x; c < end; c += gridDim.x) {
-        const ChunkEntry ce = chunks[c];
+    uint32_t c = begin + blockIdx.x;
+    ChunkEntry next{t0, 0};
+    if (c < end) next = chunks[c];
+    const uint32_t le = threadIdx.x * 8;
+#pragma unroll 1
+    for (; c < end; c += gridDim.x) {
+        const ChunkEntry ce = next;
+        if (c + gridDim.x < end) next = chunks[c + gridDim.x];
         const void* g = grads.at[ce.tensor - t0];
         if (!g) continue;
-        const TensorEntry t = tensors[ce.tensor];
-        const bool wide = wide_grad(g, t.grad_dtype);
-        uint32_t keep[kGroups];
-        Vec8 v[kGroups];
+        const TensorEntry& t = tensors[ce.tensor];
+        const int n = in_tensor(t, ce.index, le), dtype = t.grad_dtype;
+        const uint32_t keep = kept8(t, ce.index, le, n);
+        const int64_t e = (int64_t)ce.index * kChunk + le;
+        if (!keep) continue;
+        float x[8];
+        if (n == 8 && wide_grad(g, dtype)) {
+            if (dtype == PP_F32) {
+                const Vec8 v = load8(static_cast<const float*>(g) + e);
 #pragma unroll
-        for (int k = 0; k < kGroups; ++k) {
-            const uint32_t le = (k * kThreads + threadIdx.x) * 8;
-            keep[k] = kept8(t, ce.index, le, in_tensor(t, ce.index, le));
-        }
+                for (int i = 0; i < 8; ++i) x[i] = v.v[i];
+            } else {
+                RawGrad<PP_F16> raw;
+                raw.load(g, e);
+                const uint32_t w[4] = {raw.w[0].x, raw.w[0].y, raw.w[0].z, raw.w[0].w};
 #pragma unroll
-        for (int k = 0; k < kGroups; ++k) {
-            const uint32_t le = (k * kThreads + threadIdx.x) * 8;
-            if (keep[k]) v[k] = load_grad(g, t.grad_dtype, (int64_t)ce.index * kChunk + le, in_tensor(t, ce.index, le), wide);
-        }
-#pragma unroll
-        for (int k = 0; k < kGroups; ++k) {
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = keep[k] >> i & 1 ? v[k].v[i] * factor : 0.0f;
-                s = fmaf(x, x, s);
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = widen(w[i], dtype);
+                    x[2 * i] = f.x;
+                    x[2 * i + 1] = f.y;
+                }
             }
-            sum += s;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = keep >> i & 1 ? widen1(g, e + i, dtype) : 0.0f;
         }
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = keep >> i & 1 ? x[i] * factor : 0.0f;
+            s = fmaf(y, y, s);
+        }
+        sum += s;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -199,7 +215,7 @@ __device__ float chunk_squares(const TensorEntry* tensors, const ChunkEntry* chu
 // they may have been rounded away, or above 2^120) are summed again with the gradients times 2^64 or
 // 2^-64, so that the norm holds over fp32's whole range of gradients.
 template <int N>
-__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
+__global__ void __launch_bounds__(kThreads, 8) grad_norm_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
                                                              uint32_t begin, uint32_t end, uint32_t t0, Grads<N> grads,
                                                              double* sums, unsigned* counter, unsigned first_sum,
                                                              unsigned all_sums, float max_norm, float* out) {
@@ -267,11 +283,39 @@ __device__ __forceinline__ void moments(float g, float& m, float& v, float mb, f
     m = __fadd_rn(__fmul_rn(m, mb), __fmul_rn(g, a.c1));
     v = __fadd_rn(__fmul_rn(v, vb), __fmul_rn(__fmul_rn(g, g), a.c2));
 }
+// Pairs of values, two to an instruction.  The explicit rounding keeps products and sums apart.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ void moments2(float2 g, float2& m, float2& v, float mb, float vb, const AdamArgs& a) {
+    m = add2(mul2(m, both(mb)), mul2(g, both(a.c1)));
+    v = add2(mul2(v, both(vb)), mul2(mul2(g, g), both(a.c2)));
+}
 // 2^-126 keeps the root in fp32's normal range, where the approximations flush nothing: a root below
 // 2^-63 is far below any eps in use, and with eps = 0 it makes 0 / 0 zero.
 __device__ __forceinline__ float stepped(float p, float m, float v, float shrink, const AdamArgs& a) {
     const float den = approx_sqrt(fmaf(v, a.inv_bc2, 0x1p-126f)) + a.eps;
     return fmaf(-a.step_size, m * approx_rcp(den), p * shrink);
+}
+
+__device__ __forceinline__ float2 stepped2(float2 p, float2 m, float2 v, float shrink, const AdamArgs& a) {
+    const float2 w = fma2(v, both(a.inv_bc2), both(0x1p-126f));
+    const float2 den = add2(make_float2(approx_sqrt(w.x), approx_sqrt(w.y)), both(a.eps));
+    const float2 u = mul2(m, make_float2(approx_rcp(den.x), approx_rcp(den.y)));
+    return fma2(both(-a.step_size), u, mul2(p, both(shrink)));
 }
 
 __host__ __device__ inline uint32_t mix(uint32_t x) {
@@ -289,6 +333,9 @@ __device__ __forceinline__ float block_scale(uint32_t largest) {
     return __uint_as_float((uint32_t)(field < 1 ? 1 : field) << 23);
 }
 
+// the reciprocal of a power of two between 2^-126 and 2^126
+__device__ __forceinline__ float inverse_scale(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
+
 // A finite value over its block's scale, rounded to one of its two neighbours in e4m3 by the dither: 16
 // random bits, then a half, in the place of the bits below the format's three, which are filled up by it
 // and cut off.  Below 2^-6 the format's grid is that of [2^-6, 2^-5), so 2^-6 is added for the cut.
@@ -300,6 +347,18 @@ __device__ __forceinline__ float rounded_up(float t, uint32_t dither) {   // not
     const float small = t < 0x1p-6f ? 0x1p-6f : 0.0f;
     const float w = __uint_as_float((__float_as_uint(__fadd_rn(t, small)) + dither) & 0xFFF00000u) - small;
     return t > 0.0f ? fmaxf(w, 0x1p-9f) : w;
+}
+__device__ __forceinline__ float cut(float t, uint32_t dither) { return __uint_as_float((__float_as_uint(t) + dither) & 0xFFF00000u); }
+__device__ __forceinline__ float2 rounded2(float2 t, uint32_t dx, uint32_t dy) {
+    const float2 small = make_float2(fabsf(t.x) < 0x1p-6f ? copysignf(0x1p-6f, t.x) : 0.0f,
+                                     fabsf(t.y) < 0x1p-6f ? copysignf(0x1p-6f, t.y) : 0.0f);
+    t = add2(t, small);
+    return add2(make_float2(cut(t.x, dx), cut(t.y, dy)), make_float2(-small.x, -small.y));
+}
+__device__ __forceinline__ float2 rounded_up2(float2 t, uint32_t dx, uint32_t dy) {
+    const float2 small = make_float2(t.x < 0x1p-6f ? 0x1p-6f : 0.0f, t.y < 0x1p-6f ? 0x1p-6f : 0.0f);
+    const float2 u = add2(t, small), w = add2(make_float2(cut(u.x, dx), cut(u.y, dy)), make_float2(-small.x, -small.y));
+    return make_float2(t.x > 0.0f ? fmaxf(w.x, 0x1p-9f) : w.x, t.y > 0.0f ? fmaxf(w.y, 0x1p-9f) : w.y);
 }
 __device__ __forceinline__ uint32_t dither_m(uint32_t y) { return (y << 4 & 0xFFFF0u) | 8; }
 __device__ __forceinline__ uint32_t dither_v(uint32_t y) { return (y >> 12 & 0xFFFF0u) | 8; }
@@ -380,198 +439,284 @@ __device__ __forceinline__ void store_copy(const TensorEntry& t, int64_t e, floa
     static_cast<uint16_t*>(t.copy)[e] = narrow1(p, dtype);
 }
 
-// A block of a tensor without a mask: eight consecutive elements a lane, n of them in the tensor.
+// A block of any tensor, eight consecutive elements a lane, of which those in `keep` take part: the ends of
+// tensors, tensors that are not aligned, masks that keep most of a block.
 template <int BITS>
-__device__ __forceinline__ void dense_block(const TensorEntry& t, const void* gp, int64_t e, int n, float gs, float shrink,
-                                            bool wide_g, bool wide_p, const AdamArgs& a) {
+__device__ __noinline__ void any_block(const TensorEntry t, const void* gp, int64_t e, uint32_t keep, float gs, float shrink,
+                                       const AdamArgs a) {
     const int64_t s = t.state + e;
-    Vec8 g, p, m, v;
-    float mb = a.b1, vb = a.b2;
+    float m[8] = {}, v[8] = {}, mb = a.b1, vb = a.b2;
     if (BITS == 8) {
         mb *= a.m_scale[s / kBlock];
         vb *= a.v_scale[s / kBlock];
-        const uint2 mc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + s);
-        const uint2 vc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + s);
-        g = load_grad(gp, t.grad_dtype, e, n, wide_g);
-        unpack4(mc.x, m.v);
-        unpack4(mc.y, m.v + 4);
-        unpack4(vc.x, v.v);
-        unpack4(vc.y, v.v + 4);
-    } else if (n > 0) {
-        m = load8(static_cast<const float*>(a.m) + s);
-        v = load8(static_cast<const float*>(a.v) + s);
-        g = load_grad(gp, t.grad_dtype, e, n, wide_g);
-    } else {
-        return;
-    }
-    if (wide_p && n == 8) {
-        p = load8(t.param + e);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p.v[i] = i < n ? t.param[e + i] : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        moments(__fmul_rn(g.v[i], gs), m.v[i], v.v[i], mb, vb, a);
-        p.v[i] = stepped(p.v[i], m.v[i], v.v[i], shrink, a);
-    }
-    if (wide_p && n == 8) {
-        store8(t.param + e, p);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) t.param[e + i] = p.v[i];
-    }
-    if (t.copy) {
-        if (n == 8 && (reinterpret_cast<uintptr_t>(t.copy) & 15) == 0) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = narrow1(p.v[2 * i], a.copy_dtype) | (uint32_t)narrow1(p.v[2 * i + 1], a.copy_dtype) << 16;
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(t.copy) + e) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (!(keep >> i & 1)) continue;
+        if constexpr (BITS == 8) {
+            m[i] = unpack1(static_cast<const uint8_t*>(a.m)[s + i]);
+            v[i] = unpack1(static_cast<const uint8_t*>(a.v)[s + i]);
         } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) store_copy(t, e + i, p.v[i], a.copy_dtype);
+            m[i] = static_cast<const float*>(a.m)[s + i];
+            v[i] = static_cast<const float*>(a.v)[s + i];
+        }
+        moments(__fmul_rn(widen1(gp, e + i, t.grad_dtype), gs), m[i], v[i], mb, vb, a);
+        const float p = stepped(t.param[e + i], m[i], v[i], shrink, a);
+        t.param[e + i] = p;
+        if (t.copy) store_copy(t, e + i, p, a.copy_dtype);
+        if constexpr (BITS == 32) {
+            static_cast<float*>(a.m)[s + i] = m[i];
+            static_cast<float*>(a.v)[s + i] = v[i];
         }
     }
-    if (BITS == 32) {
-        store8(static_cast<float*>(a.m) + s, m);
-        store8(static_cast<float*>(a.v) + s, v);
-        return;
-    }
+    if (BITS == 32) return;
     uint32_t spoilt_m, spoilt_v;
-    const float ms = warp_scale(m.v, spoilt_m), vs = warp_scale(v.v, spoilt_v), im = 1.0f / ms, iv = 1.0f / vs;
+    const float ms = warp_scale(m, spoilt_m), vs = warp_scale(v, spoilt_v), im = inverse_scale(ms), iv = inverse_scale(vs);
     const uint32_t h = hash8(s, a.key);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        if (!(keep >> i & 1)) continue;
         const uint32_t y = own_bits(h, odd(i));
-        m.v[i] = rounded(m.v[i] * im, dither_m(y));
-        v.v[i] = rounded_up(v.v[i] * iv, dither_v(y));
+        static_cast<uint8_t*>(a.m)[s + i] = pack1(spoilt_m >> i & 1 ? NAN : rounded(m[i] * im, dither_m(y)));
+        static_cast<uint8_t*>(a.v)[s + i] = pack1(spoilt_v >> i & 1 ? NAN : rounded_up(v[i] * iv, dither_v(y)));
     }
-    spoil(m.v, spoilt_m);
-    spoil(v.v, spoilt_v);
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s) =
-        make_uint2(pack4(m.v[0], m.v[1], m.v[2], m.v[3]), pack4(m.v[4], m.v[5], m.v[6], m.v[7]));
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s) =
-        make_uint2(pack4(v.v[0], v.v[1], v.v[2], v.v[3]), pack4(v.v[4], v.v[5], v.v[6], v.v[7]));
     if (threadIdx.x % 32 == 0) {
         a.m_scale[s / kBlock] = ms;
         a.v_scale[s / kBlock] = vs;
     }
 }
 
-// A block of a tensor with a mask.  A pruned layer keeps a tenth to a half of its elements, all over the
-// block: the warp lists them, and its lanes take the listed ones in turn, so that the arithmetic is done
-// for kept elements only.  The others' states are zero and stay so.
-template <int BITS>
-__device__ __forceinline__ void masked_block(const TensorEntry& t, const void* gp, uint32_t index, uint32_t le, float gs,
-                                             float shrink, uint8_t* list, const AdamArgs& a) {
+// A whole block of an aligned tensor without a mask, eight consecutive elements a lane.
+template <int BITS, int GRAD>
+__device__ __forceinline__ void dense_block(const TensorEntry& t, const void* gp, int64_t e, float gs, float shrink, const AdamArgs& a) {
+    const int64_t s = t.state + e;
+    float m[8], v[8], mb = a.b1, vb = a.b2;
+    uint2 m8, v8;
+    RawGrad<GRAD> g;
+    if constexpr (BITS == 8) {
+        m8 = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + s));
+        v8 = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + s));
+        mb *= a.m_scale[s / kBlock];
+        vb *= a.v_scale[s / kBlock];
+    } else {
+        const Vec8 x = load8(static_cast<const float*>(a.m) + s), y = load8(static_cast<const float*>(a.v) + s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            m[i] = x.v[i];
+            v[i] = y.v[i];
+        }
+    }
+    g.load(gp, e);
+    Vec8 p = load8(t.param + e);
+    if constexpr (BITS == 8) {
+        unpack4(m8.x, m);
+        unpack4(m8.y, m + 4);
+        unpack4(v8.x, v);
+        unpack4(v8.y, v + 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float2 mi = make_float2(m[2 * i], m[2 * i + 1]), vi = make_float2(v[2 * i], v[2 * i + 1]);
+        moments2(mul2(g.pair(i), both(gs)), mi, vi, mb, vb, a);
+        const float2 pi = stepped2(make_float2(p.v[2 * i], p.v[2 * i + 1]), mi, vi, shrink, a);
+        m[2 * i] = mi.x, m[2 * i + 1] = mi.y, v[2 * i] = vi.x, v[2 * i + 1] = vi.y, p.v[2 * i] = pi.x, p.v[2 * i + 1] = pi.y;
+    }
+    store8(t.param + e, p);
+    if (t.copy) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) store_copy(t, e + i, p.v[i], a.copy_dtype);
+    }
+    if constexpr (BITS == 32) {
+        Vec8 x, y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x.v[i] = m[i];
+            y.v[i] = v[i];
+        }
+        store8(static_cast<float*>(a.m) + s, x);
+        store8(static_cast<float*>(a.v) + s, y);
+    } else {
+        uint32_t spoilt_m, spoilt_v;
+        const float ms = warp_scale(m, spoilt_m), vs = warp_scale(v, spoilt_v);
+        const float2 im = both(inverse_scale(ms)), iv = both(inverse_scale(vs));
+        const uint32_t h = hash8(s, a.key);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = own_bits(h, odd(2 * i)), y = own_bits(h, odd(2 * i + 1));
+            const float2 mi = rounded2(mul2(make_float2(m[2 * i], m[2 * i + 1]), im), dither_m(x), dither_m(y));
+            const float2 vi = rounded_up2(mul2(make_float2(v[2 * i], v[2 * i + 1]), iv), dither_v(x), dither_v(y));
+            m[2 * i] = mi.x, m[2 * i + 1] = mi.y, v[2 * i] = vi.x, v[2 * i + 1] = vi.y;
+        }
+        spoil(m, spoilt_m);
+        spoil(v, spoilt_v);
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s) = make_uint2(pack4(m[0], m[1], m[2], m[3]), pack4(m[4], m[5], m[6], m[7]));
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s) = make_uint2(pack4(v[0], v[1], v[2], v[3]), pack4(v[4], v[5], v[6], v[7]));
+        if (threadIdx.x % 32 == 0) {
+            a.m_scale[s / kBlock] = ms;
+            a.v_scale[s / kBlock] = vs;
+        }
+    }
+}
+
+// A tensor with a mask.  A pruned layer keeps a tenth to a half of its elements, all over a block: the warp
+// lists them, and its lanes take the listed ones in turn, so that the arithmetic is done for kept elements
+// only.  The others' states are zero and stay so.
+
+// Lists a block's kept elements (eight a lane, their bits in `keep`); returns how many there are.
+__device__ __forceinline__ int list_kept(uint32_t keep, uint8_t* list) {
     const int lane = threadIdx.x % 32;
-    const uint32_t keep = kept8(t, index, le, in_tensor(t, index, le));
     uint32_t upto = __popc(keep);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const uint32_t below = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += below;
     }
-    const int count = __shfl_sync(0xffffffffu, upto, 31);
-    uint32_t at = upto - __popc(keep);
-    __syncwarp();
+    uint8_t* to = list + (upto - __popc(keep));
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (keep >> i & 1) list[at++] = (uint8_t)(lane * 8 + i);
-    __syncwarp();
-    const int64_t e0 = (int64_t)index * kChunk + (le - lane * 8), s0 = t.state + e0;
-    float mb = a.b1, vb = a.b2;
-    if (BITS == 8) {
-        mb *= a.m_scale[s0 / kBlock];
-        vb *= a.v_scale[s0 / kBlock];
+        if (keep >> i & 1) *to++ = (uint8_t)(lane * 8 + i);
+    return __shfl_sync(0xffffffffu, upto, 31);
+}
+
+// What the lanes read of a block's `count` listed elements, R rounds of 32 at most; lanes past the last read
+// it again.
+template <int BITS, int R>
+struct Listed {
+    float p[R], m[R], v[R], ms, vs;
+    uint32_t g[R];                                // as they lie in memory, and m and v of 8 bits too: a conversion would
+                                                  // wait for a round's values before the next round is asked for
+    __device__ __forceinline__ static uint32_t element(const uint8_t* list, int count, int r) {
+        return list[min(r * 32 + (int)(threadIdx.x % 32), count - 1)];
     }
-    constexpr int R = 8;                  // of 32 elements: a block's 256 at most
-    const auto element = [&](int r) { return (uint32_t)list[min(r * 32 + lane, count - 1)]; };
-    float g[R], p[R], m[R], v[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        m[r] = v[r] = 0.0f;
-        if (r * 32 >= count) continue;    // the whole warp
-        const uint32_t el = element(r);
-        g[r] = widen1(gp, e0 + el, t.grad_dtype);
-        p[r] = t.param[e0 + el];
-        if (BITS == 8) {
-            m[r] = unpack1(static_cast<const uint8_t*>(a.m)[s0 + el]);
-            v[r] = unpack1(static_cast<const uint8_t*>(a.v)[s0 + el]);
-        } else {
-            m[r] = static_cast<const float*>(a.m)[s0 + el];
-            v[r] = static_cast<const float*>(a.v)[s0 + el];
+    // e0: the block's first element
+    __device__ __forceinline__ void load(const TensorEntry& t, const void* gp, int64_t e0, const uint8_t* list, int count,
+                                         const AdamArgs& a) {
+        const int64_t s0 = t.state + e0;
+        const float* params = t.param + e0;
+        const bool g32 = t.grad_dtype == PP_F32;
+        ms = vs = 1.0f;
+        if constexpr (BITS == 8) {
+            ms = a.m_scale[s0 / kBlock];
+            vs = a.v_scale[s0 / kBlock];
         }
-    }
-    __syncwarp();                         // lanes past the last element have read it again, for the scale
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (r * 32 >= count) continue;
-        moments(__fmul_rn(g[r], gs), m[r], v[r], mb, vb, a);
-        const float stepped_p = stepped(p[r], m[r], v[r], shrink, a);
-        if (r * 32 + lane < count) {
-            const uint32_t el = element(r);
-            t.param[e0 + el] = stepped_p;
-            if (t.copy) store_copy(t, e0 + el, stepped_p, a.copy_dtype);
-            if (BITS == 32) {
-                static_cast<float*>(a.m)[s0 + el] = m[r];
-                static_cast<float*>(a.v)[s0 + el] = v[r];
+        for (int r = 0; r < R; ++r) {
+            m[r] = v[r] = 0.0f;
+            if (r * 32 >= count) continue;        // the whole warp
+            const uint32_t el = element(list, count, r);
+            if (g32)
+                g[r] = (static_cast<const uint32_t*>(gp) + e0)[el];
+            else
+                g[r] = (static_cast<const uint16_t*>(gp) + e0)[el];
+            p[r] = params[el];
+            if constexpr (BITS == 8) {
+                m[r] = __uint_as_float((static_cast<const uint8_t*>(a.m) + s0)[el]);
+                v[r] = __uint_as_float((static_cast<const uint8_t*>(a.v) + s0)[el]);
+            } else {
+                m[r] = (static_cast<const float*>(a.m) + s0)[el];
+                v[r] = (static_cast<const float*>(a.v) + s0)[el];
             }
         }
     }
-    if (BITS == 32) return;
-    uint32_t spoilt_m, spoilt_v;
-    const float ms = warp_scale(m, spoilt_m), vs = warp_scale(v, spoilt_v), im = 1.0f / ms, iv = 1.0f / vs;
-    uint32_t factor = 0;                  // lane i < 8: odd(i)
+    __device__ __forceinline__ void step(const TensorEntry& t, int64_t e0, const uint8_t* list, int count, float gs, float shrink,
+                                         const AdamArgs& a) {
+        const int64_t s0 = t.state + e0;
+        const int lane = threadIdx.x % 32;
+        float* params = t.param + e0;
+        __syncwarp();                             // all lanes have read what the last one writes
 #pragma unroll
-    for (int i = 0; i < 8; ++i) factor = lane == i ? odd(i) : factor;
+        for (int r = 0; r < R; ++r) {
+            if (r * 32 >= count) continue;
+            if constexpr (BITS == 8) {
+                m[r] = unpack1((uint8_t)__float_as_uint(m[r]));
+                v[r] = unpack1((uint8_t)__float_as_uint(v[r]));
+            }
+            const float gr = t.grad_dtype == PP_F32 ? __uint_as_float(g[r]) : widen(g[r], t.grad_dtype).x;
+            moments(__fmul_rn(gr, gs), m[r], v[r], a.b1 * ms, a.b2 * vs, a);
+            const float to = stepped(p[r], m[r], v[r], shrink, a);
+            if (r * 32 + lane < count) {
+                const uint32_t el = element(list, count, r);
+                params[el] = to;
+                if (t.copy) store_copy(t, e0 + el, to, a.copy_dtype);
+                if constexpr (BITS == 32) {
+                    (static_cast<float*>(a.m) + s0)[el] = m[r];
+                    (static_cast<float*>(a.v) + s0)[el] = v[r];
+                }
+            }
+        }
+        if constexpr (BITS == 32) return;
+        uint32_t spoilt_m, spoilt_v;
+        ms = warp_scale(m, spoilt_m);
+        vs = warp_scale(v, spoilt_v);
+        const float im = inverse_scale(ms), iv = inverse_scale(vs);
+        uint32_t factor = 0;                      // lane i < 8 has odd(i)
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (r * 32 >= count) continue;
-        const uint32_t el = element(r);
-        const uint32_t y = own_bits(hash8(s0 + el, a.key), __shfl_sync(0xffffffffu, factor, el & 7));
-        m[r] = rounded(m[r] * im, dither_m(y));
-        v[r] = rounded_up(v[r] * iv, dither_v(y));
-    }
-    spoil(m, spoilt_m);
-    spoil(v, spoilt_v);
+        for (int i = 0; i < 8; ++i) factor = lane == i ? odd(i) : factor;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (r * 32 + lane >= count) continue;
-        static_cast<uint8_t*>(a.m)[s0 + element(r)] = pack1(m[r]);
-        static_cast<uint8_t*>(a.v)[s0 + element(r)] = pack1(v[r]);
+        for (int r = 0; r < R; ++r) {
+            if (r * 32 >= count) continue;
+            const uint32_t el = element(list, count, r);
+            const uint32_t y = own_bits(hash8(s0 + el, a.key), __shfl_sync(0xffffffffu, factor, el & 7));
+            m[r] = rounded(m[r] * im, dither_m(y));
+            v[r] = rounded_up(v[r] * iv, dither_v(y));
+        }
+        spoil(m, spoilt_m);
+        spoil(v, spoilt_v);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (r * 32 + lane >= count) continue;
+            const uint32_t el = element(list, count, r);
+            (static_cast<uint8_t*>(a.m) + s0)[el] = pack1(m[r]);
+            (static_cast<uint8_t*>(a.v) + s0)[el] = pack1(v[r]);
+        }
+        if (lane == 0) {
+            a.m_scale[s0 / kBlock] = ms;
+            a.v_scale[s0 / kBlock] = vs;
+        }
     }
-    if (lane == 0) {
-        a.m_scale[s0 / kBlock] = ms;
-        a.v_scale[s0 / kBlock] = vs;
-    }
-}
+};
 
-// One chunk a CTA, kGroups blocks of 256 elements a warp.
-template <int BITS, int N>
-__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
-                                                            uint32_t begin, uint32_t t0, Grads<N> grads, AdamArgs a) {
-    __shared__ uint8_t lists[kThreads / 32][kBlock];
+// A chunk a CTA, a block of 256 elements a warp: many light CTAs hide the tables' latency better than few
+// that look ahead.  MASKED: for chunks of tensors with masks.
+template <int BITS, int N, bool MASKED>
+__global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const TensorEntry* __restrict__ tensors,
+                                                            const ChunkEntry* __restrict__ chunks, uint32_t begin, uint32_t t0,
+                                                            Grads<N> grads, AdamArgs a) {
+    __shared__ uint8_t lists[MASKED ? kThreads / 32 : 1][kBlock];
     const ChunkEntry ce = chunks[begin + blockIdx.x];
     const void* gp = grads.at[ce.tensor - t0];
     if (!gp) return;                               // a tensor without a gradient is left alone
     const TensorEntry t = tensors[ce.tensor];
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
     const float shrink = fmaf(-a.lr, t.decay, 1.0f);
-    const bool wide_g = wide_grad(gp, t.grad_dtype), wide_p = (reinterpret_cast<uintptr_t>(t.param) & 31) == 0;
-    const int64_t e0 = (int64_t)ce.index * kChunk;
-#pragma unroll 1
-    for (int k = 0; k < kGroups; ++k) {
-        const uint32_t le = (k * kThreads + threadIdx.x) * 8;
-        if (e0 + (le & ~(kBlock - 1)) >= t.numel) return;       // whole warps
-        if (t.taps)
-            masked_block<BITS>(t, gp, ce.index, le, gs, shrink, lists[threadIdx.x / 32], a);
-        else
-            dense_block<BITS>(t, gp, e0 + le, in_tensor(t, ce.index, le), gs, shrink, wide_g, wide_p, a);
+    const uint32_t le = threadIdx.x * 8;
+    const int64_t e0 = (int64_t)ce.index * kChunk, warp = e0 + (le & ~(kBlock - 1));
+    if (warp >= t.numel) return;                   // whole warps
+    if constexpr (!MASKED) {
+        if (wide_grad(gp, t.grad_dtype) && (reinterpret_cast<uintptr_t>(t.param) & 31) == 0 && warp + kBlock <= t.numel) {
+            if (t.grad_dtype == PP_F32)
+                dense_block<BITS, PP_F32>(t, gp, e0 + le, gs, shrink, a);
+            else if (t.grad_dtype == PP_F16)
+                dense_block<BITS, PP_F16>(t, gp, e0 + le, gs, shrink, a);
+            else
+                dense_block<BITS, PP_BF16>(t, gp, e0 + le, gs, shrink, a);
+            return;
+        }
     }
+    const uint32_t keep = kept8(t, ce.index, le, in_tensor(t, ce.index, le));
+    if constexpr (MASKED) {
+        uint8_t* list = lists[threadIdx.x / 32];
+        const int count = list_kept(keep, list);
+        __syncwarp();
+        if (count <= 128) {
+            if (!count) return;                    // its states are zero and stay so
+            Listed<BITS, 4> x;
+            x.load(t, gp, warp, list, count, a);
+            x.step(t, warp, list, count, gs, shrink, a);
+            return;
+        }
+    }
+    any_block<BITS>(t, gp, e0 + le, keep, gs, shrink, a);
 }
 
 template <int N>
@@ -645,8 +790,16 @@ int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const
         h->image.assign(h->off_sums + 256 + std::max<size_t>(1, launches) * kSumCtas * sizeof(double), 0);
         if (n) memcpy(h->image.data(), h->tensors.data(), (size_t)n * sizeof(TensorEntry));
         ChunkEntry* c = reinterpret_cast<ChunkEntry*>(h->image.data() + h->off_chunks);
-        for (int i = 0; i < n; ++i)
-            for (uint32_t k = h->first_chunk[i]; k < h->first_chunk[i + 1]; ++k) *c++ = {(uint32_t)i, k - h->first_chunk[i]};
+        const ChunkEntry* const first = c;
+        for (int i = 0; i < n; i += kMaxGrads) {
+            const int end = std::min(n, i + kMaxGrads);
+            for (const bool masked : {true, false}) {
+                for (int k = i; k < end; ++k)
+                    if ((h->tensors[k].taps != nullptr) == masked)
+                        for (uint32_t j = 0; j < h->first_chunk[k + 1] - h->first_chunk[k]; ++j) *c++ = {(uint32_t)k, j};
+                if (masked) h->masked_end.push_back((uint32_t)(c - first));
+            }
+        }
         guard.h = nullptr;
         *out = h;
         return PP_OK;
@@ -762,22 +915,30 @@ int pp_adamw_step(pp_tensors_handle h, const void* const* grads, int state_bits,
     const int n = (int)h->tensors.size();
     for (int i = 0; i < n; i += kMaxGrads) {
         const int count = std::min(n - i, kMaxGrads);
-        const uint32_t begin = h->first_chunk[i], grid = h->first_chunk[i + count] - begin;
-        if (!grid) continue;
+        // chunks of tensors with masks, then those without: by one kernel where these are few, or all are at
+        // work at once
+        const uint32_t begin = h->first_chunk[i], end = h->first_chunk[i + count], masked = h->masked_end[i / kMaxGrads];
+        const bool one = masked > begin && ((end - masked) * 32 <= end - begin || end - begin <= kSMs * 5);
+        const uint32_t split = one ? end : masked;
         const bool few = count <= kFewGrads;
-        if (state_bits == 8 && few)
-            adamw_kernel<8, kFewGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
-                                                                 take<kFewGrads>(grads, i, count), a);
-        else if (state_bits == 8)
-            adamw_kernel<8, kMaxGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
-                                                                 take<kMaxGrads>(grads, i, count), a);
-        else if (few)
-            adamw_kernel<32, kFewGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
-                                                                  take<kFewGrads>(grads, i, count), a);
-        else
-            adamw_kernel<32, kMaxGrads><<<grid, kThreads, 0, st>>>(tensors, chunks, begin, (uint32_t)i,
-                                                                  take<kMaxGrads>(grads, i, count), a);
-        if (const int e = launched()) return e;
+        const auto launch = [&](auto bits, auto many, auto with_mask, uint32_t from, uint32_t to) {
+            constexpr int B = decltype(bits)::value, M = decltype(many)::value;
+            if (from == to) return PP_OK;
+            adamw_kernel<B, M, decltype(with_mask)::value><<<to - from, kThreads, 0, st>>>(
+                tensors, chunks, from, (uint32_t)i, take<M>(grads, i, count), a);
+            return (pp_status)launched();
+        };
+        const auto both = [&](auto bits, auto many) {
+            const int e = launch(bits, many, std::true_type(), begin, split);
+            return e ? e : (int)launch(bits, many, std::false_type(), split, end);
+        };
+        using Few = std::integral_constant<int, kFewGrads>;
+        using Many = std::integral_constant<int, kMaxGrads>;
+        using Eight = std::integral_constant<int, 8>;
+        using Full = std::integral_constant<int, 32>;
+        const int e = state_bits == 8 ? (few ? both(Eight(), Few()) : both(Eight(), Many()))
+                                      : (few ? both(Full(), Few()) : both(Full(), Many()));
+        if (e) return e;
     }
     return PP_OK;
 }
