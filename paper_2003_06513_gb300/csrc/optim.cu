@@ -1,9 +1,10 @@
 // Operators over many tensors at once, for masked retraining: the gradients' norm and AdamW steps.
 //
-// The tensors are cut into chunks of kChunk elements; a table in device memory, built once, says which
-// tensor a chunk belongs to and where that tensor's parameters, states and tap masks are.  The
-// gradients' addresses change from step to step and travel as kernel arguments, so that a step is one
-// launch however many tensors there are (of up to kMaxGrads; a launch for each kMaxGrads beyond).
+// The tensors are cut into chunks of kChunk elements; a table in device memory, built once, says where a
+// chunk's parameters, states and tap masks are: one reading of 64 bytes, 0.2 % of a step's traffic, before the
+// data.  The gradients' addresses change from step to step and travel as kernel arguments, so that a step
+// is one launch or two however many tensors there are (of up to kMaxGrads, and as many for each kMaxGrads
+// beyond).
 //
 // A tap mask is the packer's own form: nine bits for each 3x3 kernel.  An element that its mask leaves
 // out takes no part: its gradient is not used, whatever it is, and its parameter stays.
@@ -14,6 +15,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <cstdint>
 #include <cstring>
 #include <new>
@@ -27,21 +29,33 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlock = 256;               // elements that share a scale: a warp's, eight a lane
 constexpr int kChunk = kThreads * 8;      // elements of a CTA's chunk: a block a warp, eight a lane
+constexpr int kSpan = 8 * kChunk;         // elements that a CTA of the norm's kernel takes at a time
 constexpr int kFewGrads = 64, kMaxGrads = 448;   // 448 addresses and the rest are below 4 KB of arguments
 constexpr int64_t kMaxNumel = int64_t(1) << 40;
 
-struct TensorEntry {                      // of the device table
-    float* param;
-    void* copy;
-    const uint16_t* taps;
-    int64_t numel;
-    int64_t state;                        // first element in the states
-    float decay;
+struct Tensor {                           // what the handle keeps of one on the host
+    int64_t numel, state;                 // state: its first element in the states
     int grad_dtype;
+    bool masked;
 };
 
-struct ChunkEntry {
-    uint32_t tensor, index;
+struct alignas(64) Chunk {                // of the device table: consecutive elements of one tensor
+    float* param;                         // of the first one, here and below
+    uint16_t* copy;
+    const uint16_t* taps;                 // of its 3x3 kernel; NULL: no mask
+    int64_t state, first;                 // its place in the states and in the tensor
+    uint32_t tensor;
+    uint16_t count;                       // elements, 1 to kChunk
+    uint8_t tap, grad_dtype;              // tap: its place in its 3x3 kernel
+    float decay;
+};
+static_assert(sizeof(Chunk) == 64, "a line's half");
+
+struct Span {                             // the norm's table: up to kSpan consecutive elements of one tensor
+    const uint16_t* taps;                 // as a chunk's
+    int64_t first;
+    uint32_t tensor, count;
+    uint32_t tap, grad_dtype;
 };
 
 template <int N>
@@ -52,11 +66,12 @@ struct Grads {
 }  // namespace
 
 struct pp_tensors {
-    std::vector<TensorEntry> tensors;
+    std::vector<Tensor> tensors;
     std::vector<uint32_t> first_chunk;    // chunks of the tensors before each (whole launches matter), and of all
+    std::vector<uint32_t> first_span;     // the same of spans
     std::vector<uint32_t> masked_end;     // per launch: the end of its chunks of tensors with masks, which come first
-    std::vector<uint8_t> image;           // tensors | chunks | counter and partial sums (zero)
-    size_t off_chunks = 0, off_sums = 0;
+    std::vector<uint8_t> image;           // chunks | spans | counters and partial sums (zero)
+    size_t off_spans = 0, off_sums = 0;
     int64_t state_elements = 0;
     int copy_dtype = PP_F16;
     bool has_params = false;
@@ -66,7 +81,9 @@ struct pp_tensors {
 namespace {
 
 constexpr int kSMs = 152;
-constexpr int kSumCtas = kSMs * 8;           // most CTAs of the norm's kernel: partial sums
+constexpr int kSumCtas = kSMs * 5;        // most CTAs of the norm's kernel
+constexpr unsigned kCounters = 64;        // its CTAs report to one each of these, and the last of each to one more
+constexpr size_t kCounterBytes = 512;
 
 struct Vec8 {
     float v[8];
@@ -86,6 +103,23 @@ __device__ __forceinline__ void store8(float* p, const Vec8& r) {
                  "f"(r.v[3]), "f"(r.v[4]), "f"(r.v[5]), "f"(r.v[6]), "f"(r.v[7])
                  : "memory");
 }
+// Pairs of values, two to an instruction.  The explicit rounding keeps products and sums apart.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 widen(uint32_t w, int dtype) {
     if (dtype == PP_F16) {
         __half2 h;
@@ -109,24 +143,19 @@ __device__ __forceinline__ bool wide_grad(const void* g, int dtype) {
     return (reinterpret_cast<uintptr_t>(g) & (dtype == PP_F32 ? 31 : 15)) == 0;
 }
 
-// Which of the eight elements from element `le` of chunk `index` on take part: in the tensor (n of
-// them) and kept by its mask.  Eight elements touch two 3x3 kernels at most.
-__device__ __forceinline__ uint32_t kept8(const TensorEntry& t, uint32_t index, uint32_t le, int n) {
+// Which of the eight elements from element `le` of a chunk on take part: in the tensor (n of them) and kept
+// by its mask.  Eight elements touch two 3x3 kernels at most.
+__device__ __forceinline__ uint32_t kept8(const uint16_t* taps, uint32_t tap, uint32_t count, uint32_t le, int n) {
     if (n <= 0) return 0;
     const uint32_t in = n >= 8 ? 0xFFu : (1u << n) - 1;
-    if (!t.taps) return in;
-    const uint32_t past = index * (kChunk % 9);     // of whole kernels, by the chunks before this one
-    const uint32_t local = past % 9 + le, r = local % 9;
-    const int64_t k = (int64_t)index * (kChunk / 9) + past / 9 + local / 9;
-    const uint32_t a = t.taps[k] & 0x1FFu;
-    const uint32_t b = 9 * (k + 1) < t.numel ? t.taps[k + 1] & 0x1FFu : 0;
+    if (!taps) return in;
+    const uint32_t local = tap + le, k = local / 9, r = local - 9 * k;
+    const uint32_t a = taps[k] & 0x1FFu;
+    const uint32_t b = 9 * (k + 1) < tap + count ? taps[k + 1] & 0x1FFu : 0;
     return ((a | b << 9) >> r) & in;
 }
-// elements of the tensor among the eight from element `le` of chunk `index` on
-__device__ __forceinline__ int in_tensor(const TensorEntry& t, uint32_t index, uint32_t le) {
-    const int64_t left = t.numel - (int64_t)index * kChunk - le;
-    return left < 8 ? (int)(left > 0 ? left : 0) : 8;
-}
+// elements of the tensor among the eight from element `le` of a chunk on
+__device__ __forceinline__ int in_chunk(uint32_t count, uint32_t le) { return max(0, min(8, (int)count - (int)le)); }
 
 // ------------------------------------------------------------------------------------- the norm
 
@@ -142,111 +171,195 @@ struct RawGrad {
             w[0] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(g) + e));
         }
     }
+    __device__ __forceinline__ uint32_t word(int i) const {
+        const uint4 q = w[0];
+        return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
+    }
     __device__ __forceinline__ float2 pair(int i) const {
         const uint4 q = w[GRAD == PP_F32 ? i / 2 : 0];
         if constexpr (GRAD == PP_F32)
             return i % 2 ? make_float2(__uint_as_float(q.z), __uint_as_float(q.w)) : make_float2(__uint_as_float(q.x), __uint_as_float(q.y));
-        return widen(i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w, GRAD);
+        return widen(word(i), GRAD);
     }
 };
-// Sum over a CTA's chunks of (g f)^2 for a factor f: per thread in fp32 over at most a few hundred
-// squares, then over the CTA.
-template <int N>
-__device__ __forceinline__ float chunk_squares(const TensorEntry* tensors, const ChunkEntry* chunks, uint32_t begin, uint32_t end,
-                                               uint32_t t0, const Grads<N>& grads, float factor, float* smem) {
-    float sum = 0.0f;
-    uint32_t c = begin + blockIdx.x;
-    ChunkEntry next{t0, 0};
-    if (c < end) next = chunks[c];
+// A sum of positive terms and what its roundings have lost.
+struct LongSum {
+    float sum = 0.0f, lost = 0.0f;
+    __device__ __forceinline__ void add(float x) {
+        const float t = sum + x;
+        lost += x - (t - sum);
+        sum = t;
+    }
+};
+
+// Sum of (g f)^2 for a factor f over the spans that a CTA takes, U eights a thread at a time: their gradients
+// are asked for before the first is used, and with them the next ones' masks and the next span's entry.
+// WIDE: fp32 gradients among them; SCALED: f is not 1.
+template <int N, bool WIDE, bool SCALED>
+__device__ __forceinline__ float span_squares(const Span* spans, uint32_t begin, uint32_t end, uint32_t t0,
+                                              const Grads<N>& grads, float factor, float* smem) {
+    constexpr int U = WIDE ? 2 : 4;
+    LongSum sum;
     const uint32_t le = threadIdx.x * 8;
+    uint32_t c = begin + blockIdx.x;
+    Span next{};
+    if (c < end) next = spans[c];
 #pragma unroll 1
     for (; c < end; c += gridDim.x) {
-        const ChunkEntry ce = next;
-        if (c + gridDim.x < end) next = chunks[c + gridDim.x];
-        const void* g = grads.at[ce.tensor - t0];
-        if (!g) continue;
-        const TensorEntry& t = tensors[ce.tensor];
-        const int n = in_tensor(t, ce.index, le), dtype = t.grad_dtype;
-        const uint32_t keep = kept8(t, ce.index, le, n);
-        const int64_t e = (int64_t)ce.index * kChunk + le;
-        if (!keep) continue;
-        float x[8];
-        if (n == 8 && wide_grad(g, dtype)) {
-            if (dtype == PP_F32) {
-                const Vec8 v = load8(static_cast<const float*>(g) + e);
+        const Span sp = next;
+        if (c + gridDim.x < end) next = spans[c + gridDim.x];
+        const char* base = static_cast<const char*>(grads.at[sp.tensor - t0]);
+        if (!base) continue;
+        const uint32_t dtype = sp.grad_dtype, count = sp.count, size = WIDE && dtype == PP_F32 ? 4 : 2;
+        const bool wide = wide_grad(base, dtype);
+        const char* g = base + (sp.first + le) * size;
+        uint32_t from = 0;
+        if (wide && !sp.taps && !SCALED) {        // whole eights, all of them kept
+#pragma unroll 1
+            for (; from + U * kChunk <= count; from += U * kChunk, g += U * kChunk * size) {
+                uint4 raw[U][WIDE ? 2 : 1];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = v.v[i];
-            } else {
-                RawGrad<PP_F16> raw;
-                raw.load(g, e);
-                const uint32_t w[4] = {raw.w[0].x, raw.w[0].y, raw.w[0].z, raw.w[0].w};
+                for (int u = 0; u < U; ++u) {
+                    if (WIDE && dtype == PP_F32) {
+                        const Vec8 v = load8(reinterpret_cast<const float*>(g) + u * kChunk);
+                        memcpy(raw[u], &v, WIDE ? 32 : 16);
+                    } else {
+                        raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(g + u * kChunk * 2));
+                    }
+                }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = widen(w[i], dtype);
-                    x[2 * i] = f.x;
-                    x[2 * i + 1] = f.y;
+                for (int u = 0; u < U; ++u) {
+                    float2 s = make_float2(0.0f, 0.0f);
+                    const auto take = [&](const uint4& w, bool f32) {
+                        const uint32_t k[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int i = 0; i < 4; i += f32 ? 2 : 1) {
+                            const float2 x = f32 ? make_float2(__uint_as_float(k[i]), __uint_as_float(k[i + 1 < 4 ? i + 1 : i])) : widen(k[i], dtype);
+                            s = fma2(x, x, s);
+                        }
+                    };
+                    if (WIDE && dtype == PP_F32) {
+                        take(raw[u][0], true);
+                        take(raw[u][WIDE ? 1 : 0], true);
+                    } else {
+                        take(raw[u][0], false);
+                    }
+                    sum.add(s.x + s.y);
                 }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = keep >> i & 1 ? widen1(g, e + i, dtype) : 0.0f;
         }
-        float s = 0.0f;
+        if (from >= count) continue;
+        uint32_t keep[U];
+        const auto masks = [&](uint32_t from) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y = keep >> i & 1 ? x[i] * factor : 0.0f;
-            s = fmaf(y, y, s);
+            for (int u = 0; u < U; ++u) {
+                const uint32_t e = from + u * kChunk + le;
+                keep[u] = kept8(sp.taps, sp.tap, count, e, in_chunk(count, e));
+            }
+        };
+        masks(from);
+#pragma unroll 1
+        for (; from < count; from += U * kChunk, g += U * kChunk * size) {
+            uint4 raw[U][WIDE ? 2 : 1];
+            uint32_t now[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                now[u] = keep[u];
+                if (!now[u] || !wide || from + u * kChunk + le + 8 > count) continue;
+                if (WIDE && dtype == PP_F32) {
+                    const Vec8 v = load8(reinterpret_cast<const float*>(g) + u * kChunk);
+                    memcpy(raw[u], &v, WIDE ? 32 : 16);
+                } else {
+                    raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(g + u * kChunk * 2));
+                }
+            }
+            if (from + U * kChunk < count) masks(from + U * kChunk);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!now[u]) continue;
+                float x[8];
+                if (!wide || from + u * kChunk + le + 8 > count) {       // a tensor's end, or one that is not aligned
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = now[u] >> i & 1 ? widen1(g + u * kChunk * size, i, dtype) : 0.0f;
+                } else if (WIDE && dtype == PP_F32) {
+                    memcpy(x, raw[u], WIDE ? 32 : 16);
+                } else {
+                    const uint32_t w[4] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 f = widen(w[i], dtype);
+                        x[2 * i] = f.x;
+                        x[2 * i + 1] = f.y;
+                    }
+                }
+                float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float2 y = make_float2(x[2 * i], x[2 * i + 1]);
+                    if (SCALED) y = mul2(y, both(factor));
+                    y = make_float2(now[u] >> (2 * i) & 1 ? y.x : 0.0f, now[u] >> (2 * i + 1) & 1 ? y.y : 0.0f);
+                    s = fma2(y, y, s);
+                }
+                sum.add(s.x + s.y);
+            }
         }
-        sum += s;
     }
+    float s = sum.lost == sum.lost ? sum.sum + sum.lost : sum.sum;        // infinity has no rounding
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     __syncthreads();
-    if (threadIdx.x % 32 == 0) smem[threadIdx.x / 32] = sum;
+    if (threadIdx.x % 32 == 0) smem[threadIdx.x / 32] = s;
     __syncthreads();
-    sum = 0.0f;
+    s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kThreads / 32; ++i) sum += smem[i];
-    return sum;
+    for (int i = 0; i < kThreads / 32; ++i) s += smem[i];
+    return s;
 }
 
 // Partial sums of squares, one a CTA, and in the last CTA to finish of the call's last launch their sum
 // in 64 bits, the norm and the clip factor.  Squares that leave fp32's range (a sum below 2^-80, where
 // they may have been rounded away, or above 2^120) are summed again with the gradients times 2^64 or
 // 2^-64, so that the norm holds over fp32's whole range of gradients.
-template <int N>
-__global__ void __launch_bounds__(kThreads, 8) grad_norm_kernel(const TensorEntry* tensors, const ChunkEntry* chunks,
-                                                             uint32_t begin, uint32_t end, uint32_t t0, Grads<N> grads,
-                                                             double* sums, unsigned* counter, unsigned first_sum,
-                                                             unsigned all_sums, float max_norm, float* out) {
+template <int N, bool WIDE>
+__global__ void __launch_bounds__(kThreads, WIDE ? 5 : 4) grad_norm_kernel(const Span* spans, uint32_t begin, uint32_t end, uint32_t t0,
+                                                                Grads<N> grads, double* sums, unsigned* counter,
+                                                                unsigned first_sum, unsigned all_sums, float max_norm,
+                                                                float* out) {
     __shared__ float smem[kThreads / 32];
-    __shared__ double dsum[kThreads];
+    __shared__ double dsum[kThreads / 32];
     __shared__ bool last;
-    float s = chunk_squares(tensors, chunks, begin, end, t0, grads, 1.0f, smem);
+    float s = span_squares<N, WIDE, false>(spans, begin, end, t0, grads, 1.0f, smem);
     double total = s;
     if (!(s >= 0x1p-80f && s <= 0x1p120f)) {      // uniform over the CTA
         const bool small = s < 0x1p-80f;
-        s = chunk_squares(tensors, chunks, begin, end, t0, grads, small ? 0x1p64f : 0x1p-64f, smem);
+        s = span_squares<N, WIDE, true>(spans, begin, end, t0, grads, small ? 0x1p64f : 0x1p-64f, smem);
         total = (double)s * (small ? 0x1p-128 : 0x1p128);
     }
     if (threadIdx.x == 0) {
-        sums[first_sum + blockIdx.x] = total;
+        // thousands of CTAs at one counter would take 10 ns each; the last of all is the last of its counter's
+        const unsigned me = first_sum + blockIdx.x, own = me % kCounters;
+        sums[me] = total;
         __threadfence();
-        last = atomicAdd(counter, 1) == all_sums - 1;
+        last = atomicAdd(counter + 1 + own, 1) == (all_sums - own + kCounters - 1) / kCounters - 1;
+        if (last) {
+            counter[1 + own] = 0;                 // for the next call
+            __threadfence();
+            last = atomicAdd(counter, 1) == min(all_sums, kCounters) - 1;
+        }
     }
     __syncthreads();
     if (!last) return;
     __threadfence();
     double d = 0.0;
+#pragma unroll 8
     for (unsigned i = threadIdx.x; i < all_sums; i += kThreads) d += __ldcg(sums + i);
-    dsum[threadIdx.x] = d;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) d += __shfl_down_sync(0xffffffffu, d, o);
+    if (threadIdx.x % 32 == 0) dsum[threadIdx.x / 32] = d;
     __syncthreads();
-    for (int o = kThreads / 2; o; o >>= 1) {
-        if (threadIdx.x < o) dsum[threadIdx.x] += dsum[threadIdx.x + o];
-        __syncthreads();
-    }
     if (threadIdx.x == 0) {
-        const float norm = (float)sqrt(dsum[0]);
+        for (int i = 1; i < kThreads / 32; ++i) d += dsum[i];
+        const float norm = (float)sqrt(d);
         const float f = max_norm / (norm + 1e-6f);
         out[0] = norm;
         out[1] = f > 1.0f ? 1.0f : f;             // NaN stays NaN
@@ -283,23 +396,6 @@ __device__ __forceinline__ void moments(float g, float& m, float& v, float mb, f
     m = __fadd_rn(__fmul_rn(m, mb), __fmul_rn(g, a.c1));
     v = __fadd_rn(__fmul_rn(v, vb), __fmul_rn(__fmul_rn(g, g), a.c2));
 }
-// Pairs of values, two to an instruction.  The explicit rounding keeps products and sums apart.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 r;
-    asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 r;
-    asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ void moments2(float2 g, float2& m, float2& v, float mb, float vb, const AdamArgs& a) {
     m = add2(mul2(m, both(mb)), mul2(g, both(a.c1)));
     v = add2(mul2(v, both(vb)), mul2(mul2(g, g), both(a.c2)));
@@ -435,14 +531,15 @@ __device__ __forceinline__ void spoil(float (&x)[K], uint32_t spoilt) {
         if (spoilt >> i & 1) x[i] = NAN;
 }
 
-__device__ __forceinline__ void store_copy(const TensorEntry& t, int64_t e, float p, int dtype) {
-    static_cast<uint16_t*>(t.copy)[e] = narrow1(p, dtype);
+// e: of the chunk, here and below
+__device__ __forceinline__ void store_copy(const Chunk& t, uint32_t e, float p, int dtype) {
+    t.copy[e] = narrow1(p, dtype);
 }
 
 // A block of any tensor, eight consecutive elements a lane, of which those in `keep` take part: the ends of
 // tensors, tensors that are not aligned, masks that keep most of a block.
 template <int BITS>
-__device__ __noinline__ void any_block(const TensorEntry t, const void* gp, int64_t e, uint32_t keep, float gs, float shrink,
+__device__ __noinline__ void any_block(const Chunk t, const void* gp, uint32_t e, uint32_t keep, float gs, float shrink,
                                        const AdamArgs a) {
     const int64_t s = t.state + e;
     float m[8] = {}, v[8] = {}, mb = a.b1, vb = a.b2;
@@ -488,7 +585,7 @@ __device__ __noinline__ void any_block(const TensorEntry t, const void* gp, int6
 
 // A whole block of an aligned tensor without a mask, eight consecutive elements a lane.
 template <int BITS, int GRAD>
-__device__ __forceinline__ void dense_block(const TensorEntry& t, const void* gp, int64_t e, float gs, float shrink, const AdamArgs& a) {
+__device__ __forceinline__ void dense_block(const Chunk& t, const void* gp, uint32_t e, float gs, float shrink, const AdamArgs& a) {
     const int64_t s = t.state + e;
     float m[8], v[8], mb = a.b1, vb = a.b2;
     uint2 m8, v8;
@@ -589,7 +686,7 @@ struct Listed {
         return list[min(r * 32 + (int)(threadIdx.x % 32), count - 1)];
     }
     // e0: the block's first element
-    __device__ __forceinline__ void load(const TensorEntry& t, const void* gp, int64_t e0, const uint8_t* list, int count,
+    __device__ __forceinline__ void load(const Chunk& t, const void* gp, uint32_t e0, const uint8_t* list, int count,
                                          const AdamArgs& a) {
         const int64_t s0 = t.state + e0;
         const float* params = t.param + e0;
@@ -618,7 +715,7 @@ struct Listed {
             }
         }
     }
-    __device__ __forceinline__ void step(const TensorEntry& t, int64_t e0, const uint8_t* list, int count, float gs, float shrink,
+    __device__ __forceinline__ void step(const Chunk& t, uint32_t e0, const uint8_t* list, int count, float gs, float shrink,
                                          const AdamArgs& a) {
         const int64_t s0 = t.state + e0;
         const int lane = threadIdx.x % 32;
@@ -679,31 +776,30 @@ struct Listed {
 // A chunk a CTA, a block of 256 elements a warp: many light CTAs hide the tables' latency better than few
 // that look ahead.  MASKED: for chunks of tensors with masks.
 template <int BITS, int N, bool MASKED>
-__global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const TensorEntry* __restrict__ tensors,
-                                                            const ChunkEntry* __restrict__ chunks, uint32_t begin, uint32_t t0,
+__global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const Chunk* __restrict__ chunks, uint32_t begin, uint32_t t0,
                                                             Grads<N> grads, AdamArgs a) {
     __shared__ uint8_t lists[MASKED ? kThreads / 32 : 1][kBlock];
-    const ChunkEntry ce = chunks[begin + blockIdx.x];
-    const void* gp = grads.at[ce.tensor - t0];
+    const Chunk t = chunks[begin + blockIdx.x];
+    const void* gp = grads.at[t.tensor - t0];
     if (!gp) return;                               // a tensor without a gradient is left alone
-    const TensorEntry t = tensors[ce.tensor];
+    const bool wide = wide_grad(gp, t.grad_dtype) && (reinterpret_cast<uintptr_t>(t.param) & 31) == 0;
+    gp = static_cast<const char*>(gp) + t.first * (t.grad_dtype == PP_F32 ? 4 : 2);
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
     const float shrink = fmaf(-a.lr, t.decay, 1.0f);
-    const uint32_t le = threadIdx.x * 8;
-    const int64_t e0 = (int64_t)ce.index * kChunk, warp = e0 + (le & ~(kBlock - 1));
-    if (warp >= t.numel) return;                   // whole warps
+    const uint32_t le = threadIdx.x * 8, warp = le & ~(kBlock - 1);
+    if (warp >= t.count) return;                   // whole warps
     if constexpr (!MASKED) {
-        if (wide_grad(gp, t.grad_dtype) && (reinterpret_cast<uintptr_t>(t.param) & 31) == 0 && warp + kBlock <= t.numel) {
+        if (wide && warp + kBlock <= t.count) {
             if (t.grad_dtype == PP_F32)
-                dense_block<BITS, PP_F32>(t, gp, e0 + le, gs, shrink, a);
+                dense_block<BITS, PP_F32>(t, gp, le, gs, shrink, a);
             else if (t.grad_dtype == PP_F16)
-                dense_block<BITS, PP_F16>(t, gp, e0 + le, gs, shrink, a);
+                dense_block<BITS, PP_F16>(t, gp, le, gs, shrink, a);
             else
-                dense_block<BITS, PP_BF16>(t, gp, e0 + le, gs, shrink, a);
+                dense_block<BITS, PP_BF16>(t, gp, le, gs, shrink, a);
             return;
         }
     }
-    const uint32_t keep = kept8(t, ce.index, le, in_tensor(t, ce.index, le));
+    const uint32_t keep = kept8(t.taps, t.tap, t.count, le, in_chunk(t.count, le));
     if constexpr (MASKED) {
         uint8_t* list = lists[threadIdx.x / 32];
         const int count = list_kept(keep, list);
@@ -716,7 +812,7 @@ __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const TensorEntry* _
             return;
         }
     }
-    any_block<BITS>(t, gp, e0 + le, keep, gs, shrink, a);
+    any_block<BITS>(t, gp, le, keep, gs, shrink, a);
 }
 
 template <int N>
@@ -765,40 +861,55 @@ int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const
             pp_tensors* h;
             ~Guard() { delete h; }
         } guard{h};
-        uint64_t chunks = 0;
+        uint64_t chunks = 0, spans = 0;
         for (int i = 0; i < n; ++i) {
-            TensorEntry t{};
-            t.param = params ? params[i] : nullptr;
-            t.copy = copies ? copies[i] : nullptr;
-            t.taps = taps ? taps[i] : nullptr;
-            t.numel = numel[i];
-            t.state = h->state_elements;
-            t.decay = decay ? decay[i] : 0.0f;
-            t.grad_dtype = grad_dtypes[i];
+            const Tensor t{numel[i], h->state_elements, grad_dtypes[i], taps && taps[i]};
             h->tensors.push_back(t);
             h->first_chunk.push_back((uint32_t)chunks);
             h->state_elements += (numel[i] + kBlock - 1) / kBlock * kBlock;
+            h->first_span.push_back((uint32_t)spans);
             chunks += (uint64_t)((numel[i] + kChunk - 1) / kChunk);
+            spans += (uint64_t)((numel[i] + kSpan - 1) / kSpan);
             if (chunks > 0x7FFFFFFFu) return PP_ERR_SHAPE;
         }
         h->first_chunk.push_back((uint32_t)chunks);
+        h->first_span.push_back((uint32_t)spans);
         h->copy_dtype = copy_dtype;
         h->has_params = params != nullptr;
-        h->off_chunks = ((size_t)n * sizeof(TensorEntry) + 255) / 256 * 256;
-        h->off_sums = (h->off_chunks + chunks * sizeof(ChunkEntry) + 255) / 256 * 256;
+        h->off_spans = (chunks * sizeof(Chunk) + 255) / 256 * 256;
+        h->off_sums = (h->off_spans + spans * sizeof(Span) + 255) / 256 * 256;
         const size_t launches = ((size_t)n + kMaxGrads - 1) / kMaxGrads;
-        h->image.assign(h->off_sums + 256 + std::max<size_t>(1, launches) * kSumCtas * sizeof(double), 0);
-        if (n) memcpy(h->image.data(), h->tensors.data(), (size_t)n * sizeof(TensorEntry));
-        ChunkEntry* c = reinterpret_cast<ChunkEntry*>(h->image.data() + h->off_chunks);
-        const ChunkEntry* const first = c;
+        h->image.assign(h->off_sums + kCounterBytes + std::max<size_t>(1, launches) * kSumCtas * sizeof(double), 0);
+        Chunk* c = reinterpret_cast<Chunk*>(h->image.data());
+        const Chunk* const first = c;
         for (int i = 0; i < n; i += kMaxGrads) {
             const int end = std::min(n, i + kMaxGrads);
             for (const bool masked : {true, false}) {
-                for (int k = i; k < end; ++k)
-                    if ((h->tensors[k].taps != nullptr) == masked)
-                        for (uint32_t j = 0; j < h->first_chunk[k + 1] - h->first_chunk[k]; ++j) *c++ = {(uint32_t)k, j};
+                for (int k = i; k < end; ++k) {
+                    const Tensor& t = h->tensors[k];
+                    if (t.masked != masked) continue;
+                    for (int64_t e = 0; e < t.numel; e += kChunk, ++c) {
+                        c->param = params ? params[k] + e : nullptr;
+                        c->copy = copies && copies[k] ? static_cast<uint16_t*>(copies[k]) + e : nullptr;
+                        c->taps = masked ? taps[k] + e / 9 : nullptr;
+                        c->state = t.state + e;
+                        c->first = e;
+                        c->tensor = (uint32_t)k;
+                        c->count = (uint16_t)std::min<int64_t>(kChunk, t.numel - e);
+                        c->tap = (uint8_t)(e % 9);
+                        c->grad_dtype = (uint8_t)t.grad_dtype;
+                        c->decay = decay ? decay[k] : 0.0f;
+                    }
+                }
                 if (masked) h->masked_end.push_back((uint32_t)(c - first));
             }
+        }
+        Span* sp = reinterpret_cast<Span*>(h->image.data() + h->off_spans);
+        for (int k = 0; k < n; ++k) {
+            const Tensor& t = h->tensors[k];
+            for (int64_t e = 0; e < t.numel; e += kSpan)
+                *sp++ = {t.masked ? taps[k] + e / 9 : nullptr, e, (uint32_t)k, (uint32_t)std::min<int64_t>(kSpan, t.numel - e),
+                         (uint32_t)(e % 9), (uint32_t)t.grad_dtype};
         }
         guard.h = nullptr;
         *out = h;
@@ -846,10 +957,9 @@ int pp_grad_norm(pp_tensors_handle h, const void* const* grads, double max_norm,
     if (reinterpret_cast<uintptr_t>(out) % 4) return PP_ERR_ALIGN;
     if (!(max_norm > 0)) return PP_ERR_ARG;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const TensorEntry* tensors = reinterpret_cast<const TensorEntry*>(h->dev);
-    const ChunkEntry* chunks = reinterpret_cast<const ChunkEntry*>(h->dev + h->off_chunks);
+    const Span* spans = reinterpret_cast<const Span*>(h->dev + h->off_spans);
     unsigned* counter = reinterpret_cast<unsigned*>(h->dev + h->off_sums);
-    double* sums = reinterpret_cast<double*>(h->dev + h->off_sums + 256);
+    double* sums = reinterpret_cast<double*>(h->dev + h->off_sums + kCounterBytes);
     const int n = (int)h->tensors.size();
     unsigned all = 0;
     for (int pass = 0; pass < 2; ++pass) {        // count the partial sums, then launch
@@ -857,18 +967,22 @@ int pp_grad_norm(pp_tensors_handle h, const void* const* grads, double max_norm,
         int i = 0;
         do {
             const int count = std::min(n - i, kMaxGrads);
-            const uint32_t begin = h->first_chunk[i], end = h->first_chunk[i + count];
-            const unsigned grid = std::max(1u, std::min<uint32_t>(end - begin, kSumCtas));
+            const uint32_t begin = h->first_span[i], end = h->first_span[i + count];
+            const bool wide = std::any_of(h->tensors.begin() + i, h->tensors.begin() + i + count,
+                                          [](const Tensor& t) { return t.grad_dtype == PP_F32; });
+            const unsigned grid = std::max(1u, std::min<uint32_t>(end - begin, kSMs * (wide ? 5 : 4)));
             if (pass) {
-                const float mx = (float)max_norm;
+                const auto launch = [&](auto many, auto with_wide) {
+                    constexpr int M = decltype(many)::value;
+                    grad_norm_kernel<M, decltype(with_wide)::value><<<grid, kThreads, 0, st>>>(
+                        spans, begin, end, (uint32_t)i, take<M>(grads, i, count), sums, counter, done, all, (float)max_norm, out);
+                };
+                using Few = std::integral_constant<int, kFewGrads>;
+                using Many = std::integral_constant<int, kMaxGrads>;
                 if (count <= kFewGrads)
-                    grad_norm_kernel<kFewGrads><<<grid, kThreads, 0, st>>>(
-                        tensors, chunks, begin, end, (uint32_t)i, take<kFewGrads>(grads, i, count), sums, counter, done,
-                        all, mx, out);
+                    wide ? launch(Few(), std::true_type()) : launch(Few(), std::false_type());
                 else
-                    grad_norm_kernel<kMaxGrads><<<grid, kThreads, 0, st>>>(
-                        tensors, chunks, begin, end, (uint32_t)i, take<kMaxGrads>(grads, i, count), sums, counter, done,
-                        all, mx, out);
+                    wide ? launch(Many(), std::true_type()) : launch(Many(), std::false_type());
                 if (const int e = launched()) return e;
             }
             done += grid;
@@ -910,8 +1024,7 @@ int pp_adamw_step(pp_tensors_handle h, const void* const* grads, int state_bits,
     a.m_scale = m_scale;
     a.v_scale = v_scale;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const TensorEntry* tensors = reinterpret_cast<const TensorEntry*>(h->dev);
-    const ChunkEntry* chunks = reinterpret_cast<const ChunkEntry*>(h->dev + h->off_chunks);
+    const Chunk* chunks = reinterpret_cast<const Chunk*>(h->dev);
     const int n = (int)h->tensors.size();
     for (int i = 0; i < n; i += kMaxGrads) {
         const int count = std::min(n - i, kMaxGrads);
@@ -925,7 +1038,7 @@ int pp_adamw_step(pp_tensors_handle h, const void* const* grads, int state_bits,
             constexpr int B = decltype(bits)::value, M = decltype(many)::value;
             if (from == to) return PP_OK;
             adamw_kernel<B, M, decltype(with_mask)::value><<<to - from, kThreads, 0, st>>>(
-                tensors, chunks, from, (uint32_t)i, take<M>(grads, i, count), a);
+                chunks, from, (uint32_t)i, take<M>(grads, i, count), a);
             return (pp_status)launched();
         };
         const auto both = [&](auto bits, auto many) {
