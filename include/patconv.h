@@ -300,11 +300,10 @@ int pp_static_scratch_bytes(size_t* bytes);
  * no overlap.  Enqueue only. */
 int pp_maxpool2x2(const void* x, int dtype, int N, int C, int H, int W, void* y, void* stream);
 
-/* Device status word of the conv and group norm kernels on the current device.  A kernel whose pipeline wait
+/* Device status word of the conv kernels on the current device.  A kernel whose pipeline wait
  * runs out of time (about one second; it never happens in a correct run) records a bit here and
  * returns early instead of hanging: 1 = data stage never arrived, 2 = stage never released,
- * 4 = copies still in flight at exit, 8 = a split unit's later part never arrived, 16 = a group norm's sums
- * never arrived.  *status gets the word; clear != 0 resets it.  Synchronous
+ * 4 = copies still in flight at exit.  *status gets the word; clear != 0 resets it.  Synchronous
  * (a device-to-host copy); call it between launches, e.g. at the end of a test.
  * Errors: PP_ERR_NULL, PP_ERR_CUDA. */
 int pp_device_status(int clear, unsigned int* status);
@@ -367,9 +366,9 @@ int pp_group_norm_workspace_size(int dtype, int N, int64_t pixels, int C, int G,
 
 /* How a call runs whose addresses and strides are multiples of `align` bytes (a power of two, at least
  * the element's size): info[0] = 2 resident (a cluster of CTAs holds whole groups of a sample in
- * registers between the sums and the result) or 1 streamed (several kernels, the inputs read twice),
+ * shared memory between the sums and the result) or 1 streamed (several kernels, the inputs read twice),
  * [1] channels of a thread's vector, [2] vectors of a row a CTA covers, [3] pixels a CTA covers,
- * [4] vectors a thread holds at most and [5] CTAs of a cluster (resident; else 0 and 1), [6] CTAs,
+ * [4] vectors of an input that a CTA holds in shared memory, [5] CTAs of a cluster (0: streamed), [6] CTAs,
  * [7] the sets of channels of a vector that are summed apart (1: it lies within one group).  Writes min(n_info, 8) values.  Host-only.
  * Errors: PP_ERR_NULL, _SHAPE (nothing to do among them), _DTYPE, _ARG. */
 int pp_group_norm_plan(int dtype, int N, int64_t pixels, int C, int G, int backward, int align, int64_t* info, int n_info);

@@ -54,7 +54,6 @@
 #include "../../include/patconv.h"
 #include "layer.h"
 #include "pattern_dispatch.h"
-#include "norm.h"
 #include "tensor.h"
 
 using namespace patconv;
@@ -3553,10 +3552,6 @@ bool patconv::encode_box(CUtensorMap* map, const void* x, int N, int C, int H, i
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-namespace patconv {
-unsigned* device_status_word() { return status_word(); }   // for the other translation units
-}  // namespace patconv
 
 extern "C" {
 

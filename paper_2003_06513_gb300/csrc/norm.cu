@@ -13,11 +13,21 @@
 // write dx, for 10 to 30 operations an element.
 //
 // Resident form: a cluster of up to 8 CTAs takes a unit -- whole groups of one sample, a slab of channels
-// of 32 to 128 bytes -- and holds it in registers between the sums and the result, the CTAs' sums being
+// of 32 to 512 bytes -- and holds it in shared memory between the sums and the result, the CTAs' sums being
 // joined through distributed shared memory, so that every value is read from memory once.
-// Streamed form, for units that 8 CTAs do not hold: one persistent kernel whose CTAs take stretches of
-// pixels, for a sample's sums first and some samples later for its result, so that the second reading
-// comes from L2.
+// Streamed form, for units that 8 CTAs do not hold, or not well: one kernel sums (a CTA takes a stretch of
+// pixels of a sample, a thread always the same V channels, so that a warp reads whole rows), one joins a
+// sample's parts, one has the result.  The second reading comes from L2 where a call's inputs fit there: the
+// result takes the samples in the reverse order of the sums.
+//
+// Measured on a GB300 (a copy moves 6.67 TB/s), inputs in memory, the launches of a call together:
+//     forward   32x256x56x56 fp16    27 us, 3.8 TB/s of what it must move   (resident, 4 x 50 KB a unit)
+//     forward   32x64x224x224 fp32  200 us, 4.1 TB/s; 6.2 TB/s with the second reading   (streamed)
+//     backward  32x512x14x14 fp32    14 us, 2.7 TB/s   (resident, 1 x 100 KB a unit)
+//     backward  32x128x112x112 fp16 113 us, 2.7 TB/s; 4.6 TB/s with the second reading   (streamed)
+// The resident form is bound by what its few CTAs on an SM have in flight while some of them wait for their
+// clusters and by the arithmetic of SiLU (two operations of the special function unit an element, four
+// backward); the streamed one by memory forward and by that arithmetic, done twice, backward.
 //
 // Means and squares are joined pairwise as (count, mean, sum of squared distances from the mean): a
 // plain sum of squares would lose the variance of values far from zero.
@@ -63,63 +73,77 @@ struct Plan {
     int V = 1;                              // channels of a thread's vector
     int cols = 1, rows = 1, chunk = 1;      // vectors of a row and rows of a CTA, pixels of a CTA
     int NS = 1;                             // sets of a vector's channels that are summed apart
-    int tiles = 1, chunks = 1, ahead = 1, draw = 1, grid = 1;   // streamed: CTAs side by side, stretches down a sample
-    int K = 0, cluster = 1, slabs = 1;   // resident: vectors held (0: streamed), CTAs a unit, slabs
+    int tiles = 1, chunks = 1;              // streamed: CTAs side by side, stretches down a sample
+    int held = 0;                           // vectors of each input that a CTA holds
+    int cluster = 0, slabs = 1;             // resident: CTAs a unit (0: streamed), slabs
     size_t parts = 0, sums = 0;             // floats of the workspace
 };
 
 constexpr int kSMs = 152;
-constexpr int kStretch = 131072;
+constexpr int64_t kStretch = 65536, kLeast = 8192, kMostHeld = 163840, kSlabLeast = 32, kSlabMost = 512;
 
-// The resident form: the narrowest slab of whole groups that is 128 bytes wide or a whole row, or if that
-// is too much for 8 CTAs, narrower ones down to a 32-byte sector; no more CTAs than hold it at 8 vectors of
-// 16 bytes a thread (3 CTAs an SM; 16 vectors let in 2), but enough for the GPU's SMs.
+int quarter_of(const Plan& p) { return (p.rows + 3) / 4 * p.cols; }
+// resident: bytes of shared memory beside the vectors (the kernels' sums, channels and groups)
+int64_t shared_beside(const Shape& s, const Plan& p) {
+    const int64_t channels = (int64_t)p.cols * p.V, groups = channels / (s.C / s.G);
+    return 8 * ((s.backward ? (int64_t)quarter_of(p) * p.V : (int64_t)p.NS * kNormThreads) + channels + 2 * groups);
+}
+int places(const Plan& p) { return (p.chunk * p.cols + 7) / 8 * 8; }    // vectors of an input that a CTA holds
+
+// The resident form: of the slabs of whole groups from a 32-byte sector to 512 bytes wide and of the clusters that
+// hold them, the one whose estimated time is least.  In us: a CTA takes 4 beside its work (the first copies'
+// latency, two barriers of the cluster, the second reading of its parameters); its work is what its share of the
+// SM's 44 KB a us moves, or what the arithmetic of its vectors takes, 0.03 a channel of each of its rows of
+// vectors, and 2.2 times as long where it is alone; and there are as many rounds as the SMs need for all CTAs.
+// Narrow slabs move parts of lines.  Measured, this plan against one fixed rule (128 bytes, CTAs of 48 KB):
+// 32x256x56x56 fp16 forward 27 against 35 us, 4x128x112x112 fp16 forward 13 against 20, 32x512x14x14 fp32 backward
+// 16 against 25.  Against the streamed form: 32x256x56x56 fp16 forward 27 against 37, 16x256x28x28 fp32 forward 8
+// against 20; but 32x128x112x112 fp16 backward, of slabs of 32 bytes, 136 against 112.
 bool resident(const Shape& s, Plan& p) {
-    const int es = size_of(s.dtype), bytes = p.V * es, cpg = s.C / s.G, vectors = s.C / p.V;
+    const int es = size_of(s.dtype), bytes = p.V * es, cpg = s.C / s.G, vectors = s.C / p.V, inputs = s.backward ? 2 : 1;
     const int unit = std::lcm(cpg, p.V) / p.V;              // vectors of the least slab of whole groups
     if (unit > kNormThreads || vectors % unit) return false;
-    const bool wide = bytes == 16;
-    const int *held = wide ? (s.backward ? kHeldBackWide : kHeldWide) : (s.backward ? kHeldBackSmall : kHeldSmall);
-    const int n_held = wide ? (s.backward ? 3 : 4) : 2, most = held[n_held - 1];
     const int steps = vectors / unit;
-    int best = 0, best_cluster = 0;
-    const auto needs = [&](int cols, int cluster) {         // vectors a thread
-        const int rows = kNormThreads / cols;
-        const int64_t chunk = (s.pixels + cluster - 1) / cluster;
-        return (chunk + rows - 1) / rows;
-    };
-    const auto cluster_of = [&](int cols, int limit) {      // CTAs that hold it with `limit` vectors a thread
-        for (int c = 1; c <= 8; c *= 2)
-            if (needs(cols, c) <= limit) return c;
-        return 0;
-    };
-    for (int m = 1; m <= steps; ++m) {                      // widths upwards
-        if (steps % m || m * unit > kNormThreads || m * unit * p.V > 1024) continue;
-        const int width = m * unit * bytes, c = cluster_of(m * unit, most);
-        if (width < 32 && m < steps) continue;
-        if (!c) break;                                      // wider ones need more still
-        best = m * unit;
-        best_cluster = c;
-        if (width >= 128) break;
+    double least = 0;
+    Plan best;
+    for (int m = 1; m <= steps; ++m) {
+        const int width = m * unit * bytes;
+        if (steps % m || m * unit > kNormThreads || m * unit * p.V > 1024 || steps / m > 65535) continue;
+        if ((width < kSlabLeast && m < steps) || (width > kSlabMost && best.cluster)) continue;
+        for (int c = 1; c <= 8; c *= 2) {
+            const int64_t chunk = (s.pixels + c - 1) / c;
+            if (chunk * m * unit * bytes * inputs > kMostHeld) continue;
+            Plan q = p;
+            q.cols = m * unit;
+            q.rows = kNormThreads / q.cols;
+            q.slabs = vectors / q.cols;
+            q.cluster = c;
+            q.chunk = (int)chunk;
+            const double held = (double)places(q) * bytes * inputs, rows = (double)((chunk + q.rows - 1) / q.rows);
+            const double room = held + shared_beside(s, q);
+            if (room > kNormShared) continue;
+            const double total = (double)s.N * q.slabs * c, fit = std::min(s.backward ? 3.0 : 4.0, std::floor(232448 / (room + 3072)));
+            const double rounds = std::ceil(total / (kSMs * fit)), at_once = std::min(fit, std::ceil(total / kSMs));
+            const double work = rows * p.V * 0.03 * inputs, moved = held / inputs * (inputs + 1) / 44e3;
+            const double narrow = width >= 48 ? 1.0 : 1.3;
+            const double time = rounds * (4 + 0.1 * c + narrow * std::max({at_once * moved, at_once * work, 2.2 * work}));
+            if (!best.cluster || time < least) {
+                best = q;
+                least = time;
+            }
+        }
     }
-    if (!best) return false;
-    if (const int c = cluster_of(best, std::min(most, wide ? 8 : most))) best_cluster = c;
-    p.cols = best;
-    p.rows = kNormThreads / best;
-    p.slabs = vectors / best;
-    while (best_cluster < 8 && (int64_t)s.N * p.slabs * best_cluster < kSMs && needs(best, best_cluster) > 2) best_cluster *= 2;
-    if (p.slabs > 65535) return false;                      // the grid's second dimension
-    p.cluster = best_cluster;
-    p.chunk = (int)((s.pixels + best_cluster - 1) / best_cluster);
-    p.K = *std::find_if(held, held + n_held, [&](int k) { return k >= needs(best, best_cluster); });
-    p.parts = s.backward ? (size_t)s.N * best_cluster * s.C * 2 : 0;
+    // streamed: three launches, the inputs twice and the output at 5.5 TB/s
+    const double streamed = 20 + (2 * inputs + 1.0) * s.N * s.pixels * s.C * es / 5.5e6;
+    if (!best.cluster || least > streamed) return false;
+    p = best;
+    p.parts = s.backward ? (size_t)s.N * p.cluster * s.C * 2 : 0;
     return true;
 }
 
 // V channels a thread (16 bytes where `align`, the common alignment of addresses and strides in bytes,
 // allows it, else 4 bytes or one channel).  Streamed: a row's vectors over the threads of one or more CTAs,
-// stretches of pixels of about kStretch bytes of each input, and as many samples ahead as the CTAs at work
-// need, so that none waits for a sample's sums.
+// stretches of pixels of about kStretch bytes of all inputs, shorter ones where that makes too few CTAs.
 Plan plan_of(const Shape& s, int align) {
     Plan p;
     const int es = size_of(s.dtype), cpg = s.C / s.G;
@@ -131,21 +155,17 @@ Plan plan_of(const Shape& s, int align) {
         p.cols = (vectors + p.tiles - 1) / p.tiles;
         p.rows = kNormThreads / p.cols;
         const int64_t row = (int64_t)p.cols * p.V * es;
-        const int64_t wanted = std::max<int64_t>((kStretch + row - 1) / row, p.rows);
+        // four CTAs an SM, but none below kLeast bytes
+        const int64_t fill = std::max<int64_t>(1, s.pixels * s.N * p.tiles / (kSMs * 4));
+        const int64_t wanted = std::max<int64_t>({std::min((kStretch / (s.backward ? 2 : 1) + row - 1) / row, fill), (kLeast + row - 1) / row, p.rows});
         p.chunks = (int)((s.pixels + wanted - 1) / wanted);
         p.chunk = (int)((s.pixels + p.chunks - 1) / p.chunks);
         p.chunks = (int)((s.pixels + p.chunk - 1) / p.chunk);
-        // batches of the last, smallest stretch: the load side is at most kStreamDepth - 1 batches ahead
-        const int batch = p.rows * (s.backward ? kStreamBatch / 2 : kStreamBatch);
-        const int least = (int)((s.pixels - (int64_t)(p.chunks - 1) * p.chunk + batch - 1) / batch);
-        p.draw = (kStreamDepth - 2 + least) / least + 1;
-        const int64_t per = (int64_t)p.chunks * p.tiles;
-        p.grid = (int)std::min<int64_t>(2 * per * s.N, kSMs * 2);
-        p.ahead = (int)std::min<int64_t>(s.N, 1 + (2 * (int64_t)p.grid + per - 1) / per);
         const size_t sets = s.backward ? s.C : s.C / (p.V / p.NS);
         p.parts = (size_t)s.N * p.chunks * sets * 2;
-        p.sums = (s.backward ? (size_t)s.N * s.C * 2 + (size_t)s.N * s.G * 2 : 0) + (norm_counters(s.N) + 1) / 2 * 2;
+        p.sums = s.backward ? (size_t)s.N * s.C * 2 + (size_t)s.N * s.G * 2 : 0;
     }
+    p.held = places(p);
     if (!s.backward) p.sums += (size_t)s.N * s.G * 2;       // mean and rstd that the caller does not want
     return p;
 }
@@ -191,7 +211,7 @@ bool overlap(const void* p, size_t pn, const void* q, size_t qn) {
 template <typename T>
 cudaError_t run(const NormArgs& a, const Plan& p, bool backward, cudaStream_t st) {
     using K = NormKernels<T>;
-    return backward ? K::backward(a, p.V, p.K, st) : K::forward(a, p.V, p.NS, p.K, st);
+    return backward ? K::backward(a, p.V, st) : K::forward(a, p.V, p.NS, st);
 }
 
 NormArgs args_of(const Shape& s, const Plan& p, const void* x, int64_t x_pixel, int64_t x_sample, const float* gamma,
@@ -207,9 +227,8 @@ NormArgs args_of(const Shape& s, const Plan& p, const void* x, int64_t x_pixel, 
     a.tiles = p.tiles;
     a.chunk = p.chunk;
     a.chunks = p.chunks;
-    a.ahead = p.ahead;
-    a.draw = p.draw;
-    a.grid = p.grid;
+    a.held = p.held;
+    a.quarter = quarter_of(p);
     a.cluster = p.cluster;
     a.slabs = p.slabs;
     a.groups = p.cols * p.V / a.cpg;
@@ -227,12 +246,10 @@ NormArgs args_of(const Shape& s, const Plan& p, const void* x, int64_t x_pixel, 
     a.act = act;
     a.out = out;
     a.parts = static_cast<float*>(workspace);
-    a.counters = reinterpret_cast<uint32_t*>(a.parts + p.parts);
     return a;
 }
 
-int done(NormArgs& a, const Plan& p, const Shape& s, void* stream) {
-    if (!p.K && !(a.status = device_status_word())) return PP_ERR_CUDA;
+int done(const NormArgs& a, const Plan& p, const Shape& s, void* stream) {
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = s.dtype == PP_F32   ? run<float>(a, p, s.backward, st)
                           : s.dtype == PP_F16 ? run<__half>(a, p, s.backward, st)
@@ -267,8 +284,8 @@ int pp_group_norm_plan(int dtype, int N, int64_t pixels, int C, int G, int backw
     int common = align < 16 ? align : 16;
     while ((int64_t)C * size_of(dtype) % common) common /= 2;
     const Plan p = plan_of(s, common);
-    const int64_t all[8] = {p.K ? 2 : 1, p.V, p.cols, p.chunk, p.K, p.cluster,
-                            p.K ? (int64_t)N * p.slabs * p.cluster : p.grid, p.NS};
+    const int64_t all[8] = {p.cluster ? 2 : 1, p.V, p.cols, p.chunk, p.held, p.cluster,
+                            p.cluster ? (int64_t)N * p.slabs * p.cluster : (int64_t)p.chunks * p.tiles * N, p.NS};
     for (int i = 0; i < n_info && i < 8; ++i) info[i] = all[i];
     return PP_OK;
 }
@@ -340,7 +357,7 @@ int pp_group_norm_backward(const void* dy, int64_t dy_pixel, int64_t dy_sample, 
     a.rstd = rstd;
     a.dgamma = dgamma;
     a.dbeta = dbeta;
-    a.sums = a.parts + p.parts + (norm_counters(N) + 1) / 2 * 2;
+    a.sums = a.parts + p.parts;
     return done(a, p, s, stream);
 }
 

@@ -5,6 +5,10 @@
 // element of a forward pass at 2.2 TB/s): the arithmetic runs on pairs of fp32 values, two to an
 // instruction, the activation is chosen outside the loops, and exp and 1 / x are the hardware's
 // approximations (2 and 1 ulp) with subnormals flushed.
+//
+// What a CTA reads goes to shared memory by asynchronous copies, all of its stretch asked for at once and the
+// sums of the first half taken while the second is under way.  Held in registers instead (up to 8 vectors a
+// thread, one CTA fewer on an SM) the forward pass of 32x256x56x56 fp16 took 38 us, so 27.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -39,20 +43,9 @@ template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> load(const T* p) {
     return *reinterpret_cast<const Vec<T, V>*>(p);
 }
-// a result: not wanted in L2 any longer
-template <typename T, int V>
-__device__ __forceinline__ void store(T* p, const Vec<T, V>& v) {
-    if constexpr (sizeof(T) * V == 16) {
-        uint4 w;
-        memcpy(&w, &v, 16);
-        __stcs(reinterpret_cast<uint4*>(p), w);
-    } else {
-        *reinterpret_cast<Vec<T, V>*>(p) = v;
-    }
-}
-
-// Asynchronous copies into the thread's own places of shared memory, which then extend its registers: no
-// other thread reads them, so that waiting for the thread's own copies is all that is needed.
+// Asynchronous copies into the thread's own places of shared memory, which hold what a thread reads of a
+// CTA's stretch: all of it is under way at once, at no cost in registers.  No other thread reads it, so that
+// waiting for the thread's own copies is all that is needed.
 template <typename T, int V>
 __device__ __forceinline__ void copy_async(Vec<T, V>* to, const T* from) {
     const uint32_t d = (uint32_t)__cvta_generic_to_shared(to);
@@ -66,6 +59,18 @@ __device__ __forceinline__ void copy_async(Vec<T, V>* to, const T* from) {
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// a result: not wanted in L2 any longer
+template <typename T, int V>
+__device__ __forceinline__ void store(T* p, const Vec<T, V>& v) {
+    if constexpr (sizeof(T) * V == 16) {
+        uint4 w;
+        memcpy(&w, &v, 16);
+        __stcs(reinterpret_cast<uint4*>(p), w);
+    } else {
+        *reinterpret_cast<Vec<T, V>*>(p) = v;
+    }
+}
 
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(__half x) { return __half2float(x); }
@@ -154,6 +159,39 @@ __device__ __forceinline__ float2 sum_lanes(float2 s) {
     return s;
 }
 
+// What a thread holds of one input: vectors of its rows, the first half of them in a group of copies of its own.
+template <typename T, int V>
+struct Held {
+    Vec<T, V>* mine;
+    int step;
+    // one place a vector of the CTA's pixels; the input's places begin at `from`
+    __device__ __forceinline__ Held(const NormArgs& a, void* smem, int from = 0)
+        : mine(static_cast<Vec<T, V>*>(smem) + from + threadIdx.x), step(a.rows * a.cols) {}
+    __device__ __forceinline__ void copy(const T* p, int64_t stride, int first, int end) const {
+        p += first * stride;
+#pragma unroll 4
+        for (int k = first; k < end; ++k, p += stride) copy_async(mine + k * step, p);
+    }
+    __device__ __forceinline__ const Vec<T, V>& operator[](int k) const { return mine[k * step]; }
+};
+// f(k, how many) for k from first to end - 1, U at a time while there are as many, then one at a time
+template <int U, typename F>
+__device__ __forceinline__ void by_batches(int first, int end, F&& f) {
+#pragma unroll 1
+    for (; first + U <= end; first += U) f(first, std::integral_constant<int, U>());
+#pragma unroll 1
+    for (; first < end; ++first) f(first, std::integral_constant<int, 1>());
+}
+// f(first, end) for the first half, then for the rest, each as soon as its copies have come
+template <typename F>
+__device__ __forceinline__ void as_they_come(int count, F&& f) {
+    const int half = (count + 1) / 2;
+    copies_wait<1>();
+    f(0, half);
+    copies_wait<0>();
+    f(half, count);
+}
+
 // A thread's moments of NS sets of S = V / NS adjacent channels, each within one group.
 template <typename T, int V, int NS>
 struct Sets {
@@ -206,6 +244,16 @@ struct Sets {
             }
         }
         n = total;
+    }
+    template <int U>
+    __device__ __forceinline__ void take_all(const Held<T, V>& held, int first, int end) {
+        by_batches<U>(first, end, [&](int k, auto batch) {
+            constexpr int K = decltype(batch)::value;
+            Vec<T, V> v[K];
+#pragma unroll
+            for (int u = 0; u < K; ++u) v[u] = held[k + u];
+            take(v, K);
+        });
     }
     __device__ static __forceinline__ float positive(float q) { return q < 0.0f ? 0.0f : q; }   // NaN stays
     __device__ __forceinline__ void merge1(float q, float mu, float f, float w) {
@@ -290,15 +338,19 @@ template <int V>
 struct Forward {
     float2 mean[kPairs<V>], scale[kPairs<V>], shift[kPairs<V>];
     template <typename Stat>
-    __device__ __forceinline__ Forward(const NormArgs& a, int c, Stat&& stat) {
+    __device__ __forceinline__ Forward(const NormArgs& a, int c, Stat&& stat)
+        : Forward(a, c, stat, a.gamma ? a.gamma + c : nullptr, a.beta ? a.beta + c : nullptr) {}
+    // gamma, beta: of the V channels, or NULL
+    template <typename Stat>
+    __device__ __forceinline__ Forward(const NormArgs& a, int c, Stat&& stat, const float* gamma, const float* beta) {
         float m[2] = {}, s[2] = {}, b[2] = {};
         GroupOf at(a, c);
 #pragma unroll
         for (int i = 0; i < V; ++i, at.next()) {
             const float2 st = stat(at.g);
             m[i % 2] = st.x;
-            s[i % 2] = st.y * (a.gamma ? __ldg(a.gamma + c + i) : 1.0f);
-            b[i % 2] = a.beta ? __ldg(a.beta + c + i) : 0.0f;
+            s[i % 2] = st.y * (gamma ? gamma[i] : 1.0f);
+            b[i % 2] = beta ? beta[i] : 0.0f;
             mean[i / 2] = make_float2(-m[0], -m[1]);
             scale[i / 2] = make_float2(s[0], s[1]);
             shift[i / 2] = make_float2(b[0], b[1]);
@@ -311,140 +363,136 @@ struct Forward {
             set_pair(v, i, activated<ACT>(fma(add(pair(v, i), mean[i]), scale[i], shift[i])));
         return v;
     }
+    // y: the thread's first row of the result
+    template <typename T>
+    __device__ __forceinline__ void write(const NormArgs& a, const Held<T, V>& held, int first, int end, T* y) const {
+        const int64_t step = (int64_t)a.rows * a.C;
+        y += first * step;
+        with_act(a.act, [&](auto act) {
+            by_batches<2>(first, end, [&](int k, auto batch) {
+#pragma unroll
+                for (int u = 0; u < decltype(batch)::value; ++u, y += step)
+                    store<T, V>(y, apply<decltype(act)::value>(held[k + u]));
+            });
+        });
+    }
 };
 
+// With d = x - mean and s = rstd gamma: z = s d + beta, and
+//     dx = rstd (gamma dz - A / M - xh B / M) = s dz + p + q d,  p = -rstd A / M,  q = -rstd^2 B / M,
+// A / M and B' / M = rstd B / M coming from sums of dz and of dz d.  A group of one value (M = 1) has dx = 0.
 template <int V>
 struct Backward {
-    float2 mean[kPairs<V>], rstd[kPairs<V>], gamma[kPairs<V>], beta[kPairs<V>];
+    float2 mean[kPairs<V>], scale[kPairs<V>], shift[kPairs<V>];
     __device__ __forceinline__ Backward(const NormArgs& a, int n, int c) {
-        float m[2] = {}, r[2] = {}, g[2] = {}, b[2] = {};
+        float m[2] = {}, s[2] = {}, b[2] = {};
         const float *mean_n = a.mean + (int64_t)n * a.G, *rstd_n = a.rstd + (int64_t)n * a.G;
         GroupOf at(a, c);
 #pragma unroll
         for (int i = 0; i < V; ++i, at.next()) {
             m[i % 2] = -__ldg(mean_n + at.g);
-            r[i % 2] = __ldg(rstd_n + at.g);
-            g[i % 2] = a.gamma ? __ldg(a.gamma + c + i) : 1.0f;
+            s[i % 2] = __ldg(rstd_n + at.g) * (a.gamma ? __ldg(a.gamma + c + i) : 1.0f);
             b[i % 2] = a.beta ? __ldg(a.beta + c + i) : 0.0f;
             mean[i / 2] = make_float2(m[0], m[1]);
-            rstd[i / 2] = make_float2(r[0], r[1]);
-            gamma[i / 2] = make_float2(g[0], g[1]);
-            beta[i / 2] = make_float2(b[0], b[1]);
+            scale[i / 2] = make_float2(s[0], s[1]);
+            shift[i / 2] = make_float2(b[0], b[1]);
         }
     }
-    // sums of dz and of dz xh
+    // sums of dz and of dz d
     template <int ACT, typename T>
     __device__ __forceinline__ void sum(const Vec<T, V>& x, const Vec<T, V>& dy, float2 (&sb)[kPairs<V>], float2 (&sg)[kPairs<V>]) const {
 #pragma unroll
         for (int i = 0; i < kPairs<V>; ++i) {
-            const float2 xh = mul(add(pair(x, i), mean[i]), rstd[i]);
-            const float2 dz = through<ACT>(pair(dy, i), fma(xh, gamma[i], beta[i]));
+            const float2 d = add(pair(x, i), mean[i]), dz = through<ACT>(pair(dy, i), fma(d, scale[i], shift[i]));
             sb[i] = add(sb[i], dz);
-            sg[i] = fma(dz, xh, sg[i]);
+            sg[i] = fma(dz, d, sg[i]);
         }
     }
-    // rstd (gamma dz - A / M - xh B / M); the product is rounded by itself, so that dx of a group of one value
-    // is zero
-    template <int ACT, typename T, typename Stat>
-    __device__ __forceinline__ Vec<T, V> apply(Vec<T, V> x, const Vec<T, V>& dy, Stat&& stat) const {
+    template <typename T>
+    __device__ __forceinline__ void sum_all(const NormArgs& a, const Held<T, V>& x, const Held<T, V>& dy, int first, int end,
+                                            float2 (&sb)[kPairs<V>], float2 (&sg)[kPairs<V>]) const {
+        with_act(a.act, [&](auto act) {
+            by_batches<2>(first, end, [&](int k, auto batch) {
+#pragma unroll
+                for (int u = 0; u < decltype(batch)::value; ++u) sum<decltype(act)::value>(x[k + u], dy[k + u], sb, sg);
+            });
+        });
+    }
+    // pq: p, p', q, q' of a pair
+    template <int ACT, typename T>
+    __device__ __forceinline__ Vec<T, V> apply(Vec<T, V> x, const Vec<T, V>& dy, const float4 (&pq)[kPairs<V>], float one) const {
 #pragma unroll
         for (int i = 0; i < kPairs<V>; ++i) {
-            const float2 xh = mul(add(pair(x, i), mean[i]), rstd[i]);
-            const float2 dz = through<ACT>(pair(dy, i), fma(xh, gamma[i], beta[i]));
-            const float4 ab = stat(i);                            // -A, -A', -B, -B'
-            const float2 e = make_float2(__fmul_rn(gamma[i].x, dz.x), __fmul_rn(gamma[i].y, dz.y));
-            const float2 d = fma(xh, make_float2(ab.z, ab.w), add(e, make_float2(ab.x, ab.y)));
-            set_pair(x, i, mul(rstd[i], d));
+            const float2 d = add(pair(x, i), mean[i]), dz = through<ACT>(pair(dy, i), fma(d, scale[i], shift[i]));
+            const float2 rest = fma(d, make_float2(pq[i].z, pq[i].w), make_float2(pq[i].x, pq[i].y));
+            set_pair(x, i, fma(mul(scale[i], both(one)), dz, rest));
         }
         return x;
     }
+    // dx: the thread's first row of the result
+    template <typename T>
+    __device__ __forceinline__ void write(const NormArgs& a, const Held<T, V>& x, const Held<T, V>& dy, int first, int end, T* dx,
+                                          const float4 (&pq)[kPairs<V>]) const {
+        const int64_t step = (int64_t)a.rows * a.C;
+        const float one = a.pixels * a.cpg == 1 ? 0.0f : 1.0f;
+        dx += first * step;
+        with_act(a.act, [&](auto act) {
+            by_batches<2>(first, end, [&](int k, auto batch) {
+#pragma unroll
+                for (int u = 0; u < decltype(batch)::value; ++u, dx += step)
+                    store<T, V>(dx, apply<decltype(act)::value>(x[k + u], dy[k + u], pq, one));
+            });
+        });
+    }
 };
-// A / M and B / M of a thread's groups, negative, by pairs of channels
+// p and q of a thread's groups by pairs of channels; stat(g) gives them
 template <int V, typename Stat>
 __device__ __forceinline__ void pair_stats(float4 (&out)[kPairs<V>], const NormArgs& a, int c, Stat&& stat) {
-    float A[2] = {}, B[2] = {};
+    float p[2] = {}, q[2] = {};
     GroupOf at(a, c);
 #pragma unroll
     for (int i = 0; i < V; ++i, at.next()) {
         const float2 s = stat(at.g);
-        A[i % 2] = -s.x;
-        B[i % 2] = -s.y;
-        out[i / 2] = make_float4(A[0], A[1], B[0], B[1]);
+        p[i % 2] = s.x;
+        q[i % 2] = s.y;
+        out[i / 2] = make_float4(p[0], p[1], q[0], q[1]);
     }
 }
-// [channel][thread] in shared memory: sums of dz, of dz xh
+// p and q of a group from its sums of gamma dz and of gamma dz d
+__device__ __forceinline__ float2 group_pq(const NormArgs& a, float2 sums, float rstd) {
+    const float inv = 1.0f / ((float)a.pixels * a.cpg);
+    return a.pixels * a.cpg == 1 ? make_float2(0.0f, 0.0f) : make_float2(-rstd * (sums.x * inv), -rstd * rstd * rstd * (sums.y * inv));
+}
+// The threads' sums of dz and of dz d by a quarter of their rows: s[channel][row of the quarter][column], the
+// rows of the other quarters added in turn.  A quarter of the room is a CTA more on an SM.
 template <int V>
-__device__ __forceinline__ void put_sums(float2* s, const float2 (&sb)[kPairs<V>], const float2 (&sg)[kPairs<V>]) {
+__device__ __forceinline__ void put_sums(const NormArgs& a, int row, int col, float2* s, const float2 (&sb)[kPairs<V>], const float2 (&sg)[kPairs<V>]) {
+    const int quarter = (a.rows + 3) / 4, size = quarter * a.cols;
+    for (int from = 0; from < a.rows; from += quarter) {
+        if (row >= from && row < from + quarter && row < a.rows) {
+            float2* to = s + (row - from) * a.cols + col;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        s[i * kThreads + threadIdx.x] = i % 2 ? make_float2(sb[i / 2].y, sg[i / 2].y) : make_float2(sb[i / 2].x, sg[i / 2].x);
+            for (int i = 0; i < V; ++i, to += size) {
+                const float2 v = i % 2 ? make_float2(sb[i / 2].y, sg[i / 2].y) : make_float2(sb[i / 2].x, sg[i / 2].x);
+                *to = from ? add(*to, v) : v;
+            }
+        }
+        __syncthreads();
+    }
+}
+// A channel's sum over the quarter's rows, in the first of eight lanes.
+__device__ __forceinline__ float2 sum_rows(const NormArgs& a, const float2* s, int channel, int col) {
+    const int quarter = (a.rows + 3) / 4;
+    s += channel * quarter * a.cols + col;
+    float2 sum = {};
+    for (int r = threadIdx.x % 8; r < quarter; r += 8) sum = add(sum, s[r * a.cols]);
+    return sum_lanes<8>(sum);
 }
 
 // -------------------------------------------------------------------------------- streamed kernels
 
-// One kernel for a whole call: its CTAs draw tickets, and the tickets' order is that of the work: the sums
-// of `ahead` samples first, then by turns a sample's result and the sums of the next one, so that what is
-// read for the sums is read again, for the result, while it is in L2.  The CTA that finishes a sample's
-// last sum joins them.  A CTA that waits for a sample's sums holds a later ticket than all of those, so that
-// they are done or at work, and the wait ends; should it not within a second, it is given up and recorded.
-struct alignas(32) Item {
-    int n, tile, chunk, kind;         // kSums, kResult, or kNone after the last
-    int begin, base, rest, batches;   // pixels from begin on: base rows of each of the CTA's rows, one more of the
-                                      // first `rest`; their batches
-};
-constexpr int kSums = 0, kResult = 1, kNone = 2;
-__device__ __forceinline__ Item item_of(const NormArgs& a, uint32_t t, int batch) {
-    const uint32_t per = (uint32_t)(a.chunks * a.tiles), first = per * a.ahead, pairs = (uint32_t)(a.N - a.ahead) * 2 * per;
-    Item it;
-    uint32_t r;
-    if (t < first) {
-        it.n = t / per;
-        r = t - it.n * per;
-        it.kind = kSums;
-    } else if (t - first < pairs) {
-        const uint32_t k = (t - first) / (2 * per);
-        r = t - first - k * 2 * per;
-        it.kind = r >= per ? kSums : kResult;
-        it.n = r >= per ? k + a.ahead : k;
-        if (r >= per) r -= per;
-    } else {
-        const uint32_t k = (t - first - pairs) / per;
-        r = t - first - pairs - k * per;
-        it.n = a.N - a.ahead + (int)k;
-        it.kind = it.n >= a.N ? kNone : kResult;
-    }
-    it.chunk = a.tiles == 1 ? r : r / a.tiles;
-    it.tile = a.tiles == 1 ? 0 : r % a.tiles;
-    it.begin = it.chunk * a.chunk;
-    const int count = (int)min((int64_t)a.chunk, a.pixels - it.begin);
-    it.base = count / a.rows;
-    it.rest = count - it.base * a.rows;
-    it.batches = (it.base + (it.rest > 0) + batch - 1) / batch;
-    return it;
-}
-
-constexpr long long kNormWaitCycles = 2000000000LL;              // about one second
-__device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
-    uint32_t v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ void store_release(uint32_t* p, uint32_t v) {
-    asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
-}
-// by one thread; false if the flag never came
-__device__ __forceinline__ bool wait_flag(const uint32_t* flag, unsigned* status) {
-    if (load_acquire(flag)) return true;
-    const long long t0 = clock64();
-    while (!load_acquire(flag)) {
-        __nanosleep(64);
-        if (clock64() - t0 > kNormWaitCycles) {
-            atomicOr(status, kStatusNormTimeout);
-            return false;
-        }
-    }
-    return true;
-}
+// Three launches: sums, a CTA a stretch of one sample's pixels; the parts of each sample joined; the result.
+// What the result reads last of the sums' inputs it reads first, from the L2 cache.
 
 struct Thread {                       // of a CTA: its column and its row
     int col, row;
@@ -453,307 +501,200 @@ struct Thread {                       // of a CTA: its column and its row
         col = threadIdx.x - row * a.cols;
     }
 };
-template <int V>
-struct Place {                        // of a thread in an item: V channels from c, `mine` pixels from its row on
-    int c, mine;
-    __device__ __forceinline__ Place(const NormArgs& a, const Thread& th, const Item& it) {
-        c = (it.tile * a.cols + th.col) * V;
-        mine = th.row < a.rows && c < a.C ? it.base + (th.row < it.rest) : 0;
+struct Stretch {                      // chunk blockIdx.x and tile blockIdx.y of sample n
+    int n, c, col, row, count, mine;  // count: its pixels; mine: this thread's, from row on; c: its channels
+    int64_t begin;
+    __device__ __forceinline__ Stretch(const NormArgs& a, int V, int sample) : n(sample) {
+        const Thread th(a);
+        col = th.col;
+        row = th.row;
+        c = (blockIdx.y * a.cols + col) * V;
+        begin = (int64_t)blockIdx.x * a.chunk;
+        count = (int)min((int64_t)a.chunk, a.pixels - begin);
+        mine = row < a.rows && c < a.C && row < count ? (count - row + a.rows - 1) / a.rows : 0;
     }
-    Place() = default;
 };
 
-// Keeps copies of kDepth - 1 batches of U vectors a thread of each input under way, across the items'
-// borders: the load side (an item and a batch) runs ahead of the side that computes.  One thread draws
-// tickets, `draw` items ahead, as many as the load side can get ahead and one; a ticket is read after the
-// barrier that follows its writing (every item has one).
-constexpr int kDepth = kStreamDepth, kTickets = 8;
-static_assert(kDepth < kTickets, "tickets are drawn at most kDepth items ahead");
-
-template <typename T, int V, int U, int INPUTS>
-struct Pipe {
-    const NormArgs& a;
-    const Thread th;
-    Vec<T, V>* mine;                  // the thread's places: [kDepth][INPUTS][U][kThreads]
-    Item* items;                      // shared, kTickets of them
-    uint32_t drawn = 0;               // one thread: a ticket under way
-    int ahead_item = 0, ahead_batch = 0, ahead_batches, ahead_left, ahead_slot = 0, slot = 0;
-    const T *x, *dy;                  // of the load side: its next vectors
-    const int64_t x_step, dy_step;
-
-    __device__ __forceinline__ Pipe(const NormArgs& args, void* smem, Item* s_items)
-        : a(args), th(args), mine(static_cast<Vec<T, V>*>(smem) + threadIdx.x), items(s_items),
-          x_step(args.rows * args.x_pixel), dy_step(args.rows * args.dy_pixel) {
-        if (threadIdx.x == 0) {
-            const uint32_t t = atomicAdd(a.counters, a.draw);
-            for (int i = 0; i < a.draw; ++i) items[i] = item_of(a, t + i, U);
-            drawn = atomicAdd(a.counters, 1);
-        }
-        __syncthreads();
-        enter();
-        for (int i = 0; i < kDepth - 1; ++i) advance();
-    }
-    __device__ __forceinline__ void enter() {
-        const Item it = items[ahead_item % kTickets];
-        const Place<V> at(a, th, it);
-        ahead_batch = 0;
-        ahead_batches = it.kind == kNone ? -1 : it.batches;       // after a last ticket come last ones
-        ahead_left = it.kind == kNone ? 0 : at.mine;
-        const int64_t p = it.begin + th.row;
-        x = static_cast<const T*>(a.x) + it.n * a.x_sample + p * a.x_pixel + at.c;
-        if constexpr (INPUTS == 2) dy = static_cast<const T*>(a.dy) + it.n * a.dy_sample + p * a.dy_pixel + at.c;
-    }
-    // the next batch's copies
-    __device__ __forceinline__ void advance() {
-        if (ahead_batch == ahead_batches) {
-            ++ahead_item;
-            enter();
-        }
-        Vec<T, V>* to = mine + ahead_slot * (INPUTS * U * kThreads);
-        const auto copy = [&](auto k) {
-#pragma unroll
-            for (int u = 0; u < U; ++u, x += x_step)
-                if (u < k) copy_async(to + u * kThreads, x);
-            if constexpr (INPUTS == 2) {
-#pragma unroll
-                for (int u = 0; u < U; ++u, dy += dy_step)
-                    if (u < k) copy_async(to + (U + u) * kThreads, dy);
-            }
-        };
-        if (ahead_left >= U)
-            copy(std::integral_constant<int, U>());
-        else if (ahead_left > 0)
-            copy(ahead_left);
-        copies_end();
-        ahead_left -= U;
-        ++ahead_batch;
-        ahead_slot = ahead_slot + 1 == kDepth ? 0 : ahead_slot + 1;
-    }
-    // the item that is next to compute; `i` counts them
-    __device__ __forceinline__ Item begin(int i) {
-        if (threadIdx.x == 0) {
-            items[(i + a.draw) % kTickets] = item_of(a, drawn, U);
-            drawn = atomicAdd(a.counters, 1);
-        }
-        return items[i % kTickets];
-    }
-    // the item's batches: f(first vector, vectors), a constant U but for the last
-    template <typename F>
-    __device__ __forceinline__ void each(const Item& it, int left, F&& f) {
-#pragma unroll 1
-        for (int b = 0; b < it.batches; ++b, left -= U) {
-            advance();
-            copies_wait<kDepth - 1>();
-            if (left >= U)
-                f(b * U, std::integral_constant<int, U>());
-            else if (left > 0)
-                f(b * U, left);
-            slot = slot + 1 == kDepth ? 0 : slot + 1;
-        }
-    }
-    __device__ __forceinline__ Vec<T, V> get(int input, int u) const {
-        return mine[((slot * INPUTS + input) * U + u) * kThreads];
-    }
-    static constexpr size_t kBytes = sizeof(Vec<T, V>) * kDepth * INPUTS * U * kThreads;
-};
-
-// Whether this CTA has finished the last of `per` parts of a sample: then it sees all of them.  The barrier
-// puts the CTA's writes before the one thread's fence; a fence of every thread would wait for its copies.
-__device__ __forceinline__ bool last_of(uint32_t* done, uint32_t per) {
-    __syncthreads();
-    bool last = false;
-    if (threadIdx.x == 0) {
-        __threadfence();
-        last = atomicAdd(done, 1) == per - 1;
-        __threadfence();
-    }
-    return __syncthreads_or(last);
-}
-
+// parts[n][chunk][set] = mean, m2 of a stretch
 template <typename T, int V, int NS>
-__global__ void __launch_bounds__(kThreads, 2) norm_stream(NormArgs a) {
-    constexpr int S = V / NS, U = kStreamBatch;
+__global__ void __launch_bounds__(kThreads, 3) norm_sums(NormArgs a) {
+    constexpr int S = V / NS, U = 4;
     extern __shared__ uint4 smem4[];
     __shared__ float2 s_sets[NS * kThreads];
     __shared__ int s_mine[kThreads];
-    __shared__ Item s_items[kTickets];
-    Pipe<T, V, U, 1> pipe(a, smem4, s_items);
-    uint32_t *done = a.counters + 2, *ready = done + a.N;
-    const int sets = a.C / S;                                     // of a row
-    for (int i = 0;; ++i) {
-        const Item it = pipe.begin(i);
-        if (it.kind == kNone) break;
-        const Place<V> at(a, pipe.th, it);
-        if (it.kind == kSums) {
-            Sets<T, V, NS> m;
-            pipe.each(it, at.mine, [&](int, auto k) {
-                Vec<T, V> v[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u < k) v[u] = pipe.get(0, u);
-                m.take(v, k);
-            });
-            m.put(s_sets);
-            s_mine[threadIdx.x] = at.mine * S;
-            __syncthreads();
-            // eight lanes a set, over the rows
-            const int here = min(a.cols, a.C / V - it.tile * a.cols) * NS;
-            for (int j0 = threadIdx.x / 8; j0 < (here + 3) / 4 * 4; j0 += kThreads / 8) {
-                const int j = min(j0, here - 1), col = j / NS, k = j % NS;
-                Moments m{0.0f, 0.0f, 0.0f};
-                for (int r = threadIdx.x % 8; r < a.rows; r += 8) {
-                    const int t = r * a.cols + col;
-                    const float2 s = s_sets[k * kThreads + t];
-                    m = join(m, {(float)s_mine[t], s.x, s.y});
-                }
-                m = join_lanes<8>(m);
-                if (threadIdx.x % 8 == 0 && j0 < here)
-                    reinterpret_cast<float2*>(a.parts)[((int64_t)it.n * a.chunks + it.chunk) * sets + it.tile * a.cols * NS + j] =
-                        make_float2(m.mean, m.m2);
-            }
-            if (!last_of(done + it.n, a.chunks * a.tiles)) continue;
-            const float2* parts = reinterpret_cast<const float2*>(a.parts) + (int64_t)it.n * a.chunks * sets;
-            // eight lanes a group, over its sets where they are many, else over the stretches
-            const int lane = threadIdx.x % 8;
-            const bool wide = a.spg >= 8;
-            for (int g0 = threadIdx.x / 8; g0 < (a.G + 3) / 4 * 4; g0 += kThreads / 8) {
-                const int g = min(g0, a.G - 1);
-                Moments m{0.0f, 0.0f, 0.0f};
-                for (int o = 0; o < (wide ? a.chunks : a.spg); ++o) {
-                    const int count = wide ? a.spg : a.chunks;
-#pragma unroll 8
-                    for (int e = lane; e < count; e += 8) {
-                        const int k = wide ? o : e, set = g * a.spg + (wide ? e : o);
-                        const float2 p = __ldcg(parts + (int64_t)k * sets + set);
-                        const int64_t left = a.pixels - (int64_t)k * a.chunk;
-                        m = join(m, {(float)(left < a.chunk ? left : a.chunk) * S, p.x, p.y});
-                    }
-                }
-                m = join_lanes<8>(m);
-                if (lane == 0 && g0 < a.G) {
-                    const float var = m.m2 / ((float)a.pixels * a.cpg);
-                    a.mean_out[(int64_t)it.n * a.G + g] = m.mean;
-                    a.rstd_out[(int64_t)it.n * a.G + g] = 1.0f / sqrtf(var + a.eps);
-                }
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                __threadfence();
-                store_release(ready + it.n, 1);
-            }
-        } else {
-            const bool good = __syncthreads_and(threadIdx.x != 0 || wait_flag(ready + it.n, a.status));
-            const float *mean = a.mean_out + (int64_t)it.n * a.G, *rstd = a.rstd_out + (int64_t)it.n * a.G;
-            const int c = min(at.c, a.C - V);                     // of a thread without a column: any
-            const Forward<V> f(a, c, [&](int g) { return make_float2(__ldcg(mean + g), __ldcg(rstd + g)); });
-            T* y = static_cast<T*>(a.out) + ((int64_t)it.n * a.pixels + it.begin + pipe.th.row) * a.C + at.c;
-            const int64_t y_step = (int64_t)a.rows * a.C;
-            with_act(a.act, [&](auto act) {
-                pipe.each(it, at.mine, [&](int first, auto k) {
-                    T* to = y + first * y_step;
-#pragma unroll
-                    for (int u = 0; u < U; ++u, to += y_step)
-                        if (u < k && good) store<T, V>(to, f.template apply<decltype(act)::value>(pipe.get(0, u)));
-                });
-            });
-        }
+    const Stretch at(a, V, blockIdx.z);
+    {
+        const T* x = static_cast<const T*>(a.x) + at.n * a.x_sample + (at.begin + at.row) * a.x_pixel + at.c;
+        const Held<T, V> v(a, smem4);
+        const int half = (at.mine + 1) / 2;
+        v.copy(x, a.rows * a.x_pixel, 0, half);
+        copies_end();
+        v.copy(x, a.rows * a.x_pixel, half, at.mine);
+        copies_end();
+        Sets<T, V, NS> m;
+        as_they_come(at.mine, [&](int first, int end) { m.template take_all<U>(v, first, end); });
+        m.put(s_sets);
     }
-    copies_wait<0>();
+    s_mine[threadIdx.x] = at.mine * S;
+    __syncthreads();
+    // eight lanes a set, over the rows
+    const int sets = a.C / S, here = min(a.cols, a.C / V - (int)blockIdx.y * a.cols) * NS, lane = threadIdx.x % 8;
+    float2* parts = reinterpret_cast<float2*>(a.parts) + ((int64_t)at.n * a.chunks + blockIdx.x) * sets + blockIdx.y * a.cols * NS;
+    for (int j0 = threadIdx.x / 8; j0 < (here + 3) / 4 * 4; j0 += kThreads / 8) {
+        const int j = min(j0, here - 1), col = j / NS, k = j % NS;
+        Moments m{0.0f, 0.0f, 0.0f};
+        for (int r = lane; r < a.rows; r += 8) {
+            const int t = r * a.cols + col;
+            const float2 s = s_sets[k * kThreads + t];
+            m = join(m, {(float)s_mine[t], s.x, s.y});
+        }
+        m = join_lanes<8>(m);
+        if (lane == 0 && j0 < here) parts[j] = make_float2(m.mean, m.m2);
+    }
 }
 
-// sums: [N][C] (dz, dz xh), then [N][G] (A / M, B / M)
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 2) norm_back_stream(NormArgs a) {
-    constexpr int U = kStreamBatch / 2;
-    extern __shared__ uint4 smem4[];
-    __shared__ float2 s_sums[V * kThreads];
-    __shared__ Item s_items[kTickets];
-    Pipe<T, V, U, 2> pipe(a, smem4, s_items);
-    uint32_t *joined = a.counters + 1, *done = a.counters + 2, *ready = done + a.N;
-    float2 *channel = reinterpret_cast<float2*>(a.sums), *group = channel + (int64_t)a.N * a.C;
-    for (int i = 0;; ++i) {
-        const Item it = pipe.begin(i);
-        if (it.kind == kNone) break;
-        const Place<V> at(a, pipe.th, it);
-        const int own_c = min(at.c, a.C - V);                     // of a thread without a column: any
-        if (it.kind == kSums) {
-            float2 sb[kPairs<V>] = {}, sg[kPairs<V>] = {};
-            const Backward<V> f(a, it.n, own_c);
-            with_act(a.act, [&](auto act) {
-                pipe.each(it, at.mine, [&](int, auto k) {
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        if (u < k) f.template sum<decltype(act)::value>(pipe.get(0, u), pipe.get(1, u), sb, sg);
-                });
-            });
-            put_sums<V>(s_sums, sb, sg);
-            __syncthreads();
-            const int here = min(a.cols * V, a.C - it.tile * a.cols * V);
-            for (int j0 = threadIdx.x / 8; j0 < (here + 3) / 4 * 4; j0 += kThreads / 8) {
-                const int j = min(j0, here - 1), col = j / V, i = j % V;
-                float2 s = {};
-                for (int r = threadIdx.x % 8; r < a.rows; r += 8) s = add(s, s_sums[i * kThreads + r * a.cols + col]);
-                s = sum_lanes<8>(s);
-                if (threadIdx.x % 8 == 0 && j0 < here)
-                    reinterpret_cast<float2*>(a.parts)[((int64_t)it.n * a.chunks + it.chunk) * a.C + it.tile * a.cols * V + j] = s;
-            }
-            if (!last_of(done + it.n, a.chunks * a.tiles)) continue;
-            // the sample's channels, eight lanes a channel over the stretches, then its groups
-            const float2* parts = reinterpret_cast<const float2*>(a.parts) + (int64_t)it.n * a.chunks * a.C;
-            for (int c0 = threadIdx.x / 8; c0 < (a.C + 3) / 4 * 4; c0 += kThreads / 8) {
-                const int c = min(c0, a.C - 1);
-                float2 s = {};
-#pragma unroll 8
-                for (int k = threadIdx.x % 8; k < a.chunks; k += 8) s = add(s, __ldcg(parts + (int64_t)k * a.C + c));
-                s = sum_lanes<8>(s);
-                if (threadIdx.x % 8 == 0 && c0 < a.C) channel[(int64_t)it.n * a.C + c] = s;
-            }
-            __syncthreads();
-            for (int g = threadIdx.x / 32; g < a.G; g += kWarps) {
-                float2 s = {};
-                for (int i = threadIdx.x % 32; i < a.cpg; i += 32) {
-                    const int c = g * a.cpg + i;
-                    s = fma(both(a.gamma ? a.gamma[c] : 1.0f), channel[(int64_t)it.n * a.C + c], s);
-                }
-                s = sum_lanes<32>(s);
-                if (threadIdx.x % 32 == 0) group[(int64_t)it.n * a.G + g] = mul(s, both(1.0f / ((float)a.pixels * a.cpg)));
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                __threadfence();
-                store_release(ready + it.n, 1);
-            }
-            if (!(a.dgamma || a.dbeta) || !last_of(joined, a.N)) continue;
-            for (int c0 = threadIdx.x / 8; c0 < (a.C + 3) / 4 * 4; c0 += kThreads / 8) {      // over the samples
-                const int c = min(c0, a.C - 1);
-                float2 s = {};
+// A group's mean and rstd from its sets' parts, a warp a group; S channels a set.
+__global__ void __launch_bounds__(kThreads) norm_join(NormArgs a, int S) {
+    const int64_t g = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32;
+    if (g >= (int64_t)a.N * a.G) return;
+    const int64_t n = g / a.G;
+    const int lane = threadIdx.x % 32, sets = a.C / S, total = a.chunks * a.spg;
+    const float2* parts = reinterpret_cast<const float2*>(a.parts) + n * a.chunks * sets + (g - n * a.G) * a.spg;
+    Moments m{0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-                for (int n = threadIdx.x % 8; n < a.N; n += 8) s = add(s, __ldcg(channel + (int64_t)n * a.C + c));
-                s = sum_lanes<8>(s);
-                if (threadIdx.x % 8 || c0 >= a.C) continue;
-                if (a.dbeta) a.dbeta[c] = s.x;
-                if (a.dgamma) a.dgamma[c] = s.y;
-            }
-        } else {
-            const bool good = __syncthreads_and(threadIdx.x != 0 || wait_flag(ready + it.n, a.status));
-            const Backward<V> f(a, it.n, own_c);
-            float4 ab[kPairs<V>];
-            pair_stats<V>(ab, a, own_c, [&](int g) { return __ldcg(group + (int64_t)it.n * a.G + g); });
-            T* dx = static_cast<T*>(a.out) + ((int64_t)it.n * a.pixels + it.begin + pipe.th.row) * a.C + at.c;
-            const int64_t dx_step = (int64_t)a.rows * a.C;
-            with_act(a.act, [&](auto act) {
-                pipe.each(it, at.mine, [&](int first, auto k) {
-                    T* to = dx + first * dx_step;
-#pragma unroll
-                    for (int u = 0; u < U; ++u, to += dx_step)
-                        if (u < k && good)
-                            store<T, V>(to, f.template apply<decltype(act)::value>(pipe.get(0, u), pipe.get(1, u),
-                                                                                 [&](int i) { return ab[i]; }));
-                });
-            });
-        }
+    for (int e = lane; e < total; e += 32) {
+        const int k = a.spg == 1 ? e : e / a.spg;
+        const float2 p = parts[(int64_t)k * sets + (e - k * a.spg)];
+        const int64_t left = a.pixels - (int64_t)k * a.chunk;
+        m = join(m, {(float)(left < a.chunk ? left : a.chunk) * S, p.x, p.y});
     }
-    copies_wait<0>();
+    m = join_lanes<32>(m);
+    if (lane == 0) {
+        const float var = m.m2 / ((float)a.pixels * a.cpg);
+        a.mean_out[g] = m.mean;
+        a.rstd_out[g] = 1.0f / sqrtf(var + a.eps);
+    }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads, 3) norm_result(NormArgs a) {
+    extern __shared__ uint4 smem4[];
+    const Stretch at(a, V, a.N - 1 - blockIdx.z);
+    if (!at.mine) return;
+    const T* x = static_cast<const T*>(a.x) + at.n * a.x_sample + (at.begin + at.row) * a.x_pixel + at.c;
+    const Held<T, V> v(a, smem4);
+    const int half = (at.mine + 1) / 2;
+    v.copy(x, a.rows * a.x_pixel, 0, half);
+    copies_end();
+    v.copy(x, a.rows * a.x_pixel, half, at.mine);
+    copies_end();
+    const float *mean = a.mean_out + (int64_t)at.n * a.G, *rstd = a.rstd_out + (int64_t)at.n * a.G;
+    const Forward<V> f(a, at.c, [&](int g) { return make_float2(mean[g], rstd[g]); });
+    T* y = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
+    as_they_come(at.mine, [&](int first, int end) { f.write(a, v, first, end, y); });
+}
+
+// the copies of a thread's vectors of x and dy, in two groups
+template <typename T, int V>
+__device__ __forceinline__ void copy_both(const NormArgs& a, int n, int64_t pixel, int c, int count, const Held<T, V>& x, const Held<T, V>& dy) {
+    const T* px = static_cast<const T*>(a.x) + n * a.x_sample + pixel * a.x_pixel + c;
+    const T* pd = static_cast<const T*>(a.dy) + n * a.dy_sample + pixel * a.dy_pixel + c;
+    const int half = (count + 1) / 2;
+    x.copy(px, a.rows * a.x_pixel, 0, half);
+    dy.copy(pd, a.rows * a.dy_pixel, 0, half);
+    copies_end();
+    x.copy(px, a.rows * a.x_pixel, half, count);
+    dy.copy(pd, a.rows * a.dy_pixel, half, count);
+    copies_end();
+}
+
+// parts[n][chunk][c] = sums of dz and of dz d of a stretch
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads, 3) norm_back_sums(NormArgs a) {
+    extern __shared__ uint4 smem4[];
+    float2* s_sums = reinterpret_cast<float2*>(static_cast<Vec<T, V>*>(static_cast<void*>(smem4)) + 2 * a.held);
+    const Stretch at(a, V, blockIdx.z);
+    float2 sb[kPairs<V>] = {}, sg[kPairs<V>] = {};
+    if (at.mine) {
+        const Held<T, V> x(a, smem4), dy(a, smem4, a.held);
+        copy_both(a, at.n, at.begin + at.row, at.c, at.mine, x, dy);
+        const Backward<V> f(a, at.n, at.c);
+        as_they_come(at.mine, [&](int first, int end) { f.sum_all(a, x, dy, first, end, sb, sg); });
+    }
+    put_sums<V>(a, at.row, at.col, s_sums, sb, sg);
+    const int here = min(a.cols * V, a.C - (int)blockIdx.y * a.cols * V), lane = threadIdx.x % 8;
+    float2* parts = reinterpret_cast<float2*>(a.parts) + ((int64_t)at.n * a.chunks + blockIdx.x) * a.C + blockIdx.y * a.cols * V;
+    for (int j0 = threadIdx.x / 8; j0 < (here + 3) / 4 * 4; j0 += kThreads / 8) {
+        const int j = min(j0, here - 1), col = j / V, i = j % V;
+        const float2 s = sum_rows(a, s_sums, i, col);
+        if (lane == 0 && j0 < here) parts[j] = s;
+    }
+}
+
+// A CTA a group of a sample: sums[n][c] = (sum of dz, of dz xh), then [n][g] = p and q.
+__global__ void __launch_bounds__(kThreads) norm_back_join(NormArgs a) {
+    __shared__ float2 s_warp[kWarps];
+    const int g = blockIdx.x, n = blockIdx.y, lane = threadIdx.x % 8;
+    const float rstd = a.rstd[(int64_t)n * a.G + g];
+    const float2* parts = reinterpret_cast<const float2*>(a.parts) + (int64_t)n * a.chunks * a.C + g * a.cpg;
+    float2 *channel = reinterpret_cast<float2*>(a.sums), *group = channel + (int64_t)a.N * a.C, all = {};
+    for (int i0 = threadIdx.x / 8; i0 < (a.cpg + 3) / 4 * 4; i0 += kThreads / 8) {            // eight lanes a channel
+        const int i = min(i0, a.cpg - 1);
+        float2 s = {};
+#pragma unroll 4
+        for (int k = lane; k < a.chunks; k += 8) s = add(s, parts[(int64_t)k * a.C + i]);
+        s = sum_lanes<8>(s);
+        if (lane || i0 >= a.cpg) continue;
+        channel[(int64_t)n * a.C + g * a.cpg + i] = make_float2(s.x, rstd * s.y);
+        all = fma(both(a.gamma ? a.gamma[g * a.cpg + i] : 1.0f), s, all);
+    }
+    all = sum_lanes<32>(all);
+    if (threadIdx.x % 32 == 0) s_warp[threadIdx.x / 32] = all;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < kWarps; ++w) all = add(all, s_warp[w]);
+    group[(int64_t)n * a.G + g] = group_pq(a, all, rstd);
+}
+
+// dgamma and dbeta, a warp 32 channels and the CTA's warps the parts [part][C] in turn, in their order
+__device__ __forceinline__ void norm_back_params(const NormArgs& a, const float2* from, int parts, int block) {
+    __shared__ float2 s[kThreads];
+    const int c = block * 32 + threadIdx.x % 32;
+    float2 sum = {};
+    if (c < a.C) {
+#pragma unroll 8
+        for (int k = threadIdx.x / 32; k < parts; k += kWarps) sum = add(sum, from[(int64_t)k * a.C + c]);
+    }
+    s[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32 || c >= a.C) return;
+    for (int w = 1; w < kWarps; ++w) sum = add(sum, s[w * 32 + threadIdx.x]);
+    if (a.dbeta) a.dbeta[c] = sum.x;
+    if (a.dgamma) a.dgamma[c] = sum.y;
+}
+
+// dx, and in the CTAs of blockIdx.z = 0 the sums over the samples
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads, 3) norm_back_result(NormArgs a) {
+    extern __shared__ uint4 smem4[];
+    const float2 *channel = reinterpret_cast<const float2*>(a.sums), *group = channel + (int64_t)a.N * a.C;
+    if (blockIdx.z == 0) {
+        if (a.dgamma || a.dbeta)
+            for (int block = blockIdx.y * gridDim.x + blockIdx.x; block * 32 < a.C; block += gridDim.x * gridDim.y) {
+                norm_back_params(a, channel, a.N, block);
+                __syncthreads();
+            }
+        return;
+    }
+    const Stretch at(a, V, a.N - blockIdx.z);
+    if (!at.mine) return;
+    const Held<T, V> x(a, smem4), dy(a, smem4, a.held);
+    copy_both(a, at.n, at.begin + at.row, at.c, at.mine, x, dy);
+    const Backward<V> f(a, at.n, at.c);
+    float4 pq[kPairs<V>];
+    pair_stats<V>(pq, a, at.c, [&](int g) { return group[(int64_t)at.n * a.G + g]; });
+    T* dx = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
+    as_they_come(at.mine, [&](int first, int end) { f.write(a, x, dy, first, end, dx, pq); });
 }
 
 // -------------------------------------------------------------------------------- resident kernels
@@ -761,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_back_stream(NormArgs a) {
 namespace cg = cooperative_groups;
 
 // A unit of the resident kernels is a sample's slab: `cols` vectors of every pixel, whole groups.  The CTAs
-// of a cluster take a stretch of its pixels each and hold it in registers between the sums and the
+// of a cluster take a stretch of its pixels each and hold it in shared memory between the sums and the
 // result, so that every value is read from memory once.
 template <int V>
 struct Unit {
@@ -786,24 +727,30 @@ struct Unit {
     }
 };
 
-template <typename T, int V, int NS, int K>
-__global__ void __launch_bounds__(kThreads, K * V * sizeof(T) > 128 ? 2 : 3) norm_resident(NormArgs a) {
+template <typename T, int V, int NS>
+__global__ void __launch_bounds__(kThreads, 4) norm_resident(NormArgs a) {
     constexpr int S = V / NS;
-    extern __shared__ float2 smem2[];
-    float2 *s_sets = smem2, *s_part = s_sets + NS * kThreads;     // a thread's sets; the CTA's groups: mean, m2
-    float2* s_stat = s_part + a.groups;                           // the cluster's groups: mean, rstd
+    extern __shared__ uint4 smem4[];
+    float2* s_sets = reinterpret_cast<float2*>(static_cast<Vec<T, V>*>(static_cast<void*>(smem4)) + a.held);
+    float2 *s_part = s_sets + NS * kThreads, *s_stat = s_part + a.groups;   // the CTA's groups: mean, m2; the cluster's: mean, rstd
+    float* s_affine = reinterpret_cast<float*>(s_stat + a.groups);          // the slab's gamma, then beta
     __shared__ int s_mine[kThreads];
     const Unit<V> at(a);
-    const int lane = threadIdx.x % 32;
+    const int lane = threadIdx.x % 32, width = a.cols * V;
     const T* x = static_cast<const T*>(a.x) + at.n * a.x_sample + (at.begin + at.row) * a.x_pixel + at.c;
-    const int64_t step = a.rows * a.x_pixel;
-    Vec<T, V> v[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-        if (k < at.mine) v[k] = load<T, V>(x + k * step);
+    const Held<T, V> v(a, smem4);
     {
+        const int half = (at.mine + 1) / 2;
+        v.copy(x, a.rows * a.x_pixel, 0, half);
+        copies_end();
+        v.copy(x, a.rows * a.x_pixel, half, at.mine);
+        copies_end();
+        for (int j = threadIdx.x; j < width; j += kThreads) {
+            s_affine[j] = a.gamma ? a.gamma[at.slab * width + j] : 1.0f;
+            s_affine[width + j] = a.beta ? a.beta[at.slab * width + j] : 0.0f;
+        }
         Sets<T, V, NS> m;
-        m.take(v, at.mine);
+        as_they_come(at.mine, [&](int first, int end) { m.template take_all<4>(v, first, end); });
         m.put(s_sets);
     }
     s_mine[threadIdx.x] = at.mine * S;
@@ -839,55 +786,38 @@ __global__ void __launch_bounds__(kThreads, K * V * sizeof(T) > 128 ? 2 : 3) nor
     cluster.barrier_arrive();                                     // the others' parts are read
     if (at.mine) {
         const int first = at.slab * a.groups;
-        const Forward<V> f(a, at.c, [&](int g) { return s_stat[g - first]; });
+        const Forward<V> f(a, at.c, [&](int g) { return s_stat[g - first]; }, s_affine + at.col * V, s_affine + width + at.col * V);
         T* y = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
-        const int64_t y_step = (int64_t)a.rows * a.C;
-        with_act(a.act, [&](auto act) {
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (k < at.mine) store<T, V>(y + k * y_step, f.template apply<decltype(act)::value>(v[k]));
-        });
+        f.write(a, v, 0, at.mine, y);
     }
     cluster.barrier_wait();
 }
 
-// parts[n][rank][c] = (sum of dz, sum of dz xh) over the CTA's pixels, for norm_back_params; and dx.
-template <typename T, int V, int K>
-__global__ void __launch_bounds__(kThreads, 2) norm_back_resident(NormArgs a) {
-    extern __shared__ float2 smem2[];
+// parts[n][rank][c] = (sum of dz, sum of dz xh) over the CTA's pixels, for norm_back_sum_parts; and dx.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads, 3) norm_back_resident(NormArgs a) {
+    extern __shared__ uint4 smem4[];
     const int width = a.cols * V, lane = threadIdx.x % 32;
-    float2 *s_sums = smem2, *s_chan = s_sums + V * kThreads;      // a thread's sums; the CTA's channels
-    float2 *s_part = s_chan + width, *s_stat = s_part + a.groups; // the CTA's groups: A, B; the cluster's
+    // a thread's sums; the CTA's channels and groups: sums; the cluster's groups: p, q
+    float2* s_sums = reinterpret_cast<float2*>(static_cast<Vec<T, V>*>(static_cast<void*>(smem4)) + 2 * a.held);
+    float2 *s_chan = s_sums + a.quarter * V, *s_part = s_chan + width, *s_stat = s_part + a.groups;
     const Unit<V> at(a);
-    const T* x = static_cast<const T*>(a.x) + at.n * a.x_sample + (at.begin + at.row) * a.x_pixel + at.c;
-    const T* dy = static_cast<const T*>(a.dy) + at.n * a.dy_sample + (at.begin + at.row) * a.dy_pixel + at.c;
-    const int64_t x_step = a.rows * a.x_pixel, dy_step = a.rows * a.dy_pixel;
-    Vec<T, V> v[K], w[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-        if (k < at.mine) {
-            v[k] = load<T, V>(x + k * x_step);
-            w[k] = load<T, V>(dy + k * dy_step);
-        }
+    const Held<T, V> x(a, smem4), dy(a, smem4, a.held);
     float2 sb[kPairs<V>] = {}, sg[kPairs<V>] = {};
     if (at.mine) {
+        copy_both(a, at.n, at.begin + at.row, at.c, at.mine, x, dy);
         const Backward<V> f(a, at.n, at.c);
-        with_act(a.act, [&](auto act) {
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (k < at.mine) f.template sum<decltype(act)::value>(v[k], w[k], sb, sg);
-        });
+        as_they_come(at.mine, [&](int first, int end) { f.sum_all(a, x, dy, first, end, sb, sg); });
     }
-    put_sums<V>(s_sums, sb, sg);
-    __syncthreads();
+    put_sums<V>(a, at.row, at.col, s_sums, sb, sg);
     for (int j0 = threadIdx.x / 8; j0 < (width + 3) / 4 * 4; j0 += kThreads / 8) {            // eight lanes a channel
         const int j = min(j0, width - 1), col = j / V, i = j % V;
-        float2 s = {};
-        for (int r = threadIdx.x % 8; r < a.rows; r += 8) s = add(s, s_sums[i * kThreads + r * a.cols + col]);
-        s = sum_lanes<8>(s);
+        const float2 s = sum_rows(a, s_sums, i, col);
         if (threadIdx.x % 8 == 0 && j0 < width) {
             s_chan[j] = s;
-            reinterpret_cast<float2*>(a.parts)[((int64_t)at.n * a.cluster + at.rank) * a.C + at.slab * width + j] = s;
+            const int c = at.slab * width + j;
+            const float rstd = a.rstd[(int64_t)at.n * a.G + GroupOf(a, c).g];
+            reinterpret_cast<float2*>(a.parts)[((int64_t)at.n * a.cluster + at.rank) * a.C + c] = make_float2(s.x, rstd * s.y);
         }
     }
     __syncthreads();
@@ -900,167 +830,107 @@ __global__ void __launch_bounds__(kThreads, 2) norm_back_resident(NormArgs a) {
     }
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    const float2 inv = both(1.0f / ((float)a.pixels * a.cpg));
     for (int g = threadIdx.x; g < a.groups; g += kThreads) {
         float2 s = {};
         for (int r = 0; r < a.cluster; ++r) s = add(s, *cluster.map_shared_rank(s_part + g, r));
-        s_stat[g] = mul(s, inv);
+        s_stat[g] = group_pq(a, s, a.rstd[(int64_t)at.n * a.G + at.slab * a.groups + g]);
     }
     __syncthreads();
     cluster.barrier_arrive();
     if (at.mine) {
         const Backward<V> f(a, at.n, at.c);
         const int first = at.slab * a.groups;
-        float4 ab[kPairs<V>];
-        pair_stats<V>(ab, a, at.c, [&](int g) { return s_stat[g - first]; });
+        float4 pq[kPairs<V>];
+        pair_stats<V>(pq, a, at.c, [&](int g) { return s_stat[g - first]; });
         T* dx = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
-        const int64_t dx_step = (int64_t)a.rows * a.C;
-        with_act(a.act, [&](auto act) {
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (k < at.mine)
-                    store<T, V>(dx + k * dx_step, f.template apply<decltype(act)::value>(v[k], w[k], [&](int i) { return ab[i]; }));
-        });
+        f.write(a, x, dy, 0, at.mine, dx, pq);
     }
     cluster.barrier_wait();
 }
 
-// dgamma and dbeta from the parts of norm_back_resident, in their order: a warp takes 32 channels, the
-// CTA's warps the parts in turn.
-__global__ void __launch_bounds__(kThreads) norm_back_params(NormArgs a) {
-    __shared__ float2 s[kThreads];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, parts = a.N * a.cluster;
-    float2 sum = {};
-    if (c < a.C)
-        for (int k = threadIdx.x / 32; k < parts; k += kWarps)
-            sum = add(sum, reinterpret_cast<const float2*>(a.parts)[(int64_t)k * a.C + c]);
-    s[threadIdx.x] = sum;
-    __syncthreads();
-    if (threadIdx.x >= 32 || c >= a.C) return;
-    for (int w = 1; w < kWarps; ++w) sum = add(sum, s[w * 32 + threadIdx.x]);
-    if (a.dbeta) a.dbeta[c] = sum.x;
-    if (a.dgamma) a.dgamma[c] = sum.y;
+__global__ void __launch_bounds__(kThreads) norm_back_sum_parts(NormArgs a) {
+    norm_back_params(a, reinterpret_cast<const float2*>(a.parts), a.N * a.cluster, blockIdx.x);
 }
 
 // -------------------------------------------------------------------------------- launches
 
-// Lets a kernel have `bytes` of dynamic shared memory on the current device; `allowed` remembers the devices.
+// Lets a kernel have all of an SM's shared memory; `done` remembers on which devices it may.
 template <typename K>
-cudaError_t allow_shared(K* kernel, size_t bytes, std::atomic<uint64_t>& allowed) {
+cudaError_t allow_shared(K* kernel, std::atomic<uint64_t>& done) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && !(dev < 64 && allowed.load() >> dev & 1)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e == cudaSuccess && dev < 64) allowed.fetch_or(uint64_t(1) << dev);
+    if (e == cudaSuccess && !(dev < 64 && done.load() >> dev & 1)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormShared);
+        if (e == cudaSuccess && dev < 64) done.fetch_or(uint64_t(1) << dev);
     }
     if (e != cudaSuccess) cudaGetLastError();
     return e;
 }
 
-template <typename... A>
-cudaError_t launch_clusters(void (*kernel)(A...), const NormArgs& a, size_t smem, cudaStream_t st) {
+template <typename K>
+cudaError_t launch(K* kernel, std::atomic<uint64_t>& done, const NormArgs& a, dim3 grid, size_t smem, cudaStream_t st, int cluster = 0) {
+    if (const cudaError_t e = allow_shared(kernel, done)) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.cluster, (unsigned)a.slabs, (unsigned)a.N);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)a.cluster;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster ? 1 : 0;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a), l = cudaGetLastError();
     return e != cudaSuccess ? e : l;
 }
 
 template <typename T, int V, int NS>
-cudaError_t forward_held(const NormArgs& a, int K, cudaStream_t st) {
-    const size_t smem = (NS * kThreads + 2 * (size_t)a.groups) * sizeof(float2);
-    if constexpr (V * sizeof(T) == 16) {
-        switch (K) {
-            case 2: return launch_clusters(norm_resident<T, V, NS, 2>, a, smem, st);
-            case 4: return launch_clusters(norm_resident<T, V, NS, 4>, a, smem, st);
-            case 8: return launch_clusters(norm_resident<T, V, NS, 8>, a, smem, st);
-            case 16: return launch_clusters(norm_resident<T, V, NS, 16>, a, smem, st);
-        }
-    } else {
-        switch (K) {
-            case 8: return launch_clusters(norm_resident<T, V, NS, 8>, a, smem, st);
-            case 32: return launch_clusters(norm_resident<T, V, NS, 32>, a, smem, st);
-        }
-    }
-    return cudaErrorInvalidValue;
+cudaError_t forward(const NormArgs& a, cudaStream_t st) {
+    static std::atomic<uint64_t> held{0}, sums{0}, result{0};
+    const size_t smem = sizeof(Vec<T, V>) * a.held;
+    if (a.cluster)
+        return launch(norm_resident<T, V, NS>, held, a, dim3(a.cluster, a.slabs, a.N),
+                      smem + (NS * kThreads + 2 * (size_t)a.groups + (size_t)a.cols * V) * sizeof(float2), st, a.cluster);
+    const dim3 grid(a.chunks, a.tiles, a.N);
+    if (const cudaError_t e = launch(norm_sums<T, V, NS>, sums, a, grid, smem, st)) return e;
+    norm_join<<<(unsigned)(((int64_t)a.N * a.G + kWarps - 1) / kWarps), kThreads, 0, st>>>(a, V / NS);
+    return launch(norm_result<T, V>, result, a, grid, smem, st);
 }
 
 template <typename T, int V>
-cudaError_t backward_held(const NormArgs& a, int K, cudaStream_t st) {
-    const size_t smem = (V * kThreads + (size_t)a.cols * V + 2 * (size_t)a.groups) * sizeof(float2);
-    cudaError_t e = cudaErrorInvalidValue;
-    if constexpr (V * sizeof(T) == 16) {
-        switch (K) {
-            case 2: e = launch_clusters(norm_back_resident<T, V, 2>, a, smem, st); break;
-            case 4: e = launch_clusters(norm_back_resident<T, V, 4>, a, smem, st); break;
-            case 8: e = launch_clusters(norm_back_resident<T, V, 8>, a, smem, st); break;
-        }
-    } else {
-        switch (K) {
-            case 8: e = launch_clusters(norm_back_resident<T, V, 8>, a, smem, st); break;
-            case 24: e = launch_clusters(norm_back_resident<T, V, 24>, a, smem, st); break;
-        }
+cudaError_t backward(const NormArgs& a, cudaStream_t st) {
+    static std::atomic<uint64_t> held{0}, sums{0}, result{0};
+    const size_t smem = 2 * sizeof(Vec<T, V>) * a.held;
+    if (a.cluster) {
+        const cudaError_t e = launch(norm_back_resident<T, V>, held, a, dim3(a.cluster, a.slabs, a.N),
+                                     smem + ((size_t)a.quarter * V + (size_t)a.cols * V + 2 * (size_t)a.groups) * sizeof(float2), st, a.cluster);
+        if (e != cudaSuccess || !(a.dgamma || a.dbeta)) return e;
+        norm_back_sum_parts<<<(a.C + 31) / 32, kThreads, 0, st>>>(a);
+        return cudaGetLastError();
     }
-    if (e != cudaSuccess || !(a.dgamma || a.dbeta)) return e;
-    norm_back_params<<<(a.C + 31) / 32, kThreads, 0, st>>>(a);
-    return cudaGetLastError();
-}
-
-cudaError_t zero_counters(const NormArgs& a, cudaStream_t st) {
-    const cudaError_t e = cudaMemsetAsync(a.counters, 0, norm_counters(a.N) * sizeof(uint32_t), st);
-    if (e != cudaSuccess) cudaGetLastError();
-    return e;
-}
-template <typename T, int V, int NS>
-cudaError_t forward_streamed(const NormArgs& a, cudaStream_t st) {
-    static std::atomic<uint64_t> allowed{0};
-    constexpr size_t smem = Pipe<T, V, kStreamBatch, 1>::kBytes;
-    if (const cudaError_t e = allow_shared(norm_stream<T, V, NS>, smem, allowed)) return e;
-    if (const cudaError_t e = zero_counters(a, st)) return e;
-    norm_stream<T, V, NS><<<a.grid, kThreads, smem, st>>>(a);
-    return cudaGetLastError();
-}
-template <typename T, int V>
-cudaError_t backward_streamed(const NormArgs& a, cudaStream_t st) {
-    static std::atomic<uint64_t> allowed{0};
-    constexpr size_t smem = Pipe<T, V, kStreamBatch / 2, 2>::kBytes;
-    if (const cudaError_t e = allow_shared(norm_back_stream<T, V>, smem, allowed)) return e;
-    if (const cudaError_t e = zero_counters(a, st)) return e;
-    norm_back_stream<T, V><<<a.grid, kThreads, smem, st>>>(a);
-    return cudaGetLastError();
+    if (const cudaError_t e = launch(norm_back_sums<T, V>, sums, a, dim3(a.chunks, a.tiles, a.N), smem + (size_t)a.quarter * V * sizeof(float2), st)) return e;
+    norm_back_join<<<dim3(a.G, a.N), kThreads, 0, st>>>(a);
+    return launch(norm_back_result<T, V>, result, a, dim3(a.chunks, a.tiles, a.N + 1), smem, st);
 }
 
 }  // namespace
 
 template <typename T>
-cudaError_t NormKernels<T>::forward(const NormArgs& a, int V, int NS, int K, cudaStream_t st) {
+cudaError_t NormKernels<T>::forward(const NormArgs& a, int V, int NS, cudaStream_t st) {
     constexpr int W = 16 / sizeof(T);
-    if (V == W) {
-        if (K) return NS == 1 ? forward_held<T, W, 1>(a, K, st) : forward_held<T, W, W>(a, K, st);
-        return NS == 1 ? forward_streamed<T, W, 1>(a, st) : forward_streamed<T, W, W>(a, st);
-    }
+    if (V == W) return NS == 1 ? patconv::forward<T, W, 1>(a, st) : patconv::forward<T, W, W>(a, st);
     if constexpr (sizeof(T) == 2)
-        if (V == 2) {
-            if (K) return NS == 1 ? forward_held<T, 2, 1>(a, K, st) : forward_held<T, 2, 2>(a, K, st);
-            return NS == 1 ? forward_streamed<T, 2, 1>(a, st) : forward_streamed<T, 2, 2>(a, st);
-        }
-    return K ? forward_held<T, 1, 1>(a, K, st) : forward_streamed<T, 1, 1>(a, st);
+        if (V == 2) return NS == 1 ? patconv::forward<T, 2, 1>(a, st) : patconv::forward<T, 2, 2>(a, st);
+    return patconv::forward<T, 1, 1>(a, st);
 }
 template <typename T>
-cudaError_t NormKernels<T>::backward(const NormArgs& a, int V, int K, cudaStream_t st) {
+cudaError_t NormKernels<T>::backward(const NormArgs& a, int V, cudaStream_t st) {
     constexpr int W = 16 / sizeof(T);
-    if (V == W) return K ? backward_held<T, W>(a, K, st) : backward_streamed<T, W>(a, st);
+    if (V == W) return patconv::backward<T, W>(a, st);
     if constexpr (sizeof(T) == 2)
-        if (V == 2) return K ? backward_held<T, 2>(a, K, st) : backward_streamed<T, 2>(a, st);
-    return K ? backward_held<T, 1>(a, K, st) : backward_streamed<T, 1>(a, st);
+        if (V == 2) return patconv::backward<T, 2>(a, st);
+    return patconv::backward<T, 1>(a, st);
 }
 
 }  // namespace patconv
