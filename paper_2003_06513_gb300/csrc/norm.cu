@@ -22,9 +22,9 @@
 //
 // Measured on a GB300 (a copy moves 6.67 TB/s), inputs in memory, the launches of a call together:
 //     forward   32x256x56x56 fp16    27 us, 3.8 TB/s of what it must move   (resident, 4 x 50 KB a unit)
-//     forward   32x64x224x224 fp32  200 us, 4.1 TB/s; 6.2 TB/s with the second reading   (streamed)
-//     backward  32x512x14x14 fp32    14 us, 2.7 TB/s   (resident, 1 x 100 KB a unit)
-//     backward  32x128x112x112 fp16 113 us, 2.7 TB/s; 4.6 TB/s with the second reading   (streamed)
+//     forward   32x64x224x224 fp32  195 us, 4.2 TB/s; 6.3 TB/s with the second reading   (streamed)
+//     backward  32x512x14x14 fp32    14 us, 2.7 TB/s   (resident, one CTA a unit)
+//     backward  32x128x112x112 fp16 109 us, 2.8 TB/s; 4.7 TB/s with the second reading   (streamed)
 // The resident form is bound by what its few CTAs on an SM have in flight while some of them wait for their
 // clusters and by the arithmetic of SiLU (two operations of the special function unit an element, four
 // backward); the streamed one by memory forward and by that arithmetic, done twice, backward.
@@ -98,7 +98,7 @@ int places(const Plan& p) { return (p.chunk * p.cols + 7) / 8 * 8; }    // vecto
 // Narrow slabs move parts of lines.  Measured, this plan against one fixed rule (128 bytes, CTAs of 48 KB):
 // 32x256x56x56 fp16 forward 27 against 35 us, 4x128x112x112 fp16 forward 13 against 20, 32x512x14x14 fp32 backward
 // 16 against 25.  Against the streamed form: 32x256x56x56 fp16 forward 27 against 37, 16x256x28x28 fp32 forward 8
-// against 20; but 32x128x112x112 fp16 backward, of slabs of 32 bytes, 136 against 112.
+// against 20; but 32x128x112x112 fp16 backward, of slabs of 32 bytes, 136 against 112 (before the streamed form's kernels overlapped).
 bool resident(const Shape& s, Plan& p) {
     const int es = size_of(s.dtype), bytes = p.V * es, cpg = s.C / s.G, vectors = s.C / p.V, inputs = s.backward ? 2 : 1;
     const int unit = std::lcm(cpg, p.V) / p.V;              // vectors of the least slab of whole groups
