@@ -4,13 +4,14 @@ The C library (``include/patconv.h``, built in-tree by ``build.py``) holds the w
 host packer (pattern projection §4.3, connectivity pruning §4.4, filter grouping and compact
 storage §3.4) and the sm_103a CUDA kernels (pattern-sparse convolution with fused bias + ReLU,
 depthwise variant, max-pool), and the operators of masked retraining (``norm``: group norm with its
-activation, forward and backward; ``optim``: gradient norm and AdamW over many tensors).  This
-package is a thin binding over it; ``workloads`` holds the seeded synthetic inputs.  Importing the package does not load the library; the first
-call that needs it does, and fails loudly if it cannot be built or loaded.
+activation, forward and backward; ``optim``: gradient norm and AdamW over many tensors), which
+``retrain`` runs together.  This package is a thin binding over it; ``workloads`` holds the seeded
+synthetic inputs.  Importing the package does not load the library; the first call that needs it does,
+and fails loudly if it cannot be built or loaded.
 """
 
 __all__ = ["Layer", "pp_pack", "pp_conv", "pp_maxpool2x2", "default_patterns", "group_norm", "pp_group_norm",
-           "pp_group_norm_backward", "AdamW", "GradNorm", "taps_of", "PatconvError"]
+           "pp_group_norm_backward", "AdamW", "GradNorm", "taps_of", "Retrainer", "PatconvError"]
 
 
 def __getattr__(name):
@@ -23,6 +24,9 @@ def __getattr__(name):
     if name in ("AdamW", "GradNorm", "taps_of"):
         from . import optim
         return getattr(optim, name)
+    if name == "Retrainer":
+        from . import retrain
+        return retrain.Retrainer
     if name == "PatconvError":
         from ._lib import PatconvError
         return PatconvError
