@@ -80,7 +80,9 @@ struct Plan {
 };
 
 constexpr int kSMs = 152;
-constexpr int64_t kStretch = 65536, kLeast = 8192, kMostHeld = 163840, kSlabLeast = 32, kSlabMost = 512;
+constexpr double kSmShared = 232448;        // bytes of shared memory of an SM
+constexpr int64_t kStretch = 65536, kLeast = 8192;                                 // streamed: bytes of a CTA
+constexpr int64_t kMostHeld = 163840, kSlabLeast = 32, kSlabMost = 512;            // resident: bytes of a CTA, of a slab's pixel
 
 int quarter_of(const Plan& p) { return (p.rows + 3) / 4 * p.cols; }
 // resident: bytes of shared memory beside the vectors (the kernels' sums, channels and groups)
@@ -94,11 +96,12 @@ int places(const Plan& p) { return (p.chunk * p.cols + 7) / 8 * 8; }    // vecto
 // hold them, the one whose estimated time is least.  In us: a CTA takes 4 beside its work (the first copies'
 // latency, two barriers of the cluster, the second reading of its parameters); its work is what its share of the
 // SM's 44 KB a us moves, or what the arithmetic of its vectors takes, 0.03 a channel of each of its rows of
-// vectors, and 2.2 times as long where it is alone; and there are as many rounds as the SMs need for all CTAs.
-// Narrow slabs move parts of lines.  Measured, this plan against one fixed rule (128 bytes, CTAs of 48 KB):
-// 32x256x56x56 fp16 forward 27 against 35 us, 4x128x112x112 fp16 forward 13 against 20, 32x512x14x14 fp32 backward
-// 16 against 25.  Against the streamed form: 32x256x56x56 fp16 forward 27 against 37, 16x256x28x28 fp32 forward 8
-// against 20; but 32x128x112x112 fp16 backward, of slabs of 32 bytes, 136 against 112 (before the streamed form's kernels overlapped).
+// vectors (0.06 in vectors of 4 bytes, 0.12 of one channel), and 2.2 times as long where it is alone; and there
+// are as many rounds as the SMs need for all CTAs.  Narrow slabs move parts of lines.  Measured, this plan against
+// one fixed rule (128 bytes, CTAs of 48 KB): 32x256x56x56 fp16 forward 27 against 35 us, 4x128x112x112 fp16 forward
+// 13 against 20, 32x512x14x14 fp32 backward 14 against 25.  Against the streamed form: 32x256x56x56 fp16 forward 27
+// against 37, 16x256x28x28 fp32 forward 8 against 20; but 32x128x112x112 fp16 backward, whose slabs would be of 32
+// bytes, 136 against 110.
 bool resident(const Shape& s, Plan& p) {
     const int es = size_of(s.dtype), bytes = p.V * es, cpg = s.C / s.G, vectors = s.C / p.V, inputs = s.backward ? 2 : 1;
     const int unit = std::lcm(cpg, p.V) / p.V;              // vectors of the least slab of whole groups
@@ -108,8 +111,8 @@ bool resident(const Shape& s, Plan& p) {
     Plan best;
     for (int m = 1; m <= steps; ++m) {
         const int width = m * unit * bytes;
-        if (steps % m || m * unit > kNormThreads || m * unit * p.V > 1024 || steps / m > 65535) continue;
-        if ((width < kSlabLeast && m < steps) || (width > kSlabMost && best.cluster)) continue;
+        if (m * unit > kNormThreads || m * unit * p.V > 1024 || (width > kSlabMost && best.cluster)) break;
+        if (steps % m || steps / m > 65535 || (width < kSlabLeast && m < steps)) continue;
         for (int c = 1; c <= 8; c *= 2) {
             const int64_t chunk = (s.pixels + c - 1) / c;
             if (chunk * m * unit * bytes * inputs > kMostHeld) continue;
@@ -122,10 +125,10 @@ bool resident(const Shape& s, Plan& p) {
             const double held = (double)places(q) * bytes * inputs, rows = (double)((chunk + q.rows - 1) / q.rows);
             const double room = held + shared_beside(s, q);
             if (room > kNormShared) continue;
-            const double total = (double)s.N * q.slabs * c, fit = std::min(s.backward ? 3.0 : 4.0, std::floor(232448 / (room + 3072)));
+            const double total = (double)s.N * q.slabs * c, fit = std::min(s.backward ? 3.0 : 4.0, std::floor(kSmShared / (room + 3072)));
             const double rounds = std::ceil(total / (kSMs * fit)), at_once = std::min(fit, std::ceil(total / kSMs));
-            const double work = rows * p.V * 0.03 * inputs, moved = held / inputs * (inputs + 1) / 44e3;
-            const double narrow = width >= 48 ? 1.0 : 1.3;
+            const double channel = p.V == 1 ? 0.12 : bytes == 4 ? 0.06 : 0.03, narrow = width >= 48 ? 1.0 : 1.3;
+            const double work = rows * p.V * channel * inputs, moved = held / inputs * (inputs + 1) / 44e3;
             const double time = rounds * (4 + 0.1 * c + narrow * std::max({at_once * moved, at_once * work, 2.2 * work}));
             if (!best.cluster || time < least) {
                 best = q;
@@ -141,44 +144,60 @@ bool resident(const Shape& s, Plan& p) {
     return true;
 }
 
-// V channels a thread (16 bytes where `align`, the common alignment of addresses and strides in bytes,
-// allows it, else 4 bytes or one channel).  Streamed: a row's vectors over the threads of one or more CTAs,
-// stretches of pixels of about kStretch bytes of all inputs, shorter ones where that makes too few CTAs.
+void set_width(const Shape& s, Plan& p, int V) {
+    p.V = V;
+    p.NS = s.C / s.G % V ? V : 1;
+}
+
+// The streamed form: a row's vectors over the threads of one or more CTAs, stretches of pixels of about kStretch
+// bytes of all inputs, shorter ones where that makes too few CTAs.
+void streamed(const Shape& s, Plan& p) {
+    const int es = size_of(s.dtype), vectors = s.C / p.V;
+    p.tiles = (vectors + kNormThreads - 1) / kNormThreads;
+    p.cols = (vectors + p.tiles - 1) / p.tiles;
+    p.rows = kNormThreads / p.cols;
+    const int64_t row = (int64_t)p.cols * p.V * es;
+    // four CTAs an SM, but none below kLeast bytes
+    const int64_t fill = std::max<int64_t>(1, s.pixels * s.N * p.tiles / (kSMs * 4));
+    const int64_t wanted = std::max<int64_t>({std::min((kStretch / (s.backward ? 2 : 1) + row - 1) / row, fill), (kLeast + row - 1) / row, p.rows});
+    p.chunks = (int)((s.pixels + wanted - 1) / wanted);
+    p.chunk = (int)((s.pixels + p.chunks - 1) / p.chunks);
+    p.chunks = (int)((s.pixels + p.chunk - 1) / p.chunk);
+    const size_t sets = s.backward ? s.C : s.C / (p.V / p.NS);
+    p.parts = (size_t)s.N * p.chunks * sets * 2;
+    p.sums = s.backward ? (size_t)s.N * s.C * 2 + (size_t)s.N * s.G * 2 : 0;
+}
+
+// Vectors of 16 bytes a thread where `align`, the common alignment of addresses and strides in bytes, allows it,
+// else of 4 bytes or one channel.  Narrower ones than that make a slab of whole groups of odd numbers of channels
+// narrow enough for a cluster: 9x312x56x51 fp16 forward in 8 groups takes 16 us so, 31 us streamed.
 Plan plan_of(const Shape& s, int align) {
+    const int es = size_of(s.dtype), widest = align >= 16 ? 16 / es : std::max(1, std::min(align, 4) / es);
     Plan p;
-    const int es = size_of(s.dtype), cpg = s.C / s.G;
-    p.V = align >= 16 ? 16 / es : std::max(1, std::min(align, 4) / es);
-    p.NS = cpg % p.V ? p.V : 1;
-    if (!resident(s, p)) {
-        const int vectors = s.C / p.V;
-        p.tiles = (vectors + kNormThreads - 1) / kNormThreads;
-        p.cols = (vectors + p.tiles - 1) / p.tiles;
-        p.rows = kNormThreads / p.cols;
-        const int64_t row = (int64_t)p.cols * p.V * es;
-        // four CTAs an SM, but none below kLeast bytes
-        const int64_t fill = std::max<int64_t>(1, s.pixels * s.N * p.tiles / (kSMs * 4));
-        const int64_t wanted = std::max<int64_t>({std::min((kStretch / (s.backward ? 2 : 1) + row - 1) / row, fill), (kLeast + row - 1) / row, p.rows});
-        p.chunks = (int)((s.pixels + wanted - 1) / wanted);
-        p.chunk = (int)((s.pixels + p.chunks - 1) / p.chunks);
-        p.chunks = (int)((s.pixels + p.chunk - 1) / p.chunk);
-        const size_t sets = s.backward ? s.C : s.C / (p.V / p.NS);
-        p.parts = (size_t)s.N * p.chunks * sets * 2;
-        p.sums = s.backward ? (size_t)s.N * s.C * 2 + (size_t)s.N * s.G * 2 : 0;
+    for (int V = widest; V && !p.cluster; V = V * es > 4 ? 4 / es : V / 2) {
+        set_width(s, p, V);
+        resident(s, p);
+    }
+    if (!p.cluster) {
+        set_width(s, p, widest);
+        streamed(s, p);
     }
     p.held = places(p);
     if (!s.backward) p.sums += (size_t)s.N * s.G * 2;       // mean and rstd that the caller does not want
     return p;
 }
 
-// of any plan that a call's alignment may lead to
+// enough for any plan that a call's alignment may lead to
 size_t workspace_of(const Shape& s) {
-    size_t most = 0;
+    size_t most = s.backward ? (size_t)s.N * 8 * s.C * 2 : 0;           // resident, in clusters of eight
     for (int align = size_of(s.dtype); align <= 16; align *= 2)
         if ((int64_t)s.C * size_of(s.dtype) % align == 0) {
-            const Plan p = plan_of(s, align);
-            most = std::max(most, (p.parts + p.sums) * sizeof(float));
+            Plan p;
+            set_width(s, p, align >= 16 ? 16 / size_of(s.dtype) : std::max(1, std::min(align, 4) / size_of(s.dtype)));
+            streamed(s, p);
+            most = std::max(most, p.parts + p.sums);
         }
-    return most;
+    return (most + (s.backward ? 0 : (size_t)s.N * s.G * 2)) * sizeof(float);
 }
 
 int align_of(const void* p) {

@@ -562,29 +562,31 @@ __global__ void __launch_bounds__(kThreads, 3) norm_sums(NormArgs a) {
     }
 }
 
-// A group's mean and rstd from its sets' parts, a warp a group; S channels a set.
+// A group's mean and rstd from its sets' parts, a CTA a group of a sample; S channels a set.
 __global__ void __launch_bounds__(kThreads) norm_join(NormArgs a, int S) {
+    __shared__ Moments s_warp[kWarps];
     let_next_start();
     wait_for_previous();
-    const int64_t g = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32;
-    if (g >= (int64_t)a.N * a.G) return;
-    const int64_t n = g / a.G;
-    const int lane = threadIdx.x % 32, sets = a.C / S, total = a.chunks * a.spg;
-    const float2* parts = reinterpret_cast<const float2*>(a.parts) + n * a.chunks * sets + (g - n * a.G) * a.spg;
+    const int g = blockIdx.x, n = blockIdx.y, sets = a.C / S, total = a.chunks * a.spg;
+    const float2* parts = reinterpret_cast<const float2*>(a.parts) + (int64_t)n * a.chunks * sets + g * a.spg;
     Moments m{0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int e = lane; e < total; e += 32) {
+    for (int e = threadIdx.x; e < total; e += kThreads) {
         const int k = a.spg == 1 ? e : e / a.spg;
         const float2 p = parts[(int64_t)k * sets + (e - k * a.spg)];
         const int64_t left = a.pixels - (int64_t)k * a.chunk;
         m = join(m, {(float)(left < a.chunk ? left : a.chunk) * S, p.x, p.y});
     }
     m = join_lanes<32>(m);
-    if (lane == 0) {
-        const float var = m.m2 / ((float)a.pixels * a.cpg);
-        a.mean_out[g] = m.mean;
-        a.rstd_out[g] = 1.0f / sqrtf(var + a.eps);
-    }
+    if (threadIdx.x % 32 == 0) s_warp[threadIdx.x / 32] = m;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    m = threadIdx.x < kWarps ? s_warp[threadIdx.x] : Moments{0.0f, 0.0f, 0.0f};
+    m = join_lanes<kWarps>(m);
+    if (threadIdx.x) return;
+    const float var = m.m2 / ((float)a.pixels * a.cpg);
+    a.mean_out[(int64_t)n * a.G + g] = m.mean;
+    a.rstd_out[(int64_t)n * a.G + g] = 1.0f / sqrtf(var + a.eps);
 }
 
 template <typename T, int V>
@@ -924,8 +926,7 @@ cudaError_t forward(const NormArgs& a, cudaStream_t st) {
                       smem + (NS * kThreads + 2 * (size_t)a.groups + (size_t)a.cols * V) * sizeof(float2), st);
     const dim3 grid(a.chunks, a.tiles, a.N);
     if (const cudaError_t e = launch(norm_sums<T, V, NS>, sums, a, kFirst, grid, smem, st)) return e;
-    const dim3 join((unsigned)(((int64_t)a.N * a.G + kWarps - 1) / kWarps));
-    if (const cudaError_t e = launch_as(norm_join, kNext, join, 0, st, a, V / NS)) return e;
+    if (const cudaError_t e = launch_as(norm_join, kNext, dim3(a.G, a.N), 0, st, a, V / NS)) return e;
     return launch(norm_result<T, V>, result, a, kNext, grid, smem, st);
 }
 
