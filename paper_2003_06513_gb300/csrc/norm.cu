@@ -24,10 +24,10 @@
 //     forward   32x256x56x56 fp16    27 us, 3.8 TB/s of what it must move   (resident, 4 x 50 KB a unit)
 //     forward   32x64x224x224 fp32  195 us, 4.2 TB/s; 6.3 TB/s with the second reading   (streamed)
 //     backward  32x512x14x14 fp32    14 us, 2.7 TB/s   (resident, one CTA a unit)
-//     backward  32x128x112x112 fp16 109 us, 2.8 TB/s; 4.7 TB/s with the second reading   (streamed)
+//     backward  32x128x112x112 fp16  92 us, 3.4 TB/s; 5.6 TB/s with the second reading   (streamed)
 // The resident form is bound by what its few CTAs on an SM have in flight while some of them wait for their
 // clusters and by the arithmetic of SiLU (two operations of the special function unit an element, four
-// backward); the streamed one by memory forward and by that arithmetic, done twice, backward.
+// backward); the streamed one by memory, whose rate falls a little short of a copy's backward.
 //
 // Means and squares are joined pairwise as (count, mean, sum of squared distances from the mean): a
 // plain sum of squares would lose the variance of values far from zero.
@@ -74,14 +74,15 @@ struct Plan {
     int cols = 1, rows = 1, chunk = 1;      // vectors of a row and rows of a CTA, pixels of a CTA
     int NS = 1;                             // sets of a vector's channels that are summed apart
     int tiles = 1, chunks = 1;              // streamed: CTAs side by side, stretches down a sample
-    int held = 0;                           // vectors of each input that a CTA holds
+    int held = 0, depth = 1;                // vectors of each input that a CTA holds; streamed: half a thread's of them
     int cluster = 0, slabs = 1;             // resident: CTAs a unit (0: streamed), slabs
     size_t parts = 0, sums = 0;             // floats of the workspace
 };
 
 constexpr int kSMs = 152;
 constexpr double kSmShared = 232448;        // bytes of shared memory of an SM
-constexpr int64_t kStretch = 65536, kLeast = 8192;                                 // streamed: bytes of a CTA
+constexpr int64_t kStretch = 131072, kStretchBack = 1048576, kLeast = 8192;        // streamed: bytes of a CTA,
+constexpr int kRing = 65536;                                                       // of those it holds at a time
 constexpr int64_t kMostHeld = 163840, kSlabLeast = 32, kSlabMost = 512;            // resident: bytes of a CTA, of a slab's pixel
 
 int quarter_of(const Plan& p) { return (p.rows + 3) / 4 * p.cols; }
@@ -101,7 +102,7 @@ int places(const Plan& p) { return (p.chunk * p.cols + 7) / 8 * 8; }    // vecto
 // one fixed rule (128 bytes, CTAs of 48 KB): 32x256x56x56 fp16 forward 27 against 35 us, 4x128x112x112 fp16 forward
 // 13 against 20, 32x512x14x14 fp32 backward 14 against 25.  Against the streamed form: 32x256x56x56 fp16 forward 27
 // against 37, 16x256x28x28 fp32 forward 8 against 20; but 32x128x112x112 fp16 backward, whose slabs would be of 32
-// bytes, 136 against 110.
+// bytes, 136 against 92.
 bool resident(const Shape& s, Plan& p) {
     const int es = size_of(s.dtype), bytes = p.V * es, cpg = s.C / s.G, vectors = s.C / p.V, inputs = s.backward ? 2 : 1;
     const int unit = std::lcm(cpg, p.V) / p.V;              // vectors of the least slab of whole groups
@@ -149,20 +150,27 @@ void set_width(const Shape& s, Plan& p, int V) {
     p.NS = s.C / s.G % V ? V : 1;
 }
 
-// The streamed form: a row's vectors over the threads of one or more CTAs, stretches of pixels of about kStretch
-// bytes of all inputs, shorter ones where that makes too few CTAs.
+// The streamed form: a row's vectors over the threads of one or more CTAs, stretches of pixels of up to kStretch
+// bytes of all inputs (backward kStretchBack), so many that the CTAs fill the SMs a whole number of times (three on
+// each, backward two, which have the registers for it), but none below kLeast bytes.  A CTA reads its stretch
+// through kRing bytes of shared memory.  Backward a thread has eight channels' parameters to fetch and sums to join,
+// which a long stretch pays for: 32x128x112x112 fp16 takes 92 us with up to 1 MB, 99 with 256 KB, 110 with 64 KB
+// all held at once, 97 with three CTAs an SM; 48 KB of ring cost 2 us, 96 KB gain nothing.  Forward there is little
+// of that, and the stretches of many CTAs at a time are read faster: 32x64x224x224 fp32 takes 195 us with up to
+// 128 KB, 198 with 256 KB, 206 with 512 KB, 199 with 48 KB of ring.
 void streamed(const Shape& s, Plan& p) {
-    const int es = size_of(s.dtype), vectors = s.C / p.V;
+    const int es = size_of(s.dtype), vectors = s.C / p.V, inputs = s.backward ? 2 : 1;
     p.tiles = (vectors + kNormThreads - 1) / kNormThreads;
     p.cols = (vectors + p.tiles - 1) / p.tiles;
     p.rows = kNormThreads / p.cols;
-    const int64_t row = (int64_t)p.cols * p.V * es;
-    // four CTAs an SM, but none below kLeast bytes
-    const int64_t fill = std::max<int64_t>(1, s.pixels * s.N * p.tiles / (kSMs * 4));
-    const int64_t wanted = std::max<int64_t>({std::min((kStretch / (s.backward ? 2 : 1) + row - 1) / row, fill), (kLeast + row - 1) / row, p.rows});
-    p.chunks = (int)((s.pixels + wanted - 1) / wanted);
-    p.chunk = (int)((s.pixels + p.chunks - 1) / p.chunks);
+    const int64_t row = (int64_t)p.cols * p.V * es, side = (int64_t)s.N * p.tiles, full = kSMs * (s.backward ? 2 : 3);
+    const int64_t most = std::max<int64_t>(p.rows, (s.backward ? kStretchBack / 2 : kStretch) / row), least = std::max<int64_t>(p.rows, (kLeast + row - 1) / row);
+    const int64_t times = std::max<int64_t>(1, (side * ((s.pixels + most - 1) / most) + full - 1) / full);
+    const int64_t chunks = std::max<int64_t>(1, times * full / side);
+    p.chunk = (int)std::min(s.pixels, std::max(least, (s.pixels + chunks - 1) / chunks));
     p.chunks = (int)((s.pixels + p.chunk - 1) / p.chunk);
+    const int vector = p.V * es, mine = (p.chunk + p.rows - 1) / p.rows;
+    p.depth = std::min(kRing / 2 / inputs / (vector * kNormThreads), (mine + 1) / 2);
     const size_t sets = s.backward ? s.C : s.C / (p.V / p.NS);
     p.parts = (size_t)s.N * p.chunks * sets * 2;
     p.sums = s.backward ? (size_t)s.N * s.C * 2 + (size_t)s.N * s.G * 2 : 0;
@@ -170,7 +178,7 @@ void streamed(const Shape& s, Plan& p) {
 
 // Vectors of 16 bytes a thread where `align`, the common alignment of addresses and strides in bytes, allows it,
 // else of 4 bytes or one channel.  Narrower ones than that make a slab of whole groups of odd numbers of channels
-// narrow enough for a cluster: 9x312x56x51 fp16 forward in 8 groups takes 16 us so, 31 us streamed.
+// narrow enough for a cluster: 9x312x56x51 fp16 forward in 8 groups takes 14 us so, 27 us streamed.
 Plan plan_of(const Shape& s, int align) {
     const int es = size_of(s.dtype), widest = align >= 16 ? 16 / es : std::max(1, std::min(align, 4) / es);
     Plan p;
@@ -182,7 +190,7 @@ Plan plan_of(const Shape& s, int align) {
         set_width(s, p, widest);
         streamed(s, p);
     }
-    p.held = places(p);
+    p.held = p.cluster ? places(p) : (2 * p.depth * p.rows * p.cols + 7) / 8 * 8;
     if (!s.backward) p.sums += (size_t)s.N * s.G * 2;       // mean and rstd that the caller does not want
     return p;
 }
@@ -247,6 +255,7 @@ NormArgs args_of(const Shape& s, const Plan& p, const void* x, int64_t x_pixel, 
     a.chunk = p.chunk;
     a.chunks = p.chunks;
     a.held = p.held;
+    a.depth = p.depth;
     a.quarter = quarter_of(p);
     a.cluster = p.cluster;
     a.slabs = p.slabs;

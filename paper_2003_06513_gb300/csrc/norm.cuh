@@ -6,8 +6,9 @@
 // instruction, the activation is chosen outside the loops, and exp and 1 / x are the hardware's
 // approximations (2 and 1 ulp) with subnormals flushed.
 //
-// What a CTA reads goes to shared memory by asynchronous copies, all of its stretch asked for at once and the
-// sums of the first half taken while the second is under way.  Held in registers instead (up to 8 vectors a
+// What a CTA reads goes to shared memory by asynchronous copies: in the resident kernels all of its stretch asked
+// for at once, and the sums of the first half taken while the second is under way; in the streamed ones through a
+// ring of two halves, one asked for while the other is used.  Held in registers instead (up to 8 vectors a
 // thread, one CTA fewer on an SM) the forward pass of 32x256x56x56 fp16 took 38 us, so 27.
 #pragma once
 
@@ -167,12 +168,18 @@ struct Held {
     // one place a vector of the CTA's pixels; the input's places begin at `from`
     __device__ __forceinline__ Held(const NormArgs& a, void* smem, int from = 0)
         : mine(static_cast<Vec<T, V>*>(smem) + from + threadIdx.x), step(a.rows * a.cols) {}
-    __device__ __forceinline__ void copy(const T* p, int64_t stride, int first, int end) const {
-        p += first * stride;
-#pragma unroll 4
+    // asks for vectors first to end - 1, the first of them at p, which goes on to the next
+    __device__ __forceinline__ void copy(const T*& p, int64_t stride, int first, int end) const {
+#pragma unroll 2
         for (int k = first; k < end; ++k, p += stride) copy_async(mine + k * step, p);
     }
     __device__ __forceinline__ const Vec<T, V>& operator[](int k) const { return mine[k * step]; }
+    // vector k in the place of vector k - shift
+    __device__ __forceinline__ Held from(int shift) const {
+        Held h = *this;
+        h.mine -= shift * step;
+        return h;
+    }
 };
 // f(k, how many) for k from first to end - 1, U at a time while there are as many, then one at a time
 template <int U, typename F>
@@ -190,6 +197,28 @@ __device__ __forceinline__ void as_they_come(int count, F&& f) {
     f(0, half);
     copies_wait<0>();
     f(half, count);
+}
+
+// A thread's `count` vectors through places for 2 x depth of them, `depth` at a time: use(shift, first, end) gets them
+// as soon as their copies have come, with vector k in place k - shift, and copy(shift, first, end) asks for those
+// that take the places of the ones used.
+template <typename Copy, typename Use>
+__device__ __forceinline__ void flow(int count, int depth, Copy&& copy, Use&& use) {
+    copy(0, 0, min(depth, count));
+    copies_end();
+    copy(0, depth, min(2 * depth, count));
+    copies_end();
+    int shift = 0;
+    bool second = false;
+#pragma unroll 1
+    for (int k = 0; k < count; k += depth) {
+        copies_wait<1>();
+        use(shift, k, min(k + depth, count));
+        copy(shift + 2 * depth, k + 2 * depth, min(k + 3 * depth, count));
+        copies_end();
+        shift += second ? 2 * depth : 0;
+        second = !second;
+    }
 }
 
 // A thread's moments of NS sets of S = V / NS adjacent channels, each within one group.
@@ -300,7 +329,7 @@ __device__ __forceinline__ float2 through(float2 dy, float2 z) {
         const float2 d = add(make_float2(approx_exp2(e.x), approx_exp2(e.y)), both(1.0f));
         const float2 s = make_float2(approx_rcp(d.x), approx_rcp(d.y));
         // s (1 + z (1 - s))
-        return mul(mul(dy, s), fma(z, add(both(1.0f), neg(s)), both(1.0f)));
+        return mul(mul(dy, s), fma(z, fma(s, both(-1.0f), both(1.0f)), both(1.0f)));
     }
     return dy;
 }
@@ -363,17 +392,13 @@ struct Forward {
             set_pair(v, i, activated<ACT>(fma(add(pair(v, i), mean[i]), scale[i], shift[i])));
         return v;
     }
-    // y: the thread's first row of the result
-    template <typename T>
-    __device__ __forceinline__ void write(const NormArgs& a, const Held<T, V>& held, int first, int end, T* y) const {
+    // y: where vector `first` of the result goes; then where `end` would
+    template <int ACT, typename T>
+    __device__ __forceinline__ void write(const NormArgs& a, const Held<T, V>& held, int first, int end, T*& y) const {
         const int64_t step = (int64_t)a.rows * a.C;
-        y += first * step;
-        with_act(a.act, [&](auto act) {
-            by_batches<2>(first, end, [&](int k, auto batch) {
+        by_batches<2>(first, end, [&](int k, auto batch) {
 #pragma unroll
-                for (int u = 0; u < decltype(batch)::value; ++u, y += step)
-                    store<T, V>(y, apply<decltype(act)::value>(held[k + u]));
-            });
+            for (int u = 0; u < decltype(batch)::value; ++u, y += step) store<T, V>(y, apply<ACT>(held[k + u]));
         });
     }
 };
@@ -408,15 +433,11 @@ struct Backward {
             sg[i] = fma(dz, d, sg[i]);
         }
     }
-    template <typename T>
-    __device__ __forceinline__ void sum_all(const NormArgs& a, const Held<T, V>& x, const Held<T, V>& dy, int first, int end,
+    template <int ACT, typename T>
+    __device__ __forceinline__ void sum_all(const Held<T, V>& x, const Held<T, V>& dy, int first, int end,
                                             float2 (&sb)[kPairs<V>], float2 (&sg)[kPairs<V>]) const {
-        with_act(a.act, [&](auto act) {
-            by_batches<2>(first, end, [&](int k, auto batch) {
-#pragma unroll
-                for (int u = 0; u < decltype(batch)::value; ++u) sum<decltype(act)::value>(x[k + u], dy[k + u], sb, sg);
-            });
-        });
+#pragma unroll 1
+        for (int k = first; k < end; ++k) sum<ACT>(x[k], dy[k], sb, sg);
     }
     // pq: p, p', q, q' of a pair
     template <int ACT, typename T>
@@ -429,20 +450,14 @@ struct Backward {
         }
         return x;
     }
-    // dx: the thread's first row of the result
-    template <typename T>
-    __device__ __forceinline__ void write(const NormArgs& a, const Held<T, V>& x, const Held<T, V>& dy, int first, int end, T* dx,
+    // dx: where vector `first` of the result goes; then where `end` would
+    template <int ACT, typename T>
+    __device__ __forceinline__ void write(const NormArgs& a, const Held<T, V>& x, const Held<T, V>& dy, int first, int end, T*& dx,
                                           const float4 (&pq)[kPairs<V>]) const {
         const int64_t step = (int64_t)a.rows * a.C;
         const float one = a.pixels * a.cpg == 1 ? 0.0f : 1.0f;
-        dx += first * step;
-        with_act(a.act, [&](auto act) {
-            by_batches<2>(first, end, [&](int k, auto batch) {
-#pragma unroll
-                for (int u = 0; u < decltype(batch)::value; ++u, dx += step)
-                    store<T, V>(dx, apply<decltype(act)::value>(x[k + u], dy[k + u], pq, one));
-            });
-        });
+#pragma unroll 1
+        for (int k = first; k < end; ++k, dx += step) store<T, V>(dx, apply<ACT>(x[k], dy[k], pq, one));
     }
 };
 // p and q of a thread's groups by pairs of channels; stat(g) gives them
@@ -493,7 +508,7 @@ __device__ __forceinline__ float2 sum_rows(const NormArgs& a, const float2* s, i
 // waits for the end of all before it where it reads what they write.  The first kernel of a call starts after
 // everything before it in the stream, so that the call's inputs are there for any of them.  Against launches that
 // wait for one another's end: streamed forward 32x64x224x224 fp32 200 -> 195 us, streamed backward 32x128x112x112
-// fp16 113 -> 109 us, resident backward 5x150x61x45 bf16 16 -> 14 us.
+// fp16 113 -> 109 us (before its ring), resident backward 5x150x61x45 bf16 16 -> 14 us.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -535,13 +550,9 @@ __global__ void __launch_bounds__(kThreads, 3) norm_sums(NormArgs a) {
     {
         const T* x = static_cast<const T*>(a.x) + at.n * a.x_sample + (at.begin + at.row) * a.x_pixel + at.c;
         const Held<T, V> v(a, smem4);
-        const int half = (at.mine + 1) / 2;
-        v.copy(x, a.rows * a.x_pixel, 0, half);
-        copies_end();
-        v.copy(x, a.rows * a.x_pixel, half, at.mine);
-        copies_end();
         Sets<T, V, NS> m;
-        as_they_come(at.mine, [&](int first, int end) { m.template take_all<U>(v, first, end); });
+        flow(at.mine, a.depth, [&](int shift, int first, int end) { v.from(shift).copy(x, a.rows * a.x_pixel, first, end); },
+             [&](int shift, int first, int end) { m.template take_all<U>(v.from(shift), first, end); });
         m.put(s_sets);
     }
     s_mine[threadIdx.x] = at.mine * S;
@@ -596,45 +607,49 @@ __global__ void __launch_bounds__(kThreads, 3) norm_result(NormArgs a) {
     if (!at.mine) return;
     const T* x = static_cast<const T*>(a.x) + at.n * a.x_sample + (at.begin + at.row) * a.x_pixel + at.c;
     const Held<T, V> v(a, smem4);
-    const int half = (at.mine + 1) / 2;
-    v.copy(x, a.rows * a.x_pixel, 0, half);
-    copies_end();
-    v.copy(x, a.rows * a.x_pixel, half, at.mine);
-    copies_end();
+    T* y = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
     wait_for_previous();
     const float *mean = a.mean_out + (int64_t)at.n * a.G, *rstd = a.rstd_out + (int64_t)at.n * a.G;
     const Forward<V> f(a, at.c, [&](int g) { return make_float2(mean[g], rstd[g]); });
-    T* y = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
-    as_they_come(at.mine, [&](int first, int end) { f.write(a, v, first, end, y); });
+    with_act(a.act, [&](auto act) {
+        flow(at.mine, a.depth, [&](int shift, int first, int end) { v.from(shift).copy(x, a.rows * a.x_pixel, first, end); },
+             [&](int shift, int first, int end) { f.template write<decltype(act)::value>(a, v.from(shift), first, end, y); });
+    });
 }
 
-// the copies of a thread's vectors of x and dy, in two groups
+// a thread's vectors of x and dy: from pixel `pixel` of sample n on
 template <typename T, int V>
-__device__ __forceinline__ void copy_both(const NormArgs& a, int n, int64_t pixel, int c, int count, const Held<T, V>& x, const Held<T, V>& dy) {
-    const T* px = static_cast<const T*>(a.x) + n * a.x_sample + pixel * a.x_pixel + c;
-    const T* pd = static_cast<const T*>(a.dy) + n * a.dy_sample + pixel * a.dy_pixel + c;
-    const int half = (count + 1) / 2;
-    x.copy(px, a.rows * a.x_pixel, 0, half);
-    dy.copy(pd, a.rows * a.dy_pixel, 0, half);
-    copies_end();
-    x.copy(px, a.rows * a.x_pixel, half, count);
-    dy.copy(pd, a.rows * a.dy_pixel, half, count);
-    copies_end();
-}
+struct Inputs {
+    const T *x, *dy;                  // the next to ask for
+    Held<T, V> hx, hd;
+    __device__ __forceinline__ Inputs(const NormArgs& a, void* smem, int n, int64_t pixel, int c)
+        : x(static_cast<const T*>(a.x) + n * a.x_sample + pixel * a.x_pixel + c),
+          dy(static_cast<const T*>(a.dy) + n * a.dy_sample + pixel * a.dy_pixel + c),
+          hx(a, smem),
+          hd(a, smem, a.held) {}
+    __device__ __forceinline__ void copy(const NormArgs& a, int shift, int first, int end) {
+        hx.from(shift).copy(x, a.rows * a.x_pixel, first, end);
+        hd.from(shift).copy(dy, a.rows * a.dy_pixel, first, end);
+    }
+};
 
 // parts[n][chunk][c] = sums of dz and of dz d of a stretch
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 3) norm_back_sums(NormArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) norm_back_sums(NormArgs a) {
     extern __shared__ uint4 smem4[];
     float2* s_sums = reinterpret_cast<float2*>(static_cast<Vec<T, V>*>(static_cast<void*>(smem4)) + 2 * a.held);
     const Stretch at(a, V, blockIdx.z);
     let_next_start();
     float2 sb[kPairs<V>] = {}, sg[kPairs<V>] = {};
     if (at.mine) {
-        const Held<T, V> x(a, smem4), dy(a, smem4, a.held);
-        copy_both(a, at.n, at.begin + at.row, at.c, at.mine, x, dy);
+        Inputs<T, V> in(a, smem4, at.n, at.begin + at.row, at.c);
         const Backward<V> f(a, at.n, at.c);
-        as_they_come(at.mine, [&](int first, int end) { f.sum_all(a, x, dy, first, end, sb, sg); });
+        with_act(a.act, [&](auto act) {
+            flow(at.mine, a.depth, [&](int shift, int first, int end) { in.copy(a, shift, first, end); },
+                 [&](int shift, int first, int end) {
+                     f.template sum_all<decltype(act)::value>(in.hx.from(shift), in.hd.from(shift), first, end, sb, sg);
+                 });
+        });
     }
     put_sums<V>(a, at.row, at.col, s_sums, sb, sg);
     const int here = min(a.cols * V, a.C - (int)blockIdx.y * a.cols * V), lane = threadIdx.x % 8;
@@ -646,30 +661,38 @@ __global__ void __launch_bounds__(kThreads, 3) norm_back_sums(NormArgs a) {
     }
 }
 
-// A CTA a group of a sample: sums[n][c] = (sum of dz, of dz xh), then [n][g] = p and q.
-__global__ void __launch_bounds__(kThreads) norm_back_join(NormArgs a) {
-    __shared__ float2 s_warp[kWarps];
-    const int g = blockIdx.x, n = blockIdx.y, lane = threadIdx.x % 8;
+// A CTA a group of a sample: sums[n][c] = (sum of dz, of dz xh), then [n][g] = p and q.  `wide`: the power of two
+// from the group's channels on, 256 at most; the threads take as many channels and the rest of them the parts in turn.
+__global__ void __launch_bounds__(kThreads) norm_back_join(NormArgs a, int wide) {
+    __shared__ float2 s_sum[kThreads];
     let_next_start();
     wait_for_previous();
+    const int g = blockIdx.x, n = blockIdx.y, step = kThreads / wide;
     const float rstd = a.rstd[(int64_t)n * a.G + g];
     const float2* parts = reinterpret_cast<const float2*>(a.parts) + (int64_t)n * a.chunks * a.C + g * a.cpg;
     float2 *channel = reinterpret_cast<float2*>(a.sums), *group = channel + (int64_t)a.N * a.C, all = {};
-    for (int i0 = threadIdx.x / 8; i0 < (a.cpg + 3) / 4 * 4; i0 += kThreads / 8) {            // eight lanes a channel
-        const int i = min(i0, a.cpg - 1);
+    for (int i0 = 0; i0 < a.cpg; i0 += wide) {
+        const int i = i0 + threadIdx.x % wide;
         float2 s = {};
+        if (i < a.cpg)
 #pragma unroll 4
-        for (int k = lane; k < a.chunks; k += 8) s = add(s, parts[(int64_t)k * a.C + i]);
-        s = sum_lanes<8>(s);
-        if (lane || i0 >= a.cpg) continue;
-        channel[(int64_t)n * a.C + g * a.cpg + i] = make_float2(s.x, rstd * s.y);
-        all = fma(both(a.gamma ? a.gamma[g * a.cpg + i] : 1.0f), s, all);
+            for (int k = threadIdx.x / wide; k < a.chunks; k += step) s = add(s, parts[(int64_t)k * a.C + i]);
+        s_sum[threadIdx.x] = s;
+        __syncthreads();
+        for (int o = kThreads / 2; o >= wide; o /= 2) {
+            if (threadIdx.x < o) s_sum[threadIdx.x] = s = add(s, s_sum[threadIdx.x + o]);
+            __syncthreads();
+        }
+        if (threadIdx.x < wide && i < a.cpg) {
+            channel[(int64_t)n * a.C + g * a.cpg + i] = make_float2(s.x, rstd * s.y);
+            all = fma(both(a.gamma ? a.gamma[g * a.cpg + i] : 1.0f), s, all);
+        }
     }
     all = sum_lanes<32>(all);
-    if (threadIdx.x % 32 == 0) s_warp[threadIdx.x / 32] = all;
+    if (threadIdx.x % 32 == 0) s_sum[threadIdx.x / 32] = all;
     __syncthreads();
     if (threadIdx.x) return;
-    for (int w = 1; w < kWarps; ++w) all = add(all, s_warp[w]);
+    for (int w = 1; w < kWarps; ++w) all = add(all, s_sum[w]);
     group[(int64_t)n * a.G + g] = group_pq(a, all, rstd);
 }
 
@@ -692,7 +715,7 @@ __device__ __forceinline__ void norm_back_params(const NormArgs& a, const float2
 
 // dx, and in the CTAs of blockIdx.z = 0 the sums over the samples
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 3) norm_back_result(NormArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) norm_back_result(NormArgs a) {
     extern __shared__ uint4 smem4[];
     const float2 *channel = reinterpret_cast<const float2*>(a.sums), *group = channel + (int64_t)a.N * a.C;
     if (blockIdx.z == 0) {
@@ -706,14 +729,18 @@ __global__ void __launch_bounds__(kThreads, 3) norm_back_result(NormArgs a) {
     }
     const Stretch at(a, V, a.N - blockIdx.z);
     if (!at.mine) return;
-    const Held<T, V> x(a, smem4), dy(a, smem4, a.held);
-    copy_both(a, at.n, at.begin + at.row, at.c, at.mine, x, dy);
+    Inputs<T, V> in(a, smem4, at.n, at.begin + at.row, at.c);
     const Backward<V> f(a, at.n, at.c);
     wait_for_previous();
     float4 pq[kPairs<V>];
     pair_stats<V>(pq, a, at.c, [&](int g) { return group[(int64_t)at.n * a.G + g]; });
     T* dx = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
-    as_they_come(at.mine, [&](int first, int end) { f.write(a, x, dy, first, end, dx, pq); });
+    with_act(a.act, [&](auto act) {
+        flow(at.mine, a.depth, [&](int shift, int first, int end) { in.copy(a, shift, first, end); },
+             [&](int shift, int first, int end) {
+                 f.template write<decltype(act)::value>(a, in.hx.from(shift), in.hd.from(shift), first, end, dx, pq);
+             });
+    });
 }
 
 // -------------------------------------------------------------------------------- resident kernels
@@ -807,7 +834,7 @@ __global__ void __launch_bounds__(kThreads, 4) norm_resident(NormArgs a) {
         const int first = at.slab * a.groups;
         const Forward<V> f(a, at.c, [&](int g) { return s_stat[g - first]; }, s_affine + at.col * V, s_affine + width + at.col * V);
         T* y = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
-        f.write(a, v, 0, at.mine, y);
+        with_act(a.act, [&](auto act) { f.template write<decltype(act)::value>(a, v, 0, at.mine, y); });
     }
     cluster.barrier_wait();
 }
@@ -822,12 +849,18 @@ __global__ void __launch_bounds__(kThreads, 3) norm_back_resident(NormArgs a) {
     float2* s_sums = reinterpret_cast<float2*>(static_cast<Vec<T, V>*>(static_cast<void*>(smem4)) + 2 * a.held);
     float2 *s_chan = s_sums + a.quarter * V, *s_part = s_chan + width, *s_stat = s_part + a.groups;
     const Unit<V> at(a);
-    const Held<T, V> x(a, smem4), dy(a, smem4, a.held);
+    Inputs<T, V> in(a, smem4, at.n, at.begin + at.row, at.c);
     float2 sb[kPairs<V>] = {}, sg[kPairs<V>] = {};
     if (at.mine) {
-        copy_both(a, at.n, at.begin + at.row, at.c, at.mine, x, dy);
+        const int half = (at.mine + 1) / 2;
+        in.copy(a, 0, 0, half);
+        copies_end();
+        in.copy(a, 0, half, at.mine);
+        copies_end();
         const Backward<V> f(a, at.n, at.c);
-        as_they_come(at.mine, [&](int first, int end) { f.sum_all(a, x, dy, first, end, sb, sg); });
+        with_act(a.act, [&](auto act) {
+            as_they_come(at.mine, [&](int first, int end) { f.template sum_all<decltype(act)::value>(in.hx, in.hd, first, end, sb, sg); });
+        });
     }
     put_sums<V>(a, at.row, at.col, s_sums, sb, sg);
     for (int j0 = threadIdx.x / 8; j0 < (width + 3) / 4 * 4; j0 += kThreads / 8) {            // eight lanes a channel
@@ -863,7 +896,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_back_resident(NormArgs a) {
         float4 pq[kPairs<V>];
         pair_stats<V>(pq, a, at.c, [&](int g) { return s_stat[g - first]; });
         T* dx = static_cast<T*>(a.out) + ((int64_t)at.n * a.pixels + at.begin + at.row) * a.C + at.c;
-        f.write(a, x, dy, 0, at.mine, dx, pq);
+        with_act(a.act, [&](auto act) { f.template write<decltype(act)::value>(a, in.hx, in.hd, 0, at.mine, dx, pq); });
     }
     cluster.barrier_wait();
 }
@@ -942,7 +975,9 @@ cudaError_t backward(const NormArgs& a, cudaStream_t st) {
     }
     const size_t beside = (size_t)a.quarter * V * sizeof(float2);
     if (const cudaError_t e = launch(norm_back_sums<T, V>, sums, a, kFirst, dim3(a.chunks, a.tiles, a.N), smem + beside, st)) return e;
-    if (const cudaError_t e = launch_as(norm_back_join, kNext, dim3(a.G, a.N), 0, st, a)) return e;
+    int wide = 1;
+    while (wide < a.cpg && wide < kThreads) wide *= 2;
+    if (const cudaError_t e = launch_as(norm_back_join, kNext, dim3(a.G, a.N), 0, st, a, wide)) return e;
     return launch(norm_back_result<T, V>, result, a, kNext, dim3(a.chunks, a.tiles, a.N + 1), smem, st);
 }
 

@@ -24,6 +24,7 @@ struct NormArgs {
     int N, C, G, cpg, act;
     int cols, rows;                   // vectors of a row a CTA covers, rows it covers at a time
     int chunk, held, quarter;         // pixels of a CTA, vectors of each input that it holds, of a quarter of its rows
+    int depth;                        // streamed: vectors of a thread that are asked for at a time
     int spg;                          // sets of channels in a group (forward)
     uint32_t spg_mul, cpg_mul, cols_mul, rows_mul;    // ceil(2^32 / spg) and so on
     float eps;
