@@ -50,12 +50,11 @@ __device__ __forceinline__ Vec<T, V> load(const T* p) {
 template <typename T, int V>
 __device__ __forceinline__ void copy_async(Vec<T, V>* to, const T* from) {
     const uint32_t d = (uint32_t)__cvta_generic_to_shared(to);
+    static_assert(sizeof(T) * V == 16 || sizeof(T) * V == 4, "sizes that the copies have");
     if constexpr (sizeof(T) * V == 16)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(from) : "memory");
-    else if constexpr (sizeof(T) * V == 4)
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(from) : "memory");
     else
-        *to = load<T, V>(from);                                   // there is no copy of two bytes
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -160,6 +159,14 @@ __device__ __forceinline__ float2 sum_lanes(float2 s) {
     return s;
 }
 
+// f(k, how many) for k from first to end - 1, U at a time while there are as many, then one at a time
+template <int U, typename F>
+__device__ __forceinline__ void by_batches(int first, int end, F&& f) {
+#pragma unroll 1
+    for (; first + U <= end; first += U) f(first, std::integral_constant<int, U>());
+#pragma unroll 1
+    for (; first < end; ++first) f(first, std::integral_constant<int, 1>());
+}
 // What a thread holds of one input: vectors of its rows, the first half of them in a group of copies of its own.
 template <typename T, int V>
 struct Held {
@@ -170,8 +177,19 @@ struct Held {
         : mine(static_cast<Vec<T, V>*>(smem) + from + threadIdx.x), step(a.rows * a.cols) {}
     // asks for vectors first to end - 1, the first of them at p, which goes on to the next
     __device__ __forceinline__ void copy(const T*& p, int64_t stride, int first, int end) const {
+        if constexpr (sizeof(T) * V >= 4) {
 #pragma unroll 2
-        for (int k = first; k < end; ++k, p += stride) copy_async(mine + k * step, p);
+            for (int k = first; k < end; ++k, p += stride) copy_async(mine + k * step, p);
+        } else {                      // there is no copy of two bytes: eight readings under way at a time
+            by_batches<8>(first, end, [&](int k, auto batch) {
+                constexpr int K = decltype(batch)::value;
+                Vec<T, V> v[K];
+#pragma unroll
+                for (int u = 0; u < K; ++u, p += stride) v[u] = load<T, V>(p);
+#pragma unroll
+                for (int u = 0; u < K; ++u) mine[(k + u) * step] = v[u];
+            });
+        }
     }
     __device__ __forceinline__ const Vec<T, V>& operator[](int k) const { return mine[k * step]; }
     // vector k in the place of vector k - shift
@@ -181,14 +199,6 @@ struct Held {
         return h;
     }
 };
-// f(k, how many) for k from first to end - 1, U at a time while there are as many, then one at a time
-template <int U, typename F>
-__device__ __forceinline__ void by_batches(int first, int end, F&& f) {
-#pragma unroll 1
-    for (; first + U <= end; first += U) f(first, std::integral_constant<int, U>());
-#pragma unroll 1
-    for (; first < end; ++first) f(first, std::integral_constant<int, 1>());
-}
 // f(first, end) for the first half, then for the rest, each as soon as its copies have come
 template <typename F>
 __device__ __forceinline__ void as_they_come(int count, F&& f) {
