@@ -29,8 +29,9 @@
  *
  * The training side (pp_group_norm, pp_tensors_*, pp_grad_norm, pp_adamw_step) serves the masked
  * retraining of a pruned network between its convolutions and after its backward pass; its
- * activations are channels last, as training libraries keep them for convolutions, and its kernels
- * are plain launches.
+ * activations are channels last, as training libraries keep them for convolutions.  The first kernel
+ * of each of its calls is a plain launch; further kernels of a group norm's call start while the one
+ * before them ends, under capture too, unless PATCONV_PDL=0.
  *
  * Thread safety: a handle is immutable after pp_pack/pp_bind_device, so pp_conv on one handle
  * may be called from several host threads and streams at once.
@@ -369,7 +370,8 @@ int pp_group_norm_workspace_size(int dtype, int N, int64_t pixels, int C, int G,
  * shared memory between the sums and the result) or 1 streamed (several kernels, the inputs read twice),
  * [1] channels of a thread's vector, [2] vectors of a row a CTA covers, [3] pixels a CTA covers,
  * [4] vectors of an input that a CTA holds in shared memory, [5] CTAs of a cluster (0: streamed), [6] CTAs,
- * [7] the sets of channels of a vector that are summed apart (1: it lies within one group).  Writes min(n_info, 8) values.  Host-only.
+ * [7] the sets of channels of a vector that are summed apart (1: it lies within one group).  Writes
+ * min(n_info, 8) values.  Host-only.
  * Errors: PP_ERR_NULL, _SHAPE (nothing to do among them), _DTYPE, _ARG. */
 int pp_group_norm_plan(int dtype, int N, int64_t pixels, int C, int G, int backward, int align, int64_t* info, int n_info);
 
@@ -422,8 +424,8 @@ int pp_tensors_destroy(pp_tensors_handle h);
  *   grads     HOST array of the gradients' DEVICE addresses (element aligned, of the handle's types);
  *             NULL: that tensor has none this time;
  *   max_norm  above 0 (infinity: no clipping);   out  DEVICE fp32[2].
- * Sums are fp32 over a few hundred squares and 64 bits from there, in a fixed order: the same inputs
- * give the same bits.  The scratch is the handle's: order calls on one handle.  Never synchronises.
+ * A thread sums in fp32 with what its roundings lose beside it, a CTA in fp32, the CTAs in 64 bits, in
+ * a fixed order: the same inputs give the same bits.  The scratch is the handle's: order calls on one handle.  Never synchronises.
  * Errors: PP_ERR_NULL, _NOT_BOUND, _ALIGN, _ARG, _CUDA. */
 int pp_grad_norm(pp_tensors_handle h, const void* const* grads, double max_norm, float* out, void* stream);
 

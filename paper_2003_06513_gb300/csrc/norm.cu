@@ -39,6 +39,7 @@
 #include <climits>
 #include <cmath>
 #include <cstdint>
+#include <cstdlib>
 #include <numeric>
 
 #include "norm.h"
@@ -49,6 +50,14 @@ namespace patconv {
 extern template struct NormKernels<float>;
 extern template struct NormKernels<__half>;
 extern template struct NormKernels<__nv_bfloat16>;
+
+bool norm_starts_early() {
+    static const bool on = [] {
+        const char* e = std::getenv("PATCONV_PDL");
+        return !(e && e[0] == '0');
+    }();
+    return on;
+}
 
 namespace {
 

@@ -671,38 +671,39 @@ __global__ void __launch_bounds__(kThreads, 2) norm_back_sums(NormArgs a) {
     }
 }
 
-// A CTA a group of a sample: sums[n][c] = (sum of dz, of dz xh), then [n][g] = p and q.  `wide`: the power of two
-// from the group's channels on, 256 at most; the threads take as many channels and the rest of them the parts in turn.
-__global__ void __launch_bounds__(kThreads) norm_back_join(NormArgs a, int wide) {
-    __shared__ float2 s_sum[kThreads];
+// A CTA a group of a sample: sums[n][c] = (sum of dz, of dz xh), then [n][g] = p and q.  Its threads take 2^bits
+// channels (all of the group's, up to 256) and the rest of them the parts in turn.
+__global__ void __launch_bounds__(kThreads) norm_back_join(NormArgs a, int bits) {
+    __shared__ float2 s_sum[kThreads], s_warp[kWarps];
     let_next_start();
     wait_for_previous();
-    const int g = blockIdx.x, n = blockIdx.y, step = kThreads / wide;
+    const int g = blockIdx.x, n = blockIdx.y, wide = 1 << bits, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const float rstd = a.rstd[(int64_t)n * a.G + g];
     const float2* parts = reinterpret_cast<const float2*>(a.parts) + (int64_t)n * a.chunks * a.C + g * a.cpg;
     float2 *channel = reinterpret_cast<float2*>(a.sums), *group = channel + (int64_t)a.N * a.C, all = {};
     for (int i0 = 0; i0 < a.cpg; i0 += wide) {
-        const int i = i0 + threadIdx.x % wide;
+        const int i = i0 + (threadIdx.x & (wide - 1));
         float2 s = {};
         if (i < a.cpg)
 #pragma unroll 4
-            for (int k = threadIdx.x / wide; k < a.chunks; k += step) s = add(s, parts[(int64_t)k * a.C + i]);
+            for (int k = threadIdx.x >> bits; k < a.chunks; k += kThreads >> bits) s = add(s, parts[(int64_t)k * a.C + i]);
+        for (int o = 16; o >= wide; o >>= 1)                    // the warp's sums of a channel
+            s = add(s, make_float2(__shfl_down_sync(0xffffffffu, s.x, o), __shfl_down_sync(0xffffffffu, s.y, o)));
         s_sum[threadIdx.x] = s;
         __syncthreads();
-        for (int o = kThreads / 2; o >= wide; o /= 2) {
-            if (threadIdx.x < o) s_sum[threadIdx.x] = s = add(s, s_sum[threadIdx.x + o]);
-            __syncthreads();
-        }
+        const int step = max(1, wide / 32);                     // warps that hold the same channels are as far apart
         if (threadIdx.x < wide && i < a.cpg) {
+            for (int w = warp + step; w < kWarps; w += step) s = add(s, s_sum[w * 32 + lane]);
             channel[(int64_t)n * a.C + g * a.cpg + i] = make_float2(s.x, rstd * s.y);
             all = fma(both(a.gamma ? a.gamma[g * a.cpg + i] : 1.0f), s, all);
         }
+        __syncthreads();
     }
     all = sum_lanes<32>(all);
-    if (threadIdx.x % 32 == 0) s_sum[threadIdx.x / 32] = all;
+    if (lane == 0) s_warp[warp] = all;
     __syncthreads();
     if (threadIdx.x) return;
-    for (int w = 1; w < kWarps; ++w) all = add(all, s_sum[w]);
+    for (int w = 1; w < kWarps; ++w) all = add(all, s_warp[w]);
     group[(int64_t)n * a.G + g] = group_pq(a, all, rstd);
 }
 
@@ -950,7 +951,7 @@ cudaError_t launch_as(K* kernel, int how, dim3 grid, size_t smem, cudaStream_t s
         attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     }
     cfg.attrs = attr;
-    cfg.numAttrs = how != kFirst ? 1 : 0;
+    cfg.numAttrs = how > kFirst || (how == kNext && norm_starts_early()) ? 1 : 0;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...), l = cudaGetLastError();
     return e != cudaSuccess ? e : l;
 }
@@ -985,9 +986,9 @@ cudaError_t backward(const NormArgs& a, cudaStream_t st) {
     }
     const size_t beside = (size_t)a.quarter * V * sizeof(float2);
     if (const cudaError_t e = launch(norm_back_sums<T, V>, sums, a, kFirst, dim3(a.chunks, a.tiles, a.N), smem + beside, st)) return e;
-    int wide = 1;
-    while (wide < a.cpg && wide < kThreads) wide *= 2;
-    if (const cudaError_t e = launch_as(norm_back_join, kNext, dim3(a.G, a.N), 0, st, a, wide)) return e;
+    int bits = 0;
+    while (1 << bits < a.cpg && 1 << bits < kThreads) ++bits;
+    if (const cudaError_t e = launch_as(norm_back_join, kNext, dim3(a.G, a.N), 0, st, a, bits)) return e;
     return launch(norm_back_result<T, V>, result, a, kNext, dim3(a.chunks, a.tiles, a.N + 1), smem, st);
 }
 

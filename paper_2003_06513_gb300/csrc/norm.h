@@ -34,6 +34,8 @@ struct NormArgs {
 
 constexpr int kNormShared = 200 * 1024;               // dynamic shared memory of a CTA at most, beside its static arrays
 
+bool norm_starts_early();             // whether a call's kernels start while the one before ends (norm.cu)
+
 // Launches of one type's kernels, with V and NS of the plan.
 template <typename T>
 struct NormKernels {
