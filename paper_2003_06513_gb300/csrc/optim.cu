@@ -687,9 +687,9 @@ struct Listed {
     float p[R], m[R], v[R], ms, vs;
     uint32_t g[R];                                // as they lie in memory, and m and v of 8 bits too: a conversion would
                                                   // wait for a round's values before the next round is asked for
-    __device__ __forceinline__ static uint32_t element(const uint8_t* list, int count, int r) {
-        return list[min(r * 32 + (int)(threadIdx.x % 32), count - 1)];
-    }
+    static_assert(R <= 4, "a byte of `elements` a round");
+    uint32_t elements;                            // of the block, the lane's of every round
+    __device__ __forceinline__ uint32_t element(int r) const { return __byte_perm(elements, 0, 0x4440 | r); }
     // e0: the block's first element
     __device__ __forceinline__ void load(const Chunk& t, const void* gp, uint32_t e0, const uint8_t* list, int count,
                                          const AdamArgs& a) {
@@ -697,6 +697,7 @@ struct Listed {
         const float* params = t.param + e0;
         const bool g32 = t.grad_dtype == PP_F32;
         ms = vs = 1.0f;
+        elements = 0;
         if constexpr (BITS == 8) {
             ms = a.m_scale[s0 / kBlock];
             vs = a.v_scale[s0 / kBlock];
@@ -705,7 +706,8 @@ struct Listed {
         for (int r = 0; r < R; ++r) {
             m[r] = v[r] = 0.0f;
             if (r * 32 >= count) continue;        // the whole warp
-            const uint32_t el = element(list, count, r);
+            const uint32_t el = list[min(r * 32 + (int)(threadIdx.x % 32), count - 1)];
+            elements |= el << (8 * r);
             if (g32)
                 g[r] = (static_cast<const uint32_t*>(gp) + e0)[el];
             else
@@ -720,7 +722,7 @@ struct Listed {
             }
         }
     }
-    __device__ __forceinline__ void step(const Chunk& t, uint32_t e0, const uint8_t* list, int count, float gs, float shrink,
+    __device__ __forceinline__ void step(const Chunk& t, uint32_t e0, int count, float gs, float shrink,
                                          const AdamArgs& a) {
         const int64_t s0 = t.state + e0;
         const int lane = threadIdx.x % 32;
@@ -737,7 +739,7 @@ struct Listed {
             moments(__fmul_rn(gr, gs), m[r], v[r], a.b1 * ms, a.b2 * vs, a);
             const float to = stepped(p[r], m[r], v[r], shrink, a);
             if (r * 32 + lane < count) {
-                const uint32_t el = element(list, count, r);
+                const uint32_t el = element(r);
                 params[el] = to;
                 if (t.copy) store_copy(t, e0 + el, to, a.copy_dtype);
                 if constexpr (BITS == 32) {
@@ -754,11 +756,12 @@ struct Listed {
         uint32_t factor = 0;                      // lane i < 8 has odd(i)
 #pragma unroll
         for (int i = 0; i < 8; ++i) factor = lane == i ? odd(i) : factor;
+        const uint32_t hash = hash8(s0 + 8 * lane, a.key);            // of the lane's eight elements of the block
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (r * 32 >= count) continue;
-            const uint32_t el = element(list, count, r);
-            const uint32_t y = own_bits(hash8(s0 + el, a.key), __shfl_sync(0xffffffffu, factor, el & 7));
+            const uint32_t el = element(r);
+            const uint32_t y = own_bits(__shfl_sync(0xffffffffu, hash, el >> 3), __shfl_sync(0xffffffffu, factor, el & 7));
             m[r] = rounded(m[r] * im, dither_m(y));
             v[r] = rounded_up(v[r] * iv, dither_v(y));
         }
@@ -767,7 +770,7 @@ struct Listed {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (r * 32 + lane >= count) continue;
-            const uint32_t el = element(list, count, r);
+            const uint32_t el = element(r);
             (static_cast<uint8_t*>(a.m) + s0)[el] = pack1(m[r]);
             (static_cast<uint8_t*>(a.v) + s0)[el] = pack1(v[r]);
         }
@@ -787,8 +790,8 @@ struct Listed {
 //     ResNet-50's 3x3 layers, dense, fp32 gradients and states          50 us, 6.3 TB/s: memory
 //     VGG-16's, a kernel in 0.3 kept, fp32 gradients and states         49 us: the kept elements' 1.2 TB/s are
 //         4.9 TB/s of memory traffic, since what is read is whole 64-byte pieces with any kept element in them
-//     ResNet-50's, a kernel in 0.4 kept, bf16 gradients, 8-bit states   35 us: 2.7 TB/s of traffic, instructions
-//         (64 % of the issue slots) and the latency of the chain
+//     ResNet-50's, a kernel in 0.4 kept, bf16 gradients, 8-bit states   34 us: 2.8 TB/s of traffic, instructions
+//         (70 % of the issue slots) and the latency of the chain
 template <int BITS, int N, bool MASKED>
 __global__ void __launch_bounds__(kThreads, MASKED ? 6 : 5) adamw_kernel(const Chunk* __restrict__ chunks, uint32_t begin, uint32_t t0,
                                                             Grads<N> grads, AdamArgs a) {
@@ -822,7 +825,7 @@ __global__ void __launch_bounds__(kThreads, MASKED ? 6 : 5) adamw_kernel(const C
             if (!count) return;                    // its states are zero and stay so
             Listed<BITS, 4> x;
             x.load(t, gp, warp, list, count, a);
-            x.step(t, warp, list, count, gs, shrink, a);
+            x.step(t, warp, count, gs, shrink, a);
             return;
         }
     }
