@@ -1,8 +1,13 @@
 """Group norm on stretches so long that a CTA reads them through its ring of shared memory many times over:
 the same tolerances as for the other sizes."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
+from conftest import ROOT
 from paper_2003_06513_gb300 import norm
 from test_norm_gpu import DT, _check_backward, _check_forward, _inputs, _tensor
 
@@ -45,3 +50,28 @@ def test_backward(shape, dtype, kind):
     first = _check_backward(x, dy, _tensor(x, dtype), _tensor(dy, dtype), g, ga, be, kind, dtype)
     again = _check_backward(x, dy, _tensor(x, dtype), _tensor(dy, dtype), g, ga, be, kind, dtype)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+_DIGESTS = """
+import hashlib, torch
+from paper_2003_06513_gb300 import norm
+gen = torch.Generator(device="cuda").manual_seed(3)
+for n, c, h, w, g in ((2, 32, 28, 28, 8), (8, 64, 224, 224, 32)):
+    x, dy = (torch.randn(n, c, h, w, generator=gen, device="cuda").contiguous(memory_format=torch.channels_last) for _ in range(2))
+    y, mean, rstd = norm.pp_group_norm(x, g, act="silu")
+    got = (y, mean, rstd) + tuple(norm.pp_group_norm_backward(dy, x, mean, rstd, g, act="silu"))
+    print(*[hashlib.sha256(t.cpu().numpy().tobytes()).hexdigest() for t in got])
+"""
+
+
+def test_plain_launches_give_the_same_bits():
+    """PATCONV_PDL=0, read once a process: every kernel waits for the end of the one before it."""
+    assert norm.plan((2, 32, 28, 28), 8)["path"] == 2 and norm.plan((8, 64, 224, 224), 32)["path"] == 1
+
+    def digests(**env):
+        run = subprocess.run([sys.executable, "-c", _DIGESTS], env={**os.environ, **env}, cwd=ROOT, capture_output=True,
+                             text=True, timeout=300)
+        assert run.returncode == 0, run.stderr
+        return run.stdout.split()
+    early, plain = digests(PATCONV_PDL="1"), digests(PATCONV_PDL="0")
+    assert len(early) == 12 and early == plain
