@@ -54,6 +54,11 @@ int dtype_of(const at::Tensor& t) {         // pp_dtype, or -1
     }
 }
 
+// A tensor that a kernel writes: what torch has kept of it for a backward pass is no longer good.
+void changed(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The device and, where one is given (a stream's handle, None for the current one), the stream are
 // current while this lives; outputs and workspaces belong to that stream.
 struct Place {
@@ -180,6 +185,7 @@ PyObject* group_norm(PyObject* const* a, Py_ssize_t n_args) {
     const Workspace w(x, a[8], dtype, pixels, groups, 0);
     const int e = pp_group_norm(x.const_data_ptr(), l.pixel, l.sample, dtype, (int)n, pixels, (int)c, groups, gamma, beta, eps,
                                 act, y.data_ptr(), mean.data_ptr<float>(), rstd.data_ptr<float>(), w.p, w.bytes, at.stream);
+    if (!e && a[6] != Py_None) changed(y);
     return e ? PyLong_FromLong(e) : triple(y, mean, rstd);
 }
 
@@ -201,6 +207,7 @@ PyObject* group_norm_backward(PyObject* const* a, Py_ssize_t n_args) {
     const int e = pp_group_norm_backward(dy.const_data_ptr(), d.pixel, d.sample, x.const_data_ptr(), l.pixel, l.sample, dtype,
                                          (int)n, pixels, (int)c, groups, gamma, beta, mean, rstd, act, dx.data_ptr(),
                                          dgamma.data_ptr<float>(), dbeta.data_ptr<float>(), w.p, w.bytes, at.stream);
+    if (!e && a[8] != Py_None) changed(dx);
     return e ? PyLong_FromLong(e) : triple(dx, dgamma, dbeta);
 }
 
@@ -298,6 +305,7 @@ PyObject* grad_norm(PyObject* const* a, Py_ssize_t n_args) {
     const at::Tensor out = given ? given->detach().view({2}) : at::empty({2}, at::TensorOptions().dtype(at::kFloat).device(list.device));
     const int e = pp_grad_norm(list.handle, grads.data(), real(a[2]), out.data_ptr<float>(), at.stream);
     if (e) return PyLong_FromLong(e);
+    if (given) changed(*given);
     PyObject* t = PyTuple_New(2);
     if (!t) throw Raised();
     PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(out.narrow(0, 0, 1)));
@@ -305,7 +313,7 @@ PyObject* grad_norm(PyObject* const* a, Py_ssize_t n_args) {
     return t;
 }
 
-// tensors, grads, params, state_bits, m, v, m_scale, v_scale, lr, beta1, beta2, eps, step, seed, grad_scale, stream
+// tensors, grads, parameters and copies, state_bits, m, v, m_scale, v_scale, lr, beta1, beta2, eps, step, seed, grad_scale, stream
 PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
     want(n_args, 16);
     const List& list = list_of(a[0]);
@@ -320,11 +328,8 @@ PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
                                 ms ? ms->data_ptr<float>() : nullptr, vs ? vs->data_ptr<float>() : nullptr, real(a[8]), real(a[9]),
                                 real(a[10]), real(a[11]), integer(a[12]), (uint32_t)integer(a[13]),
                                 scale ? scale->const_data_ptr<float>() : nullptr, at.stream);
-    if (!e)                                  // they changed behind torch's back
-        for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i) {
-            const at::Tensor& p = tensor(PyList_GET_ITEM(a[2], i), "a parameter");
-            if (!p.is_inference()) p.unsafeGetTensorImpl()->bump_version();
-        }
+    if (!e)
+        for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i) changed(tensor(PyList_GET_ITEM(a[2], i), "a parameter"));
     return PyLong_FromLong(e);
 }
 

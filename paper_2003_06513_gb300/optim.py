@@ -22,7 +22,7 @@ from typing import Optional, Sequence, Union
 import torch
 
 from . import _lib
-from .api import _stream_ptr
+from .api import _raw_stream, _stream_ptr
 
 PP_F32, PP_F16, PP_BF16 = 0, 1, 2
 _DT = {torch.float32: PP_F32, torch.float16: PP_F16, torch.bfloat16: PP_BF16}
@@ -106,6 +106,7 @@ class _Tensors:
         self.native = _lib.binding()
         self.list = self.native.tensors(h.value, index, [(tuple(shape), tuple(stride), _DT[d])
                                                          for shape, stride, d in zip(shapes, strides, dtypes)])
+        self._home = _raw_stream(stream, self._device)      # the stream that what is allocated here belongs to
         with torch.cuda.device(index), self._on(stream):
             self._table = torch.empty(self.query(_TABLE_BYTES), dtype=torch.uint8, device=self._device)
             _lib.check("pp_tensors_bind", lib.pp_tensors_bind(h, ctypes.c_void_p(self._table.data_ptr()),
@@ -121,7 +122,17 @@ class _Tensors:
     def _on(self, stream):
         return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
+    def used(self, tensors, stream) -> None:
+        """Keeps the memory of the table and of ``tensors`` from another use before a call's stream is done with
+        them, where that is not the stream they belong to."""
+        if _raw_stream(stream, self._device) != self._home:
+            on = stream if stream is not None else torch.cuda.current_stream(self._device)
+            for t in (self._table, *tensors):
+                if t is not None:
+                    t.record_stream(on)
+
     def norm(self, grads, max_norm, out, stream):
+        self.used((), stream)
         got = self.native.grad_norm(self.list, grads, max_norm, out, None if stream is None else stream.cuda_stream)
         if type(got) is int:
             raise _lib.PatconvError("pp_grad_norm", got)
@@ -191,6 +202,7 @@ class AdamW:
             for p, c in zip(self.params, copies):
                 if c is not None and (c.shape != p.shape or c.stride() != p.stride() or c.device != device):
                     raise ValueError("a copy must have its parameter's shape, strides and device")
+        self._written = self.params + [c for c in copies or [] if c is not None]
         self.lr, self.betas, self.eps, self.seed, self.state_bits = lr, tuple(betas), eps, int(seed) & 0xFFFFFFFF, state_bits
         self.steps = 0
         self._t = _Tensors([p.shape for p in self.params], [p.stride() for p in self.params], grad_dtypes, taps, device,
@@ -243,8 +255,9 @@ class AdamW:
         alone), each times ``grad_scale`` (one float32 on the device) if given, at rate ``lr`` (default:
         the object's).  Calls on one object must be ordered."""
         t = self._t
+        t.used((self.m, self.v, self.m_scale, self.v_scale), stream)
         _lib.check("pp_adamw_step", t.native.adamw_step(
-            t.list, self._grads(grads), self.params, self.state_bits, self.m, self.v, self.m_scale, self.v_scale,
+            t.list, self._grads(grads), self._written, self.state_bits, self.m, self.v, self.m_scale, self.v_scale,
             self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.steps + 1, self.seed,
             grad_scale, None if stream is None else stream.cuda_stream))
         self.steps += 1
