@@ -103,7 +103,8 @@ __device__ __forceinline__ void store8(float* p, const Vec8& r) {
                  "f"(r.v[3]), "f"(r.v[4]), "f"(r.v[5]), "f"(r.v[6]), "f"(r.v[7])
                  : "memory");
 }
-// Pairs of values, two to an instruction.  The explicit rounding keeps products and sums apart.
+// Pairs of values, two to an instruction.  A product of mul2 and a sum of add2 that follows it may become one fused
+// operation, whatever rounding is written there: where both have to round, the sum is an fma2 (moments2).
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     float2 r;
     asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 z, x, y; mov.b64 {%0, %1}, z;}"
@@ -376,6 +377,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 5 : 4) grad_norm_kernel(const
 
 struct AdamArgs {
     float lr, step_size, b1, b2, c1, c2, inv_bc2, eps;   // step_size = lr / (1 - b1^t), c = 1 - b
+    float one;                                           // 1, which the compiler is not told
     uint32_t key;
     int copy_dtype;
     const float* grad_scale;
@@ -395,15 +397,18 @@ __device__ __forceinline__ float approx_rcp(float x) {
 }
 
 // The states' arithmetic rounds every product and sum by itself: an 8-bit state then depends on the
-// formula alone and not on how a compiler contracts it.  m and v come as values times m_unit and
-// v_unit: an 8-bit state's code and its scale times b, a product by a power of two being exact.
+// formula alone, and not on which of the kernels' paths an element takes or on how a compiler contracts it.
+// The packed form has no instructions that are kept apart: there a sum x + y is x * one + y, one rounding of
+// the sum of two rounded products, since `one` is 1 and x's own product cannot become a part of it.  It costs what
+// the packed sum does.  m and v come as values times mb and vb: an 8-bit state's code and its scale times b, a
+// product by a power of two being exact.
 __device__ __forceinline__ void moments(float g, float& m, float& v, float mb, float vb, const AdamArgs& a) {
     m = __fadd_rn(__fmul_rn(m, mb), __fmul_rn(g, a.c1));
     v = __fadd_rn(__fmul_rn(v, vb), __fmul_rn(__fmul_rn(g, g), a.c2));
 }
 __device__ __forceinline__ void moments2(float2 g, float2& m, float2& v, float mb, float vb, const AdamArgs& a) {
-    m = add2(mul2(m, both(mb)), mul2(g, both(a.c1)));
-    v = add2(mul2(v, both(vb)), mul2(mul2(g, g), both(a.c2)));
+    m = fma2(mul2(m, both(mb)), both(a.one), mul2(g, both(a.c1)));
+    v = fma2(mul2(v, both(vb)), both(a.one), mul2(mul2(g, g), both(a.c2)));
 }
 // 2^-126 keeps the root in fp32's normal range, where the approximations flush nothing: a root below
 // 2^-63 is far below any eps in use, and with eps = 0 it makes 0 / 0 zero.
@@ -1027,6 +1032,7 @@ int pp_adamw_step(pp_tensors_handle h, const void* const* grads, int state_bits,
     if (off(m, 32) || off(v, 32) || off(m_scale, 4) || off(v_scale, 4) || off(grad_scale, 4)) return PP_ERR_ALIGN;
     AdamArgs a{};
     a.lr = (float)lr;
+    a.one = 1.0f;
     a.step_size = (float)(lr / (1 - std::pow(beta1, (double)step)));
     a.b1 = (float)beta1;
     a.b2 = (float)beta2;

@@ -365,3 +365,44 @@ def test_offsets_beyond_32_bits():
     m, _ = opt.state_of(0)
     # the ends lie differently in their blocks: each value within an eighth of 0.1 g, a scale's grid beyond
     assert torch.allclose(m[-300:], 0.1 * g[-300:].float(), rtol=0.126, atol=0.2)
+
+
+def _paths(n, rng):
+    """(name, parameter of n elements, masks) that the step's kernels take by different code: whole blocks, single
+    elements, masks that keep nearly all of a block and masks that keep few."""
+    full = torch.full((n // 9,), 0x1FF, dtype=torch.int16, device="cuda")
+    few = torch.from_numpy(rng.choice(np.array([0, 0, 0x0B8, 0x017], np.int16), n // 9)).cuda()
+    for name, shift, taps in (("aligned", 0, None), ("unaligned", 1, None), ("all kept", 0, full), ("few kept", 0, few)):
+        yield name, torch.zeros(n + 8, device="cuda")[shift:shift + n].view(n // 9, 1, 3, 3), taps
+
+
+@pytest.mark.parametrize("grad", ["f32", "f16", "bf16"])
+def test_moments_round_every_product_and_sum_in_every_path(grad):
+    """fp32 moments have the bits of fp32 arithmetic with each product and sum rounded by itself."""
+    rng = np.random.default_rng(12)
+    n, b1, b2, f = 9 * 555, HYPER["b1"], HYPER["b2"], np.float32
+    for name, p, taps in _paths(n, rng):
+        opt = optim.AdamW([p], HYPER["lr"], (b1, b2), HYPER["eps"], 0.1, taps=[taps], grad_dtypes=DT[grad])
+        keep = T.kept(None if taps is None else taps.cpu().numpy(), n)
+        scale = torch.tensor([0.7], device="cuda")
+        for step in range(5):
+            g = torch.from_numpy(rng.standard_normal(n) * 10.0 ** rng.integers(-4, 2, n)).to(DT[grad])
+            m, v = (a.cpu().numpy() for a in opt.state_of(0))
+            opt.step([g.cuda().view(p.shape)], grad_scale=scale)
+            gs = g.float().numpy() * f(scale.item())
+            for got, want in zip(opt.state_of(0), (m * f(b1) + gs * f(1 - b1), v * f(b2) + (gs * gs) * f(1 - b2))):
+                np.testing.assert_array_equal(got.cpu().numpy(), np.where(keep, want, 0), err_msg=f"{name}, step {step}")
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_step_has_the_same_bits_at_any_alignment_without_a_mask(bits):
+    """Eight million elements: of 8-bit codes one in a million turns where a moment's last bit does."""
+    n, got = 1 << 23, []
+    for shift in (0, 1):
+        gen = torch.Generator(device="cuda").manual_seed(3)
+        p = torch.zeros(n + 8, device="cuda")[shift:shift + n]
+        opt = optim.AdamW([p], state_bits=bits)
+        for _ in range(3):
+            opt.step([torch.randn(n, generator=gen, device="cuda")])
+        got.append((p, opt.m.view(torch.uint8), opt.v.view(torch.uint8)))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
