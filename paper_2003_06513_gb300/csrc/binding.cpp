@@ -223,26 +223,41 @@ PyObject* layout(PyObject* const* a, Py_ssize_t n_args) {
 
 // ---------------------------------------------------------------------------------- many tensors
 
-struct Wanted {                             // of one tensor's gradient
+struct Wanted {                             // of one tensor's gradient, and of the tensor itself
     std::vector<int64_t> shape, strides;
     at::ScalarType type;
+};
+struct Written {                            // a parameter or a copy, as it was when the handle was made
+    const void* at;
+    at::ScalarType type;
+    size_t tensor;                          // whose shape and strides it has
 };
 struct List {
     pp_tensors_handle handle;
     at::Device device;
     std::vector<Wanted> wanted;
+    std::vector<Written> written;
 };
 constexpr const char* kList = "patconv.tensors";
 
 void drop(PyObject* capsule) { delete static_cast<List*>(PyCapsule_GetPointer(capsule, kList)); }
 
-// handle, device index, [(shape, strides, pp_dtype)] -> what a call's gradients are checked against
+// whether a tensor has the strides, as far as they matter
+bool in_order(const at::Tensor& t, const std::vector<int64_t>& shape, const std::vector<int64_t>& strides) {
+    if (t.strides() == at::IntArrayRef(strides) || !t.numel()) return true;
+    for (size_t k = 0; k < shape.size(); ++k)
+        if (shape[k] > 1 && t.stride((int64_t)k) != strides[k]) return false;
+    return true;
+}
+
+// handle, device index, [(shape, strides, pp_dtype)], [(parameter or copy, its tensor's number)] -> what a call's
+// gradients, and the tensors that it writes, are checked against
 PyObject* tensors(PyObject* const* a, Py_ssize_t n_args) {
-    want(n_args, 3);
+    want(n_args, 4);
     auto list = std::make_unique<List>(List{static_cast<pp_tensors_handle>(PyLong_AsVoidPtr(a[0])),
-                                            at::Device(at::kCUDA, (int8_t)integer(a[1])), {}});
+                                            at::Device(at::kCUDA, (int8_t)integer(a[1])), {}, {}});
     if (PyErr_Occurred()) throw Raised();
-    if (!PyList_Check(a[2])) refuse("a list is wanted");
+    if (!PyList_Check(a[2]) || !PyList_Check(a[3])) refuse("a list is wanted");
     for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i) {
         PyObject *shape, *strides;
         int dtype;
@@ -253,6 +268,14 @@ PyObject* tensors(PyObject* const* a, Py_ssize_t n_args) {
         for (Py_ssize_t k = 0; k < PyTuple_GET_SIZE(strides); ++k) w.strides.push_back(integer(PyTuple_GET_ITEM(strides, k)));
         w.type = dtype == PP_F32 ? at::kFloat : dtype == PP_F16 ? at::kHalf : at::kBFloat16;
         list->wanted.push_back(std::move(w));
+    }
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[3]); ++i) {
+        PyObject* o;
+        Py_ssize_t k;
+        if (!PyArg_ParseTuple(PyList_GET_ITEM(a[3], i), "On", &o, &k)) throw Raised();
+        const at::Tensor& t = tensor(o, "a parameter");
+        if (k < 0 || (size_t)k >= list->wanted.size()) refuse("there is no such tensor");
+        list->written.push_back({t.const_data_ptr(), t.scalar_type(), (size_t)k});
     }
     PyObject* capsule = PyCapsule_New(list.get(), kList, drop);
     if (capsule) list.release();
@@ -284,10 +307,7 @@ std::vector<const void*> addresses(const List& list, PyObject* grads) {
         const Wanted& w = list.wanted[i];
         if (g.scalar_type() != w.type || g.device() != list.device || g.layout() != at::kStrided || g.sizes() != at::IntArrayRef(w.shape))
             refuse("gradient " + std::to_string(i) + " is not of its tensor's shape, on its device or of the type it was announced as");
-        if (g.strides() != at::IntArrayRef(w.strides) && g.numel())
-            for (size_t k = 0; k < w.shape.size(); ++k)
-                if (w.shape[k] > 1 && g.stride((int64_t)k) != w.strides[k])
-                    refuse("gradient " + std::to_string(i) + " is not in its tensor's memory order");
+        if (!in_order(g, w.shape, w.strides)) refuse("gradient " + std::to_string(i) + " is not in its tensor's memory order");
         at[i] = g.const_data_ptr();
     }
     return at;
@@ -313,6 +333,22 @@ PyObject* grad_norm(PyObject* const* a, Py_ssize_t n_args) {
     return t;
 }
 
+// The parameters and copies are still the memory whose addresses the handle holds: a tensor that was given other
+// memory since (by its `data`, by a module's move to another order or type) has left that memory to others.
+void check_written(const List& list, PyObject* tensors) {
+    if (!PyList_Check(tensors) || (size_t)PyList_GET_SIZE(tensors) != list.written.size())
+        refuse("the parameters and copies must be those that the handle was made with");
+    for (size_t i = 0; i < list.written.size(); ++i) {
+        const Written& w = list.written[i];
+        const Wanted& like = list.wanted[w.tensor];
+        const at::Tensor& t = tensor(PyList_GET_ITEM(tensors, (Py_ssize_t)i), "a parameter");
+        if (t.scalar_type() != w.type || t.device() != list.device || t.layout() != at::kStrided ||
+            t.sizes() != at::IntArrayRef(like.shape) || t.const_data_ptr() != w.at || !in_order(t, like.shape, like.strides))
+            refuse("parameter " + std::to_string(w.tensor) + ", or its copy, has been given other memory: make a new AdamW, "
+                   "with this one's state_dict() as its state");
+    }
+}
+
 // tensors, grads, parameters and copies, state_bits, m, v, m_scale, v_scale, lr, beta1, beta2, eps, step, seed, grad_scale, stream
 PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
     want(n_args, 16);
@@ -321,7 +357,7 @@ PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
     const at::Tensor* scale = maybe(a[14], "grad_scale");
     if (scale && (scale->scalar_type() != at::kFloat || scale->numel() != 1 || scale->device() != list.device))
         refuse("grad_scale must be one float32 on the parameters' device");
-    if (!PyList_Check(a[2])) refuse("the parameters must be a list");
+    check_written(list, a[2]);
     const at::Tensor *ms = maybe(a[6], "m_scale"), *vs = maybe(a[7], "v_scale");
     const Place at(list.device, a[15]);
     const int e = pp_adamw_step(list.handle, grads.data(), (int)integer(a[3]), tensor(a[4], "m").data_ptr(), tensor(a[5], "v").data_ptr(),

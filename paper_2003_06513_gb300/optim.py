@@ -89,7 +89,8 @@ class _Tensors:
                 raise ValueError("taps go with a [Cout, Cin/groups, 3, 3] tensor, one mask a kernel")
             if t.dtype != torch.int16 or not t.is_contiguous() or t.get_device() != index:
                 raise ValueError("taps must be contiguous int16 tensors on the tensors' device")
-        self._keep_alive = (taps, params, copies)
+        # the memory that the table has addresses of: the tensors may be given other memory, and free this
+        self._keep_alive = [t.detach() for ts in (taps, params, copies) for t in ts or [] if t is not None]
         copy_dtype = next((_DT[c.dtype] for c in copies or [] if c is not None), PP_F16)
 
         def addresses(tensors):
@@ -105,7 +106,8 @@ class _Tensors:
         self._h = h
         self.native = _lib.binding()
         self.list = self.native.tensors(h.value, index, [(tuple(shape), tuple(stride), _DT[d])
-                                                         for shape, stride, d in zip(shapes, strides, dtypes)])
+                                                         for shape, stride, d in zip(shapes, strides, dtypes)],
+                                        [(t, i) for ts in (params, copies) for i, t in enumerate(ts or []) if t is not None])
         self._home = _raw_stream(stream, self._device)      # the stream that what is allocated here belongs to
         with torch.cuda.device(index), self._on(stream):
             self._table = torch.empty(self.query(_TABLE_BYTES), dtype=torch.uint8, device=self._device)
@@ -175,6 +177,8 @@ class AdamW:
     ``seed``          of the 8-bit states' rounding;
     ``state``         what ``state_dict`` gave: its tensors become this object's own.
 
+    Parameters, copies and masks keep their memory while the object is used: ``step`` refuses a parameter or copy that
+    was given other memory (``p.data = ...``, a module's move to another type or order); masks are read where they were.
     ``m`` and ``v`` (and ``m_scale``, ``v_scale``) hold all tensors' moments one after the other, each
     from a multiple of 256 elements on; ``state_of`` gives one tensor's."""
 

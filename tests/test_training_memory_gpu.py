@@ -55,3 +55,53 @@ def test_out_has_a_new_version():
     assert out._version > between
     optim.GradNorm([(4,)])([torch.ones(4, device="cuda")], out=both)
     assert both._version > before[1] and float(both[0]) == 2.0
+
+
+def _pruned():
+    w = torch.ones(6, 4, 3, 3, device="cuda")
+    w[:, :, 0] = 0
+    return w
+
+
+@pytest.mark.parametrize("state_bits", [8, 32])
+@pytest.mark.parametrize("which", ["parameter", "copy", "parameter's order", "module"])
+def test_a_parameter_that_was_given_other_memory_is_refused(which, state_bits):
+    """Its old memory may be another tensor's: nothing is written, and the step is not counted."""
+    p, q = torch.ones(40, device="cuda"), torch.ones(7, 6, device="cuda")
+    c = p.half()
+    net = torch.nn.Linear(3, 5, device="cuda")
+    opt = optim.AdamW([p, q, net.weight], state_bits=state_bits, copies=[c, None, None])
+    grads = [torch.ones_like(p), torch.ones_like(q), torch.ones_like(net.weight)]
+    opt.step(grads)
+    old = {"parameter": p, "copy": c, "parameter's order": q, "module": net.weight}[which]
+    before = old.detach()                                # its memory as it was
+    if which == "module":
+        torch.nn.utils.vector_to_parameters(torch.full((20,), 3.0, device="cuda"), net.parameters())
+    elif which == "parameter's order":
+        q.data = q.data.view(6, 7).t()                   # the same address and shape, columns first
+        assert q.shape == (7, 6) and q.stride() == (1, 7)
+    else:
+        old.data = old.data.clone()
+    kept = [t.clone() for t in (p, q, c, net.weight, before, opt.m.view(torch.uint8))]
+    with pytest.raises(ValueError, match="other memory"):
+        opt.step(grads)
+    assert opt.steps == 1
+    assert all(torch.equal(a, b) for a, b in zip(kept, (p, q, c, net.weight, before, opt.m.view(torch.uint8))))
+    again = optim.AdamW([p, q, net.weight], state_bits=state_bits, copies=[c, None, None], state=opt.state_dict())
+    again.step([torch.ones_like(p), torch.ones_like(q), torch.ones_like(net.weight)])
+    assert again.steps == 2 and bool((p < kept[0]).all()) and bool((net.weight < kept[3]).all()) and torch.equal(c, p.half())
+
+
+def test_masks_are_read_where_they_were():
+    """Masks that were given other memory: the handle holds what it reads."""
+    w = _pruned()
+    taps = optim.taps_of(w)
+    opt = optim.AdamW([w], taps=[taps], weight_decay=0.0)
+    n = optim.GradNorm([w.shape], taps=[taps])
+    taps.data = torch.zeros(5, dtype=torch.int16, device="cuda")
+    junk = [torch.full((24,), -1, dtype=torch.int16, device="cuda") for _ in range(64)]      # would take freed memory
+    g = torch.ones_like(w)
+    for norm_of in (opt.grad_norm, n):
+        assert float(norm_of([g])[0]) == pytest.approx(144 ** 0.5)                          # six of nine taps
+    opt.step([g])
+    assert bool((w[:, :, 0] == 0).all()) and bool((w[:, :, 1:] < 1).all()) and len(junk) == 64
