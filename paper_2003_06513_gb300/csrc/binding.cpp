@@ -237,6 +237,7 @@ struct List {
     at::Device device;
     std::vector<Wanted> wanted;
     std::vector<Written> written;
+    int64_t state_elements;
 };
 constexpr const char* kList = "patconv.tensors";
 
@@ -255,8 +256,9 @@ bool in_order(const at::Tensor& t, const std::vector<int64_t>& shape, const std:
 PyObject* tensors(PyObject* const* a, Py_ssize_t n_args) {
     want(n_args, 4);
     auto list = std::make_unique<List>(List{static_cast<pp_tensors_handle>(PyLong_AsVoidPtr(a[0])),
-                                            at::Device(at::kCUDA, (int8_t)integer(a[1])), {}, {}});
+                                            at::Device(at::kCUDA, (int8_t)integer(a[1])), {}, {}, 0});
     if (PyErr_Occurred()) throw Raised();
+    if (pp_tensors_query(list->handle, PP_TQ_STATE_ELEMENTS, &list->state_elements) != PP_OK) refuse("a handle is wanted");
     if (!PyList_Check(a[2]) || !PyList_Check(a[3])) refuse("a list is wanted");
     for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i) {
         PyObject *shape, *strides;
@@ -349,6 +351,14 @@ void check_written(const List& list, PyObject* tensors) {
     }
 }
 
+// A state of the handle's tensors: `count` values of a type.
+void* state_of(const List& list, PyObject* o, const char* what, at::ScalarType type, int64_t count) {
+    const at::Tensor& t = tensor(o, what);
+    if (t.scalar_type() != type || t.layout() != at::kStrided || t.numel() != count || !t.is_contiguous() || t.device() != list.device)
+        refuse(std::string(what) + " must be " + std::to_string(count) + " contiguous " + c10::toString(type) + " values on the parameters' device");
+    return t.data_ptr();
+}
+
 // tensors, grads, parameters and copies, state_bits, m, v, m_scale, v_scale, lr, beta1, beta2, eps, step, seed, grad_scale, stream
 PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
     want(n_args, 16);
@@ -358,11 +368,15 @@ PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
     if (scale && (scale->scalar_type() != at::kFloat || scale->numel() != 1 || scale->device() != list.device))
         refuse("grad_scale must be one float32 on the parameters' device");
     check_written(list, a[2]);
-    const at::Tensor *ms = maybe(a[6], "m_scale"), *vs = maybe(a[7], "v_scale");
+    const int bits = (int)integer(a[3]);
+    const int64_t count = list.state_elements, blocks = count / PP_STATE_BLOCK;
+    const at::ScalarType type = bits == 8 ? at::kFloat8_e4m3fn : at::kFloat;
+    void *m = state_of(list, a[4], "m", type, count), *v = state_of(list, a[5], "v", type, count);
+    void* ms = bits == 8 ? state_of(list, a[6], "m_scale", at::kFloat, blocks) : nullptr;
+    void* vs = bits == 8 ? state_of(list, a[7], "v_scale", at::kFloat, blocks) : nullptr;
     const Place at(list.device, a[15]);
-    const int e = pp_adamw_step(list.handle, grads.data(), (int)integer(a[3]), tensor(a[4], "m").data_ptr(), tensor(a[5], "v").data_ptr(),
-                                ms ? ms->data_ptr<float>() : nullptr, vs ? vs->data_ptr<float>() : nullptr, real(a[8]), real(a[9]),
-                                real(a[10]), real(a[11]), integer(a[12]), (uint32_t)integer(a[13]),
+    const int e = pp_adamw_step(list.handle, grads.data(), bits, m, v, static_cast<float*>(ms), static_cast<float*>(vs), real(a[8]),
+                                real(a[9]), real(a[10]), real(a[11]), integer(a[12]), (uint32_t)integer(a[13]),
                                 scale ? scale->const_data_ptr<float>() : nullptr, at.stream);
     if (!e)
         for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i) changed(tensor(PyList_GET_ITEM(a[2], i), "a parameter"));

@@ -105,3 +105,21 @@ def test_masks_are_read_where_they_were():
         assert float(norm_of([g])[0]) == pytest.approx(144 ** 0.5)                          # six of nine taps
     opt.step([g])
     assert bool((w[:, :, 0] == 0).all()) and bool((w[:, :, 1:] < 1).all()) and len(junk) == 64
+
+
+@pytest.mark.parametrize("state_bits", [8, 32])
+def test_states_of_another_size_or_type_are_refused(state_bits):
+    """m, v and their scales are the object's attributes, which a program may set."""
+    p = torch.ones(600, device="cuda")
+    opt = optim.AdamW([p], state_bits=state_bits)
+    g = [torch.ones_like(p)]
+    for name in ("m", "v") + (("m_scale", "v_scale") if state_bits == 8 else ()):
+        right = getattr(opt, name)
+        for wrong in (right[:-1], right.view(torch.uint8), right.cpu(), torch.empty(2 * right.numel(), dtype=right.dtype, device="cuda")[::2], None):
+            setattr(opt, name, wrong)
+            with pytest.raises(ValueError, match=name):
+                opt.step(g)
+        setattr(opt, name, right.clone())
+    assert opt.steps == 0 and bool((p == 1).all())
+    opt.step(g)
+    assert opt.steps == 1 and bool((p < 1).all())
