@@ -483,10 +483,12 @@ __device__ __forceinline__ void pair_stats(float4 (&out)[kPairs<V>], const NormA
         out[i / 2] = make_float4(p[0], p[1], q[0], q[1]);
     }
 }
-// p and q of a group from its sums of gamma dz and of gamma dz d
+// p and q of a group from its sums of gamma dz and of gamma dz d.  q's factors rstd are taken one at a time: the mean
+// of gamma dz d has the size of a value's distance, B / M that of dz, and rstd^3 by itself would leave fp32's range
+// for spreads above 1e12 or below 1e-13.
 __device__ __forceinline__ float2 group_pq(const NormArgs& a, float2 sums, float rstd) {
-    const float inv = 1.0f / ((float)a.pixels * a.cpg);
-    return a.pixels * a.cpg == 1 ? make_float2(0.0f, 0.0f) : make_float2(-rstd * (sums.x * inv), -rstd * rstd * rstd * (sums.y * inv));
+    const float inv = 1.0f / ((float)a.pixels * a.cpg), b = rstd * (sums.y * inv);
+    return a.pixels * a.cpg == 1 ? make_float2(0.0f, 0.0f) : make_float2(-rstd * (sums.x * inv), -rstd * (rstd * b));
 }
 // The threads' sums of dz and of dz d by a quarter of their rows: s[channel][row of the quarter][column], the
 // rows of the other quarters added in turn.  A quarter of the room is a CTA more on an SM.

@@ -302,3 +302,24 @@ def test_offsets_beyond_32_bits():
     assert not y[:2].any()
     dx, _, _ = norm.pp_group_norm_backward(y, t, mean, rstd, 32, act="relu", out=y)
     assert torch.isfinite(dx[2]).all() and not dx[:2].any() and dx[2, :, -1].any()
+
+
+@pytest.mark.parametrize("dtype,size", [("f32", 1e13), ("f32", 1e15), ("f32", 1e16), ("f32", 1e-14), ("f32", 1e-16),
+                                        ("bf16", 1e15), ("bf16", 1e-14)])
+@pytest.mark.parametrize("shape", [(2, 32, 4, 9, 11), (1, 8192, 1, 2, 2)], ids=str)
+def test_gradients_of_values_of_any_size(shape, dtype, size):
+    """Spreads whose rstd^3 fp32 does not hold, without an eps beside them; resident and streamed."""
+    n, c, g, h, w = shape
+    assert norm.plan((n, c, h, w), g, DT[dtype], True)["path"] == (1 if c == 8192 else 2)
+    x, ga, be = _inputs((n, c, h, w), dtype, 22)
+    x = torch.from_numpy(x * size).to(DT[dtype]).double().numpy()
+    dy, _, _ = _inputs((n, c, h, w), dtype, 23)
+    _, mean, rstd, _ = T.norm_forward(x, g, ga, be, 0.0, "silu")
+    mean, rstd = mean.astype(np.float32), rstd.astype(np.float32)
+    got = norm.pp_group_norm_backward(_tensor(dy, dtype), _tensor(x, dtype), torch.from_numpy(mean).cuda(), torch.from_numpy(rstd).cuda(), g,
+                                      torch.from_numpy(ga).cuda(), torch.from_numpy(be).cuda(), "silu")
+    want, bounds = T.norm_backward(dy, x, mean, rstd, g, ga, be, "silu")
+    for a, b, e, what, dt in zip(got, want, bounds, ("dx", "dgamma", "dbeta"), (dtype, "f32", "f32")):
+        _within(_host(a), b, e, dt, what)
+    # the forward pass of the same values, whose squares fp32 holds
+    _check_forward(x, _tensor(x, dtype), g, ga, be, "silu", dtype, 0.0)
