@@ -235,6 +235,10 @@ int check_input(const Shape& s, const void* p, int64_t pixel, int64_t sample) {
     return PP_OK;
 }
 
+// whether an input lies as the output does; strides between pixels, or samples, that there is one of do not count
+bool dense(const Shape& s, int64_t pixel, int64_t sample) {
+    return (s.pixels == 1 || pixel == s.C) && (s.N == 1 || sample == s.pixels * s.C);
+}
 // bytes from an input's first element to the end of its last
 size_t extent(const Shape& s, int64_t pixel, int64_t sample) {
     return (size_t)((s.N - 1) * sample + (s.pixels - 1) * pixel + s.C) * size_of(s.dtype);
@@ -343,7 +347,7 @@ int pp_group_norm(const void* x, int64_t x_pixel, int64_t x_sample, int dtype, i
     if (workspace_bytes < workspace_of(s)) return PP_ERR_BUFFER;
     const size_t yb = (size_t)N * pixels * C * size_of(dtype);
     // y may be x itself where x is dense: every value is read before it is written
-    if (!(x == y && x_pixel == C && x_sample == pixels * C) && overlap(x, extent(s, x_pixel, x_sample), y, yb))
+    if (!(x == y && dense(s, x_pixel, x_sample)) && overlap(x, extent(s, x_pixel, x_sample), y, yb))
         return PP_ERR_BUFFER;
     const Plan p = plan_of(s, std::min({align_of(x), align_of(y), align_of(C, dtype),
                                           pixels > 1 ? align_of(x_pixel, dtype) : 16,
@@ -377,7 +381,7 @@ int pp_group_norm_backward(const void* dy, int64_t dy_pixel, int64_t dy_sample, 
         return PP_ERR_ALIGN;
     if (workspace_bytes < workspace_of(s)) return PP_ERR_BUFFER;
     const size_t xb = (size_t)N * pixels * C * size_of(dtype);
-    const bool over_dy = dx == dy && dy_pixel == C && dy_sample == pixels * C;
+    const bool over_dy = dx == dy && dense(s, dy_pixel, dy_sample);
     if (overlap(x, extent(s, x_pixel, x_sample), dx, xb) ||
         (!over_dy && overlap(dy, extent(s, dy_pixel, dy_sample), dx, xb)))
         return PP_ERR_BUFFER;

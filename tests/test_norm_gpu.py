@@ -323,3 +323,19 @@ def test_gradients_of_values_of_any_size(shape, dtype, size):
         _within(_host(a), b, e, dt, what)
     # the forward pass of the same values, whose squares fp32 holds
     _check_forward(x, _tensor(x, dtype), g, ga, be, "silu", dtype, 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("shape", [(1, 64, 8, 32, 32), (1, 12, 4, 1, 1), (3, 12, 4, 1, 1), (1, 8192, 1, 2, 2), (1, 1, 1, 5, 3)], ids=str)
+def test_in_place_of_one_sample_and_of_one_pixel(shape, dtype):
+    """Where there is one sample or one pixel the strides between them say nothing."""
+    n, c, g, h, w = shape
+    x, ga, be = _inputs((n, c, h, w), dtype, 21)
+    t, dga, dbe = _tensor(x, dtype), torch.from_numpy(ga).cuda(), torch.from_numpy(be).cuda()
+    want, mean, rstd = norm.pp_group_norm(t, g, dga, dbe, act="silu")
+    dy = torch.randn_like(t)
+    dwant = norm.pp_group_norm_backward(dy, t, mean, rstd, g, dga, dbe, "silu")
+    dgot = norm.pp_group_norm_backward(dy, t, mean, rstd, g, dga, dbe, "silu", out=dy)
+    assert dgot[0].data_ptr() == dy.data_ptr() and all(torch.equal(a, b) for a, b in zip(dgot, dwant))
+    got, _, _ = norm.pp_group_norm(t, g, dga, dbe, act="silu", out=t)
+    assert got.data_ptr() == t.data_ptr() and torch.equal(got, want)
