@@ -113,13 +113,18 @@ class _Tensors:
             self._table = torch.empty(self.query(_TABLE_BYTES), dtype=torch.uint8, device=self._device)
             _lib.check("pp_tensors_bind", lib.pp_tensors_bind(h, ctypes.c_void_p(self._table.data_ptr()),
                                                               self._table.numel(), _stream_ptr(stream, self._device)))
-            if not torch.cuda.is_current_stream_capturing():
-                torch.cuda.current_stream().synchronize()
+            self.settle()
 
     def query(self, key: int) -> int:
         v = ctypes.c_int64()
         _lib.check("pp_tensors_query", _lib.load().pp_tensors_query(self._h, key, ctypes.byref(v)))
         return int(v.value)
+
+    def settle(self) -> None:
+        """Waits for what the constructor has put on the current stream, unless that is being captured: calls on any
+        stream may follow."""
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
 
     def _on(self, stream):
         return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
@@ -216,11 +221,12 @@ class AdamW:
         dtype = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
         self.m_scale = self.v_scale = None
         if state is None:
-            with self._t._on(stream):
+            with torch.cuda.device(device), self._t._on(stream):
                 self.m, self.v = (torch.zeros(count * (4 if state_bits == 32 else 1), dtype=torch.uint8,
                                               device=device).view(dtype) for _ in range(2))
                 if state_bits == 8:
                     self.m_scale, self.v_scale = (torch.ones(blocks, device=device) for _ in range(2))
+                self._t.settle()
         else:
             wanted = {"m": (dtype, count), "v": (dtype, count)}
             if state_bits == 8:

@@ -123,3 +123,25 @@ def test_states_of_another_size_or_type_are_refused(state_bits):
     assert opt.steps == 0 and bool((p == 1).all())
     opt.step(g)
     assert opt.steps == 1 and bool((p < 1).all())
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+@pytest.mark.parametrize("state_bits", [8, 32])
+def test_a_new_object_is_ready_for_calls_on_any_stream(monkeypatch, state_bits, own_stream):
+    """The states' zeros come after 0.1 s of other work on the constructor's stream: the constructor waits for them."""
+    p = torch.ones(600, device="cuda")
+    stream = torch.cuda.Stream() if own_stream else None
+    torch.cuda.synchronize()
+    zeros = torch.zeros
+
+    def late(*args, **kw):
+        torch.cuda._sleep(200_000_000)
+        return zeros(*args, **kw)
+    monkeypatch.setattr(torch, "zeros", late)
+    opt = optim.AdamW([p], state_bits=state_bits, stream=stream)
+    assert (stream or torch.cuda.current_stream()).query()
+    g = [torch.ones_like(p)]
+    torch.cuda.synchronize()
+    opt.step(g, stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert torch.allclose(opt.state_of(0)[0], torch.full_like(p, 0.1), rtol=0.07)
