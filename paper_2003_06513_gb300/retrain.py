@@ -6,8 +6,8 @@ where the layer says so, a 2x2 max-pool; then the mean over the pixels and a lin
 trains it with the framework's operators: ``norm.group_norm`` forward and backward, one gradient norm
 over all parameters, one AdamW step that leaves pruned taps alone and writes the rounded weights that the
 next forward pass reads.  The dense convolutions and the loss are torch's.  Nothing in a step waits
-for the GPU.  ``pack`` hands the retrained weights to the packer, which finds the same patterns and
-kernels again, and ``predict`` runs the packed layers.
+for the GPU.  ``pack`` hands the retrained weights and their pattern library to the packer, which finds the
+same patterns and kernels again, and ``predict`` runs the packed layers.
 
     net = Retrainer(specs, classes=10)                # specs: admm.ConvSpec with the pruned weights
     for x, labels in batches:
@@ -20,7 +20,7 @@ from __future__ import annotations
 
 import argparse
 import math
-from typing import List, Sequence, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -35,11 +35,15 @@ class Retrainer:
     ``dtype``         of activations and of the weights that the convolutions read; the weights that
                       AdamW keeps are float32;
     ``max_norm``      the gradients' norm is clipped to it;
-    ``state_bits``    of AdamW's moments, 8 or 32."""
+    ``state_bits``    of AdamW's moments, 8 or 32;
+    ``patterns``      the pattern library that the layers were pruned with, None for the default one: ``pack`` packs
+                      with it."""
 
     def __init__(self, specs: Sequence[admm.ConvSpec], classes: int, groups: int = 32, act: str = "relu",
                  dtype: torch.dtype = torch.bfloat16, lr: float = 1e-3, weight_decay: float = 0.01,
-                 max_norm: float = 1.0, state_bits: int = 8, seed: int = 0, device="cuda"):
+                 max_norm: float = 1.0, state_bits: int = 8, seed: int = 0, device="cuda",
+                 patterns: Optional[Sequence[int]] = None):
+        self.patterns = None if patterns is None else list(patterns)
         self.specs, self.act, self.dtype, self.max_norm = list(specs), act, dtype, max_norm
         self.weights = [torch.from_numpy(np.ascontiguousarray(s.weight, np.float32)).to(device) for s in self.specs]
         channels = [w.shape[0] for w in self.weights]
@@ -86,9 +90,17 @@ class Retrainer:
         return loss.detach(), total
 
     def pack(self) -> List[api.Layer]:
-        """The retrained layers as the inference library runs them."""
-        return [api.pp_pack(w.detach().cpu().numpy(), None, s.keep, 1, s.stride).bind(w.device)
-                for w, s in zip(self.weights, self.specs)]
+        """The retrained layers as the inference library runs them.  ValueError where the packer would prune a kept weight:
+        the layer was pruned with another pattern library, or keeps more kernels than its ``keep``."""
+        layers = []
+        for i, (w, s) in enumerate(zip(self.weights, self.specs)):
+            host = w.detach().cpu().numpy()
+            layer = api.pp_pack(host, self.patterns, s.keep, 1, s.stride)
+            if not np.array_equal(layer.export("dense").reshape(host.shape), host):
+                raise ValueError(f"layer {i} is not inside its constraints: `patterns` must be the library it was pruned with, "
+                                 "`keep` at least the kernels it has")
+            layers.append(layer.bind(w.device))
+        return layers
 
     @torch.no_grad()
     def predict(self, layers: Sequence[api.Layer], x: torch.Tensor) -> torch.Tensor:

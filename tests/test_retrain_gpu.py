@@ -90,3 +90,48 @@ def test_packed_layers_predict_what_the_net_does():
         assert (got - want).abs().max() <= 1e-3 * want.abs().max()
     finally:
         torch.backends.cudnn.allow_tf32 = tf32
+
+
+OTHER = [0x115, 0x151, 0x154, 0x055]                 # the centre and three corners: no pattern of the default library
+
+
+def _pruned_with(patterns, keep=0.5):
+    rng = np.random.default_rng(31)
+    specs = []
+    for cin, cout, k in ((3, 16, 1.0), (16, 32, keep)):
+        w = (rng.standard_normal((cout, cin, 3, 3)) * np.sqrt(2.0 / (9 * cin))).astype(np.float32)
+        specs.append(admm.ConvSpec(admm.project(w, patterns, k), np.zeros(cout, np.float32), keep=k))
+    return specs
+
+
+def test_another_pattern_library_comes_back_from_the_packer():
+    """fp32 activations without TF32, as above: scores agree to 1e-3 of their size."""
+    tf32 = torch.backends.cudnn.allow_tf32
+    torch.backends.cudnn.allow_tf32 = False
+    try:
+        net = retrain.Retrainer(_pruned_with(OTHER), classes=4, dtype=torch.float32, lr=3e-3, patterns=OTHER)
+        draw = retrain.synthetic_classes(4, (3, 16, 16), "cuda", seed=32)
+        for _ in range(5):
+            net.step(*draw(16))
+        layers = net.pack()
+        for w, spec, layer in zip(net.weights, net.specs, layers):
+            w = w.detach().cpu().numpy()
+            assert np.array_equal(w != 0, spec.weight != 0)
+            np.testing.assert_array_equal(layer.export("dense").reshape(w.shape), w)
+        x, _ = draw(16)
+        with torch.no_grad():
+            want = net.logits(x)
+        assert (net.predict(layers, x) - want).abs().max() <= 1e-3 * want.abs().max()
+    finally:
+        torch.backends.cudnn.allow_tf32 = tf32
+
+
+def test_pack_refuses_what_the_packer_would_prune():
+    net = retrain.Retrainer(_pruned_with(OTHER), classes=4)          # not told of its library
+    with pytest.raises(ValueError, match="constraints"):
+        net.pack()
+    specs = _pruned_with(None, 0.6)
+    specs[1].keep = 0.3                                              # fewer kernels than it has
+    with pytest.raises(ValueError, match="layer 1"):
+        retrain.Retrainer(specs, classes=4).pack()
+    assert len(retrain.Retrainer(_pruned_with(None), classes=4).pack()) == 2
