@@ -984,6 +984,12 @@ int pp_grad_norm(pp_tensors_handle h, const void* const* grads, double max_norm,
     unsigned* counter = reinterpret_cast<unsigned*>(h->dev + h->off_sums);
     double* sums = reinterpret_cast<double*>(h->dev + h->off_sums + kCounterBytes);
     const int n = (int)h->tensors.size();
+    // A call leaves its counters at zero, but one of several launches that failed between them has not: such a
+    // handle's calls begin with zeros of their own.
+    if (n > kMaxGrads && cudaMemsetAsync(counter, 0, kCounterBytes, st) != cudaSuccess) {
+        cudaGetLastError();
+        return PP_ERR_CUDA;
+    }
     unsigned all = 0;
     for (int pass = 0; pass < 2; ++pass) {        // count the partial sums, then launch
         unsigned done = 0;

@@ -406,3 +406,16 @@ def test_a_step_has_the_same_bits_at_any_alignment_without_a_mask(bits):
             opt.step([torch.randn(n, generator=gen, device="cuda")])
         got.append((p, opt.m.view(torch.uint8), opt.v.view(torch.uint8)))
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_grad_norm_after_a_call_that_ended_between_its_launches():
+    """Such a call leaves its CTAs counted (a list of a thousand is three launches): the next one's norm is right."""
+    n = optim.GradNorm([(5,)] * 1000)
+    table = n._t._table
+    counters = table[table.numel() - 512 - 3 * 152 * 5 * 8:][:4 * 65].view(torch.int32)
+    for value in (0.5, 1.5):
+        assert not counters.any()
+        counters.fill_(3)
+        out = torch.zeros(2, device="cuda")
+        n([torch.full((5,), value, device="cuda") for _ in range(1000)], 1.0, out=out)
+        assert float(out[0]) == pytest.approx(value * math.sqrt(5000), rel=1e-6)
