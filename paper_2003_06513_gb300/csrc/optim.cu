@@ -67,7 +67,7 @@ struct Grads {
 
 struct pp_tensors {
     std::vector<Tensor> tensors;
-    std::vector<uint32_t> first_chunk;    // chunks of the tensors before each (whole launches matter), and of all
+    std::vector<uint32_t> first_chunk;    // chunks of the tensors before each (whole launches matter), and of all; none without params
     std::vector<uint32_t> first_span;     // the same of spans
     std::vector<uint32_t> masked_end;     // per launch: the end of its chunks of tensors with masks, which come first
     std::vector<uint8_t> image;           // chunks | spans | counters and partial sums (zero)
@@ -891,9 +891,9 @@ int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const
             h->first_chunk.push_back((uint32_t)chunks);
             h->state_elements += (numel[i] + kBlock - 1) / kBlock * kBlock;
             h->first_span.push_back((uint32_t)spans);
-            chunks += (uint64_t)((numel[i] + kChunk - 1) / kChunk);
+            if (params) chunks += (uint64_t)((numel[i] + kChunk - 1) / kChunk);      // the norm reads spans alone
             spans += (uint64_t)((numel[i] + kSpan - 1) / kSpan);
-            if (chunks > 0x7FFFFFFFu) return PP_ERR_SHAPE;
+            if (std::max(chunks, spans) > 0x7FFFFFFFu) return PP_ERR_SHAPE;
         }
         h->first_chunk.push_back((uint32_t)chunks);
         h->first_span.push_back((uint32_t)spans);
@@ -905,14 +905,14 @@ int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const
         h->image.assign(h->off_sums + kCounterBytes + std::max<size_t>(1, launches) * kSumCtas * sizeof(double), 0);
         Chunk* c = reinterpret_cast<Chunk*>(h->image.data());
         const Chunk* const first = c;
-        for (int i = 0; i < n; i += kMaxGrads) {
+        for (int i = 0; params && i < n; i += kMaxGrads) {
             const int end = std::min(n, i + kMaxGrads);
             for (const bool masked : {true, false}) {
                 for (int k = i; k < end; ++k) {
                     const Tensor& t = h->tensors[k];
                     if (t.masked != masked) continue;
                     for (int64_t e = 0; e < t.numel; e += kChunk, ++c) {
-                        c->param = params ? params[k] + e : nullptr;
+                        c->param = params[k] + e;
                         c->copy = copies && copies[k] ? static_cast<uint16_t*>(copies[k]) + e : nullptr;
                         c->taps = masked ? taps[k] + e / 9 : nullptr;
                         c->state = t.state + e;

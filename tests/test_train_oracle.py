@@ -214,3 +214,20 @@ def test_taps_of_a_pruned_weight():
     assert optim.taps_of(w).tolist() == [0, 1, 0x0B8, 0] and optim.taps_of(w).dtype == torch.int16
     with pytest.raises(ValueError):
         optim.taps_of(torch.zeros(2, 2, 5, 5))
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_a_handle_for_the_norm_alone_has_no_table_of_steps(lib, masked):
+    """32 bytes for every 16384 elements and the partial sums of a launch; with parameters 64 for every 2048 too."""
+    numel, v = [512 * 512 * 9] * 24 + [10, 0], ctypes.c_int64()
+    taps = [1 << 20] * 24 + [None, None] if masked else None
+    sums = 512 + 152 * 5 * 8
+    got = []
+    for params in (None, [(i + 1) << 30 for i in range(26)]):
+        st, h = _create(lib, numel, [0] * 26, taps=taps, params=params)
+        assert st == 0 and lib.pp_tensors_query(h, 1, ctypes.byref(v)) == 0
+        got.append(v.value)
+        assert lib.pp_tensors_query(h, 2, ctypes.byref(v)) == 0 and v.value == 24 * 512 * 512 * 9 + 256
+        lib.pp_tensors_destroy(h)
+    spans, chunks = 24 * 144 + 1, 24 * 1152 + 1
+    assert got[0] <= 32 * spans + 256 + sums and got[1] >= 64 * chunks + 32 * spans + sums
