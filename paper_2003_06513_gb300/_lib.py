@@ -93,7 +93,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
             return _lib
         path = _build.LIB
         if build_if_missing:
-            path = _build.build()
+            path = _build.build(binding=False)
         if not os.path.exists(path):
             raise RuntimeError(f"libpatconv is not built ({path} missing); run "
                                "`python -c 'import __graft_entry__ as g; g.build()'`")
@@ -107,13 +107,14 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
 
 
 def binding():
-    """The native binding of the training side (csrc/binding.cpp), beside the library."""
+    """The native binding of the training side (csrc/binding.cpp), beside the library; built first if needed."""
     global _binding
     if _binding is None:
         import torch  # noqa: F401  (the binding links against its libraries)
         load()
         with _lock:
             if _binding is None:
+                _build.build(binding=True)
                 loader = importlib.machinery.ExtensionFileLoader("_patconv", _build.BINDING)
                 module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_patconv", loader))
                 loader.exec_module(module)

@@ -1,8 +1,8 @@
-"""Build libpatconv.so in-tree: nvcc for the sm_103a kernels, g++ for the host packer; and beside it
-_patconv.so, the native binding of the training side, which links against torch and the library.
+"""Build libpatconv.so in-tree: nvcc for the sm_103a kernels, g++ for the host packer; and beside it, where torch
+is installed, _patconv.so, the native binding of the training side, which links against torch and the library.
 
-Both are written to ``paper_2003_06513_gb300/_build/`` (git-ignored) and are rebuilt whenever a source
-file, a flag or the torch version changes.  No CMake: nine translation units compiled in parallel and
+Both are written to ``paper_2003_06513_gb300/_build/`` (git-ignored), and each is rebuilt whenever a source
+file or a flag of its own changes, the binding with the torch version too.  No CMake: nine translation units compiled in parallel and
 two links, so a fresh build takes a minute or so, the largest unit's time.
 """
 from __future__ import annotations
@@ -15,6 +15,7 @@ import subprocess
 import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
+from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -29,7 +30,7 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--expt-relaxed-constexpr", "-Xc
 GXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-I",
              os.path.join(ROOT, "include")]
 KERNELS = ["conv.cu", "tensor.cu", "norm.cu", "norm_f32.cu", "norm_f16.cu", "norm_bf16.cu", "optim.cu"]
-SOURCES = KERNELS + ["tensor.h", "norm.h", "norm.cuh", "pack.cpp", "layer.h", "gen_dispatch.py", "binding.cpp"]
+SOURCES = KERNELS + ["tensor.h", "norm.h", "norm.cuh", "pack.cpp", "layer.h", "gen_dispatch.py"]
 
 
 def _nvcc() -> str:
@@ -52,40 +53,51 @@ def _torch_version(torch_dir: str) -> str:
         return f.read()
 
 
-def _digest(extra) -> str:
-    h = hashlib.sha256(_torch_version(_torch_dir()).encode())
-    for name in SOURCES + [os.path.join("..", "..", "include", "patconv.h")]:
+def _digest(sources, *more) -> str:
+    h = hashlib.sha256()
+    for name in sources + [os.path.join("..", "..", "include", "patconv.h")]:
         with open(os.path.join(CSRC, name), "rb") as f:
             h.update(f.read())
-    h.update(repr((NVCC_FLAGS, GXX_FLAGS, extra)).encode())
+    h.update(repr(more).encode())
     return h.hexdigest()
 
 
-def build(force: bool = False, verbose: bool = False, extra_nvcc=()) -> str:
-    """Compile (if stale) and return the path of libpatconv.so."""
+def _obj(name: str) -> str:
+    return os.path.join(BUILD, name.split(".")[0] + ".o")
+
+
+class _Part:
+    """One of the two products: compiled where it, or the digest of what it is made of, is not there."""
+
+    def __init__(self, path: str, stamp: str, digest: str, force: bool):
+        self.path, self.stamp, self.digest = path, os.path.join(BUILD, stamp), digest
+        self.stale = force or not all(os.path.exists(f) for f in (path, self.stamp))
+        if not self.stale:
+            with open(self.stamp) as f:
+                self.stale = f.read().strip() != digest
+
+    def link(self, run, cmd) -> None:
+        tmp = self.path + ".tmp"
+        run([tmp if c is None else c for c in cmd])
+        os.replace(tmp, self.path)
+        with open(self.stamp, "w") as f:
+            f.write(self.digest)
+
+
+def build(force: bool = False, verbose: bool = False, extra_nvcc=(), binding: Optional[bool] = None) -> str:
+    """Compile what is stale and return the path of libpatconv.so.  The library needs nvcc and g++ alone.  ``binding``:
+    whether _patconv.so is built beside it; None: where torch is installed; True raises RuntimeError without it."""
     os.makedirs(BUILD, exist_ok=True)
-    stamp = os.path.join(BUILD, "stamp")
-    digest = _digest(tuple(extra_nvcc))
-    if not force and all(os.path.exists(f) for f in (LIB, BINDING, stamp)):
-        with open(stamp) as f:
-            if f.read().strip() == digest:
-                return LIB
+    if binding is None:
+        binding = importlib.util.find_spec("torch") is not None
+    library = _Part(LIB, "stamp", _digest(SOURCES, NVCC_FLAGS, GXX_FLAGS, tuple(extra_nvcc)), force)
+    parts = [library]
+    if binding:
+        torch_dir = _torch_dir()
+        parts.append(_Part(BINDING, "stamp_binding", _digest(["binding.cpp"], GXX_FLAGS, _torch_version(torch_dir)), force))
+    if not any(p.stale for p in parts):
+        return LIB
     nvcc = _nvcc()
-    subprocess.run([sys.executable, os.path.join(CSRC, "gen_dispatch.py"),
-                    os.path.join(BUILD, "pattern_dispatch.h")], check=True)
-    torch_dir = _torch_dir()
-    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
-    includes = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
-                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
-
-    def obj(name):
-        return os.path.join(BUILD, name.split(".")[0] + ".o")
-
-    cmds = [[nvcc, "-c", os.path.join(CSRC, name), "-o", obj(name), "-I", BUILD] + NVCC_FLAGS + list(extra_nvcc)
-            for name in KERNELS]
-    cmds += [["g++", "-c", os.path.join(CSRC, "pack.cpp"), "-o", obj("pack.cpp")] + GXX_FLAGS,
-             ["g++", "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj("binding.cpp")] + GXX_FLAGS
-             + [f for d in includes for f in ("-isystem", d)]]
 
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
@@ -95,17 +107,27 @@ def build(force: bool = False, verbose: bool = False, extra_nvcc=()) -> str:
             raise RuntimeError(f"build step failed: {' '.join(cmd[:3])}")
         return r.stdout + r.stderr
 
-    with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
-        list(ex.map(run, cmds))
-    tmp = LIB + ".tmp"
-    run([nvcc, "-shared", "-o", tmp] + [obj(name) for name in KERNELS + ["pack.cpp"]] + ARCH + ["-cudart", "static"])
-    os.replace(tmp, LIB)
-    tmp, lib = BINDING + ".tmp", os.path.join(torch_dir, "lib")
-    run(["g++", "-shared", "-o", tmp, obj("binding.cpp"), "-L", BUILD, "-l:libpatconv.so", "-L", lib, "-lc10", "-lc10_cuda",
-         "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN:" + lib])
-    os.replace(tmp, BINDING)
-    with open(stamp, "w") as f:
-        f.write(digest)
+    with ThreadPoolExecutor(max_workers=len(KERNELS) + 2) as ex:
+        glue = None
+        if binding and parts[1].stale:
+            cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
+            includes = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+                        os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+            glue = ex.submit(run, ["g++", "-c", os.path.join(CSRC, "binding.cpp"), "-o", _obj("binding.cpp")] + GXX_FLAGS
+                             + [f for d in includes for f in ("-isystem", d)])
+        if library.stale:
+            run([sys.executable, os.path.join(CSRC, "gen_dispatch.py"), os.path.join(BUILD, "pattern_dispatch.h")])
+            cmds = [[nvcc, "-c", os.path.join(CSRC, name), "-o", _obj(name), "-I", BUILD] + NVCC_FLAGS + list(extra_nvcc)
+                    for name in KERNELS]
+            cmds += [["g++", "-c", os.path.join(CSRC, "pack.cpp"), "-o", _obj("pack.cpp")] + GXX_FLAGS]
+            list(ex.map(run, cmds))
+            library.link(run, [nvcc, "-shared", "-o", None] + [_obj(name) for name in KERNELS + ["pack.cpp"]] + ARCH
+                         + ["-cudart", "static"])
+        if glue is not None:
+            glue.result()
+            lib = os.path.join(torch_dir, "lib")
+            parts[1].link(run, ["g++", "-shared", "-o", None, _obj("binding.cpp"), "-L", BUILD, "-l:libpatconv.so", "-L", lib, "-lc10",
+                                "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN:" + lib])
     return LIB
 
 
