@@ -423,7 +423,7 @@ int pp_tensors_destroy(pp_tensors_handle h);
  * 1e-6)), the factor that clips them; NaN where a kept gradient is NaN.
  *   grads     HOST array of the gradients' DEVICE addresses (element aligned, of the handle's types);
  *             NULL: that tensor has none this time;
- *   max_norm  above 0 (infinity: no clipping);   out  DEVICE fp32[2].
+ *   max_norm  above 0 (infinity: no clipping, the factor is 1 whatever the norm but NaN);   out  DEVICE fp32[2].
  * A thread sums in fp32 with what its roundings lose beside it, a CTA in fp32, the CTAs in 64 bits, in
  * a fixed order: the same inputs give the same bits.  The scratch is the handle's: order calls on one handle.  Never synchronises.
  * Errors: PP_ERR_NULL, _NOT_BOUND, _ALIGN, _ARG, _CUDA. */

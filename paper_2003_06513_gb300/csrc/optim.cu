@@ -366,9 +366,10 @@ __global__ void __launch_bounds__(kThreads, WIDE ? 5 : 4) grad_norm_kernel(const
     if (threadIdx.x == 0) {
         for (int i = 1; i < kThreads / 32; ++i) d += dsum[i];
         const float norm = (float)sqrt(d);
-        const float f = max_norm / (norm + 1e-6f);
+        // no clipping where max_norm is infinite, of an infinite norm either; NaN stays NaN
+        const float f = max_norm == INFINITY && norm == INFINITY ? 1.0f : max_norm / (norm + 1e-6f);
         out[0] = norm;
-        out[1] = f > 1.0f ? 1.0f : f;             // NaN stays NaN
+        out[1] = f > 1.0f ? 1.0f : f;
         *counter = 0;                             // for the next call
     }
 }

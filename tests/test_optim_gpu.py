@@ -419,3 +419,17 @@ def test_grad_norm_after_a_call_that_ended_between_its_launches():
         out = torch.zeros(2, device="cuda")
         n([torch.full((5,), value, device="cuda") for _ in range(1000)], 1.0, out=out)
         assert float(out[0]) == pytest.approx(value * math.sqrt(5000), rel=1e-6)
+
+
+@pytest.mark.parametrize("values", [[1.0, math.inf, 2.0, 0.0], [3e38] * 4, [1.0, -math.inf, math.inf, 3e38]], ids=str)
+def test_an_infinite_norm_is_not_clipped_by_an_infinite_bound(values):
+    """The default bound: the factor must not make NaN of the other gradients."""
+    n, g = optim.GradNorm([(4,)]), [torch.tensor(values, device="cuda")]
+    assert [float(a) for a in n(g)] == [math.inf, 1.0]
+    assert [float(a) for a in n(g, 1e30)] == [math.inf, 0.0]
+    p = torch.ones(4, device="cuda")
+    opt = optim.AdamW([p])
+    opt.step(g, grad_scale=opt.grad_norm(g)[1])
+    assert torch.isfinite(p[g[0].abs() < 1e30]).all()
+    g[0][0] = math.nan
+    assert all(math.isnan(float(a)) for a in n(g))
