@@ -338,7 +338,16 @@ int pp_group_norm(const void* x, int64_t x_pixel, int64_t x_sample, int dtype, i
     if (const int e = check_shape(s)) return e;
     if (act != PP_ACT_NONE && act != PP_ACT_RELU && act != PP_ACT_SILU) return PP_ERR_ARG;
     if (!(eps >= 0) || !std::isfinite(eps)) return PP_ERR_ARG;
-    if (!N || !pixels) return PP_OK;
+    if (!N || !pixels) {                            // all bits set are a NaN: there are no values
+        for (float* p : {mean, rstd}) {
+            if (off4(p)) return PP_ERR_ALIGN;
+            if (p && N && cudaMemsetAsync(p, 0xFF, (size_t)N * G * 4, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+                cudaGetLastError();
+                return PP_ERR_CUDA;
+            }
+        }
+        return PP_OK;
+    }
     if (const int e = check_input(s, x, x_pixel, x_sample)) return e;
     if (!y || !workspace) return PP_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(y) % size_of(dtype) || off4(gamma) || off4(beta) || off4(mean) || off4(rstd) ||
@@ -370,8 +379,11 @@ int pp_group_norm_backward(const void* dy, int64_t dy_pixel, int64_t dy_sample, 
     if (off4(gamma) || off4(beta) || off4(mean) || off4(rstd) || off4(dgamma) || off4(dbeta)) return PP_ERR_ALIGN;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!N || !pixels) {                            // sums over nothing
-        if (dgamma && cudaMemsetAsync(dgamma, 0, (size_t)C * 4, st) != cudaSuccess) return PP_ERR_CUDA;
-        if (dbeta && cudaMemsetAsync(dbeta, 0, (size_t)C * 4, st) != cudaSuccess) return PP_ERR_CUDA;
+        for (float* p : {dgamma, dbeta})
+            if (p && cudaMemsetAsync(p, 0, (size_t)C * 4, st) != cudaSuccess) {
+                cudaGetLastError();
+                return PP_ERR_CUDA;
+            }
         return PP_OK;
     }
     if (const int e = check_input(s, dy, dy_pixel, dy_sample)) return e;

@@ -339,3 +339,14 @@ def test_in_place_of_one_sample_and_of_one_pixel(shape, dtype):
     assert dgot[0].data_ptr() == dy.data_ptr() and all(torch.equal(a, b) for a, b in zip(dgot, dwant))
     got, _, _ = norm.pp_group_norm(t, g, dga, dbe, act="silu", out=t)
     assert got.data_ptr() == t.data_ptr() and torch.equal(got, want)
+
+
+def test_moments_of_no_pixels_are_nan():
+    x = torch.zeros((2, 8, 0, 3), device="cuda").contiguous(memory_format=torch.channels_last)
+    for value in (1.0, -2.0):
+        junk = [torch.full((2, 2), value, device="cuda") for _ in range(8)]
+        del junk                                          # memory that the outputs are likely to take
+        y, mean, rstd = norm.pp_group_norm(x, 2)
+        assert y.shape == x.shape and torch.isnan(mean).all() and torch.isnan(rstd).all()
+    _, mean, rstd = norm.pp_group_norm(torch.zeros((0, 8, 4, 3), device="cuda").contiguous(memory_format=torch.channels_last), 2)
+    assert mean.shape == rstd.shape == (0, 2)
