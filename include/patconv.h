@@ -402,7 +402,8 @@ typedef enum {
  *   copies       NULL, or per tensor NULL or a copy of the parameters in copy_dtype (PP_F16,
  *                PP_BF16) that each step writes beside them, rounded to nearest;
  *   decay        NULL (zeros) or the weight decay of each tensor.
- * Host-only.  Errors: PP_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _ARG (decay not finite), _ALLOC. */
+ * Parameters and copies share no memory among them.  Host-only.
+ * Errors: PP_ERR_NULL, _SHAPE, _DTYPE, _ALIGN, _BUFFER (shared memory), _ARG (decay not finite), _ALLOC. */
 int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const uint16_t* const* taps,
                       float* const* params, void* const* copies, int copy_dtype, const float* decay,
                       pp_tensors_handle* out);

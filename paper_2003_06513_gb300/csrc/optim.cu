@@ -20,6 +20,7 @@
 #include <cstring>
 #include <new>
 #include <type_traits>
+#include <utility>
 #include <vector>
 
 #include "patconv.h"
@@ -857,6 +858,21 @@ int check_grads(const pp_tensors* h, const void* const* grads) {
     return PP_OK;
 }
 
+// whether two of the stretches of memory that a step writes share a byte: their elements would be written in no order
+bool shared(int n, const int64_t* numel, float* const* params, void* const* copies) {
+    std::vector<std::pair<uintptr_t, uintptr_t>> at;      // begin, end
+    for (int i = 0; i < n; ++i) {
+        const uintptr_t p = params && params[i] ? reinterpret_cast<uintptr_t>(params[i]) : 0;
+        const uintptr_t c = copies && copies[i] ? reinterpret_cast<uintptr_t>(copies[i]) : 0;
+        if (p && numel[i]) at.emplace_back(p, p + (uintptr_t)numel[i] * 4);
+        if (c && numel[i]) at.emplace_back(c, c + (uintptr_t)numel[i] * 2);
+    }
+    std::sort(at.begin(), at.end());
+    for (size_t i = 1; i < at.size(); ++i)
+        if (at[i].first < at[i - 1].second) return true;
+    return false;
+}
+
 int launched() { return cudaGetLastError() == cudaSuccess ? PP_OK : PP_ERR_CUDA; }
 
 }  // namespace
@@ -880,6 +896,7 @@ int pp_tensors_create(int n, const int64_t* numel, const int* grad_dtypes, const
         if (decay && !std::isfinite(decay[i])) return PP_ERR_ARG;
     }
     try {
+        if (shared(n, numel, params, copies)) return PP_ERR_BUFFER;
         pp_tensors* h = new pp_tensors;
         struct Guard {
             pp_tensors* h;

@@ -182,6 +182,7 @@ class AdamW:
     ``seed``          of the 8-bit states' rounding;
     ``state``         what ``state_dict`` gave: its tensors become this object's own.
 
+    Parameters and copies share no memory: one that is used twice is given once, with the sum of its gradients.
     Parameters, copies and masks keep their memory while the object is used: ``step`` refuses a parameter or copy that
     was given other memory (``p.data = ...``, a module's move to another type or order); masks are read where they were.
     ``m`` and ``v`` (and ``m_scale``, ``v_scale``) hold all tensors' moments one after the other, each

@@ -231,3 +231,17 @@ def test_a_handle_for_the_norm_alone_has_no_table_of_steps(lib, masked):
         lib.pp_tensors_destroy(h)
     spans, chunks = 24 * 144 + 1, 24 * 1152 + 1
     assert got[0] <= 32 * spans + 256 + sums and got[1] >= 64 * chunks + 32 * spans + sums
+
+
+def test_parameters_and_copies_that_share_memory_are_refused(lib):
+    """A step would write them in no order."""
+    both = [0, 0]
+    for kw in (dict(params=[4096, 4096]), dict(params=[4096, 4096 + 36]), dict(params=[4096 + 36, 4096]),
+               dict(params=[4096, 8192], copies=[1024, 1024 + 18]), dict(params=[4096, 8192], copies=[None, 4096 + 32]),
+               dict(params=[4096, 8192], copies=[8192, None])):
+        assert _create(lib, [10, 10], both, **kw)[0] == BUFFER, kw
+    for kw in (dict(params=[4096, 4096 + 40]), dict(params=[4096, 8192], copies=[4096 + 40, 4096 - 20])):
+        st, h = _create(lib, [10, 10], both, **kw)
+        assert st == 0 and lib.pp_tensors_destroy(h) == 0
+    st, h = _create(lib, [10, 0], both, params=[4096, 4096])      # of no elements
+    assert st == 0 and lib.pp_tensors_destroy(h) == 0
