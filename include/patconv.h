@@ -441,7 +441,9 @@ int pp_grad_norm(pp_tensors_handle h, const void* const* grads, double max_norm,
  *               mantissa bits; 448 the largest, 0x7F NaN), and m_scale and v_scale DEVICE fp32 hold a
  *               power of two for every PP_STATE_BLOCK of them.  Both 32-byte aligned; zeros to begin
  *               with (scales any), and zero wherever an element is left out or beyond its tensor;
- *   step        1 for the first step;   grad_scale  DEVICE fp32[1] or NULL (1);
+ *   step        1 for the first step, of all tensors of the call: tensors whose counts differ (some had no
+ *               gradient at earlier steps) are stepped by calls of their own, the others' gradients NULL;
+ *   grad_scale  DEVICE fp32[1] or NULL (1);
  *   seed        8-bit states only.  A new state is rounded to one of its two neighbours, up with a
  *               probability equal to its distance from the lower one: to the nearest, a second moment
  *               that shrinks by a thousandth a step would never move, codes being a sixteenth to an

@@ -11,6 +11,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <memory>
 #include <optional>
 #include <stdexcept>
@@ -238,6 +239,7 @@ struct List {
     std::vector<Wanted> wanted;
     std::vector<Written> written;
     int64_t state_elements;
+    std::vector<int64_t> missed;            // steps at which each tensor had no gradient
 };
 constexpr const char* kList = "patconv.tensors";
 
@@ -256,7 +258,7 @@ bool in_order(const at::Tensor& t, const std::vector<int64_t>& shape, const std:
 PyObject* tensors(PyObject* const* a, Py_ssize_t n_args) {
     want(n_args, 4);
     auto list = std::make_unique<List>(List{static_cast<pp_tensors_handle>(PyLong_AsVoidPtr(a[0])),
-                                            at::Device(at::kCUDA, (int8_t)integer(a[1])), {}, {}, 0});
+                                            at::Device(at::kCUDA, (int8_t)integer(a[1])), {}, {}, 0, {}});
     if (PyErr_Occurred()) throw Raised();
     if (pp_tensors_query(list->handle, PP_TQ_STATE_ELEMENTS, &list->state_elements) != PP_OK) refuse("a handle is wanted");
     if (!PyList_Check(a[2]) || !PyList_Check(a[3])) refuse("a list is wanted");
@@ -279,6 +281,7 @@ PyObject* tensors(PyObject* const* a, Py_ssize_t n_args) {
         if (k < 0 || (size_t)k >= list->wanted.size()) refuse("there is no such tensor");
         list->written.push_back({t.const_data_ptr(), t.scalar_type(), (size_t)k});
     }
+    list->missed.assign(list->wanted.size(), 0);
     PyObject* capsule = PyCapsule_New(list.get(), kList, drop);
     if (capsule) list.release();
     return capsule;
@@ -362,7 +365,7 @@ void* state_of(const List& list, PyObject* o, const char* what, at::ScalarType t
 // tensors, grads, parameters and copies, state_bits, m, v, m_scale, v_scale, lr, beta1, beta2, eps, step, seed, grad_scale, stream
 PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
     want(n_args, 16);
-    const List& list = list_of(a[0]);
+    List& list = list_of(a[0]);
     const std::vector<const void*> grads = addresses(list, a[1]);
     const at::Tensor* scale = maybe(a[14], "grad_scale");
     if (scale && (scale->scalar_type() != at::kFloat || scale->numel() != 1 || scale->device() != list.device))
@@ -375,12 +378,52 @@ PyObject* adamw_step(PyObject* const* a, Py_ssize_t n_args) {
     void* ms = bits == 8 ? state_of(list, a[6], "m_scale", at::kFloat, blocks) : nullptr;
     void* vs = bits == 8 ? state_of(list, a[7], "v_scale", at::kFloat, blocks) : nullptr;
     const Place at(list.device, a[15]);
-    const int e = pp_adamw_step(list.handle, grads.data(), bits, m, v, static_cast<float*>(ms), static_cast<float*>(vs), real(a[8]),
-                                real(a[9]), real(a[10]), real(a[11]), integer(a[12]), (uint32_t)integer(a[13]),
-                                scale ? scale->const_data_ptr<float>() : nullptr, at.stream);
-    if (!e)
-        for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i) changed(tensor(PyList_GET_ITEM(a[2], i), "a parameter"));
-    return PyLong_FromLong(e);
+    const double lr = real(a[8]), b1 = real(a[9]), b2 = real(a[10]), eps = real(a[11]);
+    const int64_t step = integer(a[12]);
+    const uint32_t seed = (uint32_t)integer(a[13]);
+    // A tensor's step number counts the steps at which it had a gradient.  It is one for all as a rule; tensors that
+    // have missed some take launches of their own, those that have missed as many together.
+    std::vector<int64_t> apart;
+    for (size_t i = 0; i < list.missed.size(); ++i)
+        if (grads[i]) {
+            if (list.missed[i] >= step) refuse("tensor " + std::to_string(i) + " has missed more steps than were taken");
+            if (std::find(apart.begin(), apart.end(), list.missed[i]) == apart.end()) apart.push_back(list.missed[i]);
+        }
+    if (apart.empty()) apart.push_back(0);
+    std::vector<const void*> some;
+    for (const int64_t missed : apart) {
+        if (apart.size() > 1) {
+            some = grads;
+            for (size_t i = 0; i < list.missed.size(); ++i)
+                if (list.missed[i] != missed) some[i] = nullptr;
+        }
+        const int e = pp_adamw_step(list.handle, apart.size() > 1 ? some.data() : grads.data(), bits, m, v, static_cast<float*>(ms),
+                                    static_cast<float*>(vs), lr, b1, b2, eps, step - missed, seed,
+                                    scale ? scale->const_data_ptr<float>() : nullptr, at.stream);
+        if (e) return PyLong_FromLong(e);
+    }
+    for (size_t i = 0; i < list.missed.size(); ++i) list.missed[i] += !grads[i];
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i) changed(tensor(PyList_GET_ITEM(a[2], i), "a parameter"));
+    return PyLong_FromLong(PP_OK);
+}
+
+// tensors, None -> the steps that each tensor has missed, a list; tensors, list -> sets them
+PyObject* missed(PyObject* const* a, Py_ssize_t n_args) {
+    want(n_args, 2);
+    List& list = list_of(a[0]);
+    if (a[1] == Py_None) {
+        PyObject* out = PyList_New((Py_ssize_t)list.missed.size());
+        if (!out) throw Raised();
+        for (size_t i = 0; i < list.missed.size(); ++i) PyList_SET_ITEM(out, (Py_ssize_t)i, PyLong_FromLongLong(list.missed[i]));
+        return out;
+    }
+    if (!PyList_Check(a[1]) || (size_t)PyList_GET_SIZE(a[1]) != list.missed.size()) refuse("missed must be a list of one count a tensor");
+    std::vector<int64_t> to;
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[1]); ++i) to.push_back(integer(PyList_GET_ITEM(a[1], i)));
+    for (const int64_t k : to)
+        if (k < 0) refuse("missed must be counts");
+    list.missed = std::move(to);
+    Py_RETURN_NONE;
 }
 
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
@@ -406,6 +449,7 @@ PyMethodDef methods[] = {{"group_norm", fast<group_norm>(), METH_FASTCALL, nullp
                          {"tensors", fast<tensors>(), METH_FASTCALL, nullptr},
                          {"grad_norm", fast<grad_norm>(), METH_FASTCALL, nullptr},
                          {"adamw_step", fast<adamw_step>(), METH_FASTCALL, nullptr},
+                         {"missed", fast<missed>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_patconv", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

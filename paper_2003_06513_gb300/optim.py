@@ -238,10 +238,13 @@ class AdamW:
                     raise ValueError(f"state {name} must be {size} contiguous {dt} values on {device}")
                 setattr(self, name, t)
             self.steps = int(state["step"])
+            if "missed" in state:
+                self._t.native.missed(self._t.list, list(state["missed"]))
 
     def state_dict(self) -> dict:
-        """The moments and the step count; the tensors are this object's own, not copies."""
-        d = {"m": self.m, "v": self.v, "step": self.steps}
+        """The moments, the step count and, per tensor, the steps at which it had no gradient; the tensors are this
+        object's own, not copies."""
+        d = {"m": self.m, "v": self.v, "step": self.steps, "missed": self._t.native.missed(self._t.list, None)}
         if self.state_bits == 8:
             d |= {"m_scale": self.m_scale, "v_scale": self.v_scale}
         return d
@@ -264,7 +267,8 @@ class AdamW:
              lr: Optional[float] = None, stream=None) -> None:
         """One step with the gradients (default: the parameters' ``grad``; None: that tensor is left
         alone), each times ``grad_scale`` (one float32 on the device) if given, at rate ``lr`` (default:
-        the object's).  Calls on one object must be ordered."""
+        the object's).  The bias corrections go by a tensor's own count of steps: tensors that have missed some
+        take a launch of their own, one for all that have missed as many.  Calls on one object must be ordered."""
         t = self._t
         t.used((self.m, self.v, self.m_scale, self.v_scale), stream)
         _lib.check("pp_adamw_step", t.native.adamw_step(

@@ -433,3 +433,41 @@ def test_an_infinite_norm_is_not_clipped_by_an_infinite_bound(values):
     assert torch.isfinite(p[g[0].abs() < 1e30]).all()
     g[0][0] = math.nan
     assert all(math.isnan(float(a)) for a in n(g))
+
+
+def test_bias_corrections_go_by_a_tensors_own_steps():
+    """Tensors whose gradients come late, or now and then, against torch.optim.AdamW: fp32 steps of 0.01, each right to
+    some roundings of a parameter near 1."""
+    torch.manual_seed(9)
+    start = [torch.randn(300, device="cuda") for _ in range(4)]
+    p, q = [a.clone() for a in start], [a.clone().requires_grad_(True) for a in start]
+    opt, ref = optim.AdamW(p, lr=0.01, weight_decay=0.1), torch.optim.AdamW(q, lr=0.01, weight_decay=0.1)
+    for step in range(24):
+        if step == 15:
+            opt = optim.AdamW(p, lr=0.01, weight_decay=0.1, state=opt.state_dict())
+        g = [torch.randn(300, device="cuda") if on else None for on in (True, step >= 12, step % 2, step == 20)]
+        for a, b in zip(q, g):
+            a.grad = b
+        opt.step(g)
+        ref.step()
+    assert opt.steps == 24 and opt.state_dict()["missed"] == [0, 12, 12, 23]
+    assert all(torch.allclose(a, b, rtol=1e-5, atol=1e-6) for a, b in zip(p, q))
+    for bad in ([0, 0], [0, 0, 0, -1]):
+        with pytest.raises(ValueError, match="missed"):
+            optim.AdamW(p, state=opt.state_dict() | {"missed": bad})
+    with pytest.raises(ValueError, match="missed"):
+        optim.AdamW(p, state=opt.state_dict() | {"missed": [0, 0, 0, 25]}).step(g[:3] + [torch.zeros(300, device="cuda")])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_tensor_that_comes_late_steps_as_it_would_alone(bits):
+    torch.manual_seed(10)
+    start = torch.randn(3000, device="cuda")
+    x, y, alone = start.clone(), torch.zeros(50, device="cuda"), start.clone()
+    both, one = optim.AdamW([x, y], state_bits=bits, seed=3), optim.AdamW([alone], state_bits=bits, seed=3)
+    for step in range(9):
+        g = torch.randn(3000, device="cuda") if step > 4 else None
+        both.step([g, torch.randn(50, device="cuda") if step != 7 else None])
+        if g is not None:
+            one.step([g])
+    assert torch.equal(x, alone) and all(torch.equal(a, b) for a, b in zip(both.state_of(0), one.state_of(0)))
