@@ -344,10 +344,11 @@ typedef enum { PP_ACT_NONE = 0, PP_ACT_RELU = 1, PP_ACT_SILU = 2 } pp_act;
  *   mean, rstd DEVICE fp32 [N][G], kept for the backward pass, or NULL;
  *   workspace  DEVICE, 16-byte aligned, pp_group_norm_workspace_size bytes (backward 0).
  * Sums are fp32, joined as means and squared distances, in a fixed order: the same inputs and strides
- * give the same bits.  A NaN or an infinity makes its own group NaN.  Pointers need element alignment
- * only; 16-byte aligned addresses and strides are fastest.  N == 0 or pixels == 0: mean and rstd, of
- * nothing, become NaN, and that is all.  Never synchronises.  Errors: PP_ERR_NULL, _SHAPE (C not a multiple of G, N above 65534, strides), _ALIGN,
- * _DTYPE, _BUFFER (workspace too small, overlap), _ARG (act, eps), _CUDA. */
+ * give the same bits.  A NaN or an infinity makes its own group NaN; the sum of a group's squared
+ * distances from the mean has to be in fp32's range.  Pointers need element alignment only; 16-byte
+ * aligned addresses and strides are fastest.  N == 0 or pixels == 0: mean and rstd, of nothing, become
+ * NaN, and that is all.  Never synchronises.  Errors: PP_ERR_NULL, _SHAPE (C not a multiple of G, N above
+ * 65534, strides), _ALIGN, _DTYPE, _BUFFER (workspace too small, overlap), _ARG (act, eps), _CUDA. */
 int pp_group_norm(const void* x, int64_t x_pixel, int64_t x_sample, int dtype, int N, int64_t pixels, int C, int G,
                   const float* gamma, const float* beta, float eps, int act, void* y, float* mean, float* rstd,
                   void* workspace, size_t workspace_bytes, void* stream);

@@ -23,8 +23,8 @@
 // Measured on a GB300 (a copy moves 6.67 TB/s), inputs in memory, the launches of a call together:
 //     forward   32x256x56x56 fp16    27 us, 3.8 TB/s of what it must move   (resident, 4 x 50 KB a unit)
 //     forward   32x64x224x224 fp32  195 us, 4.2 TB/s; 6.3 TB/s with the second reading   (streamed)
-//     backward  32x512x14x14 fp32    14 us, 2.7 TB/s   (resident, one CTA a unit)
-//     backward  32x128x112x112 fp16  92 us, 3.4 TB/s; 5.6 TB/s with the second reading   (streamed)
+//     backward  32x512x14x14 fp32    13 us, 3.0 TB/s   (resident, one CTA a unit)
+//     backward  32x128x112x112 fp16  91 us, 3.4 TB/s; 5.6 TB/s with the second reading   (streamed)
 // The resident form is bound by what its few CTAs on an SM have in flight while some of them wait for their
 // clusters and by the arithmetic of SiLU (two operations of the special function unit an element, four
 // backward); the streamed one by memory, whose rate falls a little short of a copy's backward.

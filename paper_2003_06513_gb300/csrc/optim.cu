@@ -2,7 +2,7 @@
 //
 // The tensors are cut into chunks of kChunk elements; a table in device memory, built once, says where a
 // chunk's parameters, states and tap masks are: one reading of 64 bytes, 0.2 % of a step's traffic, before the
-// data.  The gradients' addresses change from step to step and travel as kernel arguments, so that a step
+// data.  The norm, which needs no more than masks, has a table of its own, of spans of kSpan elements.  The gradients' addresses change from step to step and travel as kernel arguments, so that a step
 // is one launch or two however many tensors there are (of up to kMaxGrads, and as many for each kMaxGrads
 // beyond).
 //
@@ -794,7 +794,7 @@ struct Listed {
 // the pruned layers below take 5 % less time than with five; eight leave too few registers.
 //
 // Measured on a GB300 (a copy moves 6.67 TB/s), states and parameters in memory:
-//     24 dense layers, 56.6 M elements, fp32 gradients, 8-bit states   143 us, 6.3 TB/s: memory
+//     24 dense layers, 56.6 M elements, fp32 gradients, 8-bit states   145 us, 6.3 TB/s: memory
 //     ResNet-50's 3x3 layers, dense, fp32 gradients and states          50 us, 6.3 TB/s: memory
 //     VGG-16's, a kernel in 0.3 kept, fp32 gradients and states         49 us: the kept elements' 1.2 TB/s are
 //         4.9 TB/s of memory traffic, since what is read is whole 64-byte pieces with any kept element in them
