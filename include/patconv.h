@@ -27,7 +27,8 @@
  *     before that kernel has completed, so stream order holds as for a plain launch.  The
  *     environment variable PATCONV_PDL=0 (read once) makes every launch a plain one.
  *
- * The training side (pp_group_norm, pp_tensors_*, pp_grad_norm, pp_adamw_step) serves the masked
+ * The training side (pp_group_norm, pp_block_norm, pp_top_logits, pp_distill, pp_tensors_*, pp_grad_norm,
+ * pp_adamw_step) serves the masked
  * retraining of a pruned network between its convolutions and after its backward pass; its
  * activations are channels last, as training libraries keep them for convolutions.  The first kernel
  * of each of its calls is a plain launch; further kernels of a group norm's call start while the one
@@ -375,6 +376,102 @@ int pp_group_norm_workspace_size(int dtype, int N, int64_t pixels, int C, int G,
  * min(n_info, 8) values.  Host-only.
  * Errors: PP_ERR_NULL, _SHAPE (nothing to do among them), _DTYPE, _ARG. */
 int pp_group_norm_plan(int dtype, int N, int64_t pixels, int C, int G, int backward, int align, int64_t* info, int n_info);
+
+/* ------------------------------------------------------------------------------------------------
+ * Block norm, channels last: how a residual block joins its stream, and what the next block reads of it (the
+ * paper's ResNets have residual blocks; their norms are left open there). */
+
+typedef enum {
+    PP_NORM_NONE = 0,
+    PP_NORM_RMS = 1,          /* v / sqrt(mean of v^2 + eps)                                     */
+    PP_NORM_LAYER = 2         /* (v - mean) / sqrt(mean of (v - mean)^2 + eps)                   */
+} pp_norm;
+
+/* For every pixel, means over its C channels:
+ *     u = post_weight norm_post(block) + post_bias,   h = x + scale gate_n u,
+ *     y = act(weight norm_pre(h) + bias),
+ * the second norm being of h as it is stored.
+ *   x          DEVICE [N][pixels][C] of `x_dtype`, the residual stream: channels adjacent, pixels x_pixel >= C elements
+ *              apart, samples x_sample elements (0: the same sample again);
+ *   block      DEVICE [N][pixels][C] of `dtype` with strides of its own, the block's output; NULL: there is none, h is x
+ *              and is not written, and post, scale and gate must be absent;
+ *   x_dtype    is `dtype`, or PP_F32;
+ *   post, pre  pp_norm: the norms of the block's output and of the stream; with PP_NORM_NONE for pre there is no y, and
+ *              act must be PP_ACT_NONE;
+ *   post_weight, post_bias, weight, bias, scale    DEVICE fp32 [C], gate DEVICE fp32 [N][C]; each may be NULL (ones, for
+ *              the biases zeros), and a norm that is not there has none;
+ *   h          DEVICE, dense, of `x_dtype`; may be x itself where that is dense, else must not overlap;
+ *   y          DEVICE, dense, of `dtype`; may be block itself where that is dense, else must not overlap.
+ * Sums are fp32, in a fixed order; C is at most 4096.  Pointers need element alignment only; vectors of eight channels
+ * on 16-byte boundaries are fastest.  Never synchronises.  Errors: PP_ERR_NULL, _SHAPE (sizes, strides), _ALIGN,
+ * _DTYPE, _BUFFER (overlap), _ARG (kinds, eps, a parameter of a norm that is not there), _CUDA. */
+int pp_block_norm(const void* x, int64_t x_pixel, int64_t x_sample, int x_dtype, const void* block, int64_t block_pixel,
+                  int64_t block_sample, int dtype, int N, int64_t pixels, int C, int post, const float* post_weight,
+                  const float* post_bias, const float* scale, const float* gate, int pre, const float* weight,
+                  const float* bias, int act, float eps, void* h, void* y, void* stream);
+
+/* The gradients of pp_block_norm from those of h and of y (dh of x_dtype, dy of dtype, strides of their own; NULL: zero):
+ * dx of x_dtype and dblock of dtype, dense (dx may be dh itself and dblock dy, where those are dense), and of the
+ * parameters, fp32, [N][C] of the gate and [C] of the others; any of these may be NULL.  h is the forward pass's, with
+ * strides of its own (not read without dy), the parameters are as they were there.  Where x is the stream itself its
+ * gradient is dx alone: dh goes into it.  At z = 0 the ReLU's slope is 0, and on which side of it a z lies is taken in
+ * 64 bits where fp32 cannot tell.  The sums are fp32, in a fixed order.
+ *   workspace  DEVICE, 16-byte aligned, pp_block_norm_workspace_size bytes.
+ * N == 0 or pixels == 0: the parameters' gradients become zero.  Otherwise as pp_block_norm. */
+int pp_block_norm_backward(const void* dh, int64_t dh_pixel, int64_t dh_sample, const void* dy, int64_t dy_pixel,
+                           int64_t dy_sample, const void* h, int64_t h_pixel, int64_t h_sample, int x_dtype,
+                           const void* block, int64_t block_pixel, int64_t block_sample, int dtype, int N, int64_t pixels,
+                           int C, int post, const float* post_weight, const float* post_bias, const float* scale,
+                           const float* gate, int pre, const float* weight, const float* bias, int act, float eps, void* dx,
+                           void* dblock, float* dpost_weight, float* dpost_bias, float* dscale, float* dgate, float* dweight,
+                           float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of pp_block_norm_backward.  Host-only. */
+int pp_block_norm_workspace_size(int N, int64_t pixels, int C, size_t* bytes);
+
+/* ------------------------------------------------------------------------------------------------
+ * Distillation: the pruned net is trained on the largest logits of the dense net that it came from, beside the labels
+ * (the paper prunes a layer towards the dense net's outputs; what retraining is trained on is left open there). */
+
+#define PP_MOST_KEPT 256      /* logits kept of a row, at most      */
+#define PP_MOST_CLASSES 1048576
+
+/* Of each row of logits (DEVICE [rows][classes], rows `stride` elements apart, of dtype PP_F32, PP_F16 or PP_BF16) the
+ * k <= PP_MOST_KEPT largest, in order, equal ones by their places (-0 and 0 are equal, NaN is above everything):
+ *   values     DEVICE [rows][k] of `dtype`;   indices  DEVICE [rows][k];
+ *   rest       DEVICE fp32 [rows]: the log-sum-exp of the other logits over `temperature`, -infinity where there are none
+ *              (k == classes) or all are -infinity; NaN where one of them is.
+ * 0.001 <= temperature <= 1000; logits over the temperature have to be in fp32's range.  Pointers need element alignment.
+ * The same inputs and strides give the same bits.  Outputs overlap nothing.  Never synchronises.
+ * Errors: PP_ERR_NULL, _SHAPE (classes above PP_MOST_CLASSES, k, stride), _ALIGN, _DTYPE, _BUFFER, _ARG, _CUDA. */
+int pp_top_logits(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t classes, int k, double temperature,
+                  void* values, int* indices, float* rest, void* stream);
+
+/* Loss of each row: with s its logits (as above), t_k the teacher's kept logits of classes i_k and T the temperature,
+ *     (1 - alpha) (log-sum-exp of s - s_label) + alpha T^2 sum p (log p - log q),
+ * p the softmax of t_k / T, q the student's probabilities at T.  With `rest` the classes that are not kept are one more
+ * class, in p with the logit rest, in q with the sum of their probabilities; without, p is the kept logits' alone.
+ *   values     DEVICE [rows][kept] of value_type (pp_dtype), indices DEVICE [rows][kept]: an index outside 0 ..
+ *              classes - 1 is an empty place; a class that is given twice has both masses; a logit of -infinity has none;
+ *   rest       DEVICE fp32 [rows], or NULL;
+ *   labels     DEVICE [rows], or NULL (then there is no label's part): outside 0 .. classes - 1 a row has none;
+ *   loss       DEVICE fp32 [rows];
+ *   stats      DEVICE fp32 [rows][5], for the backward pass: the largest logit m, the sum of exp(s - m) (0 without
+ *              labels), the sum of exp((s - m) / T), and, of the classes that are not kept (without `rest`: of all), the
+ *              largest logit and the sum of exp((s - it) / T).
+ * A row that has neither a label nor a kept logit or rest above -infinity (a padded row) is not read: its loss and stats
+ * are 0.  NaN and +infinity in a row that counts give NaN.  0 <= alpha <= 1.  Otherwise as pp_top_logits. */
+int pp_distill(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t classes, const void* values,
+               int value_type, const int* indices, int kept, const float* rest, const int64_t* labels, double temperature,
+               double alpha, float* loss, float* stats, void* stream);
+
+/* The gradient of pp_distill by the logits, DEVICE dense [rows][classes] of `dtype` (may be the logits themselves where those
+ * are dense), from that of the losses (DEVICE fp32, `dloss_stride` elements apart, 0: one for all rows) and the forward
+ * pass's stats; the other arguments as they were there.  Where dloss is 0, or the row has nothing to learn from, it is 0.
+ * Errors as pp_distill. */
+int pp_distill_backward(const float* dloss, int64_t dloss_stride, const void* logits, int64_t stride, int dtype, int64_t rows,
+                        int64_t classes, const float* stats, const void* values, int value_type, const int* indices, int kept,
+                        const float* rest, const int64_t* labels, double temperature, double alpha, void* dlogits, void* stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Many tensors at once: the gradients' norm and AdamW steps of masked retraining (the paper's

@@ -63,6 +63,22 @@ SIGNATURES = {
                                               ctypes.POINTER(_c_size_t)]),
     "pp_group_norm_plan": (_c_int, [_c_int, _c_int, _c_i64, _c_int, _c_int, _c_int, _c_int,
                                     ctypes.POINTER(_c_i64), _c_int]),
+    "pp_block_norm": (_c_int, [_c_void_p, _c_i64, _c_i64, _c_int, _c_void_p, _c_i64, _c_i64, _c_int, _c_int, _c_i64, _c_int,
+                               _c_int, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_int, _c_void_p, _c_void_p, _c_int,
+                               _c_float, _c_void_p, _c_void_p, _c_void_p]),
+    "pp_block_norm_backward": (_c_int, [_c_void_p, _c_i64, _c_i64, _c_void_p, _c_i64, _c_i64, _c_void_p, _c_i64, _c_i64,
+                                        _c_int, _c_void_p, _c_i64, _c_i64, _c_int, _c_int, _c_i64, _c_int, _c_int,
+                                        _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_int, _c_void_p, _c_void_p, _c_int,
+                                        _c_float, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+                                        _c_void_p, _c_void_p, _c_void_p, _c_size_t, _c_void_p]),
+    "pp_block_norm_workspace_size": (_c_int, [_c_int, _c_i64, _c_int, ctypes.POINTER(_c_size_t)]),
+    "pp_top_logits": (_c_int, [_c_void_p, _c_i64, _c_int, _c_i64, _c_i64, _c_int, _c_double, _c_void_p, _c_void_p,
+                               _c_void_p, _c_void_p]),
+    "pp_distill": (_c_int, [_c_void_p, _c_i64, _c_int, _c_i64, _c_i64, _c_void_p, _c_int, _c_void_p, _c_int, _c_void_p,
+                            _c_void_p, _c_double, _c_double, _c_void_p, _c_void_p, _c_void_p]),
+    "pp_distill_backward": (_c_int, [_c_void_p, _c_i64, _c_void_p, _c_i64, _c_int, _c_i64, _c_i64, _c_void_p, _c_void_p,
+                                     _c_int, _c_void_p, _c_int, _c_void_p, _c_void_p, _c_double, _c_double, _c_void_p,
+                                     _c_void_p]),
     "pp_tensors_create": (_c_int, [_c_int, ctypes.POINTER(_c_i64), ctypes.POINTER(_c_int),
                                    ctypes.POINTER(_c_void_p), ctypes.POINTER(_c_void_p),
                                    ctypes.POINTER(_c_void_p), _c_int, ctypes.POINTER(_c_float),

@@ -3,7 +3,7 @@
 // ctypes the same took 25 to 40 us a call (fifty gradients to look at, three outputs to make), several
 // times what the small calls take on the GPU; here it is 5 to 8 us.
 //
-// The functions take positional arguments from norm.py and optim.py, which hold the defaults and the
+// The functions take positional arguments from norm.py, distill.py and optim.py, which hold the defaults and the
 // documentation, and return the entry point's status where that is not 0; arguments that are no fit raise
 // ValueError.  Tensors are only looked at and allocated: no operator of torch runs here.
 #include <ATen/ATen.h>
@@ -220,6 +220,231 @@ PyObject* layout(PyObject* const* a, Py_ssize_t n_args) {
     Layout l;
     if (!layout_of(t, l)) Py_RETURN_NONE;
     return Py_BuildValue("(LL)", (long long)l.pixel, (long long)l.sample);
+}
+
+// ---------------------------------------------------------------------------------- block norm
+
+// an input like x in shape and device, of a type
+Layout alike(const at::Tensor& t, const at::Tensor& x, at::ScalarType type, const char* what) {
+    const Layout l = input(t, what);
+    if (t.sizes() != x.sizes() || t.device() != x.device() || t.scalar_type() != type)
+        refuse(std::string(what) + " must have the stream's shape and device, and be " + c10::toString(type));
+    return l;
+}
+// a dense channels-last result like x, of a type: the one that is given, or a new one
+at::Tensor result(PyObject* o, const at::Tensor& x, at::ScalarType type, const char* what) {
+    const at::Tensor* out = maybe(o, what);
+    if (!out) return at::empty(x.sizes(), x.options().dtype(type).requires_grad(false), at::MemoryFormat::ChannelsLast);
+    if (out->sizes() != x.sizes() || out->scalar_type() != type || out->device() != x.device() ||
+        !out->is_contiguous(at::MemoryFormat::ChannelsLast))
+        refuse(std::string(what) + " must be a dense channels-last tensor of the stream's shape and device, " + c10::toString(type));
+    return *out;
+}
+struct Parameters {
+    int post, pre, act;
+    const float *post_weight, *post_bias, *scale, *gate, *weight, *bias;
+    float eps;
+    // post, post_weight, post_bias, scale, gate, pre, weight, bias, act, eps
+    Parameters(PyObject* const* a, const at::Tensor& x) {
+        const int64_t n = x.size(0), c = x.size(1);
+        post = (int)integer(a[0]);
+        post_weight = values(a[1], c, x, "post_weight");
+        post_bias = values(a[2], c, x, "post_bias");
+        scale = values(a[3], c, x, "scale");
+        gate = values(a[4], n * c, x, "gate");
+        if (gate && (tensor(a[4], "gate").dim() != 2 || tensor(a[4], "gate").size(1) != c)) refuse("gate must be [N, C]");
+        pre = (int)integer(a[5]);
+        weight = values(a[6], c, x, "weight");
+        bias = values(a[7], c, x, "bias");
+        act = (int)integer(a[8]);
+        eps = (float)real(a[9]);
+    }
+};
+
+// x, block, then Parameters' ten, out_h, out_y, stream -> (h, y or None)
+PyObject* block_norm(PyObject* const* a, Py_ssize_t n_args) {
+    want(n_args, 15);
+    const at::Tensor& x = tensor(a[0], "x");
+    const Layout l = input(x, "x");
+    const at::Tensor* b = maybe(a[1], "block");
+    if (b && x.scalar_type() != b->scalar_type() && x.scalar_type() != at::kFloat) refuse("x must have the block's type, or be float32");
+    const at::ScalarType type = b ? b->scalar_type() : x.scalar_type();
+    const Layout lb = b ? alike(*b, x, type, "block") : Layout();
+    if (too_large(x)) return PyLong_FromLong(PP_ERR_SHAPE);
+    const Parameters p(a + 2, x);
+    const Place at(x.device(), a[14]);
+    const at::Tensor h = b ? result(a[12], x, x.scalar_type(), "h") : x;
+    const bool normed = p.pre != PP_NORM_NONE;
+    const at::Tensor y = normed ? result(a[13], x, type, "y") : at::Tensor();
+    const int e = pp_block_norm(x.const_data_ptr(), l.pixel, l.sample, dtype_of(x), b ? b->const_data_ptr() : nullptr, lb.pixel, lb.sample,
+                                b ? dtype_of(*b) : dtype_of(x), (int)x.size(0), x.size(2) * x.size(3), (int)x.size(1), p.post,
+                                p.post_weight, p.post_bias, p.scale, p.gate, p.pre, p.weight, p.bias, p.act, p.eps,
+                                b ? h.data_ptr() : nullptr, normed ? y.data_ptr() : nullptr, at.stream);
+    if (e) return PyLong_FromLong(e);
+    if (b && a[12] != Py_None) changed(h);
+    if (normed && a[13] != Py_None) changed(y);
+    PyObject* t = PyTuple_New(2);
+    if (!t) throw Raised();
+    if (b) {
+        PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(h));
+    } else {
+        Py_INCREF(a[0]);
+        PyTuple_SET_ITEM(t, 0, a[0]);
+    }
+    if (normed) {
+        PyTuple_SET_ITEM(t, 1, THPVariable_Wrap(y));
+    } else {
+        Py_INCREF(Py_None);
+        PyTuple_SET_ITEM(t, 1, Py_None);
+    }
+    return t;
+}
+
+// dh, dy, h, block, then Parameters' ten, stream, workspace -> (dx, dblock, dpost_weight, dpost_bias, dscale, dgate, dweight, dbias),
+// None for what is not there
+PyObject* block_norm_backward(PyObject* const* a, Py_ssize_t n_args) {
+    want(n_args, 16);
+    const at::Tensor& h = tensor(a[2], "h");
+    const Layout l = input(h, "h");
+    const at::Tensor *dh = maybe(a[0], "dh"), *dy = maybe(a[1], "dy"), *b = maybe(a[3], "block");
+    if (b && h.scalar_type() != b->scalar_type() && h.scalar_type() != at::kFloat) refuse("h must have the block's type, or be float32");
+    const at::ScalarType type = b ? b->scalar_type() : h.scalar_type();
+    const Layout lb = b ? alike(*b, h, type, "block") : Layout(), ld = dh ? alike(*dh, h, h.scalar_type(), "dh") : Layout(),
+                 ly = dy ? alike(*dy, h, type, "dy") : Layout();
+    if (too_large(h)) return PyLong_FromLong(PP_ERR_SHAPE);
+    const Parameters p(a + 4, h);
+    const int n = (int)h.size(0), c = (int)h.size(1), dtype = b ? dtype_of(*b) : dtype_of(h);
+    const int64_t pixels = h.size(2) * h.size(3);
+    const Place at(h.device(), a[14]);
+    at::Tensor grads[8];                        // in the order of the result
+    grads[0] = result(Py_None, h, h.scalar_type(), "dx");
+    if (b) grads[1] = result(Py_None, h, type, "dblock");
+    const int of[6] = {5, 6, 7, 8, 10, 11};     // the parameters among the arguments
+    float* sums[6];
+    for (int i = 0; i < 6; ++i) {
+        const bool given = a[of[i]] != Py_None;
+        if (given) grads[2 + i] = i == 3 ? floats({n, c}, h) : floats({c}, h);
+        sums[i] = given ? grads[2 + i].data_ptr<float>() : nullptr;
+    }
+    size_t bytes = 0;
+    void* space = nullptr;
+    at::Tensor held;
+    if (const at::Tensor* w = maybe(a[15], "workspace")) {
+        if (!w->is_contiguous() || w->device() != h.device()) refuse("workspace must be a contiguous CUDA tensor on the stream's device");
+        space = w->data_ptr();
+        bytes = w->nbytes();
+    } else if (pp_block_norm_workspace_size(n, pixels, c, &bytes) == PP_OK && bytes) {
+        held = at::empty({(int64_t)bytes}, h.options().dtype(at::kByte).requires_grad(false));
+        space = held.data_ptr();
+    }
+    const int e = pp_block_norm_backward(
+        dh ? dh->const_data_ptr() : nullptr, ld.pixel, ld.sample, dy ? dy->const_data_ptr() : nullptr, ly.pixel, ly.sample, h.const_data_ptr(),
+        l.pixel, l.sample, dtype_of(h), b ? b->const_data_ptr() : nullptr, lb.pixel, lb.sample, dtype, n, pixels, c, p.post,
+        p.post_weight, p.post_bias, p.scale, p.gate, p.pre, p.weight, p.bias, p.act, p.eps, grads[0].data_ptr(),
+        b ? grads[1].data_ptr() : nullptr, sums[0], sums[1], sums[2], sums[3], sums[4], sums[5], space, bytes, at.stream);
+    if (e) return PyLong_FromLong(e);
+    PyObject* t = PyTuple_New(8);
+    if (!t) throw Raised();
+    for (int i = 0; i < 8; ++i) {
+        PyObject* o = grads[i].defined() ? THPVariable_Wrap(grads[i]) : Py_None;
+        if (o == Py_None) Py_INCREF(o);
+        PyTuple_SET_ITEM(t, i, o);
+    }
+    return t;
+}
+
+// ---------------------------------------------------------------------------------- distillation
+
+int64_t row_stride(const at::Tensor& t, const char* what) {
+    if (!t.is_cuda() || t.layout() != at::kStrided || dtype_of(t) < 0 || t.dim() != 2)
+        refuse(std::string(what) + " must be a 2-d CUDA float32, float16 or bfloat16 tensor");
+    if ((t.size(1) > 1 && t.stride(1) != 1) || (t.size(0) > 1 && t.stride(0) < t.size(1)))
+        refuse(std::string(what) + " must have its classes adjacent, and rows that do not overlap");
+    return t.size(0) > 1 ? t.stride(0) : t.size(1);
+}
+
+// logits, k, temperature, stream -> (values, indices, rest)
+PyObject* top_logits(PyObject* const* a, Py_ssize_t n_args) {
+    want(n_args, 4);
+    const at::Tensor& s = tensor(a[0], "logits");
+    const int64_t stride = row_stride(s, "logits"), k = integer(a[1]);
+    const double temperature = real(a[2]);
+    if (k < 1 || k > PP_MOST_KEPT || k > s.size(1))
+        refuse("k must be 1 to " + std::to_string(PP_MOST_KEPT) + " and no more than the classes");
+    const Place at(s.device(), a[3]);
+    const at::Tensor values = at::empty({s.size(0), k}, s.options().requires_grad(false)), rest = floats({s.size(0)}, s);
+    const at::Tensor indices = at::empty({s.size(0), k}, s.options().dtype(at::kInt).requires_grad(false));
+    const int e = pp_top_logits(s.const_data_ptr(), stride, dtype_of(s), s.size(0), s.size(1), (int)k, temperature, values.data_ptr(),
+                                indices.data_ptr<int>(), rest.data_ptr<float>(), at.stream);
+    return e ? PyLong_FromLong(e) : triple(values, indices, rest);
+}
+
+struct Teacher {
+    const at::Tensor *values, *indices, *rest, *labels;
+    double temperature, alpha;
+    // values, indices, rest, labels, temperature, alpha
+    Teacher(PyObject* const* a, const at::Tensor& s) {
+        values = &tensor(a[0], "values"), indices = &tensor(a[1], "indices"), rest = maybe(a[2], "rest"), labels = maybe(a[3], "labels");
+        const int64_t n = s.size(0);
+        if (values->dim() != 2 || values->size(0) != n || dtype_of(*values) < 0 || !values->is_contiguous() || values->device() != s.device())
+            refuse("values must be a contiguous [rows, kept] float32, float16 or bfloat16 tensor on the logits' device");
+        if (indices->sizes() != values->sizes() || indices->scalar_type() != at::kInt || !indices->is_contiguous() || indices->device() != s.device())
+            refuse("indices must be a contiguous int32 tensor of values' shape on the logits' device");
+        if (rest && (rest->dim() != 1 || rest->size(0) != n || rest->scalar_type() != at::kFloat || !rest->is_contiguous() || rest->device() != s.device()))
+            refuse("rest must be a contiguous float32 tensor [rows] on the logits' device");
+        if (labels && (labels->dim() != 1 || labels->size(0) != n || labels->scalar_type() != at::kLong || !labels->is_contiguous() || labels->device() != s.device()))
+            refuse("labels must be a contiguous int64 tensor [rows] on the logits' device");
+        if (values->size(1) < 1 || values->size(1) > PP_MOST_KEPT || values->size(1) > s.size(1))
+            refuse("kept logits must be 1 to " + std::to_string(PP_MOST_KEPT) + " a row and no more than the classes");
+        temperature = real(a[4]);
+        alpha = real(a[5]);
+    }
+    int kept() const { return (int)values->size(1); }
+    const float* rest_ptr() const { return rest ? rest->const_data_ptr<float>() : nullptr; }
+    const int64_t* labels_ptr() const { return labels ? labels->const_data_ptr<int64_t>() : nullptr; }
+};
+
+// logits, then Teacher's six, stream -> (loss, stats)
+PyObject* distill(PyObject* const* a, Py_ssize_t n_args) {
+    want(n_args, 8);
+    const at::Tensor& s = tensor(a[0], "logits");
+    const int64_t stride = row_stride(s, "logits");
+    const Teacher t(a + 1, s);
+    const Place at(s.device(), a[7]);
+    const at::Tensor loss = floats({s.size(0)}, s), stats = floats({s.size(0), 5}, s);
+    const int e = pp_distill(s.const_data_ptr(), stride, dtype_of(s), s.size(0), s.size(1), t.values->const_data_ptr(), dtype_of(*t.values),
+                             t.indices->const_data_ptr<int>(), t.kept(), t.rest_ptr(), t.labels_ptr(), t.temperature, t.alpha,
+                             loss.data_ptr<float>(), stats.data_ptr<float>(), at.stream);
+    if (e) return PyLong_FromLong(e);
+    PyObject* r = PyTuple_New(2);
+    if (!r) throw Raised();
+    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(loss));
+    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(stats));
+    return r;
+}
+
+// dloss, logits, stats, then Teacher's six, out, stream -> dlogits
+PyObject* distill_backward(PyObject* const* a, Py_ssize_t n_args) {
+    want(n_args, 11);
+    const at::Tensor &d = tensor(a[0], "dloss"), &s = tensor(a[1], "logits"), &stats = tensor(a[2], "stats");
+    const int64_t stride = row_stride(s, "logits"), n = s.size(0);
+    if (d.dim() != 1 || d.size(0) != n || d.scalar_type() != at::kFloat || d.device() != s.device())
+        refuse("dloss must be a float32 tensor [rows] on the logits' device");
+    if (stats.dim() != 2 || stats.size(0) != n || stats.size(1) != 5 || stats.scalar_type() != at::kFloat || !stats.is_contiguous() || stats.device() != s.device())
+        refuse("stats must be the contiguous float32 [rows, 5] of the forward pass");
+    const Teacher t(a + 3, s);
+    const Place at(s.device(), a[10]);
+    const at::Tensor* given = maybe(a[9], "out");
+    if (given && (given->sizes() != s.sizes() || given->scalar_type() != s.scalar_type() || given->device() != s.device() || !given->is_contiguous()))
+        refuse("out must be a contiguous tensor of the logits' shape, type and device");
+    const at::Tensor out = given ? *given : at::empty(s.sizes(), s.options().requires_grad(false));
+    const int e = pp_distill_backward(d.const_data_ptr<float>(), n > 1 ? d.stride(0) : 0, s.const_data_ptr(), stride, dtype_of(s), n, s.size(1),
+                                      stats.const_data_ptr<float>(), t.values->const_data_ptr(), dtype_of(*t.values),
+                                      t.indices->const_data_ptr<int>(), t.kept(), t.rest_ptr(), t.labels_ptr(), t.temperature, t.alpha,
+                                      out.data_ptr(), at.stream);
+    if (e) return PyLong_FromLong(e);
+    if (given) changed(out);
+    return THPVariable_Wrap(out);
 }
 
 // ---------------------------------------------------------------------------------- many tensors
@@ -445,6 +670,11 @@ constexpr PyCFunction fast() {
 
 PyMethodDef methods[] = {{"group_norm", fast<group_norm>(), METH_FASTCALL, nullptr},
                          {"group_norm_backward", fast<group_norm_backward>(), METH_FASTCALL, nullptr},
+                         {"block_norm", fast<block_norm>(), METH_FASTCALL, nullptr},
+                         {"block_norm_backward", fast<block_norm_backward>(), METH_FASTCALL, nullptr},
+                         {"top_logits", fast<top_logits>(), METH_FASTCALL, nullptr},
+                         {"distill", fast<distill>(), METH_FASTCALL, nullptr},
+                         {"distill_backward", fast<distill_backward>(), METH_FASTCALL, nullptr},
                          {"layout", fast<layout>(), METH_FASTCALL, nullptr},
                          {"tensors", fast<tensors>(), METH_FASTCALL, nullptr},
                          {"grad_norm", fast<grad_norm>(), METH_FASTCALL, nullptr},

@@ -1,0 +1,387 @@
+// Distillation from a teacher's top logits: loss of each row (this file) and its gradient (distill_back.cu).
+//
+// Of a row of C logits s the teacher kept K classes i_k with logits t_k and, if given, the log-sum-exp over T of its
+// other logits, `rest`.  With p the softmax of (t_k / T, rest) and q the student's probabilities at T of the same
+// classes -- q_k = exp((s_{i_k} - m) / T) / Z_T, and of the others together q_0 = the sum over them --
+//     loss = (1 - alpha) (log Z_1 + m - s_label) + alpha T^2 sum p (log p - log q),
+// m the largest logit, Z_1 and Z_T the sums of exp(s - m) and exp((s - m) / T).
+//
+// q_0 is summed over the classes that are not kept, as 1 - sum q_k would lose it where the kept classes have nearly
+// all: a bit a class in shared memory says which are, read beside each 16-byte vector of logits.  A thread keeps a
+// running maximum and the sums below it, so that the row is read once; the kept logits are fetched by the threads
+// that hold the teacher's and join at the end.
+//
+// What bounds it is memory: a row is read, next to nothing is written.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "rows.cuh"
+
+namespace patconv {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kWide = 256;            // threads of a CTA that has a row, or a part of one
+constexpr int kRowsOfCta = 4;         // rows of a CTA whose warps have one each
+constexpr int kMostOfWarp = 2048;     // classes of a warp's row at most
+
+// what a thread sums of the classes it sees: the largest x, and the sums of 2^((x - m) c) relative to it
+template <bool TWO>
+struct Running {
+    float m = kNone, ref = 0;         // and m, or 0 before there is one
+    float2 z1 = {0, 0}, zt = {0, 0};
+    __device__ __forceinline__ void below(float top, float c1, float ct) {
+        if (!(top > m)) return;
+        if (m != kNone) {
+            zt = mul(zt, both(power(m, top, ct)));
+            if (TWO) z1 = mul(z1, both(power(m, top, c1)));
+        }
+        m = ref = top;
+    }
+    __device__ __forceinline__ void add_pair(float2 x, float2 c1, float2 ct) {
+        const float2 d = add(x, both(-ref)), e = mul(d, ct);
+        zt = add(zt, make_float2(approx_exp2(e.x), approx_exp2(e.y)));
+        if (TWO) {
+            const float2 f = mul(d, c1);
+            z1 = add(z1, make_float2(approx_exp2(f.x), approx_exp2(f.y)));
+        }
+    }
+};
+
+template <typename T, bool REST, bool TWO, int N>
+__global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(DistillArgs a) {
+    constexpr int W = 16 / sizeof(T), U = 4;
+    extern __shared__ uint4 dynamic[];
+    __shared__ float scratch[N == 32 ? 1 : 2 * (N / 32) * 8];
+    __shared__ float parts[16][3];
+    __shared__ int kept_of[N == 32 ? kRowsOfCta : 1][N == 32 ? 32 : kMostKept];
+    const int slot = N == 32 ? threadIdx.x / 32 : 0;
+    const int part = N == 32 ? 0 : blockIdx.x % a.parts;
+    const int row = N == 32 ? blockIdx.x * kRowsOfCta + slot : blockIdx.x / a.parts;
+    if (row >= a.rows) return;
+    Group<N> g(scratch);
+    const T* s = static_cast<const T*>(a.s) + row * a.stride;
+    const Row<T, W> r(s, a.classes);
+    // this group's vectors
+    const int each = (r.vectors() + a.parts - 1) / a.parts, first = part * each, last = min(r.vectors(), first + each);
+    unsigned* bits = reinterpret_cast<unsigned*>(dynamic) + (N == 32 ? slot * ((kMostOfWarp + 2 * W) / 32 + 1) : 0);
+    int* kept = kept_of[slot];
+
+    // the teacher's entry of this thread
+    const bool mine = g.lane < a.kept;
+    int at = -1;
+    float u = kNone, x = kNone;
+    if (mine) {
+        const int64_t j = (int64_t)row * a.kept + g.lane;
+        at = a.indices[j];
+        if (at >= 0 && at < a.classes) {
+            u = value_at(a.values, a.value_type, j) * a.inv_t;
+            x = widen(s[at]);
+        } else {
+            at = -1;
+        }
+        kept[g.lane] = at;
+    }
+    const float rest = REST ? a.rest[row] : kNone;
+    int64_t label = a.labels ? a.labels[row] : -1;
+    if (label >= a.classes) label = -1;
+    if (REST)
+        for (int w = g.lane; w < (max(0, last - first) * W + 31) / 32; w += N) bits[w] = 0;
+    const bool taught = g.any((at >= 0 && u != kNone) || (REST && rest != kNone));
+    if (!taught && label < 0) {                       // uniform over the row's CTAs: nothing to learn from this row
+        if (part == 0 && g.lane < 5) {
+            a.stats[(int64_t)row * 5 + g.lane] = 0;
+            if (g.lane == 0) a.loss[row] = 0;
+        }
+        return;
+    }
+    bool once = at >= 0;                              // of places that are given twice the first one
+    if (REST) {
+        if constexpr (N == 32) g.sync();
+        if (once) {
+            for (int j = 0; j < g.lane; ++j) once = once && kept[j] != at;
+            const int place = at + r.pad - first * W;
+            if (place >= 0 && place < (last - first) * W) atomicOr(&bits[place / 32], 1u << (place % 32));
+        }
+        g.sync();
+    }
+
+    if constexpr (N > 32)                             // the first CTA's memory is written by the others, once it has begun
+        if (a.parts > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+
+    Running<TWO> sum;
+    const float2 c1 = both(a.c1), ct = both(a.ct);
+    const unsigned char* marks = reinterpret_cast<const unsigned char*>(bits);
+    const auto mark = [&](int v) -> unsigned {        // the bits of vector v's classes
+        if constexpr (!REST) return 0;
+        const int k = v - first;
+        return W == 8 ? marks[k] : (marks[k / 2] >> (k % 2 * 4)) & 15u;
+    };
+    const auto take = [&](const auto& batch, const unsigned* m) {
+        constexpr int K = std::extent<std::remove_reference_t<decltype(batch)>>::value;
+        float2 f[K * W / 2];
+        float top = kNone;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) f[k * W / 2 + i] = pair(batch[k], i);
+            if (REST && m[k])
+#pragma unroll
+                for (int i = 0; i < W / 2; ++i) {
+                    if (m[k] >> (2 * i) & 1) f[k * W / 2 + i].x = kNone;
+                    if (m[k] >> (2 * i + 1) & 1) f[k * W / 2 + i].y = kNone;
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < K * W / 2; ++i) top = fmaxf(top, fmaxf(f[i].x, f[i].y));
+        sum.below(top, a.c1, a.ct);
+#pragma unroll
+        for (int i = 0; i < K * W / 2; ++i) sum.add_pair(f[i], c1, ct);
+    };
+    int from = first, to = last;
+    // the ends of a row that are no whole vectors
+    for (int end = 0; end < 2; ++end) {
+        const int v = end ? last - 1 : first;
+        if (last <= first || r.whole(v) || (end && v == first)) continue;
+        if (end)
+            --to;
+        else
+            ++from;
+        if (g.lane == (end ? N - 1 : 0)) {
+            const unsigned m = mark(v);
+            for (int i = 0; i < W; ++i) {
+                const int place = v * W + i;
+                if (place < r.pad || place >= r.end || (m >> i & 1)) continue;
+                const float y = widen(r.base[place]);
+                sum.below(y, a.c1, a.ct);
+                sum.zt.x += power(y, sum.ref, a.ct);
+                if (TWO) sum.z1.x += power(y, sum.ref, a.c1);
+            }
+        }
+    }
+    int v = from + g.lane;
+    for (; v + (U - 1) * N < to; v += U * N) {
+        Vec<T, W> b[U];
+        unsigned m[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) b[k] = r.at(v + k * N);
+#pragma unroll
+        for (int k = 0; k < U; ++k) m[k] = mark(v + k * N);
+        take(b, m);
+    }
+    for (; v < to; v += N) {
+        const Vec<T, W> b[1] = {r.at(v)};
+        const unsigned m[1] = {mark(v)};
+        take(b, m);
+    }
+
+    // the group's maxima: of the classes seen, of the kept ones, of the teacher's; then the sums below them
+    const float z1 = sum.z1.x + sum.z1.y, zt = sum.zt.x + sum.zt.y;
+    float top[3] = {sum.m, at >= 0 ? x : kNone, fmaxf(u, rest)};
+    g.max(top);
+    const float mu = reference(top[2]), mx = reference(top[1]);
+    const float e = at >= 0 ? power(u, mu, a.c1) : 0.0f;
+    float total[6] = {zt == 0.0f ? 0.0f : zt * factor(sum.m, top[0], a.ct), !TWO || z1 == 0.0f ? 0.0f : z1 * factor(sum.m, top[0], a.c1), 0, 0, e, 0};
+    if (REST && once) {
+        total[2] = power(x, mx, a.ct);
+        if (TWO) total[3] = power(x, mx, a.c1);
+    }
+    if (e != 0.0f) total[5] = e * ((u - mu) - (x - mx) * a.inv_t);
+    g.sum(total);
+    float m = top[0], sum_t = total[0], sum_1 = total[1];
+    if constexpr (N > 32) {
+        if (a.parts > 1) {                            // the parts' sums, in the first CTA of the cluster
+            cg::cluster_group cluster = cg::this_cluster();
+            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+            if (g.lane == 0) {
+                float* to0 = cluster.map_shared_rank(&parts[part][0], 0);
+                to0[0] = m, to0[1] = sum_t, to0[2] = sum_1;
+            }
+            cluster.sync();
+            if (part) return;
+            m = kNone;
+            for (int i = 0; i < a.parts; ++i) m = fmaxf(m, parts[i][0]);
+            sum_t = sum_1 = 0;
+            for (int i = 0; i < a.parts; ++i) {
+                sum_t += parts[i][1] == 0.0f ? 0.0f : parts[i][1] * factor(parts[i][0], m, a.ct);
+                sum_1 += parts[i][2] == 0.0f ? 0.0f : parts[i][2] * factor(parts[i][0], m, a.c1);
+            }
+        }
+    }
+    if (g.lane) return;
+    const float other = m, other_t = sum_t;           // without `rest` the classes seen are all there are
+    if (REST) {
+        m = fmaxf(m, top[1]);
+        sum_t = (other_t == 0.0f ? 0.0f : other_t * factor(other, m, a.ct)) + (total[2] == 0.0f ? 0.0f : total[2] * factor(top[1], m, a.ct));
+        sum_1 = (sum_1 == 0.0f ? 0.0f : sum_1 * factor(other, m, a.c1)) + (total[3] == 0.0f ? 0.0f : total[3] * factor(top[1], m, a.c1));
+    }
+    if (!TWO) sum_1 = sum_t;
+    float loss = 0;
+    const float log_t = logf(sum_t);
+    if (taught) {
+        float whole = total[4], d = total[5];
+        if (whole != 0.0f) d += whole * ((m - mx) * a.inv_t);
+        if (REST) {
+            const float e0 = factor(rest, mu, a.c1);
+            if (e0 != 0.0f) d += e0 * ((rest - mu) - ((other - m) * a.inv_t + logf(other_t)));
+            whole += e0;
+        }
+        loss = a.soft_loss * (d / whole - logf(whole) + log_t);
+    }
+    if (label >= 0) loss += a.hard * (logf(sum_1) - (widen(s[label]) - m));
+    a.loss[row] = loss;
+    float* out = a.stats + (int64_t)row * 5;
+    out[0] = m;
+    out[1] = a.labels ? sum_1 : 0.0f;
+    out[2] = sum_t;
+    out[3] = other;
+    out[4] = other_t;
+}
+
+template <typename T, bool REST, bool TWO>
+cudaError_t launch(DistillArgs a, cudaStream_t st) {
+    constexpr int W = 16 / sizeof(T);
+    if (a.classes <= kMostOfWarp && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
+        a.parts = 1;
+        const size_t smem = REST ? kRowsOfCta * ((kMostOfWarp + 2 * W) / 32 + 1) * 4 : 0;
+        distill_rows<T, REST, TWO, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, smem, st>>>(a);
+        return cudaGetLastError();
+    }
+    // few long rows: a cluster of CTAs has one
+    a.parts = 1;
+    while (a.parts < 8 && (int64_t)a.rows * a.parts < 2 * kSMs && a.classes / a.parts >= 4096 * 2) a.parts *= 2;
+    const int vectors = (a.classes + 2 * W - 2) / W, each = (vectors + a.parts - 1) / a.parts;
+    const size_t smem = REST ? ((size_t)each * W + 31) / 32 * 4 : 0;
+    static std::atomic<uint64_t> allowed{0};
+    if (smem > 40960) {
+        int dev = 0;
+        if (const cudaError_t e = cudaGetDevice(&dev)) return e;
+        if (dev >= 64 || !(allowed.load() >> dev & 1)) {
+            if (const cudaError_t e = cudaFuncSetAttribute(distill_rows<T, REST, TWO, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                           kMostClasses / 8 + 64)) {
+                cudaGetLastError();
+                return e;
+            }
+            if (dev < 64) allowed.fetch_or(uint64_t(1) << dev);
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.rows * (unsigned)a.parts);
+    cfg.blockDim = dim3(kWide);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.parts > 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, distill_rows<T, REST, TWO, kWide>, a), l = cudaGetLastError();
+    return e != cudaSuccess ? e : l;
+}
+
+template <typename T>
+cudaError_t forward(const DistillArgs& a, cudaStream_t st) {
+    const bool two = a.labels && a.ct != a.c1;        // at T = 1 both sums are one
+    if (a.rest) return two ? launch<T, true, true>(a, st) : launch<T, true, false>(a, st);
+    return two ? launch<T, false, true>(a, st) : launch<T, false, false>(a, st);
+}
+
+int check(const void* s, int64_t stride, int dtype, int64_t rows, int64_t classes, int kept, const void* values, int value_type,
+          const int* indices, const float* rest, const int64_t* labels, double temperature, double alpha) {
+    if (!known(dtype) || !known(value_type)) return PP_ERR_DTYPE;
+    if (rows < 0 || rows > (1 << 27) || classes < 1 || classes > kMostClasses || kept < 1 || kept > kMostKept || kept > classes ||
+        (rows > 1 && stride < classes))
+        return PP_ERR_SHAPE;
+    if (!(temperature >= 1e-3 && temperature <= 1e3) || !(alpha >= 0 && alpha <= 1)) return PP_ERR_ARG;
+    if (!rows) return PP_OK;
+    if (!s || !values || !indices) return PP_ERR_NULL;
+    if (off(s, size_of(dtype)) || off(values, size_of(value_type)) || off(indices, 4) || off(rest, 4) || off(labels, 8))
+        return PP_ERR_ALIGN;
+    return PP_OK;
+}
+
+DistillArgs args_of(const void* s, int64_t stride, int64_t rows, int64_t classes, int kept, const void* values, int value_type,
+                    const int* indices, const float* rest, const int64_t* labels, double temperature, double alpha) {
+    DistillArgs a{};
+    a.s = s;
+    a.stride = rows > 1 ? stride : classes;
+    a.rows = (int)rows;
+    a.classes = (int)classes;
+    a.kept = kept;
+    a.value_type = value_type;
+    a.values = values;
+    a.indices = indices;
+    a.rest = rest;
+    a.labels = labels;
+    const double log2e = 1.4426950408889634;
+    a.c1 = (float)log2e;
+    a.ct = (float)(log2e / temperature);
+    a.inv_t = (float)(1 / temperature);
+    a.hard = labels ? (float)(1 - alpha) : 0.0f;
+    a.soft_loss = (float)(alpha * temperature * temperature);
+    a.soft_slope = (float)(alpha * temperature);
+    return a;
+}
+
+}  // namespace
+
+cudaError_t distill_forward(const DistillArgs& a, int dtype, cudaStream_t st) {
+    return dtype == PP_F32 ? forward<float>(a, st) : dtype == PP_F16 ? forward<__half>(a, st) : forward<__nv_bfloat16>(a, st);
+}
+
+}  // namespace patconv
+
+using namespace patconv;
+
+extern "C" {
+
+int pp_distill(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t classes, const void* values, int value_type,
+               const int* indices, int kept, const float* rest, const int64_t* labels, double temperature, double alpha,
+               float* loss, float* stats, void* stream) {
+    if (const int e = check(logits, stride, dtype, rows, classes, kept, values, value_type, indices, rest, labels, temperature, alpha))
+        return e;
+    if (!rows) return PP_OK;
+    if (!loss || !stats) return PP_ERR_NULL;
+    if (off(loss, 4) || off(stats, 4)) return PP_ERR_ALIGN;
+    const size_t sb = (size_t)row_extent(rows, stride, classes) * size_of(dtype), lb = (size_t)rows * 4;
+    const struct { const void* p; size_t n; } in[] = {{logits, sb}, {values, lb / 4 * kept * size_of(value_type)}, {indices, lb * kept},
+                                                      {rest, rest ? lb : 0}, {labels, labels ? 2 * lb : 0}};
+    for (const auto& i : in)
+        if (overlap(i.p, i.n, loss, lb) || overlap(i.p, i.n, stats, 5 * lb)) return PP_ERR_BUFFER;
+    if (overlap(loss, lb, stats, 5 * lb)) return PP_ERR_BUFFER;
+    DistillArgs a = args_of(logits, stride, rows, classes, kept, values, value_type, indices, rest, labels, temperature, alpha);
+    a.loss = loss;
+    a.stats = stats;
+    return distill_forward(a, dtype, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PP_OK : PP_ERR_CUDA;
+}
+
+int pp_distill_backward(const float* dloss, int64_t dloss_stride, const void* logits, int64_t stride, int dtype, int64_t rows,
+                        int64_t classes, const float* stats, const void* values, int value_type, const int* indices, int kept,
+                        const float* rest, const int64_t* labels, double temperature, double alpha, void* dlogits, void* stream) {
+    if (const int e = check(logits, stride, dtype, rows, classes, kept, values, value_type, indices, rest, labels, temperature, alpha))
+        return e;
+    if (dloss_stride < 0) return PP_ERR_SHAPE;
+    if (!rows) return PP_OK;
+    if (!dloss || !stats || !dlogits) return PP_ERR_NULL;
+    if (off(dloss, 4) || off(stats, 4) || off(dlogits, size_of(dtype))) return PP_ERR_ALIGN;
+    const size_t es = size_of(dtype), lb = (size_t)rows * 4, ob = (size_t)rows * classes * es;
+    const bool over = dlogits == logits && (rows == 1 || stride == classes);      // every logit is read before it is written
+    const struct { const void* p; size_t n; } in[] = {{logits, over ? 0 : (size_t)row_extent(rows, stride, classes) * es},
+                                                      {values, lb / 4 * kept * size_of(value_type)}, {indices, lb * kept},
+                                                      {rest, rest ? lb : 0}, {labels, labels ? 2 * lb : 0}, {stats, 5 * lb},
+                                                      {dloss, (size_t)row_extent(rows, dloss_stride, 1) * 4}};
+    for (const auto& i : in)
+        if (overlap(i.p, i.n, dlogits, ob)) return PP_ERR_BUFFER;
+    DistillArgs a = args_of(logits, stride, rows, classes, kept, values, value_type, indices, rest, labels, temperature, alpha);
+    a.dloss = dloss;
+    a.dloss_stride = dloss_stride;
+    a.stats = const_cast<float*>(stats);
+    a.ds = dlogits;
+    return distill_backward(a, dtype, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PP_OK : PP_ERR_CUDA;
+}
+
+}  // extern "C"

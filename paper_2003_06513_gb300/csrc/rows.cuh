@@ -1,0 +1,100 @@
+// Kernel parts that top.cu, distill.cu and distill_back.cu share: a row of logits as aligned vectors, groups of
+// threads (a warp, or a CTA) that take a row together, and the base-2 exponentials.
+#pragma once
+
+#include <climits>
+#include <cmath>
+
+#include "rows.h"
+#include "vec.cuh"
+
+namespace patconv {
+namespace {
+
+constexpr float kNone = -INFINITY;
+
+// A row (or a slice of one) of `count` values from p on, as vectors of W that lie on 16-byte boundaries: places are
+// counted from the boundary at or before p, so that value i is at place i + pad and vector v holds places v W to
+// v W + W - 1, of which the row has those from pad to end - 1.
+template <typename T, int W>
+struct Row {
+    const T* base;                    // place 0
+    int pad, end;
+    __device__ __forceinline__ Row(const T* p, int count) {
+        pad = W == 1 ? 0 : (int)(reinterpret_cast<uintptr_t>(p) % (W * sizeof(T)) / sizeof(T));
+        base = p - pad;
+        end = count + pad;
+    }
+    __device__ __forceinline__ int vectors() const { return (end + W - 1) / W; }
+    __device__ __forceinline__ bool whole(int v) const { return v * W >= pad && v * W + W <= end; }
+    __device__ __forceinline__ Vec<T, W> at(int v) const { return load<T, W>(base + (int64_t)v * W); }
+};
+
+// The threads that take a row together: a warp of several in a CTA (N = 32), or a CTA.
+template <int N>
+struct Group {
+    static constexpr int kWarps = N / 32;
+    int lane;                         // of the group
+    float* scratch;                   // 2 x kWarps x 8 floats (N > 32)
+    int turn = 0;
+    __device__ __forceinline__ explicit Group(float* s) : lane(N == 32 ? threadIdx.x % 32 : threadIdx.x), scratch(s) {}
+    __device__ __forceinline__ static void sync() {
+        if constexpr (N == 32)
+            __syncwarp();
+        else
+            __syncthreads();
+    }
+    __device__ __forceinline__ static bool any(bool x) {
+        if constexpr (N == 32)
+            return __any_sync(0xffffffffu, x);
+        else
+            return __syncthreads_or(x);
+    }
+    // the group's results of up to 8 values, to every thread, joined in a fixed order; the scratch is used in turns, so
+    // that one barrier a call is enough
+    template <int K, typename Op>
+    __device__ __forceinline__ void join(float (&v)[K], Op op) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] = op(v[k], __shfl_xor_sync(0xffffffffu, v[k], o));
+        if constexpr (N > 32) {
+            float* mine = scratch + turn * kWarps * 8;
+            turn ^= 1;
+            if (threadIdx.x % 32 == 0)
+#pragma unroll
+                for (int k = 0; k < K; ++k) mine[threadIdx.x / 32 * 8 + k] = v[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                v[k] = mine[k];
+                for (int w = 1; w < kWarps; ++w) v[k] = op(v[k], mine[w * 8 + k]);
+            }
+        }
+    }
+    template <int K>
+    __device__ __forceinline__ void max(float (&v)[K]) {
+        join(v, [](float a, float b) { return fmaxf(a, b); });
+    }
+    template <int K>
+    __device__ __forceinline__ void sum(float (&v)[K]) {
+        join(v, [](float a, float b) { return a + b; });
+    }
+};
+
+// What exponentials are relative to: 2^((x - m) c), c = log2(e) / T, for the largest value m; 0 where there is no value (-inf).
+// The difference comes first: x c by itself would leave fp32's range where x is the type's lowest value, as masks have it.
+__device__ __forceinline__ float reference(float m) { return m == kNone ? 0.0f : m; }
+__device__ __forceinline__ float power(float x, float m, float c) { return approx_exp2((x - m) * c); }
+// 2^((a - m) c), 0 where there is no a
+__device__ __forceinline__ float factor(float a, float m, float c) { return a == kNone ? 0.0f : approx_exp2((a - m) * c); }
+
+// kept value j of a row, in fp32
+__device__ __forceinline__ float value_at(const void* values, int type, int64_t j) {
+    if (type == PP_F32) return static_cast<const float*>(values)[j];
+    if (type == PP_F16) return __half2float(static_cast<const __half*>(values)[j]);
+    return __bfloat162float(static_cast<const __nv_bfloat16*>(values)[j]);
+}
+
+}  // namespace
+}  // namespace patconv
