@@ -140,7 +140,7 @@ struct Input {
 int check_shape(const Shape& s) {
     if (!known(s.x_dtype) || !known(s.dtype) || (s.x_dtype != s.dtype && s.x_dtype != PP_F32)) return PP_ERR_DTYPE;
     if (s.N < 0 || s.pixels < 0 || s.C < 1 || s.C > kBlockMost) return PP_ERR_SHAPE;
-    if (s.N && s.pixels && s.pixels > (INT_MAX - 65536) / s.N) return PP_ERR_SHAPE;
+    if (s.N && s.pixels && s.pixels > (INT_MAX - (1 << 20)) / s.N) return PP_ERR_SHAPE;
     return PP_OK;
 }
 int check_input(const Shape& s, const Input& t) {

@@ -28,32 +28,63 @@ __device__ __forceinline__ int channel(int lane, int threads, int k) {
     return (lane + k / V * threads) * V + k % V;
 }
 template <typename T, int V>
-__device__ __forceinline__ Vec<T, V> load_wide(const T* p) {
-    if constexpr (sizeof(T) * V > 16) {               // eight fp32 values: two vectors
-        Vec<T, V> r;
-        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-        memcpy(&r, &a, 16);
-        memcpy(&r.v[4], &b, 16);
-        return r;
-    } else {
-        return load<T, V>(p);
-    }
-}
-template <typename T, int V>
 struct Raw {                                          // as it is read
     Vec<T, V> v[E / V];
 };
+// What a thread reads of an input, a round ahead of its use: asynchronous copies of 4 to 16 bytes into the thread's own
+// places of shared memory, which no other thread reads, so that waiting for its own copies is all that is needed, and what
+// is under way costs no registers.  There is no copy of two bytes: single halves are read when they are used.
 template <typename T, int V>
-__device__ __forceinline__ void fetch(Raw<T, V>& r, const T* row, int lane, const BlockArgs& a, bool there) {
-#pragma unroll
-    for (int j = 0; j < E / V; ++j) {
-        const int at = lane + j * a.threads;
-        if (there && at < a.vectors)
-            r.v[j] = load_wide<T, V>(row + (int64_t)at * V);
-        else
-            r.v[j] = Vec<T, V>{};
+struct Ahead {
+    static constexpr int S = sizeof(T) * V > 16 ? 16 : sizeof(T) * V, P = E * (int)sizeof(T) / S;
+    static constexpr bool kAsync = S >= 4;
+    static constexpr int kBytes = kAsync ? E * (int)sizeof(T) : 0;       // of a thread and round
+    // bytes from the row's first channel to piece k, and whether the row has it
+    static __device__ __forceinline__ int64_t offset(int lane, const BlockArgs& a, int k) {
+        return sizeof(T) * V > 16 ? (int64_t)lane * V * sizeof(T) + k * S : (int64_t)(lane + k * a.threads) * S;
     }
-}
+    static __device__ __forceinline__ bool has(int lane, const BlockArgs& a, int k) {
+        return (sizeof(T) * V > 16 ? lane : lane + k * a.threads) < a.vectors;
+    }
+    static __device__ __forceinline__ void ask(uint32_t place, const T* row, int lane, const BlockArgs& a, bool there) {
+        if constexpr (kAsync) {
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const bool wanted = there && has(lane, a, k);
+                const char* from = reinterpret_cast<const char*>(row) + (wanted ? offset(lane, a, k) : 0);
+                const uint32_t to = place + (k * blockDim.x + threadIdx.x) * S;
+                const int n = wanted ? S : 0;          // what is not copied becomes 0
+                if constexpr (S == 16)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
+                else
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(S), "r"(n) : "memory");
+            }
+        }
+    }
+    static __device__ __forceinline__ Raw<T, V> get(const char* place, const T* row, int lane, const BlockArgs& a, bool there) {
+        Raw<T, V> r;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            char* to = reinterpret_cast<char*>(&r) + k * S;
+            if constexpr (kAsync) {
+                Vec<char, S> v = *reinterpret_cast<const Vec<char, S>*>(place + (k * blockDim.x + threadIdx.x) * S);
+                memcpy(to, &v, S);
+            } else {
+                T v = T(0.0f);
+                if (there && has(lane, a, k)) v = row[lane + k * a.threads];
+                memcpy(to, &v, S);
+            }
+        }
+        return r;
+    }
+};
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+constexpr int kRounds = 4;                            // of rows that a CTA has under way, and in the backward pass; two there
+template <typename TX, typename TB, bool WIDE>        // where 512 threads with all of it in fp32 would take more than there is
+constexpr int kRoundsBack = WIDE && sizeof(TX) + sizeof(TB) == 8 ? 2 : 3;
+
 template <typename T, int V>
 __device__ __forceinline__ Eight widened(const Raw<T, V>& r) {
     Eight e;
@@ -219,7 +250,8 @@ __device__ __forceinline__ float act_of(float z, int act) {
 // -------------------------------------------------------------------------------- forward
 
 template <typename TX, typename TB, int V, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads) block_rows(BlockArgs a) {
+__global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 3) block_rows(BlockArgs a) {
+    extern __shared__ __align__(16) char ring[];
     __shared__ float2 scratch[WIDE ? 64 : 1];
     const int lane = WIDE ? threadIdx.x : threadIdx.x % a.threads;
     const int here = WIDE ? 1 : kBlockThreads / a.threads, mine = WIDE ? 0 : threadIdx.x / a.threads;
@@ -233,21 +265,38 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads) block_rows(BlockAr
     Eight gate = parameter<V>(nullptr, 1.0f, lane, a);
     int gate_of = -1;
 
-    for (int base = blockIdx.x * here; base < a.rows; base += gridDim.x * here) {
+    using X = Ahead<TX, V>;
+    using B = Ahead<TB, V>;
+    const int step = gridDim.x * here;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const int round = (X::kBytes + B::kBytes) * blockDim.x, b_at = X::kBytes * blockDim.x;
+    const auto ask = [&](int row, int slot) {
+        if (row - mine < a.rows) {                    // (of the CTA's first row: the same for all)
+            const bool there = row < a.rows;
+            const At at = at_row(there ? row : 0, a);
+            X::ask(ring_at + slot * round, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
+            if (a.b) B::ask(ring_at + slot * round + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there);
+        }
+        copies_end();
+    };
+    for (int k = 0; k < kRounds - 1; ++k) ask(blockIdx.x * here + k * step + mine, k);
+    int slot = 0;
+    for (int base = blockIdx.x * here; base < a.rows; base += step) {
         const int row = base + mine;
         const bool there = row < a.rows;
         const At at = at_row(there ? row : 0, a);
-        Raw<TX, V> rx;
-        Raw<TB, V> rb;
-        if (a.x) fetch(rx, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
-        if (a.b) fetch(rb, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there);
+        ask(row + (kRounds - 1) * step, slot == 0 ? kRounds - 1 : slot - 1);     // into the places that the round before has read
+        copies_wait<kRounds - 1>();
+        const char* place = ring + slot * round;
+        slot = slot == kRounds - 1 ? 0 : slot + 1;
         if (a.gate && there && at.sample != gate_of) {
             gate = parameter<V>(a.gate + (int64_t)at.sample * a.C, 1.0f, lane, a);
             gate_of = at.sample;
         }
+        const Raw<TX, V> rx = X::get(place, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
         Eight h = widened(rx);
         if (a.b) {
-            Eight b = widened(rb);
+            Eight b = widened(B::get(place + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there));
             if (a.post == PP_NORM_LAYER) centre<V>(b, sum(across(sum_of(b))) * a.inv_c, lane, a);
             float2 q = make_float2(0.0f, 0.0f);
             if (a.post != PP_NORM_NONE) q = sum(make_float2(across(sum_of(b)), dot(b, b)));
@@ -277,8 +326,9 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads) block_rows(BlockAr
 
 // Whether z = w (h - mean) r + bias is above 0, where fp32 cannot tell: mean and root in 64 bits.  Every thread of the CTA
 // (WIDE) or of the warp calls it.
-template <int V, bool WIDE>
-__device__ __noinline__ unsigned above_zero(Eight h, const BlockArgs& a, int lane, RowSum<WIDE>& sum) {
+template <typename TX, int V, bool WIDE>
+__device__ __noinline__ unsigned above_zero(const char* place, const TX* row, bool there, const BlockArgs& a, int lane, RowSum<WIDE>& sum) {
+    const Eight h = widened(Ahead<TX, V>::get(place, row, lane, a, there));
     const float* f = reinterpret_cast<const float*>(h.v);
     double mean = 0, square = 0;
     if (a.pre == PP_NORM_LAYER) {
@@ -300,6 +350,8 @@ __device__ __noinline__ unsigned above_zero(Eight h, const BlockArgs& a, int lan
 
 template <typename TX, typename TB, int V, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) block_back_rows(BlockArgs a) {
+    constexpr int R = kRoundsBack<TX, TB, WIDE>;
+    extern __shared__ __align__(16) char ring[];
     __shared__ float2 scratch[WIDE ? 64 : 1];
     __shared__ float lanes_sum[WIDE ? 1 : 2 * kBlockThreads * E];
     const int lane = WIDE ? threadIdx.x : threadIdx.x % a.threads;
@@ -309,9 +361,31 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
     const Eight w = parameter<V>(a.weight, 1.0f, lane, a), bias = parameter<V>(a.bias, 0.0f, lane, a);
     const Eight zero{};
     Eight s_w = zero, s_b = zero, s_e = zero, s_f = zero;        // sums of dz h^, dz, and of a sample dh b^, dh
-    // the sums over all samples that the threads of channel c hold (not WIDE: thread c; WIDE: the thread's eight)
+    // the sums over all samples, in shared memory: of post_weight, post_bias and scale, thread c's (WIDE: the thread's eight channels')
     constexpr int OWN = WIDE ? E : 1;
-    float t_pw[OWN] = {}, t_pb[OWN] = {}, t_s[OWN] = {};
+    float* totals = reinterpret_cast<float*>(ring + R * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) * blockDim.x) + threadIdx.x;
+    const auto total = [&](int which, int i) -> float& { return totals[(which * OWN + i) * blockDim.x]; };
+#pragma unroll
+    for (int i = 0; i < 3 * OWN; ++i) total(0, i) = 0.0f;
+
+    using X = Ahead<TX, V>;
+    using B = Ahead<TB, V>;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const int x_bytes = X::kBytes * blockDim.x, b_bytes = B::kBytes * blockDim.x, round = 2 * (x_bytes + b_bytes);
+    const int d_at = 0, h_at = x_bytes, y_at = 2 * x_bytes, b_at = y_at + b_bytes;
+    // asks for a round of rows, `last` the end of their sample's
+    const auto ask = [&](int base, int last, int slot) {
+        if (base < last) {
+            const bool there = base + mine < last;
+            const At at = at_row(there ? base + mine : base, a);
+            const uint32_t place = ring_at + slot * round;
+            if (pre) X::ask(place + h_at, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
+            if (a.b) B::ask(place + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there);
+            if (pre) B::ask(place + y_at, row_of<TB>(a.dy, at, a.dy_pixel, a.dy_sample), lane, a, there);
+            if (a.dh) X::ask(place + d_at, row_of<TX>(a.dh, at, a.dh_pixel, a.dh_sample), lane, a, there);
+        }
+        copies_end();
+    };
 
     const int begin = blockIdx.x * a.stretch, end = min(a.rows, begin + a.stretch);
     for (int from = begin; from < end;) {
@@ -324,26 +398,26 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) k.v[i] = mul(k.v[i], mul(sc.v[i], ga.v[i]));
 
+        for (int k = 0; k < R - 1; ++k) ask(from + k * here, to, k);
+        int slot = 0;
         for (int base = from; base < to; base += here) {
             const int row = base + mine;
             const bool there = row < to;
-            const At at = at_row(there ? row : from, a);
-            Raw<TX, V> rd, rh;
-            Raw<TB, V> ry, rb;
-            if (a.dh) fetch(rd, row_of<TX>(a.dh, at, a.dh_pixel, a.dh_sample), lane, a, there);
-            if (a.b) fetch(rb, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there);
-            if (pre) {
-                fetch(rh, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
-                fetch(ry, row_of<TB>(a.dy, at, a.dy_pixel, a.dy_sample), lane, a, there);
-            }
-            Eight d = a.dh ? widened(rd) : zero, b = a.b ? widened(rb) : zero, h = pre ? widened(rh) : zero;
+            const At at = at_row(there ? row : base, a);
+            ask(base + (R - 1) * here, to, slot == 0 ? R - 1 : slot - 1);
+            copies_wait<R - 1>();
+            const char* place = ring + slot * round;
+            slot = slot == R - 1 ? 0 : slot + 1;
+            const TX* h_row = row_of<TX>(a.x, at, a.x_pixel, a.x_sample);
+            Eight h = zero, b = zero;
+            if (pre) h = widened(X::get(place + h_at, h_row, lane, a, there));
+            if (a.b) b = widened(B::get(place + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there));
             // both norms
             float2 mean = make_float2(0.0f, 0.0f);
             if (a.pre == PP_NORM_LAYER || a.post == PP_NORM_LAYER) {
                 mean = sum(make_float2(a.pre == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, a.post == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f));
                 mean = mul(mean, both(a.inv_c));
             }
-            const Eight h0 = h;
             if (a.pre == PP_NORM_LAYER) centre<V>(h, mean.x, lane, a);
             if (a.post == PP_NORM_LAYER) centre<V>(b, mean.y, lane, a);
             float2 both_sums[2] = {make_float2(across(sum_of(h)), across(sum_of(b))), make_float2(dot(h, h), dot(b, b))};
@@ -354,8 +428,10 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
 #pragma unroll
             for (int i = 0; i < E / 2; ++i)
                 h.v[i] = fma(h.v[i], both(r.x), both(shift.x)), b.v[i] = fma(b.v[i], both(r.y), both(shift.y));
+            Eight d = zero;
+            if (!pre && a.dh) d = widened(X::get(place + d_at, row_of<TX>(a.dh, at, a.dh_pixel, a.dh_sample), lane, a, there));
             if (pre) {
-                Eight dz = widened(ry);
+                Eight dz = widened(B::get(place + y_at, row_of<TB>(a.dy, at, a.dy_pixel, a.dy_sample), lane, a, there));
                 if (a.act == PP_ACT_RELU) {
                     // fp32's z is off by less than 2^-18 of its terms' sizes (each value, the mean, and the root by some 16 roundings
                     // of the row's sums): there the sign is taken in 64 bits
@@ -372,7 +448,8 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
                         close |= fabsf(z) <= 3.8147e-6f * (fabsf(wf[e]) * (fabsf(hf[e]) + spread) + fabsf(bf[e])) && inside<V>(lane, a, e);
                     }
                     close = close && there;
-                    if (WIDE ? __syncthreads_or(close) : __any_sync(0xffffffffu, close)) above = above_zero<V, WIDE>(h0, a, lane, sum);
+                    if (WIDE ? __syncthreads_or(close) : __any_sync(0xffffffffu, close)) 
+                        above = above_zero<TX, V, WIDE>(place + h_at, h_row, there, a, lane, sum);
                     float* f = reinterpret_cast<float*>(dz.v);
 #pragma unroll
                     for (int e = 0; e < E; ++e)
@@ -395,6 +472,7 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
                 }
                 float2 q = sum(make_float2(a.pre == PP_NORM_LAYER ? across(sum_of(t)) : 0.0f, dot(t, h)));
                 q = mul(q, both(a.inv_c));
+                if (a.dh) d = widened(X::get(place + d_at, row_of<TX>(a.dh, at, a.dh_pixel, a.dh_sample), lane, a, there));
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i)
                     d.v[i] = fma(fma(h.v[i], both(-q.y), add(t.v[i], both(-q.x))), both(r.x), d.v[i]);
@@ -448,9 +526,9 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
                 }
                 const float ga_c = gate ? gate[c] : 1.0f, sc_c = a.scale ? a.scale[c] : 1.0f;
                 const float joined = fmaf(a.post_weight ? a.post_weight[c] : 1.0f, e, a.post_bias ? a.post_bias[c] * f : 0.0f);
-                t_pw[i] = fmaf(sc_c * ga_c, e, t_pw[i]);
-                t_pb[i] = fmaf(sc_c * ga_c, f, t_pb[i]);
-                t_s[i] = fmaf(ga_c, joined, t_s[i]);
+                total(0, i) = fmaf(sc_c * ga_c, e, total(0, i));
+                total(1, i) = fmaf(sc_c * ga_c, f, total(1, i));
+                total(2, i) = fmaf(ga_c, joined, total(2, i));
                 if (a.dgate) {
                     if (whole)
                         a.dgate[(int64_t)start.sample * a.C + c] = sc_c * joined;
@@ -490,30 +568,49 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
         }
         out[c] = e;
         out[a.C + c] = f;
-        out[2 * a.C + c] = t_pw[i];
-        out[3 * a.C + c] = t_pb[i];
-        out[4 * a.C + c] = t_s[i];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) out[(2 + k) * a.C + c] = total(k, i);
     }
 }
 
+// more shared memory than a launch has by itself: once for each kernel and device
+template <typename K>
+cudaError_t allow_shared(K* kernel, std::atomic<uint64_t>& done, size_t bytes) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 64 || !(done.load(std::memory_order_relaxed) >> dev & 1))) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e == cudaSuccess && dev < 64) done.fetch_or(uint64_t(1) << dev);
+    }
+    if (e != cudaSuccess) cudaGetLastError();
+    return e;
+}
+template <typename TX, typename TB, int V, bool WIDE>
+cudaError_t forward_rows(const BlockArgs& a, int threads, int ctas, cudaStream_t st) {
+    constexpr int kRound = Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes;
+    static std::atomic<uint64_t> allowed{0};
+    if (const cudaError_t e = allow_shared(block_rows<TX, TB, V, WIDE>, allowed, kRounds * kRound * (WIDE ? 512 : kBlockThreads))) return e;
+    block_rows<TX, TB, V, WIDE><<<ctas, threads, kRounds * kRound * threads, st>>>(a);
+    return cudaGetLastError();
+}
 template <typename TX, typename TB, int V>
 cudaError_t forward_as(const BlockArgs& a, cudaStream_t st) {
-    if (a.threads > 32) {
-        const int ctas = std::min(a.rows, 152 * std::max(1, 1536 / a.threads));
-        block_rows<TX, TB, V, true><<<ctas, a.threads, 0, st>>>(a);
-    } else {
-        const int here = kBlockThreads / a.threads, ctas = std::min((a.rows + here - 1) / here, 152 * 4);
-        block_rows<TX, TB, V, false><<<ctas, kBlockThreads, 0, st>>>(a);
-    }
+    if (a.threads > 32) return forward_rows<TX, TB, V, true>(a, a.threads, std::min(a.rows, 152 * std::max(1, 768 / a.threads)), st);
+    const int here = kBlockThreads / a.threads;
+    return forward_rows<TX, TB, V, false>(a, kBlockThreads, std::min((a.rows + here - 1) / here, 152 * 3), st);
+}
+template <typename TX, typename TB, int V, bool WIDE>
+cudaError_t backward_rows(const BlockArgs& a, int threads, cudaStream_t st) {
+    constexpr int kEach = kRoundsBack<TX, TB, WIDE> * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) + 3 * (WIDE ? E : 1) * (int)sizeof(float);   // of a thread
+    static std::atomic<uint64_t> allowed{0};
+    if (const cudaError_t e = allow_shared(block_back_rows<TX, TB, V, WIDE>, allowed, kEach * (WIDE ? 512 : kBlockThreads))) return e;
+    block_back_rows<TX, TB, V, WIDE><<<a.ctas, threads, kEach * threads, st>>>(a);
     return cudaGetLastError();
 }
 template <typename TX, typename TB, int V>
 cudaError_t backward_as(const BlockArgs& a, cudaStream_t st) {
-    if (a.threads > 32)
-        block_back_rows<TX, TB, V, true><<<a.ctas, a.threads, 0, st>>>(a);
-    else
-        block_back_rows<TX, TB, V, false><<<a.ctas, kBlockThreads, 0, st>>>(a);
-    if (const cudaError_t e = cudaGetLastError()) return e;
+    if (const cudaError_t e = a.threads > 32 ? backward_rows<TX, TB, V, true>(a, a.threads, st) : backward_rows<TX, TB, V, false>(a, kBlockThreads, st))
+        return e;
     return block_join(a, st);
 }
 

@@ -29,7 +29,11 @@ constexpr int kRowsOfCta = 4;         // rows of a CTA whose warps have one each
 constexpr int kMostOfWarp = 2048;     // classes of a warp's row at most
 
 // what a thread sums of the classes it sees: the largest x, and the sums of 2^((x - m) c) relative to it
-template <bool TWO>
+// HARD: how the sum at T = 1 is had beside the one at T.  kNone: there are no labels, or T is 1; kApart: by an exponential of its
+// own; kSquare, kFourth: T is 2 or 4, and exp(d) is exp(d / T) to that power -- the special function unit, with two
+// exponentials a value, would bound the kernel before memory does.
+enum { kNoHard = 0, kApart = 1, kSquare = 2, kFourth = 4 };
+template <int HARD>
 struct Running {
     float m = kNone, ref = 0;         // and m, or 0 before there is one
     float2 z1 = {0, 0}, zt = {0, 0};
@@ -37,21 +41,26 @@ struct Running {
         if (!(top > m)) return;
         if (m != kNone) {
             zt = mul(zt, both(power(m, top, ct)));
-            if (TWO) z1 = mul(z1, both(power(m, top, c1)));
+            if (HARD) z1 = mul(z1, both(power(m, top, c1)));
         }
         m = ref = top;
     }
     __device__ __forceinline__ void add_pair(float2 x, float2 c1, float2 ct) {
-        const float2 d = add(x, both(-ref)), e = mul(d, ct);
-        zt = add(zt, make_float2(approx_exp2(e.x), approx_exp2(e.y)));
-        if (TWO) {
+        const float2 d = add(x, both(-ref)), l = mul(d, ct), e = make_float2(approx_exp2(l.x), approx_exp2(l.y));
+        zt = add(zt, e);
+        if (HARD == kApart) {
             const float2 f = mul(d, c1);
             z1 = add(z1, make_float2(approx_exp2(f.x), approx_exp2(f.y)));
+        } else if (HARD == kSquare) {
+            z1 = fma(e, e, z1);
+        } else if (HARD == kFourth) {
+            const float2 q = mul(e, e);
+            z1 = fma(q, q, z1);
         }
     }
 };
 
-template <typename T, bool REST, bool TWO, int N>
+template <typename T, bool REST, int HARD, int N>
 __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(DistillArgs a) {
     constexpr int W = 16 / sizeof(T), U = 4;
     extern __shared__ uint4 dynamic[];
@@ -112,7 +121,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
     if constexpr (N > 32)                             // the first CTA's memory is written by the others, once it has begun
         if (a.parts > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
 
-    Running<TWO> sum;
+    Running<HARD> sum;
     const float2 c1 = both(a.c1), ct = both(a.ct);
     const unsigned char* marks = reinterpret_cast<const unsigned char*>(bits);
     const auto mark = [&](int v) -> unsigned {        // the bits of vector v's classes
@@ -158,7 +167,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
                 const float y = widen(r.base[place]);
                 sum.below(y, a.c1, a.ct);
                 sum.zt.x += power(y, sum.ref, a.ct);
-                if (TWO) sum.z1.x += power(y, sum.ref, a.c1);
+                if (HARD) sum.z1.x += power(y, sum.ref, a.c1);
             }
         }
     }
@@ -184,12 +193,12 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
     g.max(top);
     const float mu = reference(top[2]), mx = reference(top[1]);
     const float e = at >= 0 ? power(u, mu, a.c1) : 0.0f;
-    float total[6] = {zt == 0.0f ? 0.0f : zt * factor(sum.m, top[0], a.ct), !TWO || z1 == 0.0f ? 0.0f : z1 * factor(sum.m, top[0], a.c1), 0, 0, e, 0};
+    float total[6] = {zt == 0.0f ? 0.0f : zt * factor(sum.m, top[0], a.ct), !HARD || z1 == 0.0f ? 0.0f : z1 * factor(sum.m, top[0], a.c1), 0, 0, e, 0};
     if (REST && once) {
         total[2] = power(x, mx, a.ct);
-        if (TWO) total[3] = power(x, mx, a.c1);
+        if (HARD) total[3] = power(x, mx, a.c1);
     }
-    if (e != 0.0f) total[5] = e * ((u - mu) - (x - mx) * a.inv_t);
+    if (!REST && e != 0.0f) total[5] = e * ((u - mu) - (x - mx) * a.inv_t);
     g.sum(total);
     float m = top[0], sum_t = total[0], sum_1 = total[1];
     if constexpr (N > 32) {
@@ -211,25 +220,46 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
             }
         }
     }
-    if (g.lane) return;
     const float other = m, other_t = sum_t;           // without `rest` the classes seen are all there are
+    float kept_t = 0;
     if (REST) {
         m = fmaxf(m, top[1]);
-        sum_t = (other_t == 0.0f ? 0.0f : other_t * factor(other, m, a.ct)) + (total[2] == 0.0f ? 0.0f : total[2] * factor(top[1], m, a.ct));
+        kept_t = total[2] == 0.0f ? 0.0f : total[2] * factor(top[1], m, a.ct);
+        sum_t = (other_t == 0.0f ? 0.0f : other_t * factor(other, m, a.ct)) + kept_t;
         sum_1 = (sum_1 == 0.0f ? 0.0f : sum_1 * factor(other, m, a.c1)) + (total[3] == 0.0f ? 0.0f : total[3] * factor(top[1], m, a.c1));
     }
-    if (!TWO) sum_1 = sum_t;
+    if (!HARD) sum_1 = sum_t;
     float loss = 0;
-    const float log_t = logf(sum_t);
-    if (taught) {
-        float whole = total[4], d = total[5];
-        if (whole != 0.0f) d += whole * ((m - mx) * a.inv_t);
-        if (REST) {
-            const float e0 = factor(rest, mu, a.c1);
-            if (e0 != 0.0f) d += e0 * ((rest - mu) - ((other - m) * a.inv_t + logf(other_t)));
-            whole += e0;
+    if (REST && taught) {
+        // Both sides are whole distributions over the kept classes and the others: sum p (log p - log q) is the sum of
+        // q - p - p delta, delta = log q - log p, whose terms are all positive, p delta^2 / 2 for a small delta; summed as they stand
+        // the logarithms would cancel where student and teacher agree.
+        const float e0 = factor(rest, mu, a.c1), whole = total[4] + e0, per_t = 1.0f / sum_t, level = logf(sum_t / whole);
+        const auto term = [](float p, float q, float delta, bool with_q) {
+            if (p == 0.0f) return with_q ? q : 0.0f;
+            if (with_q && fabsf(delta) < 0.25f)       // (e^delta - 1 - delta) / (delta^2 / 2) by its series, to delta^7 / 181440
+                return p * delta * delta * fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, 1.0f / 40320, 1.0f / 5040), 1.0f / 720),
+                                                                                   1.0f / 120), 1.0f / 24), 1.0f / 6), 0.5f);
+            return (with_q ? q : 0.0f) - fmaf(p, delta, p);
+        };
+        float kl[1] = {0};
+        if (at >= 0) kl[0] = term(e / whole, power(x, reference(m), a.ct) * per_t, (x - m) * a.inv_t - (u - mu) - level, once);
+        if (g.lane == 0) {
+            const float others = other_t * factor(other, m, a.ct);      // (of nothing: 0 times 0)
+            // log p_0 and log q_0 as those of one minus what the kept classes have, and by their exponents where hardly
+            // anything is left, or less than fp32 holds
+            const float log_p = e0 > 1e-30f ? -log1pf(total[4] / e0) : (rest - mu) - logf(whole);
+            const float log_q = others > 1e-30f ? -log1pf(kept_t / others) : (other - m) * a.inv_t + logf(other_t) - logf(sum_t);
+            const float delta = log_q - log_p;
+            kl[0] += term(e0 / whole, others * per_t, delta, true);
         }
-        loss = a.soft_loss * (d / whole - logf(whole) + log_t);
+        g.sum(kl);
+        loss = a.soft_loss * kl[0];
+    }
+    if (g.lane) return;
+    if (!REST && taught) {
+        const float whole = total[4], d = fmaf(whole, (m - mx) * a.inv_t, total[5]);
+        loss = a.soft_loss * (d / whole - logf(whole) + logf(sum_t));
     }
     if (label >= 0) loss += a.hard * (logf(sum_1) - (widen(s[label]) - m));
     a.loss[row] = loss;
@@ -241,13 +271,13 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
     out[4] = other_t;
 }
 
-template <typename T, bool REST, bool TWO>
+template <typename T, bool REST, int HARD>
 cudaError_t launch(DistillArgs a, cudaStream_t st) {
     constexpr int W = 16 / sizeof(T);
     if (a.classes <= kMostOfWarp && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
         a.parts = 1;
         const size_t smem = REST ? kRowsOfCta * ((kMostOfWarp + 2 * W) / 32 + 1) * 4 : 0;
-        distill_rows<T, REST, TWO, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, smem, st>>>(a);
+        distill_rows<T, REST, HARD, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, smem, st>>>(a);
         return cudaGetLastError();
     }
     // few long rows: a cluster of CTAs has one
@@ -260,7 +290,7 @@ cudaError_t launch(DistillArgs a, cudaStream_t st) {
         int dev = 0;
         if (const cudaError_t e = cudaGetDevice(&dev)) return e;
         if (dev >= 64 || !(allowed.load() >> dev & 1)) {
-            if (const cudaError_t e = cudaFuncSetAttribute(distill_rows<T, REST, TWO, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+            if (const cudaError_t e = cudaFuncSetAttribute(distill_rows<T, REST, HARD, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                            kMostClasses / 8 + 64)) {
                 cudaGetLastError();
                 return e;
@@ -279,15 +309,21 @@ cudaError_t launch(DistillArgs a, cudaStream_t st) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.parts > 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, distill_rows<T, REST, TWO, kWide>, a), l = cudaGetLastError();
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, distill_rows<T, REST, HARD, kWide>, a), l = cudaGetLastError();
     return e != cudaSuccess ? e : l;
 }
 
+template <typename T, bool REST>
+cudaError_t forward(const DistillArgs& a, cudaStream_t st) {
+    const float t = a.c1 / a.ct;
+    if (!a.labels || t == 1.0f) return launch<T, REST, kNoHard>(a, st);
+    if (t == 2.0f) return launch<T, REST, kSquare>(a, st);
+    if (t == 4.0f) return launch<T, REST, kFourth>(a, st);
+    return launch<T, REST, kApart>(a, st);
+}
 template <typename T>
 cudaError_t forward(const DistillArgs& a, cudaStream_t st) {
-    const bool two = a.labels && a.ct != a.c1;        // at T = 1 both sums are one
-    if (a.rest) return two ? launch<T, true, true>(a, st) : launch<T, true, false>(a, st);
-    return two ? launch<T, false, true>(a, st) : launch<T, false, false>(a, st);
+    return a.rest ? forward<T, true>(a, st) : forward<T, false>(a, st);
 }
 
 int check(const void* s, int64_t stride, int dtype, int64_t rows, int64_t classes, int kept, const void* values, int value_type,

@@ -3,16 +3,15 @@
 //
 // Values are compared as keys, integers in the same order: -0 and 0 are one, a NaN is above everything.
 // A row is read once and kept in shared memory where it fits (a cluster of CTAs has a long row, each its slice).
-//   1. A thread takes the largest of its values.  With j = ceil((k + 1) / warps), the least of the warps' j-th largest
-//      thread maxima is a bound that at least k + 1 values reach, and few more on rows in no special order.
-//   2. The values that reach it are listed, and each one's rank among them is counted.  That orders the first k, and
-//      the one after them is the largest of the others.
-//   3. The others' exponentials, relative to that one, are summed.
+//   1. A thread takes the largest of its values.  A bound that at least k + 1 of these reach, and not many more, is found
+//      by halving their range and counting: at least k + 1 values of the row reach it, and few more on rows in no special order.
+//   2. The values that reach it are listed, the exponentials of all others summed relative to it.
+//   3. The listed values' ranks are counted: that orders the first k, and those after them join the others' sum, in order.
 // Where more values reach the bound than the list holds (many equal ones, or the large ones all in a few threads'
 // places), the (k + 1)-th in order is found by halving the keys' range, and the places' among its equals: 32 and at
 // most 20 countings, which any row ends after.
 //
-// What bounds it is memory, then the three readings of shared memory.
+// What bounds it is memory, then the two readings of shared memory.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -49,39 +48,48 @@ __device__ __forceinline__ int key_of(float x) {
 __device__ __forceinline__ float of_key(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
 constexpr int kLeast = INT_MIN;       // below every key
 
-// the j-th largest (from 1) of the lanes' keys: a sorting network over the warp, the largest in lane 0
-__device__ __forceinline__ int sorted(int x) {
-    const int lane = threadIdx.x % 32;
-#pragma unroll
-    for (int size = 2; size <= 32; size *= 2)
-#pragma unroll
-        for (int step = size / 2; step; step /= 2) {
-            const int y = __shfl_xor_sync(0xffffffffu, x, step);
-            const bool larger_first = (lane & size) == 0, lower = (lane & step) == 0;
-            x = larger_first == lower ? max(x, y) : min(x, y);
-        }
-    return x;
+// The largest of values as they come, a NaN above all: packed where two share a register.
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+template <int W>
+__device__ __forceinline__ float largest(const Vec<float, W>& v) {
+    return larger(larger(v.v[0], v.v[1]), larger(v.v[2], v.v[3]));
+}
+template <int W>
+__device__ __forceinline__ float largest(const Vec<__half, W>& v) {
+    __half2 h[4];
+    memcpy(h, &v, 16);
+    const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+    return larger(__low2float(m), __high2float(m));
+}
+template <int W>
+__device__ __forceinline__ float largest(const Vec<__nv_bfloat16, W>& v) {
+    __nv_bfloat162 h[4];
+    memcpy(h, &v, 16);
+    const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+    return larger(__low2float(m), __high2float(m));
 }
 
 // what the CTAs of a row tell one another
 struct Shared {
-    unsigned long long list[kList];   // (key, ~place) of the values that reach the bound; the first CTA's: of all CTAs
-    int bound[kClusterMost * 16];     // each warp's, from all CTAs
-    int warps[kClusterMost];          // warps that gave a bound, of each CTA
-    int counts[kClusterMost];
+    unsigned long long list[kList];   // (key, ~place) of the values that reach the bound; the first CTA's, of all CTAs
+    float after[kList];               // of those the ones after the k-th, in order
+    int found;                        // how many (the first CTA's)
+    int bounds[kClusterMost];
     int counted[2][kClusterMost];
-    float sums[kClusterMost];
-    int found, count;
-    unsigned long long after, bottom; // the (k + 1)-th, and the last that is kept
+    float sums[kClusterMost];         // of the values that are not listed (the first CTA's)
 };
 
 template <typename T, int N>
-__global__ void __launch_bounds__(N) top_rows(TopArgs a) {
+__global__ void __launch_bounds__(N, N == 512 ? 3 : 8) top_rows(TopArgs a) {
     constexpr int W = 16 / sizeof(T), kWarps = N / 32, U = 4;
     extern __shared__ uint4 dynamic[];
     __shared__ Shared sh;
     __shared__ float scratch[2 * kWarps * 8];
-    __shared__ int warp_counts[2][kWarps];
+    __shared__ int warp_counts[2][kWarps], warp_ends[2][kWarps];
     cg::cluster_group cluster = cg::this_cluster();
     const int part = blockIdx.x % a.parts, row = blockIdx.x / a.parts, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const T* s = static_cast<const T*>(a.s) + row * a.stride;
@@ -99,108 +107,116 @@ __global__ void __launch_bounds__(N) top_rows(TopArgs a) {
 
     // 1. the largest of each thread's values; all of the slice goes to shared memory
     if (threadIdx.x == 0) sh.found = 0;
-    int most = kLeast;
-    const auto edge = [&](int v) {                    // a vector of which the row has a part: the rest lies outside
+    float most = kNone;
+    const auto edge = [&](int v) {                    // a vector of which the row has a part: nothing beside it
         Vec<T, W> b;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             const int place = v * W + i;
-            b.v[i] = place >= r.pad && place < r.end ? r.base[place] : T(0.0f);
+            b.v[i] = place >= r.pad && place < r.end ? r.base[place] : T(kNone);
         }
         return b;
-    };
-    const auto see = [&](const Vec<T, W>& b, int v, bool whole) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const int key = key_of(widen(b.v[i]));
-            if (whole || (v * W + i >= r.pad && v * W + i < r.end)) most = max(most, key);
-        }
-        if (a.held) held[v - first] = b;
     };
     int v = first + threadIdx.x;
     for (; v + (U - 1) * N < last; v += U * N) {
         Vec<T, W> b[U];
-        bool whole[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) b[k] = r.whole(v + k * N) ? r.at(v + k * N) : edge(v + k * N);
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            whole[k] = r.whole(v + k * N);
-            b[k] = whole[k] ? r.at(v + k * N) : edge(v + k * N);
+            most = larger(most, largest(b[k]));
+            if (a.held) held[v + k * N - first] = b[k];
         }
-#pragma unroll
-        for (int k = 0; k < U; ++k) see(b[k], v + k * N, whole[k]);
     }
     for (; v < last; v += N) {
-        const bool whole = r.whole(v);
-        see(whole ? r.at(v) : edge(v), v, whole);
+        const Vec<T, W> b = r.whole(v) ? r.at(v) : edge(v);
+        most = larger(most, largest(b));
+        if (a.held) held[v - first] = b;
     }
 
-    // the bound
-    const auto full_warps = [&](int p) {              // warps of part p whose lanes all have a whole vector
-        const int n = min(r.vectors(), (p + 1) * each) - min(r.vectors(), p * each) - 2;
-        return n < 0 ? 0 : min(kWarps, n / 32);
-    };
-    int warps = 0;
-    for (int p = 0; p < a.parts; ++p) warps += full_warps(p);
-    const int j = warps ? (wanted + warps - 1) / warps : 33;
-    const int order = sorted(most);
-    if (a.parts > 1) cluster.sync();                  // every CTA has begun: its memory can be written
-    if (lane == min(j, 32) - 1)
-        for (int p = 0; p < a.parts; ++p) of(p)->bound[part * kWarps + warp] = j <= 32 && warp < full_warps(part) ? order : INT_MAX;
-    everyone();
-    int bound = INT_MAX;
-    for (int w = lane; w < a.parts * kWarps; w += 32) bound = min(bound, sh.bound[w]);
-    bound = __reduce_min_sync(0xffffffffu, bound);
-    if (bound == INT_MAX) bound = kLeast;             // too few values for one
-
-    // f(key, place) for each of the slice's values; from place on the row's own count
-    const auto each_value = [&](auto&& f) {
-        for (int v = first + threadIdx.x; v < last; v += N) {
-            const bool whole = r.whole(v);
-            const Vec<T, W> b = a.held ? held[v - first] : whole ? r.at(v) : edge(v);
-#pragma unroll
-            for (int i = 0; i < W; ++i)
-                if (whole || (v * W + i >= r.pad && v * W + i < r.end)) f(widen(b.v[i]), v * W + i - r.pad);
+    // the bound: this CTA's share of the values wanted reach it here, so that all of them do where the least of the CTAs' does
+    const int share = (wanted + a.parts - 1) / a.parts, own = min(N, last - first);
+    const int key = (int)threadIdx.x < own ? key_of(most) : kLeast;
+    int bound = kLeast;
+    {
+        const int high_lane = __reduce_max_sync(0xffffffffu, key), low_lane = __reduce_min_sync(0xffffffffu, (int)threadIdx.x < own ? key : INT_MAX);
+        if (lane == 0) warp_ends[0][warp] = low_lane, warp_ends[1][warp] = high_lane;
+        __syncthreads();
+        long long low = INT_MAX, high = INT_MIN;
+        for (int w = 0; w < kWarps; ++w) low = min(low, (long long)warp_ends[0][w]), high = max(high, (long long)warp_ends[1][w]);
+        ++high;                                       // `share` of them reach low, and not high
+        if (own >= share) {
+            for (int k = 0; k < 20 && high - low > 1; ++k) {
+                const int middle = (int)((low + high) >> 1), n = __syncthreads_count(key >= middle);
+                if (n >= share)
+                    low = middle;
+                else
+                    high = middle;
+                if (n >= share && n <= share + max(2, share / 4)) break;
+            }
+            bound = (int)low;
         }
-    };
-    const auto entry = [](int key, int place) {
-        return (unsigned long long)((unsigned)key ^ 0x80000000u) << 32 | (unsigned)~place;
-    };
-    const auto list = [&](float x, int place) {
-        const int n = atomicAdd(&sh.found, 1);
-        if (n < kList) sh.list[n] = entry(key_of(x), place);
-    };
-
-    // 2. the values that reach the bound
-    const float limit = of_key(bound);
-    if (bound == kLeast)
-        each_value(list);
-    else
-        each_value([&](float x, int place) {
-            if (!(x < limit)) list(x, place);
-        });
-    __syncthreads();
-    const auto gather = [&] {                         // all CTAs' numbers of listed values, then the lists, in the first CTA
-        if (a.parts == 1) return sh.found;
-        if (threadIdx.x < a.parts) of(threadIdx.x)->counts[part] = sh.found;
+    }
+    if (a.parts > 1) {
+        cluster.sync();                               // every CTA has begun: its memory can be written
+        if (threadIdx.x < a.parts) of(threadIdx.x)->bounds[part] = bound;
         cluster.sync();
-        int all = 0, before = 0;
-        for (int p = 0; p < a.parts; ++p) {
-            if (p < part) before += sh.counts[p];
-            all += sh.counts[p];
+        for (int p = 0; p < a.parts; ++p) bound = min(bound, sh.bounds[p]);
+    }
+
+    // 2. what is listed: the values above key `bound`, and of those with this key the ones up to place `until`; the others' sum
+    Shared* leader = of(0);
+    Group<N> g(scratch);
+    const float2 ct = both(a.c);
+    const auto vector_at = [&](int v) { return a.held ? held[v - first] : r.whole(v) ? r.at(v) : edge(v); };
+    const auto collect = [&](int bound, int until) {
+        const float limit = of_key(bound), below = reference(limit);
+        const float2 far = both(-below);
+        float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll 2
+        for (int v = first + threadIdx.x; v < last; v += N) {
+            const Vec<T, W> b = vector_at(v);
+            if (bound != kLeast && largest(b) < limit) {               // (places beside the row hold -inf, which adds nothing)
+#pragma unroll
+                for (int i = 0; i < W / 2; ++i) {
+                    const float2 e = mul(add(pair(b, i), far), ct);
+                    sum = add(sum, make_float2(approx_exp2(e.x), approx_exp2(e.y)));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const int place = v * W + i - r.pad;
+                    if (place < 0 || place >= a.classes) continue;
+                    const float x = widen(b.v[i]);
+                    const int k = key_of(x);
+                    if (k > bound || (k == bound && place <= until)) {
+                        const int n = atomicAdd(&leader->found, 1);
+                        if (n < kList) leader->list[n] = (unsigned long long)((unsigned)k ^ 0x80000000u) << 32 | (unsigned)~place;
+                    } else {
+                        sum.x += power(x, below, a.c);
+                    }
+                }
+            }
         }
-        if (all <= kList) {
-            if (part)
-                for (int i = threadIdx.x; i < sh.found; i += N) of(0)->list[before + i] = sh.list[i];
-            cluster.sync();
-        }
-        return all;
+        float total[1] = {sum.x + sum.y};
+        g.sum(total);
+        if (threadIdx.x == 0) leader->sums[part] = total[0];
+        everyone();
+        return leader->found;
     };
-    int all = gather();
+    int all = collect(bound, INT_MAX);
     if (all > kList) {                                // the same in every CTA of the row
         int turn = 0;
         const auto counted = [&](auto&& pred) {       // how many of the row's values are so, to every thread
             int n = 0;
-            each_value([&](float x, int place) { n += pred(key_of(x), place); });
+            for (int v = first + threadIdx.x; v < last; v += N) {
+                const Vec<T, W> b = vector_at(v);
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const int place = v * W + i - r.pad;
+                    n += place >= 0 && place < a.classes && pred(key_of(widen(b.v[i])), place);
+                }
+            }
             n = __reduce_add_sync(0xffffffffu, n);
             turn ^= 1;
             if (lane == 0) warp_counts[turn][warp] = n;
@@ -234,15 +250,13 @@ __global__ void __launch_bounds__(N) top_rows(TopArgs a) {
             else
                 left = middle + 1;
         }
-        if (threadIdx.x == 0) sh.found = 0;
+        if (part == 0 && threadIdx.x == 0) sh.found = 0;
         everyone();
-        each_value([&](float x, int place) {
-            const int key = key_of(x);
-            if (key > low || (key == low && place <= left)) list(x, place);
-        });
-        __syncthreads();
-        all = gather();
+        bound = low;
+        all = collect(low, left);
     }
+
+    // 3. the listed values in order
     if (part == 0) {
         T* values = static_cast<T*>(a.values) + (int64_t)row * a.k;
         int* indices = a.indices + (int64_t)row * a.k;
@@ -255,38 +269,27 @@ __global__ void __launch_bounds__(N) top_rows(TopArgs a) {
                 const int place = (int)~(unsigned)mine;
                 values[rank] = s[place];
                 indices[rank] = place;
-                if (rank == a.k - 1) sh.bottom = mine;
-            } else if (rank == a.k) {
-                sh.after = mine;
+            } else {
+                sh.after[rank - a.k] = of_key((int)((unsigned)(mine >> 32) ^ 0x80000000u));
+            }
+        }
+        __syncthreads();
+        if (a.k == a.classes) {
+            if (threadIdx.x == 0) a.rest[row] = kNone;
+        } else {
+            const float m = sh.after[0], below = reference(m);
+            float sum[1] = {0};
+            for (int i = threadIdx.x; i < all - a.k; i += N) sum[0] += power(sh.after[i], below, a.c);
+            g.sum(sum);
+            if (threadIdx.x == 0) {
+                float others = 0;
+                for (int p = 0; p < a.parts; ++p) others += sh.sums[p];
+                if (others != 0.0f) others *= factor(of_key(bound), m, a.c);
+                a.rest[row] = fabsf(m) == INFINITY ? m : m * a.inv_t + logf(sum[0] + others);
             }
         }
     }
-    everyone();
-    // 3. the others
-    if (a.k == a.classes) {
-        if (part == 0 && threadIdx.x == 0) a.rest[row] = kNone;
-        return;
-    }
-    const Shared* leader = of(0);
-    const unsigned long long bottom = leader->bottom, after = leader->after;
-    const float last_kept = of_key((int)((unsigned)(bottom >> 32) ^ 0x80000000u)), m = of_key((int)((unsigned)(after >> 32) ^ 0x80000000u));
-    const int last_place = (int)~(unsigned)bottom;
-    const float below = reference(m);
-    float sum[1] = {0};
-    each_value([&](float x, int place) {
-        if (x < last_kept || (!(x > last_kept) && place > last_place && key_of(x) == key_of(last_kept)) ||
-            (x == x && last_kept != last_kept))
-            sum[0] += power(x, below, a.c);
-    });
-    Group<N> g(scratch);
-    g.sum(sum);
-    if (a.parts > 1) {
-        if (threadIdx.x == 0) of(0)->sums[part] = sum[0];
-        cluster.sync();
-        sum[0] = 0;
-        for (int p = 0; p < a.parts; ++p) sum[0] += sh.sums[p];
-    }
-    if (part == 0 && threadIdx.x == 0) a.rest[row] = fabsf(m) == INFINITY ? m : m * a.inv_t + logf(sum[0]);
+    if (a.parts > 1) cluster.sync();                  // the first CTA's memory has been read by the others
 }
 
 template <typename T, int N>
@@ -324,7 +327,7 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t top(const TopArgs& a, cudaStream_t st) {
-    return a.classes <= 4096 ? launch<T, 128>(a, st) : launch<T, 512>(a, st);
+    return a.classes <= 4096 && a.k < 96 ? launch<T, 128>(a, st) : launch<T, 512>(a, st);
 }
 
 }  // namespace
