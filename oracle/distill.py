@@ -148,14 +148,24 @@ def _image(t, like):
 E = 2.0 ** -19      # 32 fp32 roundings, as for the group norm
 
 
+def _hat_error(v, hat, r, kind):
+    """Of v^ in fp32.  Its own roundings and the root's are relative to |v^|.  A layer norm's mean is the sum of C distances from a
+    value near it, over C: the sum's 3 + 5 + 4 levels of additions (a thread's eight values, a warp, sixteen warps) round by
+    2^-24 of the distances' mean size each, which is at most 1 / r (the root of their mean square) and the near value's own distance,
+    at most that again for values in no special order; times r that is 12 * 2 * 2^-24 < E, whatever |v^|.  And values far from
+    zero hold their distances to 2^-24 of the mean's size alone, which E / 8 of it covers four times."""
+    if kind == "none":
+        return 0 * hat
+    return E * (np.abs(hat) + ((1 + np.abs(v.mean(-1, keepdims=True)) * r * 2.0 ** -3) if kind == "layer" else 0.0))
+
+
 def block_h(x, b, post, pw, pb, scale, gate, eps):
     """(h before it is rounded, bound of its fp32 error): x + scale gate (pw b^ + pb)."""
     v = _rows(b)
     hat, r = _hat(v, post, eps)
     f = _or(scale, 1.0) * (1.0 if gate is None else np.asarray(gate, np.float64)[:, None])
     u = _or(pw, 1.0) * hat + _or(pb, 0.0)
-    far = np.abs(v.mean(-1, keepdims=True)) * r if post == "layer" else 0.0
-    bound = E * (np.abs(f) * (np.abs(_or(pw, 1.0)) * (np.abs(hat) + far * 2.0 ** -3) + np.abs(_or(pb, 0.0)))) + U * 4 * np.abs(_rows(x))
+    bound = np.abs(f) * (np.abs(_or(pw, 1.0)) * (_hat_error(v, hat, r, post) + E * np.abs(hat)) + E * np.abs(_or(pb, 0.0))) + U * 4 * np.abs(_rows(x))
     return _image(_rows(x) + f * u, x), _image(bound + 0 * hat, x)
 
 
@@ -165,8 +175,7 @@ def block_y(h, pre, w, bias, kind, eps):
     hat, r = _hat(v, pre, eps)
     z = _or(w, 1.0) * hat + _or(bias, 0.0)
     y = act(z, kind)
-    far = np.abs(v.mean(-1, keepdims=True)) * r if pre == "layer" else 0.0
-    bound = 1.1 * E * (np.abs(_or(w, 1.0)) * (np.abs(hat) + far * 2.0 ** -3) + np.abs(_or(bias, 0.0))) + E * np.abs(y)
+    bound = 1.1 * (np.abs(_or(w, 1.0)) * _hat_error(v, hat, r, pre) + E * np.abs(_or(bias, 0.0))) + E * np.abs(y)
     return _image(y, h), _image(bound, h)
 
 
@@ -188,13 +197,10 @@ def block_backward(dh, dy, h, b, post, pw, pb, scale, gate, pre, w, bias, kind, 
         e = r * (g_e + a_e + np.abs(hat) * c_e + hat_e * np.abs(c) + E * (np.abs(g) + np.abs(a) + np.abs(hat * c)))
         return full, e
 
-    def errors(v, hat, r, layer):
-        return E * (np.abs(hat) + (np.abs(v.mean(-1, keepdims=True)) * r * 2.0 ** -3 if layer else 0.0))
-
     if dy is not None and pre != "none":
         v = _rows(h)
         hat, r = _hat(v, pre, eps)
-        hat_e = errors(v, hat, r, pre == "layer")
+        hat_e = _hat_error(v, hat, r, pre)
         z = _or(w, 1.0) * hat + _or(bias, 0.0)
         g = _rows(dy)
         dz = g * slope(z, kind)
@@ -211,7 +217,7 @@ def block_backward(dh, dy, h, b, post, pw, pb, scale, gate, pre, w, bias, kind, 
         return out, bound
     v = _rows(b)
     hat, r = _hat(v, post, eps)
-    hat_e = errors(v, hat, r, post == "layer") if post != "none" else 0 * hat
+    hat_e = _hat_error(v, hat, r, post)
     sc = _or(scale, 1.0) * np.ones(h.shape[1])
     ga = np.ones((n, h.shape[1])) if gate is None else np.asarray(gate, np.float64)
     pwv, pbv = _or(pw, 1.0) * np.ones(h.shape[1]), _or(pb, 0.0) * np.ones(h.shape[1])

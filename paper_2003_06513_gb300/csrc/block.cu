@@ -146,7 +146,7 @@ int check_shape(const Shape& s) {
 int check_input(const Shape& s, const Input& t) {
     if (!t.p) return PP_ERR_NULL;
     if (off(t.p, t.es)) return PP_ERR_ALIGN;
-    if ((s.pixels > 1 && t.pixel < s.C) || (s.N > 1 && t.sample < 0) || t.pixel > (int64_t(1) << 40) || t.sample > (int64_t(1) << 50))
+    if ((s.pixels > 1 && t.pixel < s.C) || (s.N > 1 && t.sample < 0) || t.pixel > INT_MAX || t.sample > (int64_t(1) << 50))
         return PP_ERR_SHAPE;
     return PP_OK;
 }
@@ -186,9 +186,13 @@ BlockArgs args_of(const Shape& s, const float* post_weight, const float* post_bi
     a.pixels_shift = 31 + bits;
     a.pixels_mul = s.pixels > 1 ? (uint32_t)(((uint64_t(1) << a.pixels_shift) + s.pixels - 1) / s.pixels) : 0;
     a.threads = row_threads(s.C);
+    a.ragged = a.threads * kBlockEight != s.C;
+    a.flat = a.dense = 1;
     return a;
 }
 void set(BlockArgs& a, const void* BlockArgs::*p, int64_t BlockArgs::*pixel, int64_t BlockArgs::*sample, const Input& t) {
+    if (t.p && a.N > 1 && t.sample != a.pixels * t.pixel) a.flat = 0;
+    if (t.p && !t.dense(Shape{0, 0, a.N, a.C, a.pixels})) a.dense = 0;
     a.*p = t.p;
     a.*pixel = t.pixel;
     a.*sample = t.sample;

@@ -19,6 +19,11 @@ namespace {
 
 constexpr int E = kBlockEight;
 
+// Forms of the kernels.  kLong: a CTA has one row, of whole warps.  kShort: several rows, of a power of two of threads each.
+// 8, 16, 32: the same with so many threads, known beforehand, on dense tensors in vectors of eight channels: with loops
+// that unroll and one offset for all tensors a row takes half the instructions, which bound the kernels before memory does.
+enum { kLong = -1, kShort = 0 };
+
 // eight channels of a row: V adjacent ones, then those `threads` vectors on, and so on
 struct Eight {
     float2 v[E / 2];
@@ -39,21 +44,18 @@ struct Ahead {
     static constexpr int S = sizeof(T) * V > 16 ? 16 : sizeof(T) * V, P = E * (int)sizeof(T) / S;
     static constexpr bool kAsync = S >= 4;
     static constexpr int kBytes = kAsync ? E * (int)sizeof(T) : 0;       // of a thread and round
-    // bytes from the row's first channel to piece k, and whether the row has it
-    static __device__ __forceinline__ int64_t offset(int lane, const BlockArgs& a, int k) {
-        return sizeof(T) * V > 16 ? (int64_t)lane * V * sizeof(T) + k * S : (int64_t)(lane + k * a.threads) * S;
-    }
-    static __device__ __forceinline__ bool has(int lane, const BlockArgs& a, int k) {
-        return (sizeof(T) * V > 16 ? lane : lane + k * a.threads) < a.vectors;
-    }
-    static __device__ __forceinline__ void ask(uint32_t place, const T* row, int lane, const BlockArgs& a, bool there) {
+    // channels from the thread's first one to piece k
+    static __device__ __forceinline__ int apart(int threads, int k) { return sizeof(T) * V > 16 ? k * (S / (int)sizeof(T)) : k * threads * V; }
+    // the thread's own channels from `mine` on, those that `live(k)` says are there; what is not copied becomes 0
+    template <typename Live>
+    static __device__ __forceinline__ void ask(uint32_t place, const T* mine, int threads, Live&& live) {
         if constexpr (kAsync) {
 #pragma unroll
             for (int k = 0; k < P; ++k) {
-                const bool wanted = there && has(lane, a, k);
-                const char* from = reinterpret_cast<const char*>(row) + (wanted ? offset(lane, a, k) : 0);
+                const bool wanted = live(sizeof(T) * V > 16 ? 0 : k);
+                const T* from = wanted ? mine + apart(threads, k) : mine;
                 const uint32_t to = place + (k * blockDim.x + threadIdx.x) * S;
-                const int n = wanted ? S : 0;          // what is not copied becomes 0
+                const int n = wanted ? S : 0;
                 if constexpr (S == 16)
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
                 else
@@ -61,17 +63,28 @@ struct Ahead {
             }
         }
     }
-    static __device__ __forceinline__ Raw<T, V> get(const char* place, const T* row, int lane, const BlockArgs& a, bool there) {
+    template <typename Live>
+    static __device__ __forceinline__ Raw<T, V> get(uint32_t place, const T* mine, int threads, Live&& live) {
         Raw<T, V> r;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             char* to = reinterpret_cast<char*>(&r) + k * S;
-            if constexpr (kAsync) {
-                Vec<char, S> v = *reinterpret_cast<const Vec<char, S>*>(place + (k * blockDim.x + threadIdx.x) * S);
-                memcpy(to, &v, S);
+            const uint32_t from = place + (k * blockDim.x + threadIdx.x) * S;
+            if constexpr (S == 16) {
+                uint4 v;
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+                memcpy(to, &v, 16);
+            } else if constexpr (S == 8) {
+                uint2 v;
+                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(from) : "memory");
+                memcpy(to, &v, 8);
+            } else if constexpr (S == 4) {
+                uint32_t v;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
+                memcpy(to, &v, 4);
             } else {
                 T v = T(0.0f);
-                if (there && has(lane, a, k)) v = row[lane + k * a.threads];
+                if (live(k)) v = mine[apart(threads, k)];
                 memcpy(to, &v, S);
             }
         }
@@ -112,13 +125,12 @@ __device__ __forceinline__ Raw<T, V> narrowed(const Eight& e) {
     }
     return r;
 }
-template <typename T, int V>
-__device__ __forceinline__ void put(T* row, const Raw<T, V>& r, int lane, const BlockArgs& a, bool there) {
+template <typename T, int V, typename Live>
+__device__ __forceinline__ void put(T* mine, const Raw<T, V>& r, int threads, Live&& live) {
 #pragma unroll
     for (int j = 0; j < E / V; ++j) {
-        const int at = lane + j * a.threads;
-        if (!there || at >= a.vectors) continue;
-        T* p = row + (int64_t)at * V;
+        if (!live(j)) continue;
+        T* p = mine + j * threads * V;
         if constexpr (sizeof(T) * V > 16) {
             float4 lo, hi;
             memcpy(&lo, &r.v[j], 16);
@@ -146,21 +158,38 @@ __device__ __forceinline__ Eight parameter(const float* p, float otherwise, int 
 template <int V>
 __device__ __forceinline__ bool inside(int lane, const BlockArgs& a, int k) { return lane + k / V * a.threads < a.vectors; }
 
-// Sums over a row's threads, to all of them, in a fixed order.  WIDE: the CTA is one row's.
-template <bool WIDE>
+template <int V>
+__device__ __forceinline__ float own_channels(int lane, const BlockArgs& a) {
+    int n = 0;
+    for (int k = 0; k < E; ++k) n += inside<V>(lane, a, k);
+    return (float)n;
+}
+
+// Sums over a row's threads, to all of them, in a fixed order.
+template <int FORM>
 struct RowSum {
+    static constexpr bool WIDE = FORM == kLong;
     int threads;
-    float2* scratch;                                  // WIDE: 2 x 32
+    float* scratch;                                   // kLong: 2 x 64
     int turn = 0;
-    template <int K>
-    __device__ __forceinline__ void all(float2 (&s)[K]) {
-        const int span = WIDE ? 32 : threads;
-        for (int o = 1; o < span; o *= 2)
+    template <typename T, int K>
+    __device__ __forceinline__ void over_lanes(T (&s)[K]) const {
+        if constexpr (FORM == kShort) {
+            for (int o = 1; o < threads; o *= 2)
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                s[k] = add(s[k], make_float2(__shfl_xor_sync(0xffffffffu, s[k].x, o), __shfl_xor_sync(0xffffffffu, s[k].y, o)));
+                for (int k = 0; k < K; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+        } else {
+#pragma unroll
+            for (int o = 1; o < (FORM == kLong ? 32 : FORM); o *= 2)
+#pragma unroll
+                for (int k = 0; k < K; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+        }
+    }
+    template <int K>
+    __device__ __forceinline__ void all(float (&s)[K]) {
+        over_lanes(s);
         if (WIDE) {
-            float2* mine = scratch + turn * 32;
+            float* mine = scratch + turn * 64;
             turn ^= 1;                                // in turns: one barrier a sum
             if (threadIdx.x % 32 == 0)
 #pragma unroll
@@ -170,21 +199,32 @@ struct RowSum {
             for (int k = 0; k < K; ++k) s[k] = mine[k];
             for (int w = 1; w < threads / 32; ++w)
 #pragma unroll
-                for (int k = 0; k < K; ++k) s[k] = add(s[k], mine[w * K + k]);
+                for (int k = 0; k < K; ++k) s[k] += mine[w * K + k];
         }
     }
-    __device__ __forceinline__ float2 operator()(float2 s) {
-        float2 v[1] = {s};
-        all(v);
+    // near the mean of a row: of a short row the mean of its first thread's values, of a long one the mean but for its rounding
+    __device__ __forceinline__ void near(float (&s)[2], float inv_own, float inv_c) {
+        if (WIDE) {
+            all(s);
+            s[0] *= inv_c, s[1] *= inv_c;
+        } else {
+            const int first = threadIdx.x % 32 & ~(threads - 1);
+            s[0] = __shfl_sync(0xffffffffu, s[0] * inv_own, first);
+            s[1] = __shfl_sync(0xffffffffu, s[1] * inv_own, first);
+        }
+    }
+    __device__ __forceinline__ float near(float s, float inv_own, float inv_c) {
+        float v[2] = {s, 0.0f};
+        near(v, inv_own, inv_c);
         return v[0];
     }
-    __device__ __forceinline__ float operator()(float s) { return (*this)(make_float2(s, 0.0f)).x; }
     // the same in 64 bits, of one value; every thread of the CTA calls it
     __device__ __forceinline__ double exactly(double s) {
-        const int span = WIDE ? 32 : threads;
-        for (int o = 1; o < span; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+        double v[1] = {s};
+        over_lanes(v);
+        s = v[0];
         if (WIDE) {
-            double* mine = reinterpret_cast<double*>(scratch + turn * 32);
+            double* mine = reinterpret_cast<double*>(scratch + turn * 64);
             turn ^= 1;
             if (threadIdx.x % 32 == 0) mine[threadIdx.x / 32] = s;
             __syncthreads();
@@ -207,21 +247,24 @@ __device__ __forceinline__ float dot(const Eight& p, const Eight& q) {
 template <int V>
 __device__ __forceinline__ void centre(Eight& e, float mean, int lane, const BlockArgs& a) {
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-        e.v[i] = add(e.v[i], both(-mean));
-        if (!inside<V>(lane, a, 2 * i)) e.v[i].x = 0.0f;
-        if (!inside<V>(lane, a, 2 * i + 1)) e.v[i].y = 0.0f;
-    }
+    for (int i = 0; i < E / 2; ++i) e.v[i] = add(e.v[i], both(-mean));
+    if (a.ragged)
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            if (!inside<V>(lane, a, 2 * i)) e.v[i].x = 0.0f;
+            if (!inside<V>(lane, a, 2 * i + 1)) e.v[i].y = 0.0f;
+        }
 }
-// From the sums over a row of what was centred (or, of a norm by the root of the mean square, of the values) and of its squares:
-// v^ = root v + shift.  The mean that was taken out is off by its own rounding, which here comes out too: a row of equal
-// values is 0, and one far from zero keeps its spread.
+// From the sums over a row of its values and of their squares -- of a layer norm, of their distances from a value near the
+// mean: v^ = root v + shift.  The first thread's mean is near enough: its square from the mean is at most a thread's
+// share of the row's sum of squares, so that the difference loses at most five bits in rows of 256 channels, and with
+// values in no special order none.  A row of equal values is 0, and one far from zero keeps its spread.
 struct Scaling {
     float root, shift;
     __device__ __forceinline__ Scaling(int kind, float total, float square, const BlockArgs& a) {
         const float left = kind == PP_NORM_LAYER ? total * a.inv_c : 0.0f;
-        root = kind == PP_NORM_NONE ? 1.0f : rsqrtf(fmaf(-left, left, fmaf(square, a.inv_c, a.eps)));
-        shift = kind == PP_NORM_LAYER ? -left * root : 0.0f;
+        root = kind == PP_NORM_NONE ? 1.0f : rsqrtf(fmaxf(fmaf(-left, left, square * a.inv_c), 0.0f) + a.eps);
+        shift = -left * root;
     }
 };
 
@@ -232,30 +275,40 @@ __device__ __forceinline__ At at_row(int row, const BlockArgs& a) {
     const int n = a.pixels == 1 ? row : (int)((uint64_t)(uint32_t)row * a.pixels_mul >> a.pixels_shift);
     return {n, row - n * (int)a.pixels};
 }
-template <typename T>
-__device__ __forceinline__ const T* row_of(const void* p, At at, int64_t pixel, int64_t sample) {
-    return static_cast<const T*>(p) + at.sample * sample + at.pixel * pixel;
-}
-template <typename T>
-__device__ __forceinline__ T* dense_row(void* p, int row, const BlockArgs& a) {
-    return static_cast<T*>(p) + (int64_t)row * a.C;
+// the same, or, where every tensor's samples follow one another as its pixels do, all as one sample
+__device__ __forceinline__ At place_of(int row, const BlockArgs& a) { return a.flat ? At{0, row} : at_row(row, a); }
+// Where a row's channels are: of a dense tensor `offset` channels from the first, of others by their strides.
+struct Spot {
+    At at;
+    int64_t offset;
+};
+template <bool DENSE, typename T>
+__device__ __forceinline__ const T* spot_in(const void* p, const Spot& s, int64_t pixel, int64_t sample, int lane_first) {
+    if (DENSE) return static_cast<const T*>(p) + s.offset;
+    return static_cast<const T*>(p) + s.at.sample * sample + (int64_t)s.at.pixel * (int)pixel + lane_first;
 }
 
 __device__ __forceinline__ float act_of(float z, int act) {
-    if (act == PP_ACT_RELU) return z != z ? z : fmaxf(z, 0.0f);
+    if (act == PP_ACT_RELU) {
+        float y;
+        asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(z));
+        return y;
+    }
     if (act == PP_ACT_SILU) return z * approx_rcp(1.0f + approx_exp2(-1.4426950408889634f * z));
     return z;
 }
 
 // -------------------------------------------------------------------------------- forward
 
-template <typename TX, typename TB, int V, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 3) block_rows(BlockArgs a) {
+template <typename TX, typename TB, int V, int FORM>
+__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 3) block_rows(BlockArgs a) {
+    constexpr bool WIDE = FORM == kLong, DENSE = FORM > 0;
     extern __shared__ __align__(16) char ring[];
-    __shared__ float2 scratch[WIDE ? 64 : 1];
-    const int lane = WIDE ? threadIdx.x : threadIdx.x % a.threads;
-    const int here = WIDE ? 1 : kBlockThreads / a.threads, mine = WIDE ? 0 : threadIdx.x / a.threads;
-    RowSum<WIDE> sum{a.threads, scratch};
+    __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
+    const int threads = FORM > 0 ? FORM : a.threads;
+    const int lane = WIDE ? threadIdx.x : threadIdx.x % threads;
+    const int here = WIDE ? 1 : kBlockThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
+    RowSum<FORM> sum{threads, scratch};
     // the block's weight and bias with the residual scale in them, the stream's
     Eight wb = parameter<V>(a.post_weight, 1.0f, lane, a), bb = parameter<V>(a.post_bias, 0.0f, lane, a);
     const Eight sc = parameter<V>(a.scale, 1.0f, lane, a);
@@ -264,61 +317,73 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 3) bloc
     for (int i = 0; i < E / 2; ++i) wb.v[i] = mul(wb.v[i], sc.v[i]), bb.v[i] = mul(bb.v[i], sc.v[i]);
     Eight gate = parameter<V>(nullptr, 1.0f, lane, a);
     int gate_of = -1;
+    const float inv_own = 1.0f / own_channels<V>(lane, a);
 
     using X = Ahead<TX, V>;
     using B = Ahead<TB, V>;
-    const int step = gridDim.x * here;
+    const int step = gridDim.x * here, first = blockIdx.x * here + mine;
+    const int64_t stride = (int64_t)step * a.C;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const int round = (X::kBytes + B::kBytes) * blockDim.x, b_at = X::kBytes * blockDim.x;
-    const auto ask = [&](int row, int slot) {
+    const auto spot_of = [&](int row, bool there, int64_t offset) { return Spot{DENSE ? At{0, 0} : place_of(there ? row : 0, a), offset}; };
+    const auto x_in = [&](const Spot& s) { return spot_in<DENSE, TX>(a.x, s, a.x_pixel, a.x_sample, lane * V); };
+    const auto b_in = [&](const Spot& s) { return spot_in<DENSE, TB>(a.b, s, a.b_pixel, a.b_sample, lane * V); };
+    const bool in_row = lane < a.vectors;             // (V = 8)
+    const auto live_if = [&](bool there) {
+        return [=, &a](int k) { return there && (V == 8 ? in_row : lane + k * threads < a.vectors); };
+    };
+    const auto ask = [&](int row, int64_t offset, int slot) {
         if (row - mine < a.rows) {                    // (of the CTA's first row: the same for all)
             const bool there = row < a.rows;
-            const At at = at_row(there ? row : 0, a);
-            X::ask(ring_at + slot * round, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
-            if (a.b) B::ask(ring_at + slot * round + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there);
+            const Spot s = spot_of(row, there, there ? offset : 0);
+            X::ask(ring_at + slot * round, x_in(s), threads, live_if(there));
+            if (a.b) B::ask(ring_at + slot * round + b_at, b_in(s), threads, live_if(there));
         }
         copies_end();
     };
-    for (int k = 0; k < kRounds - 1; ++k) ask(blockIdx.x * here + k * step + mine, k);
+    int64_t offset = (int64_t)first * a.C + lane * V;
+    for (int k = 0; k < kRounds - 1; ++k) ask(first + k * step, offset + k * stride, k);
     int slot = 0;
-    for (int base = blockIdx.x * here; base < a.rows; base += step) {
-        const int row = base + mine;
+    for (int row = first; row - mine < a.rows; row += step, offset += stride) {
         const bool there = row < a.rows;
-        const At at = at_row(there ? row : 0, a);
-        ask(row + (kRounds - 1) * step, slot == 0 ? kRounds - 1 : slot - 1);     // into the places that the round before has read
+        ask(row + (kRounds - 1) * step, offset + (kRounds - 1) * stride, slot == 0 ? kRounds - 1 : slot - 1);    // where the round before has read
         copies_wait<kRounds - 1>();
-        const char* place = ring + slot * round;
+        const uint32_t place = ring_at + slot * round;
         slot = slot == kRounds - 1 ? 0 : slot + 1;
-        if (a.gate && there && at.sample != gate_of) {
-            gate = parameter<V>(a.gate + (int64_t)at.sample * a.C, 1.0f, lane, a);
-            gate_of = at.sample;
+        const auto live = live_if(there);
+        const Spot at = spot_of(row, there, offset);
+        if (a.gate) {
+            const int sample = at_row(there ? row : 0, a).sample;
+            if (there && sample != gate_of) {
+                gate = parameter<V>(a.gate + (int64_t)sample * a.C, 1.0f, lane, a);
+                gate_of = sample;
+            }
         }
-        const Raw<TX, V> rx = X::get(place, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
-        Eight h = widened(rx);
+        Eight h = widened(X::get(place, x_in(at), threads, live));
         if (a.b) {
-            Eight b = widened(B::get(place + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there));
-            if (a.post == PP_NORM_LAYER) centre<V>(b, sum(across(sum_of(b))) * a.inv_c, lane, a);
-            float2 q = make_float2(0.0f, 0.0f);
-            if (a.post != PP_NORM_NONE) q = sum(make_float2(across(sum_of(b)), dot(b, b)));
-            const Scaling r(a.post, q.x, q.y, a);
+            Eight b = widened(B::get(place + b_at, b_in(at), threads, live));
+            if (a.post == PP_NORM_LAYER) centre<V>(b, sum.near(across(sum_of(b)), inv_own, a.inv_c), lane, a);
+            float q[2] = {a.post == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f, dot(b, b)};
+            if (a.post != PP_NORM_NONE) sum.all(q);
+            const Scaling r(a.post, q[0], q[1], a);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i)
                 h.v[i] = fma(fma(fma(b.v[i], both(r.root), both(r.shift)), wb.v[i], bb.v[i]), gate.v[i], h.v[i]);
             const Raw<TX, V> out = narrowed<TX, V>(h);
-            put(dense_row<TX>(a.h, row, a), out, lane, a, there);
+            put(static_cast<TX*>(a.h) + offset, out, threads, live);
             h = widened(out);                         // the second norm is of the stream as it is stored
         }
         if (a.pre == PP_NORM_NONE) continue;
-        if (a.pre == PP_NORM_LAYER) centre<V>(h, sum(across(sum_of(h))) * a.inv_c, lane, a);
-        const float2 q = sum(make_float2(across(sum_of(h)), dot(h, h)));
-        const Scaling r(a.pre, q.x, q.y, a);
+        if (a.pre == PP_NORM_LAYER) centre<V>(h, sum.near(across(sum_of(h)), inv_own, a.inv_c), lane, a);
+        float q[2] = {a.pre == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, dot(h, h)};
+        sum.all(q);
+        const Scaling r(a.pre, q[0], q[1], a);
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-            float2 z = fma(fma(h.v[i], both(r.root), both(r.shift)), w.v[i], bias.v[i]);
-            if (a.act != PP_ACT_NONE) z = make_float2(act_of(z.x, a.act), act_of(z.y, a.act));
-            h.v[i] = z;
-        }
-        put(dense_row<TB>(a.y, row, a), narrowed<TB, V>(h), lane, a, there);
+        for (int i = 0; i < E / 2; ++i) h.v[i] = fma(fma(h.v[i], both(r.root), both(r.shift)), w.v[i], bias.v[i]);
+        if (a.act != PP_ACT_NONE)
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) h.v[i] = make_float2(act_of(h.v[i].x, a.act), act_of(h.v[i].y, a.act));
+        put(static_cast<TB*>(a.y) + offset, narrowed<TB, V>(h), threads, live);
     }
 }
 
@@ -326,9 +391,9 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 3) bloc
 
 // Whether z = w (h - mean) r + bias is above 0, where fp32 cannot tell: mean and root in 64 bits.  Every thread of the CTA
 // (WIDE) or of the warp calls it.
-template <typename TX, int V, bool WIDE>
-__device__ __noinline__ unsigned above_zero(const char* place, const TX* row, bool there, const BlockArgs& a, int lane, RowSum<WIDE>& sum) {
-    const Eight h = widened(Ahead<TX, V>::get(place, row, lane, a, there));
+template <typename TX, int V, int FORM>
+__device__ __noinline__ unsigned above_zero(uint32_t place, const TX* mine, bool there, const BlockArgs& a, int lane, RowSum<FORM>& sum) {
+    const Eight h = widened(Ahead<TX, V>::get(place, mine, sum.threads, [&](int k) { return there && inside<V>(lane, a, k * V); }));
     const float* f = reinterpret_cast<const float*>(h.v);
     double mean = 0, square = 0;
     if (a.pre == PP_NORM_LAYER) {
@@ -348,18 +413,33 @@ __device__ __noinline__ unsigned above_zero(const char* place, const TX* row, bo
     return above;
 }
 
-template <typename TX, typename TB, int V, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) block_back_rows(BlockArgs a) {
+template <typename TX, typename TB, int V, int FORM>
+__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 2) block_back_rows(BlockArgs a) {
+    constexpr bool WIDE = FORM == kLong, DENSE = FORM > 0;
     constexpr int R = kRoundsBack<TX, TB, WIDE>;
     extern __shared__ __align__(16) char ring[];
-    __shared__ float2 scratch[WIDE ? 64 : 1];
+    __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
     __shared__ float lanes_sum[WIDE ? 1 : 2 * kBlockThreads * E];
-    const int lane = WIDE ? threadIdx.x : threadIdx.x % a.threads;
-    const int here = WIDE ? 1 : kBlockThreads / a.threads, mine = WIDE ? 0 : threadIdx.x / a.threads;
-    RowSum<WIDE> sum{a.threads, scratch};
+    const int threads = FORM > 0 ? FORM : a.threads;
+    const int lane = WIDE ? threadIdx.x : threadIdx.x % threads;
+    const int here = WIDE ? 1 : kBlockThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
+    RowSum<FORM> sum{threads, scratch};
     const bool pre = a.pre != PP_NORM_NONE, post = a.post != PP_NORM_NONE;
     const Eight w = parameter<V>(a.weight, 1.0f, lane, a), bias = parameter<V>(a.bias, 0.0f, lane, a);
     const Eight zero{};
+    const float inv_own = 1.0f / own_channels<V>(lane, a);
+    float reach = 0;                                  // how near to 0 a z of this thread's may be without its sign being sure
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i)
+        reach = fmaxf(reach, fmaxf(fmaf(fabsf(w.v[i].x), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].x)),
+                                   fmaf(fabsf(w.v[i].y), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].y))));
+    reach *= 3.8147e-6f;
+    // the means over a row of t (of a layer norm) and of t v^
+    const auto means = [&](int kind, const Eight& t, const Eight& v) {
+        float q[2] = {kind == PP_NORM_LAYER ? across(sum_of(t)) : 0.0f, dot(t, v)};
+        sum.all(q);
+        return make_float2(q[0] * a.inv_c, q[1] * a.inv_c);
+    };
     Eight s_w = zero, s_b = zero, s_e = zero, s_f = zero;        // sums of dz h^, dz, and of a sample dh b^, dh
     // the sums over all samples, in shared memory: of post_weight, post_bias and scale, thread c's (WIDE: the thread's eight channels')
     constexpr int OWN = WIDE ? E : 1;
@@ -373,16 +453,26 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const int x_bytes = X::kBytes * blockDim.x, b_bytes = B::kBytes * blockDim.x, round = 2 * (x_bytes + b_bytes);
     const int d_at = 0, h_at = x_bytes, y_at = 2 * x_bytes, b_at = y_at + b_bytes;
+    const auto spot_of = [&](int row, int64_t offset) { return Spot{DENSE ? At{0, 0} : place_of(row, a), offset}; };
+    const auto h_in = [&](const Spot& s) { return spot_in<DENSE, TX>(a.x, s, a.x_pixel, a.x_sample, lane * V); };
+    const auto b_in = [&](const Spot& s) { return spot_in<DENSE, TB>(a.b, s, a.b_pixel, a.b_sample, lane * V); };
+    const auto d_in = [&](const Spot& s) { return spot_in<DENSE, TX>(a.dh, s, a.dh_pixel, a.dh_sample, lane * V); };
+    const auto y_in = [&](const Spot& s) { return spot_in<DENSE, TB>(a.dy, s, a.dy_pixel, a.dy_sample, lane * V); };
+    const bool in_row = lane < a.vectors;             // (V = 8)
+    const auto live_if = [&](bool there) {
+        return [=, &a](int k) { return there && (V == 8 ? in_row : lane + k * threads < a.vectors); };
+    };
     // asks for a round of rows, `last` the end of their sample's
-    const auto ask = [&](int base, int last, int slot) {
+    const auto ask = [&](int base, int last, int64_t offset, int slot) {
         if (base < last) {
             const bool there = base + mine < last;
-            const At at = at_row(there ? base + mine : base, a);
+            const Spot s = spot_of(there ? base + mine : base, there ? offset : 0);
+            const auto live = live_if(there);
             const uint32_t place = ring_at + slot * round;
-            if (pre) X::ask(place + h_at, row_of<TX>(a.x, at, a.x_pixel, a.x_sample), lane, a, there);
-            if (a.b) B::ask(place + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there);
-            if (pre) B::ask(place + y_at, row_of<TB>(a.dy, at, a.dy_pixel, a.dy_sample), lane, a, there);
-            if (a.dh) X::ask(place + d_at, row_of<TX>(a.dh, at, a.dh_pixel, a.dh_sample), lane, a, there);
+            if (pre) X::ask(place + h_at, h_in(s), threads, live);
+            if (a.b) B::ask(place + b_at, b_in(s), threads, live);
+            if (pre) B::ask(place + y_at, y_in(s), threads, live);
+            if (a.dh) X::ask(place + d_at, d_in(s), threads, live);
         }
         copies_end();
     };
@@ -398,62 +488,69 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) k.v[i] = mul(k.v[i], mul(sc.v[i], ga.v[i]));
 
-        for (int k = 0; k < R - 1; ++k) ask(from + k * here, to, k);
+        const int64_t stride = (int64_t)here * a.C;
+        int64_t offset = (int64_t)(from + mine) * a.C + lane * V;
+        for (int k = 0; k < R - 1; ++k) ask(from + k * here, to, offset + k * stride, k);
         int slot = 0;
-        for (int base = from; base < to; base += here) {
+        for (int base = from; base < to; base += here, offset += stride) {
             const int row = base + mine;
             const bool there = row < to;
-            const At at = at_row(there ? row : base, a);
-            ask(base + (R - 1) * here, to, slot == 0 ? R - 1 : slot - 1);
+            ask(base + (R - 1) * here, to, offset + (R - 1) * stride, slot == 0 ? R - 1 : slot - 1);
             copies_wait<R - 1>();
-            const char* place = ring + slot * round;
+            const uint32_t place = ring_at + slot * round;
             slot = slot == R - 1 ? 0 : slot + 1;
-            const TX* h_row = row_of<TX>(a.x, at, a.x_pixel, a.x_sample);
+            const auto live = live_if(there);
+            const Spot at = spot_of(there ? row : base, offset);
             Eight h = zero, b = zero;
-            if (pre) h = widened(X::get(place + h_at, h_row, lane, a, there));
-            if (a.b) b = widened(B::get(place + b_at, row_of<TB>(a.b, at, a.b_pixel, a.b_sample), lane, a, there));
+            if (pre) h = widened(X::get(place + h_at, h_in(at), threads, live));
+            if (a.b) b = widened(B::get(place + b_at, b_in(at), threads, live));
             // both norms
-            float2 mean = make_float2(0.0f, 0.0f);
+            float centres[2] = {0, 0};
             if (a.pre == PP_NORM_LAYER || a.post == PP_NORM_LAYER) {
-                mean = sum(make_float2(a.pre == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, a.post == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f));
-                mean = mul(mean, both(a.inv_c));
+                centres[0] = across(sum_of(h)), centres[1] = across(sum_of(b));
+                sum.near(centres, inv_own, a.inv_c);
             }
-            if (a.pre == PP_NORM_LAYER) centre<V>(h, mean.x, lane, a);
-            if (a.post == PP_NORM_LAYER) centre<V>(b, mean.y, lane, a);
-            float2 both_sums[2] = {make_float2(across(sum_of(h)), across(sum_of(b))), make_float2(dot(h, h), dot(b, b))};
-            if (pre || post) sum.all(both_sums);
-            const Scaling sh(a.pre, both_sums[0].x, both_sums[1].x, a), sb(a.post, both_sums[0].y, both_sums[1].y, a);
+            if (a.pre == PP_NORM_LAYER) centre<V>(h, centres[0], lane, a);
+            if (a.post == PP_NORM_LAYER) centre<V>(b, centres[1], lane, a);
+            float moments[4] = {a.pre == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, a.post == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f, dot(h, h), dot(b, b)};
+            if (pre || post) sum.all(moments);
+            const Scaling sh(a.pre, moments[0], moments[2], a), sb(a.post, moments[1], moments[3], a);
             const float2 r = there ? make_float2(sh.root, sb.root) : make_float2(0.0f, 0.0f);
             const float2 shift = there ? make_float2(sh.shift, sb.shift) : make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i)
                 h.v[i] = fma(h.v[i], both(r.x), both(shift.x)), b.v[i] = fma(b.v[i], both(r.y), both(shift.y));
             Eight d = zero;
-            if (!pre && a.dh) d = widened(X::get(place + d_at, row_of<TX>(a.dh, at, a.dh_pixel, a.dh_sample), lane, a, there));
+            if (!pre && a.dh) d = widened(X::get(place + d_at, d_in(at), threads, live));
             if (pre) {
-                Eight dz = widened(B::get(place + y_at, row_of<TB>(a.dy, at, a.dy_pixel, a.dy_sample), lane, a, there));
+                Eight dz = widened(B::get(place + y_at, y_in(at), threads, live));
                 if (a.act == PP_ACT_RELU) {
                     // fp32's z is off by less than 2^-18 of its terms' sizes (each value, the mean, and the root by some 16 roundings
-                    // of the row's sums): there the sign is taken in 64 bits
-                    bool close = false;
-                    unsigned above = 0;
-                    const float* hf = reinterpret_cast<const float*>(h.v);
-                    const float* wf = reinterpret_cast<const float*>(w.v);
-                    const float* bf = reinterpret_cast<const float*>(bias.v);
-                    const float spread = 1.0f + 2.0f * fabsf(mean.x) * r.x;
+                    // of the row's sums), |h^| is at most the root of C: where the smallest z is nearer to 0 than that the
+                    // signs are taken in 64 bits
+                    float2 z[E / 2];
+                    float least = INFINITY;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float z = fmaf(hf[e], wf[e], bf[e]);
-                        above |= (unsigned)(z > 0.0f) << e;
-                        close |= fabsf(z) <= 3.8147e-6f * (fabsf(wf[e]) * (fabsf(hf[e]) + spread) + fabsf(bf[e])) && inside<V>(lane, a, e);
+                    for (int i = 0; i < E / 2; ++i) {
+                        z[i] = fma(h.v[i], w.v[i], bias.v[i]);
+                        least = fminf(least, fminf(fabsf(z[i].x), fabsf(z[i].y)));
                     }
-                    close = close && there;
-                    if (WIDE ? __syncthreads_or(close) : __any_sync(0xffffffffu, close)) 
-                        above = above_zero<TX, V, WIDE>(place + h_at, h_row, there, a, lane, sum);
-                    float* f = reinterpret_cast<float*>(dz.v);
+                    const float spread = 1.0f + 2.0f * fabsf(a.pre == PP_NORM_LAYER ? centres[0] * r.x : 0.0f);
+                    const bool close = there && least <= reach * spread;
+                    if (WIDE ? __syncthreads_or(close) : __any_sync(0xffffffffu, close)) {
+                        const unsigned above = above_zero<TX, V, FORM>(place + h_at, h_in(at), there, a, lane, sum);
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (!(above >> e & 1)) f[e] = 0.0f;
+                        for (int i = 0; i < E / 2; ++i) {
+                            if (!(above >> (2 * i) & 1)) dz.v[i].x = 0.0f;
+                            if (!(above >> (2 * i + 1) & 1)) dz.v[i].y = 0.0f;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < E / 2; ++i) {
+                            if (!(z[i].x > 0.0f)) dz.v[i].x = 0.0f;
+                            if (!(z[i].y > 0.0f)) dz.v[i].y = 0.0f;
+                        }
+                    }
                 } else if (a.act == PP_ACT_SILU) {
 #pragma unroll
                     for (int i = 0; i < E / 2; ++i) {
@@ -470,30 +567,27 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
                     s_b.v[i] = add(dz.v[i], s_b.v[i]);
                     t.v[i] = mul(dz.v[i], w.v[i]);
                 }
-                float2 q = sum(make_float2(a.pre == PP_NORM_LAYER ? across(sum_of(t)) : 0.0f, dot(t, h)));
-                q = mul(q, both(a.inv_c));
-                if (a.dh) d = widened(X::get(place + d_at, row_of<TX>(a.dh, at, a.dh_pixel, a.dh_sample), lane, a, there));
+                const float2 q = means(a.pre, t, h);
+                if (a.dh) d = widened(X::get(place + d_at, d_in(at), threads, live));
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i)
                     d.v[i] = fma(fma(h.v[i], both(-q.y), add(t.v[i], both(-q.x))), both(r.x), d.v[i]);
             }
-            if (a.dx) put(dense_row<TX>(a.dx, row, a), narrowed<TX, V>(d), lane, a, there);
+            if (a.dx) put(static_cast<TX*>(a.dx) + offset, narrowed<TX, V>(d), threads, live);
             if (!a.b) continue;
             Eight t;
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
-                const float2 live = there ? d.v[i] : make_float2(0.0f, 0.0f);
-                s_e.v[i] = fma(live, b.v[i], s_e.v[i]);
-                s_f.v[i] = add(live, s_f.v[i]);
+                s_e.v[i] = fma(d.v[i], b.v[i], s_e.v[i]);     // (of no row d is 0)
+                s_f.v[i] = add(d.v[i], s_f.v[i]);
                 t.v[i] = mul(d.v[i], k.v[i]);
             }
             if (post) {
-                float2 q = sum(make_float2(a.post == PP_NORM_LAYER ? across(sum_of(t)) : 0.0f, dot(t, b)));
-                q = mul(q, both(a.inv_c));
+                const float2 q = means(a.post, t, b);
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) t.v[i] = mul(fma(b.v[i], both(-q.y), add(t.v[i], both(-q.x))), both(r.y));
             }
-            put(dense_row<TB>(a.db, row, a), narrowed<TB, V>(t), lane, a, there);
+            put(static_cast<TB*>(a.db) + offset, narrowed<TB, V>(t), threads, live);
         }
 
         // the sample's sums: of the block's norm, the gate and the scale
@@ -506,23 +600,23 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
                 const float* pf = reinterpret_cast<const float*>(s_f.v);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const int c = channel<V>(lane, a.threads, i);
-                    e_all[mine * a.threads * E + c] = pe[i];
-                    f_all[mine * a.threads * E + c] = pf[i];
+                    const int c = channel<V>(lane, threads, i);
+                    e_all[mine * threads * E + c] = pe[i];
+                    f_all[mine * threads * E + c] = pf[i];
                 }
                 __syncthreads();
             }
             const bool first = from == begin, whole = (first ? start.pixel == 0 : true) && (to < end || at_row(end - 1, a).pixel == a.pixels - 1);
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-                const int c = WIDE ? channel<V>(lane, a.threads, i) : threadIdx.x;
+                const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x;
                 if (c >= a.C) continue;
                 float e = 0, f = 0;
                 if (WIDE) {
                     e = reinterpret_cast<const float*>(s_e.v)[i];
                     f = reinterpret_cast<const float*>(s_f.v)[i];
                 } else {
-                    for (int g = 0; g < here; ++g) e += e_all[g * a.threads * E + c], f += f_all[g * a.threads * E + c];
+                    for (int g = 0; g < here; ++g) e += e_all[g * threads * E + c], f += f_all[g * threads * E + c];
                 }
                 const float ga_c = gate ? gate[c] : 1.0f, sc_c = a.scale ? a.scale[c] : 1.0f;
                 const float joined = fmaf(a.post_weight ? a.post_weight[c] : 1.0f, e, a.post_bias ? a.post_bias[c] * f : 0.0f);
@@ -549,22 +643,22 @@ __global__ void __launch_bounds__(WIDE ? 512 : kBlockThreads, WIDE ? 1 : 2) bloc
         const float* pb = reinterpret_cast<const float*>(s_b.v);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const int c = channel<V>(lane, a.threads, i);
-            lanes_sum[mine * a.threads * E + c] = pw[i];
-            lanes_sum[kBlockThreads * E + mine * a.threads * E + c] = pb[i];
+            const int c = channel<V>(lane, threads, i);
+            lanes_sum[mine * threads * E + c] = pw[i];
+            lanes_sum[kBlockThreads * E + mine * threads * E + c] = pb[i];
         }
         __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
-        const int c = WIDE ? channel<V>(lane, a.threads, i) : threadIdx.x;
+        const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x;
         if (c >= a.C) continue;
         float e = 0, f = 0;
         if (WIDE) {
             e = reinterpret_cast<const float*>(s_w.v)[i];
             f = reinterpret_cast<const float*>(s_b.v)[i];
         } else {
-            for (int g = 0; g < here; ++g) e += lanes_sum[g * a.threads * E + c], f += lanes_sum[kBlockThreads * E + g * a.threads * E + c];
+            for (int g = 0; g < here; ++g) e += lanes_sum[g * threads * E + c], f += lanes_sum[kBlockThreads * E + g * threads * E + c];
         }
         out[c] = e;
         out[a.C + c] = f;
@@ -585,33 +679,46 @@ cudaError_t allow_shared(K* kernel, std::atomic<uint64_t>& done, size_t bytes) {
     if (e != cudaSuccess) cudaGetLastError();
     return e;
 }
-template <typename TX, typename TB, int V, bool WIDE>
-cudaError_t forward_rows(const BlockArgs& a, int threads, int ctas, cudaStream_t st) {
-    constexpr int kRound = Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes;
+template <typename TX, typename TB, int V, int FORM>
+cudaError_t forward_rows(const BlockArgs& a, cudaStream_t st) {
+    constexpr int kRound = Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes, kMost = FORM == kLong ? 512 : kBlockThreads;
     static std::atomic<uint64_t> allowed{0};
-    if (const cudaError_t e = allow_shared(block_rows<TX, TB, V, WIDE>, allowed, kRounds * kRound * (WIDE ? 512 : kBlockThreads))) return e;
-    block_rows<TX, TB, V, WIDE><<<ctas, threads, kRounds * kRound * threads, st>>>(a);
+    if (const cudaError_t e = allow_shared(block_rows<TX, TB, V, FORM>, allowed, kRounds * kRound * kMost)) return e;
+    const int threads = FORM == kLong ? a.threads : kBlockThreads, here = threads / a.threads;
+    const int most = 152 * (FORM == kLong ? std::max(1, 768 / threads) : 3);
+    block_rows<TX, TB, V, FORM><<<std::min((a.rows + here - 1) / here, most), threads, kRounds * kRound * threads, st>>>(a);
     return cudaGetLastError();
+}
+template <typename TX, typename TB, int V, int FORM>
+cudaError_t backward_rows(const BlockArgs& a, cudaStream_t st) {
+    constexpr int kEach = kRoundsBack<TX, TB, FORM == kLong> * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) +
+                          3 * (FORM == kLong ? E : 1) * (int)sizeof(float);      // of a thread
+    static std::atomic<uint64_t> allowed{0};
+    if (const cudaError_t e = allow_shared(block_back_rows<TX, TB, V, FORM>, allowed, kEach * (FORM == kLong ? 512 : kBlockThreads))) return e;
+    const int threads = FORM == kLong ? a.threads : kBlockThreads;
+    block_back_rows<TX, TB, V, FORM><<<a.ctas, threads, kEach * threads, st>>>(a);
+    if (const cudaError_t e = cudaGetLastError()) return e;
+    return block_join(a, st);
+}
+// f with the form of the kernels that a call takes
+template <int V, typename F>
+cudaError_t by_form(const BlockArgs& a, F&& f) {
+    if (a.threads > 32) return f(std::integral_constant<int, kLong>());
+    if constexpr (V == 8)
+        if (a.dense) {
+            if (a.threads == 32) return f(std::integral_constant<int, 32>());
+            if (a.threads == 16) return f(std::integral_constant<int, 16>());
+            if (a.threads == 8) return f(std::integral_constant<int, 8>());
+        }
+    return f(std::integral_constant<int, kShort>());
 }
 template <typename TX, typename TB, int V>
 cudaError_t forward_as(const BlockArgs& a, cudaStream_t st) {
-    if (a.threads > 32) return forward_rows<TX, TB, V, true>(a, a.threads, std::min(a.rows, 152 * std::max(1, 768 / a.threads)), st);
-    const int here = kBlockThreads / a.threads;
-    return forward_rows<TX, TB, V, false>(a, kBlockThreads, std::min((a.rows + here - 1) / here, 152 * 3), st);
-}
-template <typename TX, typename TB, int V, bool WIDE>
-cudaError_t backward_rows(const BlockArgs& a, int threads, cudaStream_t st) {
-    constexpr int kEach = kRoundsBack<TX, TB, WIDE> * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) + 3 * (WIDE ? E : 1) * (int)sizeof(float);   // of a thread
-    static std::atomic<uint64_t> allowed{0};
-    if (const cudaError_t e = allow_shared(block_back_rows<TX, TB, V, WIDE>, allowed, kEach * (WIDE ? 512 : kBlockThreads))) return e;
-    block_back_rows<TX, TB, V, WIDE><<<a.ctas, threads, kEach * threads, st>>>(a);
-    return cudaGetLastError();
+    return by_form<V>(a, [&](auto form) { return forward_rows<TX, TB, V, decltype(form)::value>(a, st); });
 }
 template <typename TX, typename TB, int V>
 cudaError_t backward_as(const BlockArgs& a, cudaStream_t st) {
-    if (const cudaError_t e = a.threads > 32 ? backward_rows<TX, TB, V, true>(a, a.threads, st) : backward_rows<TX, TB, V, false>(a, kBlockThreads, st))
-        return e;
-    return block_join(a, st);
+    return by_form<V>(a, [&](auto form) { return backward_rows<TX, TB, V, decltype(form)::value>(a, st); });
 }
 
 }  // namespace

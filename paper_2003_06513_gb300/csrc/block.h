@@ -25,6 +25,8 @@ struct BlockArgs {
     int pixels_shift;
     int threads;                                      // of a row
     int vectors;                                      // of a row
+    int ragged;                                       // whether its threads have more channels than it has
+    int flat, dense;                                  // whether every tensor's samples follow one another as its pixels do; and those too
     void *h, *y;                                      // (forward)
     void *dx, *db;                                    // (backward)
     float *dweight, *dbias, *dpost_weight, *dpost_bias, *dscale, *dgate;

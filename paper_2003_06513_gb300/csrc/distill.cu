@@ -7,15 +7,14 @@
 // m the largest logit, Z_1 and Z_T the sums of exp(s - m) and exp((s - m) / T).
 //
 // q_0 is summed over the classes that are not kept, as 1 - sum q_k would lose it where the kept classes have nearly
-// all: a bit a class in shared memory says which are, read beside each 16-byte vector of logits.  A thread keeps a
-// running maximum and the sums below it, so that the row is read once; the kept logits are fetched by the threads
-// that hold the teacher's and join at the end.
+// all: a bit for each 16-byte vector of logits in shared memory says whether a kept class is in it, and such a vector is left
+// to the thread that has that class of the teacher's.  A thread keeps a running maximum and the sums below it, so that the
+// row is read once; the kept logits themselves join at the end.
 //
 // What bounds it is memory: a row is read, next to nothing is written.
 #include <cooperative_groups.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "rows.cuh"
 
@@ -24,9 +23,12 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kWide = 256;            // threads of a CTA that has a row, or a part of one
+constexpr int kWide = 128;            // threads of a CTA that has a row, or a part of one
 constexpr int kRowsOfCta = 4;         // rows of a CTA whose warps have one each
 constexpr int kMostOfWarp = 2048;     // classes of a warp's row at most
+
+template <int W>
+constexpr int kBitsOfWarp = ((kMostOfWarp + 2 * W - 2) / W + 31) / 32;       // words of a warp's row: a bit a vector
 
 // what a thread sums of the classes it sees: the largest x, and the sums of 2^((x - m) c) relative to it
 // HARD: how the sum at T = 1 is had beside the one at T.  kNone: there are no labels, or T is 1; kApart: by an exponential of its
@@ -60,46 +62,62 @@ struct Running {
     }
 };
 
+// The threads of a row read it together; then their sums and the teacher's entries are joined by one warp, the others being
+// done.  A row's fixed work is a good part of a row of 64 KB: 128 threads to a CTA and one warp at the end have it overlap
+// the reading of the seven other rows on the SM, and cost four warps and not eight.
 template <typename T, bool REST, int HARD, int N>
-__global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(DistillArgs a) {
-    constexpr int W = 16 / sizeof(T), U = 4;
+__global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8) distill_rows(DistillArgs a) {
+    constexpr int W = 16 / sizeof(T), U = 4, kWarps = N / 32, kEntries = N == 32 ? 32 : kMostKept;
     extern __shared__ uint4 dynamic[];
-    __shared__ float scratch[N == 32 ? 1 : 2 * (N / 32) * 8];
-    __shared__ float parts[16][3];
-    __shared__ int kept_of[N == 32 ? kRowsOfCta : 1][N == 32 ? 32 : kMostKept];
+    __shared__ float parts[16][3];                    // of a cluster's CTAs, in the first one
+    __shared__ float sums[kRowsOfCta][kWarps][3];
+    __shared__ __align__(16) int places[N == 32 ? kRowsOfCta : 1][kEntries];
+    __shared__ float teacher[N == 32 ? kRowsOfCta : 1][kEntries], student[N == 32 ? kRowsOfCta : 1][kEntries];
+    __shared__ bool before[N == 32 ? kRowsOfCta : 1][kEntries];
     const int slot = N == 32 ? threadIdx.x / 32 : 0;
     const int part = N == 32 ? 0 : blockIdx.x % a.parts;
     const int row = N == 32 ? blockIdx.x * kRowsOfCta + slot : blockIdx.x / a.parts;
     if (row >= a.rows) return;
-    Group<N> g(scratch);
+    Group<N> g(nullptr);
     const T* s = static_cast<const T*>(a.s) + row * a.stride;
     const Row<T, W> r(s, a.classes);
     // this group's vectors
     const int each = (r.vectors() + a.parts - 1) / a.parts, first = part * each, last = min(r.vectors(), first + each);
-    unsigned* bits = reinterpret_cast<unsigned*>(dynamic) + (N == 32 ? slot * ((kMostOfWarp + 2 * W) / 32 + 1) : 0);
-    int* kept = kept_of[slot];
+    unsigned* bits = reinterpret_cast<unsigned*>(dynamic) + (N == 32 ? slot * kBitsOfWarp<W> : 0);
+    int* kept = places[slot];                         // the entries' places in the row, -1: empty
+    bool* came = before[slot];                        // whether an entry's class is that of an earlier one
+    float *us = teacher[slot], *xs = student[slot];
+    // the ends of a row that are no whole vectors are taken by themselves
+    const int from = first < last && !r.whole(first) ? first + 1 : first;
+    const int to = last > from && !r.whole(last - 1) ? last - 1 : last;
+    // the first logits are asked for at once, whatever the teacher's entries then say
+    int v = from + g.lane;
+    Vec<T, W> batch[U];
+    const bool early = v + (U - 1) * N < to;
+    if (early)
+#pragma unroll
+        for (int k = 0; k < U; ++k) batch[k] = r.at(v + k * N);
 
-    // the teacher's entry of this thread
-    const bool mine = g.lane < a.kept;
-    int at = -1;
-    float u = kNone, x = kNone;
-    if (mine) {
-        const int64_t j = (int64_t)row * a.kept + g.lane;
-        at = a.indices[j];
-        if (at >= 0 && at < a.classes) {
+    // the teacher's entries
+    bool any = false;
+    for (int k = g.lane; k < (a.kept + 3) / 4 * 4; k += N) {
+        const int64_t j = (int64_t)row * a.kept + k;
+        int at = k < a.kept ? a.indices[j] : -1;
+        float u = kNone;
+        if (at >= 0 && at < a.classes)
             u = value_at(a.values, a.value_type, j) * a.inv_t;
-            x = widen(s[at]);
-        } else {
+        else
             at = -1;
-        }
-        kept[g.lane] = at;
+        kept[k] = at < 0 ? -1 : at + r.pad;
+        us[k] = u;
+        any = any || u != kNone;
     }
     const float rest = REST ? a.rest[row] : kNone;
     int64_t label = a.labels ? a.labels[row] : -1;
     if (label >= a.classes) label = -1;
     if (REST)
-        for (int w = g.lane; w < (max(0, last - first) * W + 31) / 32; w += N) bits[w] = 0;
-    const bool taught = g.any((at >= 0 && u != kNone) || (REST && rest != kNone));
+        for (int w = g.lane; w < (max(0, last - first) + 31) / 32; w += N) bits[w] = 0;
+    const bool taught = g.any(any || (REST && rest != kNone));
     if (!taught && label < 0) {                       // uniform over the row's CTAs: nothing to learn from this row
         if (part == 0 && g.lane < 5) {
             a.stats[(int64_t)row * 5 + g.lane] = 0;
@@ -107,126 +125,163 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
         }
         return;
     }
-    bool once = at >= 0;                              // of places that are given twice the first one
     if (REST) {
         if constexpr (N == 32) g.sync();
-        if (once) {
-            for (int j = 0; j < g.lane; ++j) once = once && kept[j] != at;
-            const int place = at + r.pad - first * W;
-            if (place >= 0 && place < (last - first) * W) atomicOr(&bits[place / 32], 1u << (place % 32));
+        for (int k = g.lane; k < a.kept; k += N) {
+            const int home = kept[k] / W;
+            if (kept[k] >= 0 && home >= first && home < last) atomicOr(&bits[(home - first) / 32], 1u << ((home - first) % 32));
         }
         g.sync();
     }
-
     if constexpr (N > 32)                             // the first CTA's memory is written by the others, once it has begun
         if (a.parts > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
 
     Running<HARD> sum;
     const float2 c1 = both(a.c1), ct = both(a.ct);
-    const unsigned char* marks = reinterpret_cast<const unsigned char*>(bits);
-    const auto mark = [&](int v) -> unsigned {        // the bits of vector v's classes
-        if constexpr (!REST) return 0;
-        const int k = v - first;
-        return W == 8 ? marks[k] : (marks[k / 2] >> (k % 2 * 4)) & 15u;
-    };
-    const auto take = [&](const auto& batch, const unsigned* m) {
-        constexpr int K = std::extent<std::remove_reference_t<decltype(batch)>>::value;
+    // whether vector v is left out: its bit is the same one of a word for all of a thread's vectors
+    const unsigned bit = 1u << ((v - first) % 32);
+    const auto left_out = [&](int v) { return REST && bits[(v - first) / 32] & bit; };
+    const auto take = [&](const auto& b) {
+        constexpr int K = std::extent<std::remove_reference_t<decltype(b)>>::value;
         float2 f[K * W / 2];
-        float top = kNone;
+        Largest<T> top;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
+        for (int k = 0; k < K; ++k) top.take(b[k]);
 #pragma unroll
-            for (int i = 0; i < W / 2; ++i) f[k * W / 2 + i] = pair(batch[k], i);
-            if (REST && m[k])
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int i = 0; i < W / 2; ++i) {
-                    if (m[k] >> (2 * i) & 1) f[k * W / 2 + i].x = kNone;
-                    if (m[k] >> (2 * i + 1) & 1) f[k * W / 2 + i].y = kNone;
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < K * W / 2; ++i) top = fmaxf(top, fmaxf(f[i].x, f[i].y));
-        sum.below(top, a.c1, a.ct);
+            for (int i = 0; i < W / 2; ++i) f[k * W / 2 + i] = pair(b[k], i);
+        sum.below(top.get(), a.c1, a.ct);
 #pragma unroll
         for (int i = 0; i < K * W / 2; ++i) sum.add_pair(f[i], c1, ct);
     };
-    int from = first, to = last;
-    // the ends of a row that are no whole vectors
-    for (int end = 0; end < 2; ++end) {
-        const int v = end ? last - 1 : first;
-        if (last <= first || r.whole(v) || (end && v == first)) continue;
-        if (end)
-            --to;
-        else
-            ++from;
-        if (g.lane == (end ? N - 1 : 0)) {
-            const unsigned m = mark(v);
-            for (int i = 0; i < W; ++i) {
-                const int place = v * W + i;
-                if (place < r.pad || place >= r.end || (m >> i & 1)) continue;
-                const float y = widen(r.base[place]);
-                sum.below(y, a.c1, a.ct);
-                sum.zt.x += power(y, sum.ref, a.ct);
-                if (HARD) sum.z1.x += power(y, sum.ref, a.c1);
-            }
+    const auto clear = [&](Vec<T, W>& b, bool all) {  // nothing is there: -inf
+        uint4 w;
+        memcpy(&w, &b, 16);
+        const unsigned none = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00FC00u : 0xFF80FF80u;
+        w.x = all ? none : w.x, w.y = all ? none : w.y, w.z = all ? none : w.z, w.w = all ? none : w.w;
+        memcpy(&b, &w, 16);
+    };
+    const auto values_of = [&](const Vec<T, W>& b, unsigned but) {     // a vector's values one by one, but for some
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if (but >> i & 1) continue;
+            const float y = widen(b.v[i]);
+            sum.below(y, a.c1, a.ct);
+            sum.zt.x += power(y, sum.ref, a.ct);
+            if (HARD) sum.z1.x += power(y, sum.ref, a.c1);
         }
-    }
-    int v = from + g.lane;
-    for (; v + (U - 1) * N < to; v += U * N) {
-        Vec<T, W> b[U];
-        unsigned m[U];
+    };
+    for (bool ready = early; ready; ready = v + (U - 1) * N < to) {
+        if (!(early && v == from + g.lane))
 #pragma unroll
-        for (int k = 0; k < U; ++k) b[k] = r.at(v + k * N);
+            for (int k = 0; k < U; ++k) batch[k] = r.at(v + k * N);
+        if (REST)
 #pragma unroll
-        for (int k = 0; k < U; ++k) m[k] = mark(v + k * N);
-        take(b, m);
+            for (int k = 0; k < U; ++k) clear(batch[k], left_out(v + k * N));
+        take(batch);
+        v += U * N;
     }
     for (; v < to; v += N) {
-        const Vec<T, W> b[1] = {r.at(v)};
-        const unsigned m[1] = {mark(v)};
-        take(b, m);
+        Vec<T, W> b[1] = {r.at(v)};
+        if (REST) clear(b[0], left_out(v));
+        take(b);
+    }
+    const auto marked = [&](int v) { return REST && bits[(v - first) / 32] >> ((v - first) % 32) & 1; };
+    if (from > first && g.lane == 0 && !marked(first)) values_of(r.some(first), 0);
+    if (to < last && g.lane == N - 1 && !marked(to)) values_of(r.some(to), 0);
+    // the kept classes' logits, and the others in the vectors that were left out for them: of those with several kept classes
+    // the first entry has it
+    for (int k = g.lane; k < a.kept; k += N) {
+        const int place = kept[k], home = place / W;
+        float x = kNone;
+        bool again = false;
+        if (place >= 0) {
+            x = widen(r.base[place]);
+            if (REST) {
+                unsigned inside = 0;
+                bool keeper = home >= first && home < last;
+                for (int j = 0; j < a.kept; j += 4) {
+                    const int4 four = *reinterpret_cast<const int4*>(kept + j);
+                    const int others[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if ((unsigned)(others[i] ^ place) < (unsigned)W) {     // (-1 is far from every place)
+                            inside |= 1u << (others[i] % W);
+                            if (j + i < k) keeper = false;
+                            again = again || (others[i] == place && j + i < k);
+                        }
+                }
+                if (keeper) values_of(r.some(home), inside);
+            }
+        }
+        xs[k] = x;
+        came[k] = again;
     }
 
-    // the group's maxima: of the classes seen, of the kept ones, of the teacher's; then the sums below them
-    const float z1 = sum.z1.x + sum.z1.y, zt = sum.zt.x + sum.zt.y;
-    float top[3] = {sum.m, at >= 0 ? x : kNone, fmaxf(u, rest)};
-    g.max(top);
-    const float mu = reference(top[2]), mx = reference(top[1]);
-    const float e = at >= 0 ? power(u, mu, a.c1) : 0.0f;
-    float total[6] = {zt == 0.0f ? 0.0f : zt * factor(sum.m, top[0], a.ct), !HARD || z1 == 0.0f ? 0.0f : z1 * factor(sum.m, top[0], a.c1), 0, 0, e, 0};
-    if (REST && once) {
-        total[2] = power(x, mx, a.ct);
-        if (HARD) total[3] = power(x, mx, a.c1);
+    // the warps' sums, and from here on one warp
+    const int lane = threadIdx.x % 32, warp = N == 32 ? 0 : threadIdx.x / 32;
+    Group<32> one(nullptr);
+    float m, sum_t, sum_1;
+    {
+        float top[1] = {sum.m};
+        one.max(top);
+        const float zt = sum.zt.x + sum.zt.y, z1 = sum.z1.x + sum.z1.y;
+        float z[2] = {zt == 0.0f ? 0.0f : zt * factor(sum.m, top[0], a.ct), !HARD || z1 == 0.0f ? 0.0f : z1 * factor(sum.m, top[0], a.c1)};
+        one.sum(z);
+        m = top[0], sum_t = z[0], sum_1 = z[1];
     }
-    if (!REST && e != 0.0f) total[5] = e * ((u - mu) - (x - mx) * a.inv_t);
-    g.sum(total);
-    float m = top[0], sum_t = total[0], sum_1 = total[1];
-    if constexpr (N > 32) {
+    const auto joined = [&](const float (*of)[3], int n) {
+        m = kNone;
+        for (int i = 0; i < n; ++i) m = fmaxf(m, of[i][0]);
+        sum_t = sum_1 = 0;
+        for (int i = 0; i < n; ++i) {
+            sum_t += of[i][1] == 0.0f ? 0.0f : of[i][1] * factor(of[i][0], m, a.ct);
+            sum_1 += of[i][2] == 0.0f ? 0.0f : of[i][2] * factor(of[i][0], m, a.c1);
+        }
+    };
+    if constexpr (N == 32) {
+        g.sync();
+    } else {
+        if (lane == 0) sums[0][warp][0] = m, sums[0][warp][1] = sum_t, sums[0][warp][2] = sum_1;
+        __syncthreads();
+        if (a.parts == 1 && warp) return;
+        joined(sums[0], kWarps);
         if (a.parts > 1) {                            // the parts' sums, in the first CTA of the cluster
             cg::cluster_group cluster = cg::this_cluster();
             asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-            if (g.lane == 0) {
+            if (threadIdx.x == 0) {
                 float* to0 = cluster.map_shared_rank(&parts[part][0], 0);
                 to0[0] = m, to0[1] = sum_t, to0[2] = sum_1;
             }
             cluster.sync();
-            if (part) return;
-            m = kNone;
-            for (int i = 0; i < a.parts; ++i) m = fmaxf(m, parts[i][0]);
-            sum_t = sum_1 = 0;
-            for (int i = 0; i < a.parts; ++i) {
-                sum_t += parts[i][1] == 0.0f ? 0.0f : parts[i][1] * factor(parts[i][0], m, a.ct);
-                sum_1 += parts[i][2] == 0.0f ? 0.0f : parts[i][2] * factor(parts[i][0], m, a.c1);
-            }
+            if (part || warp) return;
+            joined(parts, a.parts);
         }
     }
+    float top[2] = {rest, kNone};                     // the largest of the teacher's, and of the kept classes' logits
+    for (int k = lane; k < a.kept; k += 32) top[0] = fmaxf(top[0], us[k]), top[1] = fmaxf(top[1], xs[k]);
+    one.max(top);
+    const float mu = reference(top[0]), mx = reference(top[1]);
+    float total[4] = {0, 0, 0, 0};                    // of the teacher's masses; of the kept classes' at T and at 1; of p (log p - log q)
+    for (int k = lane; k < a.kept; k += 32) {
+        if (kept[k] < 0) continue;
+        const float u = us[k], x = xs[k], e = power(u, mu, a.c1);
+        total[0] += e;
+        if (REST && !came[k]) {
+            total[1] += power(x, mx, a.ct);
+            if (HARD) total[2] += power(x, mx, a.c1);
+        }
+        if (!REST && e != 0.0f) total[3] += e * ((u - mu) - (x - mx) * a.inv_t);
+    }
+    one.sum(total);
     const float other = m, other_t = sum_t;           // without `rest` the classes seen are all there are
     float kept_t = 0;
     if (REST) {
         m = fmaxf(m, top[1]);
-        kept_t = total[2] == 0.0f ? 0.0f : total[2] * factor(top[1], m, a.ct);
+        kept_t = total[1] == 0.0f ? 0.0f : total[1] * factor(top[1], m, a.ct);
         sum_t = (other_t == 0.0f ? 0.0f : other_t * factor(other, m, a.ct)) + kept_t;
-        sum_1 = (sum_1 == 0.0f ? 0.0f : sum_1 * factor(other, m, a.c1)) + (total[3] == 0.0f ? 0.0f : total[3] * factor(top[1], m, a.c1));
+        sum_1 = (sum_1 == 0.0f ? 0.0f : sum_1 * factor(other, m, a.c1)) + (total[2] == 0.0f ? 0.0f : total[2] * factor(top[1], m, a.c1));
     }
     if (!HARD) sum_1 = sum_t;
     float loss = 0;
@@ -234,7 +289,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
         // Both sides are whole distributions over the kept classes and the others: sum p (log p - log q) is the sum of
         // q - p - p delta, delta = log q - log p, whose terms are all positive, p delta^2 / 2 for a small delta; summed as they stand
         // the logarithms would cancel where student and teacher agree.
-        const float e0 = factor(rest, mu, a.c1), whole = total[4] + e0, per_t = 1.0f / sum_t, level = logf(sum_t / whole);
+        const float e0 = factor(rest, mu, a.c1), whole = total[0] + e0, per_t = 1.0f / sum_t, level = logf(sum_t / whole);
         const auto term = [](float p, float q, float delta, bool with_q) {
             if (p == 0.0f) return with_q ? q : 0.0f;
             if (with_q && fabsf(delta) < 0.25f)       // (e^delta - 1 - delta) / (delta^2 / 2) by its series, to delta^7 / 181440
@@ -243,22 +298,25 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_rows(Di
             return (with_q ? q : 0.0f) - fmaf(p, delta, p);
         };
         float kl[1] = {0};
-        if (at >= 0) kl[0] = term(e / whole, power(x, reference(m), a.ct) * per_t, (x - m) * a.inv_t - (u - mu) - level, once);
-        if (g.lane == 0) {
+        for (int k = lane; k < a.kept; k += 32)
+            if (kept[k] >= 0) {
+                const float u = us[k], x = xs[k];
+                kl[0] += term(power(u, mu, a.c1) / whole, power(x, reference(m), a.ct) * per_t, (x - m) * a.inv_t - (u - mu) - level, !came[k]);
+            }
+        if (lane == 0) {
             const float others = other_t * factor(other, m, a.ct);      // (of nothing: 0 times 0)
             // log p_0 and log q_0 as those of one minus what the kept classes have, and by their exponents where hardly
             // anything is left, or less than fp32 holds
-            const float log_p = e0 > 1e-30f ? -log1pf(total[4] / e0) : (rest - mu) - logf(whole);
+            const float log_p = e0 > 1e-30f ? -log1pf(total[0] / e0) : (rest - mu) - logf(whole);
             const float log_q = others > 1e-30f ? -log1pf(kept_t / others) : (other - m) * a.inv_t + logf(other_t) - logf(sum_t);
-            const float delta = log_q - log_p;
-            kl[0] += term(e0 / whole, others * per_t, delta, true);
+            kl[0] += term(e0 / whole, others * per_t, log_q - log_p, true);
         }
-        g.sum(kl);
+        one.sum(kl);
         loss = a.soft_loss * kl[0];
     }
-    if (g.lane) return;
+    if (lane) return;
     if (!REST && taught) {
-        const float whole = total[4], d = fmaf(whole, (m - mx) * a.inv_t, total[5]);
+        const float whole = total[0], d = fmaf(whole, (m - mx) * a.inv_t, total[3]);
         loss = a.soft_loss * (d / whole - logf(whole) + logf(sum_t));
     }
     if (label >= 0) loss += a.hard * (logf(sum_1) - (widen(s[label]) - m));
@@ -276,7 +334,7 @@ cudaError_t launch(DistillArgs a, cudaStream_t st) {
     constexpr int W = 16 / sizeof(T);
     if (a.classes <= kMostOfWarp && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
         a.parts = 1;
-        const size_t smem = REST ? kRowsOfCta * ((kMostOfWarp + 2 * W) / 32 + 1) * 4 : 0;
+        const size_t smem = REST ? kRowsOfCta * kBitsOfWarp<W> * 4 : 0;
         distill_rows<T, REST, HARD, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, smem, st>>>(a);
         return cudaGetLastError();
     }
@@ -284,20 +342,7 @@ cudaError_t launch(DistillArgs a, cudaStream_t st) {
     a.parts = 1;
     while (a.parts < 8 && (int64_t)a.rows * a.parts < 2 * kSMs && a.classes / a.parts >= 4096 * 2) a.parts *= 2;
     const int vectors = (a.classes + 2 * W - 2) / W, each = (vectors + a.parts - 1) / a.parts;
-    const size_t smem = REST ? ((size_t)each * W + 31) / 32 * 4 : 0;
-    static std::atomic<uint64_t> allowed{0};
-    if (smem > 40960) {
-        int dev = 0;
-        if (const cudaError_t e = cudaGetDevice(&dev)) return e;
-        if (dev >= 64 || !(allowed.load() >> dev & 1)) {
-            if (const cudaError_t e = cudaFuncSetAttribute(distill_rows<T, REST, HARD, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                           kMostClasses / 8 + 64)) {
-                cudaGetLastError();
-                return e;
-            }
-            if (dev < 64) allowed.fetch_or(uint64_t(1) << dev);
-        }
-    }
+    const size_t smem = REST ? ((size_t)each + 31) / 32 * 4 : 0;    // at most 32 KB
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.rows * (unsigned)a.parts);
     cfg.blockDim = dim3(kWide);

@@ -28,6 +28,17 @@ struct Row {
     __device__ __forceinline__ int vectors() const { return (end + W - 1) / W; }
     __device__ __forceinline__ bool whole(int v) const { return v * W >= pad && v * W + W <= end; }
     __device__ __forceinline__ Vec<T, W> at(int v) const { return load<T, W>(base + (int64_t)v * W); }
+    // a vector that may lie partly outside the row, where it is -inf
+    __device__ __forceinline__ Vec<T, W> some(int v) const {
+        if (whole(v)) return at(v);
+        Vec<T, W> b;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const int place = v * W + i;
+            b.v[i] = place >= pad && place < end ? base[place] : T(kNone);
+        }
+        return b;
+    }
 };
 
 // The threads that take a row together: a warp of several in a CTA (N = 32), or a CTA.
@@ -88,6 +99,47 @@ __device__ __forceinline__ float reference(float m) { return m == kNone ? 0.0f :
 __device__ __forceinline__ float power(float x, float m, float c) { return approx_exp2((x - m) * c); }
 // 2^((a - m) c), 0 where there is no a
 __device__ __forceinline__ float factor(float a, float m, float c) { return a == kNone ? 0.0f : approx_exp2((a - m) * c); }
+
+// The largest of values as they come, a NaN above all: packed where two share a register.
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+template <typename T>
+struct Largest;
+template <>
+struct Largest<float> {
+    float m = kNone;
+    __device__ __forceinline__ void take(const Vec<float, 4>& v) { m = larger(larger(m, v.v[0]), larger(larger(v.v[1], v.v[2]), v.v[3])); }
+    __device__ __forceinline__ float get() const { return m; }
+};
+template <>
+struct Largest<__half> {
+    __half2 m = __float2half2_rn(kNone);
+    __device__ __forceinline__ void take(const Vec<__half, 8>& v) {
+        __half2 h[4];
+        memcpy(h, &v, 16);
+        m = __hmax2_nan(__hmax2_nan(m, h[0]), __hmax2_nan(__hmax2_nan(h[1], h[2]), h[3]));
+    }
+    __device__ __forceinline__ float get() const { return larger(__low2float(m), __high2float(m)); }
+};
+template <>
+struct Largest<__nv_bfloat16> {
+    __nv_bfloat162 m = __float2bfloat162_rn(kNone);
+    __device__ __forceinline__ void take(const Vec<__nv_bfloat16, 8>& v) {
+        __nv_bfloat162 h[4];
+        memcpy(h, &v, 16);
+        m = __hmax2_nan(__hmax2_nan(m, h[0]), __hmax2_nan(__hmax2_nan(h[1], h[2]), h[3]));
+    }
+    __device__ __forceinline__ float get() const { return larger(__low2float(m), __high2float(m)); }
+};
+template <typename T, int W>
+__device__ __forceinline__ float largest(const Vec<T, W>& v) {
+    Largest<T> l;
+    l.take(v);
+    return l.get();
+}
 
 // kept value j of a row, in fp32
 __device__ __forceinline__ float value_at(const void* values, int type, int64_t j) {

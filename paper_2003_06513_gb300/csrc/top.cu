@@ -24,7 +24,6 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kList = 1024;           // values that reach the bound at most
 constexpr int kClusterMost = 8;
 constexpr size_t kHeld = 96 * 1024;   // bytes of a CTA's slice in shared memory at most: two CTAs on an SM
 
@@ -37,7 +36,8 @@ struct TopArgs {
     int* indices;                     // [rows][k]
     float* rest;                      // [rows]
     int parts;                        // CTAs of a row, a cluster
-    int held;                         // whether a slice is kept in shared memory
+    int held;                         // bytes of a slice that is kept in shared memory, 0: it is not
+    int list;                         // values that reach the bound at most: 512, with many kept 1024
 };
 
 // an integer in the values' order
@@ -48,43 +48,18 @@ __device__ __forceinline__ int key_of(float x) {
 __device__ __forceinline__ float of_key(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
 constexpr int kLeast = INT_MIN;       // below every key
 
-// The largest of values as they come, a NaN above all: packed where two share a register.
-__device__ __forceinline__ float larger(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-template <int W>
-__device__ __forceinline__ float largest(const Vec<float, W>& v) {
-    return larger(larger(v.v[0], v.v[1]), larger(v.v[2], v.v[3]));
-}
-template <int W>
-__device__ __forceinline__ float largest(const Vec<__half, W>& v) {
-    __half2 h[4];
-    memcpy(h, &v, 16);
-    const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-    return larger(__low2float(m), __high2float(m));
-}
-template <int W>
-__device__ __forceinline__ float largest(const Vec<__nv_bfloat16, W>& v) {
-    __nv_bfloat162 h[4];
-    memcpy(h, &v, 16);
-    const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-    return larger(__low2float(m), __high2float(m));
-}
-
 // what the CTAs of a row tell one another
 struct Shared {
-    unsigned long long list[kList];   // (key, ~place) of the values that reach the bound; the first CTA's, of all CTAs
-    float after[kList];               // of those the ones after the k-th, in order
-    int found;                        // how many (the first CTA's)
+    int found;                        // how many values are listed (the first CTA's)
+    int flagged;                      // how many vectors of this CTA are noted
+    unsigned long long beside;        // the sum of their other values' exponentials, in units of 2^-52
     int bounds[kClusterMost];
     int counted[2][kClusterMost];
     float sums[kClusterMost];         // of the values that are not listed (the first CTA's)
 };
 
 template <typename T, int N>
-__global__ void __launch_bounds__(N, N == 512 ? 3 : 8) top_rows(TopArgs a) {
+__global__ void __launch_bounds__(N, N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(TopArgs a) {
     constexpr int W = 16 / sizeof(T), kWarps = N / 32, U = 4;
     extern __shared__ uint4 dynamic[];
     __shared__ Shared sh;
@@ -103,40 +78,36 @@ __global__ void __launch_bounds__(N, N == 512 ? 3 : 8) top_rows(TopArgs a) {
         else
             __syncthreads();
     };
+    // (key, ~place) of the values that reach the bound, the first CTA's those of all; the vectors that hold some; at the end, of
+    // the values those after the k-th, in order, in the vectors' place
+    unsigned long long* list = reinterpret_cast<unsigned long long*>(reinterpret_cast<char*>(dynamic) + a.held);
+    int* noted = reinterpret_cast<int*>(list + a.list);
+    float* after = reinterpret_cast<float*>(noted);
     const auto of = [&](int p) { return a.parts > 1 ? cluster.map_shared_rank(&sh, p) : &sh; };
 
     // 1. the largest of each thread's values; all of the slice goes to shared memory
-    if (threadIdx.x == 0) sh.found = 0;
-    float most = kNone;
-    const auto edge = [&](int v) {                    // a vector of which the row has a part: nothing beside it
-        Vec<T, W> b;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const int place = v * W + i;
-            b.v[i] = place >= r.pad && place < r.end ? r.base[place] : T(kNone);
-        }
-        return b;
-    };
+    if (threadIdx.x == 0) sh.found = sh.flagged = 0, sh.beside = 0;
+    Largest<T> seen;
     int v = first + threadIdx.x;
     for (; v + (U - 1) * N < last; v += U * N) {
         Vec<T, W> b[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) b[k] = r.whole(v + k * N) ? r.at(v + k * N) : edge(v + k * N);
+        for (int k = 0; k < U; ++k) b[k] = r.some(v + k * N);
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            most = larger(most, largest(b[k]));
+            seen.take(b[k]);
             if (a.held) held[v + k * N - first] = b[k];
         }
     }
     for (; v < last; v += N) {
-        const Vec<T, W> b = r.whole(v) ? r.at(v) : edge(v);
-        most = larger(most, largest(b));
+        const Vec<T, W> b = r.some(v);
+        seen.take(b);
         if (a.held) held[v - first] = b;
     }
 
     // the bound: this CTA's share of the values wanted reach it here, so that all of them do where the least of the CTAs' does
     const int share = (wanted + a.parts - 1) / a.parts, own = min(N, last - first);
-    const int key = (int)threadIdx.x < own ? key_of(most) : kLeast;
+    const int key = (int)threadIdx.x < own ? key_of(seen.get()) : kLeast;
     int bound = kLeast;
     {
         const int high_lane = __reduce_max_sync(0xffffffffu, key), low_lane = __reduce_min_sync(0xffffffffu, (int)threadIdx.x < own ? key : INT_MAX);
@@ -164,48 +135,92 @@ __global__ void __launch_bounds__(N, N == 512 ? 3 : 8) top_rows(TopArgs a) {
         for (int p = 0; p < a.parts; ++p) bound = min(bound, sh.bounds[p]);
     }
 
-    // 2. what is listed: the values above key `bound`, and of those with this key the ones up to place `until`; the others' sum
+    // 2. what is listed: the values that reach `bound`; the sum of the others.  A vector below the bound, as nearly all are, is
+    // summed as it is read; the others are noted, and all threads go through their values afterwards.
     Shared* leader = of(0);
+    unsigned long long* leader_list = a.parts > 1 ? cluster.map_shared_rank(list, 0) : list;
     Group<N> g(scratch);
     const float2 ct = both(a.c);
-    const auto vector_at = [&](int v) { return a.held ? held[v - first] : r.whole(v) ? r.at(v) : edge(v); };
-    const auto collect = [&](int bound, int until) {
-        const float limit = of_key(bound), below = reference(limit);
-        const float2 far = both(-below);
-        float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll 2
-        for (int v = first + threadIdx.x; v < last; v += N) {
-            const Vec<T, W> b = vector_at(v);
-            if (bound != kLeast && largest(b) < limit) {               // (places beside the row hold -inf, which adds nothing)
+    const auto vector_at = [&](int v) { return a.held ? held[v - first] : r.some(v); };
+    const auto add_vector = [&](float2& sum, const Vec<T, W>& b, float2 far) {
 #pragma unroll
-                for (int i = 0; i < W / 2; ++i) {
-                    const float2 e = mul(add(pair(b, i), far), ct);
-                    sum = add(sum, make_float2(approx_exp2(e.x), approx_exp2(e.y)));
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const int place = v * W + i - r.pad;
-                    if (place < 0 || place >= a.classes) continue;
-                    const float x = widen(b.v[i]);
-                    const int k = key_of(x);
-                    if (k > bound || (k == bound && place <= until)) {
-                        const int n = atomicAdd(&leader->found, 1);
-                        if (n < kList) leader->list[n] = (unsigned long long)((unsigned)k ^ 0x80000000u) << 32 | (unsigned)~place;
-                    } else {
-                        sum.x += power(x, below, a.c);
-                    }
-                }
-            }
+        for (int i = 0; i < W / 2; ++i) {
+            const float2 e = mul(add(pair(b, i), far), ct);
+            sum = add(sum, make_float2(approx_exp2(e.x), approx_exp2(e.y)));
         }
+    };
+    const auto note = [&](int key, int place) {
+        const int n = atomicAdd(&leader->found, 1);
+        if (n < a.list) leader_list[n] = (unsigned long long)((unsigned)key ^ 0x80000000u) << 32 | (unsigned)~place;
+    };
+    const auto tell = [&](float2 sum) {               // every thread's sum, to the first CTA; how many values are listed
         float total[1] = {sum.x + sum.y};
         g.sum(total);
-        if (threadIdx.x == 0) leader->sums[part] = total[0];
+        if (threadIdx.x == 0) leader->sums[part] = total[0] + (float)sh.beside * 2.220446e-16f;
         everyone();
         return leader->found;
     };
-    int all = collect(bound, INT_MAX);
-    if (all > kList) {                                // the same in every CTA of the row
+    const auto collect = [&](int bound) {
+        const float limit = of_key(bound), below = reference(limit);
+        const float2 far = both(-below);
+        float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll 1
+        for (int v = first + threadIdx.x; v < last; v += N) {
+            const Vec<T, W> b = vector_at(v);
+            if (bound != kLeast && largest(b) < limit) {               // (places beside the row hold -inf, which adds nothing)
+                add_vector(sum, b, far);
+            } else {
+                const int n = atomicAdd(&sh.flagged, 1);
+                if (n < a.list) noted[n] = v;
+            }
+        }
+        __syncthreads();
+        const int flagged = sh.flagged, values = min(flagged, a.list) * W;
+        if (flagged > a.list && threadIdx.x == 0) atomicAdd(&leader->found, flagged);     // each has one at least
+        for (int i = threadIdx.x; i - lane < values; i += N) {         // (whole warps)
+            const int v = i < values ? noted[i / W] : 0, place = v * W + i % W - r.pad;
+            unsigned high = 0, low = 0;
+            if (i < values && place >= 0 && place < a.classes) {
+                const float x = widen(a.held ? held[v - first].v[i % W] : s[place]);
+                const int key = key_of(x);
+                if (key >= bound) {
+                    note(key, place);
+                } else {                              // integers: the vectors are noted in no order
+                    const float e = power(x, below, a.c) * 67108864.0f;
+                    high = (unsigned)e;
+                    low = (unsigned)((e - (float)high) * 67108864.0f);
+                }
+            }
+            high = __reduce_add_sync(0xffffffffu, high);
+            low = __reduce_add_sync(0xffffffffu, low);
+            if (lane == 0 && (high | low)) atomicAdd(&sh.beside, ((unsigned long long)high << 26) + low);
+        }
+        __syncthreads();
+        return tell(sum);
+    };
+    // the same, where ever so many equal one another: the values above key `bound`, and of those with this key the ones up to
+    // place `until`
+    const auto collect_exactly = [&](int bound, int until) {
+        const float below = reference(of_key(bound));
+        float2 sum = make_float2(0.0f, 0.0f);
+        for (int v = first + threadIdx.x; v < last; v += N) {
+            const Vec<T, W> b = vector_at(v);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const int place = v * W + i - r.pad;
+                if (place < 0 || place >= a.classes) continue;
+                const float x = widen(b.v[i]);
+                const int key = key_of(x);
+                if (key > bound || (key == bound && place <= until))
+                    note(key, place);
+                else
+                    sum.x += power(x, below, a.c);
+            }
+        }
+        return tell(sum);
+    };
+    int all = collect(bound);
+    if (all > a.list) {                                // the same in every CTA of the row
         int turn = 0;
         const auto counted = [&](auto&& pred) {       // how many of the row's values are so, to every thread
             int n = 0;
@@ -250,10 +265,10 @@ __global__ void __launch_bounds__(N, N == 512 ? 3 : 8) top_rows(TopArgs a) {
             else
                 left = middle + 1;
         }
-        if (part == 0 && threadIdx.x == 0) sh.found = 0;
+        if (threadIdx.x == 0) sh.found = 0, sh.beside = 0;
         everyone();
         bound = low;
-        all = collect(low, left);
+        all = collect_exactly(low, left);
     }
 
     // 3. the listed values in order
@@ -261,25 +276,25 @@ __global__ void __launch_bounds__(N, N == 512 ? 3 : 8) top_rows(TopArgs a) {
         T* values = static_cast<T*>(a.values) + (int64_t)row * a.k;
         int* indices = a.indices + (int64_t)row * a.k;
         for (int i = threadIdx.x; i < all; i += N) {
-            const unsigned long long mine = sh.list[i];
+            const unsigned long long mine = list[i];
             int rank = 0;
 #pragma unroll 8
-            for (int n = 0; n < all; ++n) rank += sh.list[n] > mine;
+            for (int n = 0; n < all; ++n) rank += list[n] > mine;
             if (rank < a.k) {
                 const int place = (int)~(unsigned)mine;
                 values[rank] = s[place];
                 indices[rank] = place;
             } else {
-                sh.after[rank - a.k] = of_key((int)((unsigned)(mine >> 32) ^ 0x80000000u));
+                after[rank - a.k] = of_key((int)((unsigned)(mine >> 32) ^ 0x80000000u));
             }
         }
         __syncthreads();
         if (a.k == a.classes) {
             if (threadIdx.x == 0) a.rest[row] = kNone;
         } else {
-            const float m = sh.after[0], below = reference(m);
+            const float m = after[0], below = reference(m);
             float sum[1] = {0};
-            for (int i = threadIdx.x; i < all - a.k; i += N) sum[0] += power(sh.after[i], below, a.c);
+            for (int i = threadIdx.x; i < all - a.k; i += N) sum[0] += power(after[i], below, a.c);
             g.sum(sum);
             if (threadIdx.x == 0) {
                 float others = 0;
@@ -300,12 +315,14 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
     a.parts = 1;
     // a cluster where a slice does not fit, or where the rows are too few for the SMs
     while (N > 128 && a.parts < kClusterMost && (slice() > kHeld || ((int64_t)a.rows * a.parts < kSMs && slice() >= 16384))) a.parts *= 2;
-    a.held = slice() <= kHeld;
+    a.held = slice() <= kHeld ? (int)slice() : 0;
+    a.list = a.k < 128 ? 512 : 1024;
+    constexpr int kLists = 1024 * 12;
     static std::atomic<uint64_t> allowed{0};
     int dev = 0;
     if (const cudaError_t e = cudaGetDevice(&dev)) return e;
     if (dev >= 64 || !(allowed.load() >> dev & 1)) {
-        if (const cudaError_t e = cudaFuncSetAttribute(top_rows<T, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kHeld)) {
+        if (const cudaError_t e = cudaFuncSetAttribute(top_rows<T, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kHeld + kLists)) {
             cudaGetLastError();
             return e;
         }
@@ -314,7 +331,7 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.rows * (unsigned)a.parts);
     cfg.blockDim = dim3(N);
-    cfg.dynamicSmemBytes = a.held ? slice() : 0;
+    cfg.dynamicSmemBytes = a.held + a.list * 12;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -327,7 +344,9 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t top(const TopArgs& a, cudaStream_t st) {
-    return a.classes <= 4096 && a.k < 96 ? launch<T, 128>(a, st) : launch<T, 512>(a, st);
+    // a bound takes more threads than values are wanted; beyond that fewer threads have less to do beside reading
+    if (a.classes <= 4096 && a.k < 96) return launch<T, 128>(a, st);
+    return a.k < 192 ? launch<T, 256>(a, st) : launch<T, 512>(a, st);
 }
 
 }  // namespace
