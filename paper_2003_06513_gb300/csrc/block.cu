@@ -49,9 +49,10 @@ int row_threads(int C) {
 
 constexpr int kJoinChannels = 32, kJoinParts = 32;
 
-// Sums of the CTAs' parts: blockIdx.y below kBlockSums one of the sums over all rows, else the gate's gradient of the last
-// sample of CTA blockIdx.y - kBlockSums, where further CTAs have the rest of it.
+// Sums of the CTAs' parts: blockIdx.y below kBlockSums one of the sums over all rows, else the gate's gradient of a
+// sample that several CTAs have parts of.
 __global__ void __launch_bounds__(kJoinChannels* kJoinParts) block_sums(BlockArgs a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");        // its launch overlaps the end of the kernel before it
     __shared__ float parts[kJoinParts][kJoinChannels + 1];
     const int c = blockIdx.x * kJoinChannels + threadIdx.x % kJoinChannels, part = threadIdx.x / kJoinChannels;
     const float* from;
@@ -66,10 +67,12 @@ __global__ void __launch_bounds__(kJoinChannels* kJoinParts) block_sums(BlockArg
         step = (int64_t)kBlockSums * a.C;
         n = a.ctas;
     } else {
-        const int64_t i = blockIdx.y - kBlockSums, begin = i * a.stretch, end = begin + a.stretch;
+        // of N samples, or of the last one of each CTA where those are fewer: the one that begins in CTA i and ends in another
+        const int64_t y = blockIdx.y - kBlockSums, i = a.N <= a.ctas ? y * a.pixels / a.stretch : y;
+        const int64_t begin = i * a.stretch, end = begin + a.stretch;
         if (end >= a.rows) return;                    // the last CTA's samples end there
-        const int64_t sample = (end - 1) / a.pixels, first = sample * a.pixels, last = first + a.pixels;
-        if (last == end || first < begin) return;     // it ends with this CTA, or began in an earlier one
+        const int64_t sample = a.N <= a.ctas ? y : (end - 1) / a.pixels, first = sample * a.pixels, last = first + a.pixels;
+        if (last <= end || first < begin) return;     // it ends with this CTA, or began in an earlier one
         const int64_t until = (last - 1) / a.stretch;
         // its first part is the CTA's last, or its only, segment; in the others it is the first one
         to = a.dgate + sample * a.C;
@@ -216,10 +219,10 @@ size_t workspace_of(const Shape& s) {
 
 }  // namespace
 
-// One wave of CTAs: two of 256 threads on an SM, or as many of longer rows' threads; each of four rounds of rows at least.
+// One wave of CTAs: five of 128 threads on an SM, or as many of longer rows' threads; each of four rounds of rows at least.
 int block_ctas(int64_t rows, int C, int64_t* stretch) {
-    const int threads = row_threads(C), here = threads > 32 ? 1 : kBlockThreads / threads;
-    const int64_t most = threads > 32 ? kSMs * std::max(1, 512 / threads) : kSMs * 2;
+    const int threads = row_threads(C), here = threads > 32 ? 1 : kBlockBackThreads / threads;
+    const int64_t most = threads > 32 ? kSMs * std::max(1, 512 / threads) : kSMs * 5;
     const int64_t n = std::max<int64_t>(1, std::min(most, rows / (4 * here)));
     *stretch = (rows + n - 1) / n;
     return (int)((rows + *stretch - 1) / *stretch);
@@ -227,9 +230,18 @@ int block_ctas(int64_t rows, int C, int64_t* stretch) {
 
 cudaError_t block_join(const BlockArgs& a, cudaStream_t st) {
     if (!a.dweight && !a.dbias && !a.dpost_weight && !a.dpost_bias && !a.dscale && !a.dgate) return cudaSuccess;
-    const dim3 grid((a.C + kJoinChannels - 1) / kJoinChannels, kBlockSums + (a.dgate ? a.ctas : 0));
-    block_sums<<<grid, kJoinChannels * kJoinParts, 0, st>>>(a);
-    return cudaGetLastError();
+    const dim3 grid((a.C + kJoinChannels - 1) / kJoinChannels, kBlockSums + (a.dgate ? std::min(a.N, a.ctas) : 0));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kJoinChannels * kJoinParts);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = norm_starts_early();
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, block_sums, a), l = cudaGetLastError();
+    return e != cudaSuccess ? e : l;
 }
 
 }  // namespace patconv
@@ -275,6 +287,7 @@ int pp_block_norm(const void* x, int64_t x_pixel, int64_t x_sample, int x_dtype,
     set(a, &BlockArgs::b, &BlockArgs::b_pixel, &BlockArgs::b_sample, b);
     a.h = h;
     a.y = y;
+    if (!block) a.dense = 0;
     const int V = std::min({in.vector(s), block ? b.vector(s) : 8, vector_of(s, h, in.es), vector_of(s, y, b.es)});
     a.vectors = C / V;
     return by_type(s, [&](auto k) { return k.forward(a, V, static_cast<cudaStream_t>(stream)); });
@@ -342,6 +355,7 @@ int pp_block_norm_backward(const void* dh, int64_t dh_pixel, int64_t dh_sample, 
     for (const Input* t : {&d, &e, &in, &b})
         if (t->p && (t != &in || norm)) V = std::min(V, t->vector(s));
     a.vectors = C / V;
+    if (!block || !dh || !norm) a.dense = 0;
     int64_t stretch;
     a.ctas = block_ctas((int64_t)N * pixels, C, &stretch);
     a.stretch = (int)stretch;

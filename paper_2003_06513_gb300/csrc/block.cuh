@@ -20,8 +20,9 @@ namespace {
 constexpr int E = kBlockEight;
 
 // Forms of the kernels.  kLong: a CTA has one row, of whole warps.  kShort: several rows, of a power of two of threads each.
-// 8, 16, 32: the same with so many threads, known beforehand, on dense tensors in vectors of eight channels: with loops
-// that unroll and one offset for all tensors a row takes half the instructions, which bound the kernels before memory does.
+// 8, 16, 32: the same with so many threads, known beforehand, on dense tensors in vectors of eight channels, with both norms of
+// one kind (KIND) and all inputs there: with loops that unroll, one 32-bit offset for all tensors and no choices left a row takes
+// half the instructions, which bound the kernels before memory does.
 enum { kLong = -1, kShort = 0 };
 
 // eight channels of a row: V adjacent ones, then those `threads` vectors on, and so on
@@ -60,6 +61,25 @@ struct Ahead {
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
                 else
                     asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(S), "r"(n) : "memory");
+            }
+        }
+    }
+    // the k-th of the thread's eight values
+    static __device__ __forceinline__ float one(uint32_t place, const T* mine, int threads, int k) {
+        if constexpr (!kAsync) {
+            return widen(mine[apart(threads, k)]);
+        } else {
+            const int byte = k * (int)sizeof(T), from = place + ((byte / S) * blockDim.x + threadIdx.x) * S + byte % S;
+            if constexpr (sizeof(T) == 4) {
+                float x;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(from) : "memory");
+                return x;
+            } else {
+                uint16_t bits;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(bits) : "r"(from) : "memory");
+                T x;
+                memcpy(&x, &bits, 2);
+                return widen(x);
             }
         }
     }
@@ -154,6 +174,39 @@ __device__ __forceinline__ Eight parameter(const float* p, float otherwise, int 
     }
     return e;
 }
+// A parameter's values where they are used: of a long row in the thread's registers, of short ones in shared memory, where the
+// CTA's rows share them, and which leaves registers for a third of the warps more.
+template <int FORM>
+struct Held {
+    Eight e;
+    uint32_t place;                                   // this thread's first four values, the others `threads` places on
+    __device__ __forceinline__ Held(float* shared, int lane) : place((uint32_t)__cvta_generic_to_shared(shared) + lane * 16) {}
+    // by every thread of a long row, by those of one of the short ones; a barrier before they are used
+    __device__ __forceinline__ void set(const Eight& v, int threads, bool mine) {
+        if (FORM == kLong) {
+            e = v;
+        } else if (mine) {
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(place), "f"(v.v[0].x), "f"(v.v[0].y), "f"(v.v[1].x), "f"(v.v[1].y) : "memory");
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(place + threads * 16), "f"(v.v[2].x), "f"(v.v[2].y), "f"(v.v[3].x), "f"(v.v[3].y) : "memory");
+        }
+    }
+    __device__ __forceinline__ Eight get(int threads) const {
+        if (FORM == kLong) return e;
+        Eight v;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.v[0].x), "=f"(v.v[0].y), "=f"(v.v[1].x), "=f"(v.v[1].y) : "r"(place) : "memory");
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.v[2].x), "=f"(v.v[2].y), "=f"(v.v[3].x), "=f"(v.v[3].y) : "r"(place + threads * 16) : "memory");
+        return v;
+    }
+};
+template <int FORM>
+constexpr int kHeldFloats = FORM == kLong ? 1 : FORM == kShort ? 32 * E : FORM * E;
+template <int V>
+__device__ __forceinline__ Eight times(const Eight& p, const Eight& q) {
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) r.v[i] = mul(p.v[i], q.v[i]);
+    return r;
+}
 // whether each of the eight is one of the row's channels
 template <int V>
 __device__ __forceinline__ bool inside(int lane, const BlockArgs& a, int k) { return lane + k / V * a.threads < a.vectors; }
@@ -181,8 +234,16 @@ struct RowSum {
         } else {
 #pragma unroll
             for (int o = 1; o < (FORM == kLong ? 32 : FORM); o *= 2)
+                if constexpr (std::is_same<T, float>::value && K % 2 == 0) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+                    for (int k = 0; k < K; k += 2) {
+                        const float2 t = add(make_float2(s[k], s[k + 1]), make_float2(__shfl_xor_sync(0xffffffffu, s[k], o), __shfl_xor_sync(0xffffffffu, s[k + 1], o)));
+                        s[k] = t.x, s[k + 1] = t.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < K; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+                }
         }
     }
     template <int K>
@@ -277,14 +338,15 @@ __device__ __forceinline__ At at_row(int row, const BlockArgs& a) {
 }
 // the same, or, where every tensor's samples follow one another as its pixels do, all as one sample
 __device__ __forceinline__ At place_of(int row, const BlockArgs& a) { return a.flat ? At{0, row} : at_row(row, a); }
-// Where a row's channels are: of a dense tensor `offset` channels from the first, of others by their strides.
+// Where a thread's channels of a row are: of a dense tensor so many from the CTA's first row on, of others by their strides.
 struct Spot {
     At at;
-    int64_t offset;
+    int64_t begin;                                    // (dense) the CTA's first row: the same for all threads
+    uint32_t offset;
 };
 template <bool DENSE, typename T>
 __device__ __forceinline__ const T* spot_in(const void* p, const Spot& s, int64_t pixel, int64_t sample, int lane_first) {
-    if (DENSE) return static_cast<const T*>(p) + s.offset;
+    if (DENSE) return static_cast<const T*>(p) + s.begin + s.offset;
     return static_cast<const T*>(p) + s.at.sample * sample + (int64_t)s.at.pixel * (int)pixel + lane_first;
 }
 
@@ -300,9 +362,11 @@ __device__ __forceinline__ float act_of(float z, int act) {
 
 // -------------------------------------------------------------------------------- forward
 
-template <typename TX, typename TB, int V, int FORM>
-__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 3) block_rows(BlockArgs a) {
+template <typename TX, typename TB, int V, int FORM, int KIND>
+__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 4) block_rows(BlockArgs a) {
     constexpr bool WIDE = FORM == kLong, DENSE = FORM > 0;
+    const int post = KIND ? KIND : a.post, pre = KIND ? KIND : a.pre;
+    const bool has_b = KIND || a.b;
     extern __shared__ __align__(16) char ring[];
     __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
     const int threads = FORM > 0 ? FORM : a.threads;
@@ -310,43 +374,51 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
     const int here = WIDE ? 1 : kBlockThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
     RowSum<FORM> sum{threads, scratch};
     // the block's weight and bias with the residual scale in them, the stream's
-    Eight wb = parameter<V>(a.post_weight, 1.0f, lane, a), bb = parameter<V>(a.post_bias, 0.0f, lane, a);
-    const Eight sc = parameter<V>(a.scale, 1.0f, lane, a);
-    const Eight w = parameter<V>(a.weight, 1.0f, lane, a), bias = parameter<V>(a.bias, 0.0f, lane, a);
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) wb.v[i] = mul(wb.v[i], sc.v[i]), bb.v[i] = mul(bb.v[i], sc.v[i]);
+    __shared__ __align__(16) float shared[4][kHeldFloats<FORM>];
+    Held<FORM> wb(shared[0], lane), bb(shared[1], lane), w(shared[2], lane), bias(shared[3], lane);
+    {
+        const Eight sc = parameter<V>(a.scale, 1.0f, lane, a);
+        wb.set(times<V>(parameter<V>(a.post_weight, 1.0f, lane, a), sc), threads, mine == 0);
+        bb.set(times<V>(parameter<V>(a.post_bias, 0.0f, lane, a), sc), threads, mine == 0);
+        w.set(parameter<V>(a.weight, 1.0f, lane, a), threads, mine == 0);
+        bias.set(parameter<V>(a.bias, 0.0f, lane, a), threads, mine == 0);
+        if (!WIDE) __syncthreads();
+    }
     Eight gate = parameter<V>(nullptr, 1.0f, lane, a);
     int gate_of = -1;
     const float inv_own = 1.0f / own_channels<V>(lane, a);
 
     using X = Ahead<TX, V>;
     using B = Ahead<TB, V>;
-    const int step = gridDim.x * here, first = blockIdx.x * here + mine;
-    const int64_t stride = (int64_t)step * a.C;
+    // consecutive rows: the gate changes with the sample
+    const int begin = blockIdx.x * a.stretch, end = min(a.rows, begin + a.stretch);
+    const uint32_t stride = (uint32_t)(here * a.C);
+    const int64_t begin_at = (int64_t)begin * a.C;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const int round = (X::kBytes + B::kBytes) * blockDim.x, b_at = X::kBytes * blockDim.x;
-    const auto spot_of = [&](int row, bool there, int64_t offset) { return Spot{DENSE ? At{0, 0} : place_of(there ? row : 0, a), offset}; };
+    const auto spot_of = [&](int row, bool there, uint32_t offset) { return Spot{DENSE ? At{0, 0} : place_of(there ? row : 0, a), begin_at, offset}; };
     const auto x_in = [&](const Spot& s) { return spot_in<DENSE, TX>(a.x, s, a.x_pixel, a.x_sample, lane * V); };
     const auto b_in = [&](const Spot& s) { return spot_in<DENSE, TB>(a.b, s, a.b_pixel, a.b_sample, lane * V); };
     const bool in_row = lane < a.vectors;             // (V = 8)
     const auto live_if = [&](bool there) {
         return [=, &a](int k) { return there && (V == 8 ? in_row : lane + k * threads < a.vectors); };
     };
-    const auto ask = [&](int row, int64_t offset, int slot) {
-        if (row - mine < a.rows) {                    // (of the CTA's first row: the same for all)
-            const bool there = row < a.rows;
-            const Spot s = spot_of(row, there, there ? offset : 0);
+    const auto ask = [&](int base, uint32_t offset, int slot) {
+        if (base < end) {
+            const bool there = base + mine < end;
+            const Spot s = spot_of(base + mine, there, offset);
             X::ask(ring_at + slot * round, x_in(s), threads, live_if(there));
-            if (a.b) B::ask(ring_at + slot * round + b_at, b_in(s), threads, live_if(there));
+            if (has_b) B::ask(ring_at + slot * round + b_at, b_in(s), threads, live_if(there));
         }
         copies_end();
     };
-    int64_t offset = (int64_t)first * a.C + lane * V;
-    for (int k = 0; k < kRounds - 1; ++k) ask(first + k * step, offset + k * stride, k);
+    uint32_t offset = (uint32_t)(mine * a.C + lane * V);
+    for (int k = 0; k < kRounds - 1; ++k) ask(begin + k * here, offset + k * stride, k);
     int slot = 0;
-    for (int row = first; row - mine < a.rows; row += step, offset += stride) {
-        const bool there = row < a.rows;
-        ask(row + (kRounds - 1) * step, offset + (kRounds - 1) * stride, slot == 0 ? kRounds - 1 : slot - 1);    // where the round before has read
+    for (int base = begin; base < end; base += here, offset += stride) {
+        const int row = base + mine;
+        const bool there = row < end;
+        ask(base + (kRounds - 1) * here, offset + (kRounds - 1) * stride, slot == 0 ? kRounds - 1 : slot - 1);   // where the round before has read
         copies_wait<kRounds - 1>();
         const uint32_t place = ring_at + slot * round;
         slot = slot == kRounds - 1 ? 0 : slot + 1;
@@ -360,80 +432,91 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
             }
         }
         Eight h = widened(X::get(place, x_in(at), threads, live));
-        if (a.b) {
+        if (has_b) {
             Eight b = widened(B::get(place + b_at, b_in(at), threads, live));
-            if (a.post == PP_NORM_LAYER) centre<V>(b, sum.near(across(sum_of(b)), inv_own, a.inv_c), lane, a);
-            float q[2] = {a.post == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f, dot(b, b)};
-            if (a.post != PP_NORM_NONE) sum.all(q);
-            const Scaling r(a.post, q[0], q[1], a);
+            if (post == PP_NORM_LAYER) centre<V>(b, sum.near(across(sum_of(b)), inv_own, a.inv_c), lane, a);
+            float q[2] = {post == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f, dot(b, b)};
+            if (post != PP_NORM_NONE) sum.all(q);
+            const Scaling r(post, q[0], q[1], a);
+            const Eight pw = wb.get(threads), pb = bb.get(threads);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i)
-                h.v[i] = fma(fma(fma(b.v[i], both(r.root), both(r.shift)), wb.v[i], bb.v[i]), gate.v[i], h.v[i]);
+                h.v[i] = fma(fma(fma(b.v[i], both(r.root), both(r.shift)), pw.v[i], pb.v[i]), gate.v[i], h.v[i]);
             const Raw<TX, V> out = narrowed<TX, V>(h);
-            put(static_cast<TX*>(a.h) + offset, out, threads, live);
+            put(static_cast<TX*>(a.h) + begin_at + offset, out, threads, live);
             h = widened(out);                         // the second norm is of the stream as it is stored
         }
-        if (a.pre == PP_NORM_NONE) continue;
-        if (a.pre == PP_NORM_LAYER) centre<V>(h, sum.near(across(sum_of(h)), inv_own, a.inv_c), lane, a);
-        float q[2] = {a.pre == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, dot(h, h)};
+        if (pre == PP_NORM_NONE) continue;
+        if (pre == PP_NORM_LAYER) centre<V>(h, sum.near(across(sum_of(h)), inv_own, a.inv_c), lane, a);
+        float q[2] = {pre == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, dot(h, h)};
         sum.all(q);
-        const Scaling r(a.pre, q[0], q[1], a);
+        const Scaling r(pre, q[0], q[1], a);
+        const Eight nw = w.get(threads), nb = bias.get(threads);
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) h.v[i] = fma(fma(h.v[i], both(r.root), both(r.shift)), w.v[i], bias.v[i]);
+        for (int i = 0; i < E / 2; ++i) h.v[i] = fma(fma(h.v[i], both(r.root), both(r.shift)), nw.v[i], nb.v[i]);
         if (a.act != PP_ACT_NONE)
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) h.v[i] = make_float2(act_of(h.v[i].x, a.act), act_of(h.v[i].y, a.act));
-        put(static_cast<TB*>(a.y) + offset, narrowed<TB, V>(h), threads, live);
+        put(static_cast<TB*>(a.y) + begin_at + offset, narrowed<TB, V>(h), threads, live);
     }
 }
 
 // -------------------------------------------------------------------------------- backward
 
 // Whether z = w (h - mean) r + bias is above 0, where fp32 cannot tell: mean and root in 64 bits.  Every thread of the CTA
-// (WIDE) or of the warp calls it.
-template <typename TX, int V, int FORM>
-__device__ __noinline__ unsigned above_zero(uint32_t place, const TX* mine, bool there, const BlockArgs& a, int lane, RowSum<FORM>& sum) {
-    const Eight h = widened(Ahead<TX, V>::get(place, mine, sum.threads, [&](int k) { return there && inside<V>(lane, a, k * V); }));
-    const float* f = reinterpret_cast<const float*>(h.v);
+// (kLong) or of the warp calls it; value(k) is the thread's k-th channel's.  One channel at a time: it is rarely come to, and
+// is to take few registers from what is.
+template <int V, int FORM, typename F>
+__device__ __forceinline__ unsigned above_zero(F&& value, const BlockArgs& a, int lane, RowSum<FORM>& sum) {
     double mean = 0, square = 0;
     if (a.pre == PP_NORM_LAYER) {
-        for (int k = 0; k < E; ++k) mean += (double)f[k];                // beyond the row they are 0
+#pragma unroll 1
+        for (int k = 0; k < E; ++k) mean += (double)value(k);            // beyond the row they are 0
         mean = sum.exactly(mean) / a.C;
     }
+#pragma unroll 1
     for (int k = 0; k < E; ++k)
-        if (inside<V>(lane, a, k)) square += ((double)f[k] - mean) * ((double)f[k] - mean);
+        if (inside<V>(lane, a, k)) square += ((double)value(k) - mean) * ((double)value(k) - mean);
     const double r = 1.0 / sqrt(sum.exactly(square) / a.C + (double)a.eps);
     unsigned above = 0;
+#pragma unroll 1
     for (int k = 0; k < E; ++k) {
-        const int c = channel<V>(lane, a.threads, k);
+        const int c = channel<V>(lane, sum.threads, k);
         if (c >= a.C) continue;
-        const double z = ((double)f[k] - mean) * r * (a.weight ? (double)a.weight[c] : 1.0) + (a.bias ? (double)a.bias[c] : 0.0);
+        const double z = ((double)value(k) - mean) * r * (a.weight ? (double)a.weight[c] : 1.0) + (a.bias ? (double)a.bias[c] : 0.0);
         above |= (unsigned)(z > 0) << k;
     }
     return above;
 }
 
-template <typename TX, typename TB, int V, int FORM>
-__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 2) block_back_rows(BlockArgs a) {
+template <typename TX, typename TB, int V, int FORM, int KIND>
+__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM == kLong ? 1 : 5) block_back_rows(BlockArgs a) {
     constexpr bool WIDE = FORM == kLong, DENSE = FORM > 0;
     constexpr int R = kRoundsBack<TX, TB, WIDE>;
     extern __shared__ __align__(16) char ring[];
     __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
-    __shared__ float lanes_sum[WIDE ? 1 : 2 * kBlockThreads * E];
+    __shared__ float lanes_sum[WIDE ? 1 : 2 * kBlockBackThreads * E];
     const int threads = FORM > 0 ? FORM : a.threads;
     const int lane = WIDE ? threadIdx.x : threadIdx.x % threads;
-    const int here = WIDE ? 1 : kBlockThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
+    const int here = WIDE ? 1 : kBlockBackThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
     RowSum<FORM> sum{threads, scratch};
-    const bool pre = a.pre != PP_NORM_NONE, post = a.post != PP_NORM_NONE;
-    const Eight w = parameter<V>(a.weight, 1.0f, lane, a), bias = parameter<V>(a.bias, 0.0f, lane, a);
+    const int post_kind = KIND ? KIND : a.post, pre_kind = KIND ? KIND : a.pre;
+    const bool pre = pre_kind != PP_NORM_NONE, post = post_kind != PP_NORM_NONE, has_b = KIND || a.b, has_dh = KIND || a.dh;
+    __shared__ __align__(16) float shared[3][kHeldFloats<FORM>];
+    Held<FORM> w_held(shared[0], lane), bias_held(shared[1], lane), k_held(shared[2], lane);
     const Eight zero{};
     const float inv_own = 1.0f / own_channels<V>(lane, a);
     float reach = 0;                                  // how near to 0 a z of this thread's may be without its sign being sure
+    {
+        const Eight w = parameter<V>(a.weight, 1.0f, lane, a), bias = parameter<V>(a.bias, 0.0f, lane, a);
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i)
-        reach = fmaxf(reach, fmaxf(fmaf(fabsf(w.v[i].x), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].x)),
-                                   fmaf(fabsf(w.v[i].y), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].y))));
-    reach *= 3.8147e-6f;
+        for (int i = 0; i < E / 2; ++i)
+            reach = fmaxf(reach, fmaxf(fmaf(fabsf(w.v[i].x), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].x)),
+                                       fmaf(fabsf(w.v[i].y), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].y))));
+        reach *= 3.8147e-6f;
+        w_held.set(w, threads, mine == 0);
+        bias_held.set(bias, threads, mine == 0);
+    }
     // the means over a row of t (of a layer norm) and of t v^
     const auto means = [&](int kind, const Eight& t, const Eight& v) {
         float q[2] = {kind == PP_NORM_LAYER ? across(sum_of(t)) : 0.0f, dot(t, v)};
@@ -441,8 +524,8 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
         return make_float2(q[0] * a.inv_c, q[1] * a.inv_c);
     };
     Eight s_w = zero, s_b = zero, s_e = zero, s_f = zero;        // sums of dz h^, dz, and of a sample dh b^, dh
-    // the sums over all samples, in shared memory: of post_weight, post_bias and scale, thread c's (WIDE: the thread's eight channels')
-    constexpr int OWN = WIDE ? E : 1;
+    // the sums over all samples, in shared memory: of post_weight, post_bias and scale, thread c's, and so on (WIDE: the thread's eight channels')
+    constexpr int OWN = WIDE ? E : 32 * E / kBlockBackThreads;
     float* totals = reinterpret_cast<float*>(ring + R * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) * blockDim.x) + threadIdx.x;
     const auto total = [&](int which, int i) -> float& { return totals[(which * OWN + i) * blockDim.x]; };
 #pragma unroll
@@ -453,7 +536,9 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const int x_bytes = X::kBytes * blockDim.x, b_bytes = B::kBytes * blockDim.x, round = 2 * (x_bytes + b_bytes);
     const int d_at = 0, h_at = x_bytes, y_at = 2 * x_bytes, b_at = y_at + b_bytes;
-    const auto spot_of = [&](int row, int64_t offset) { return Spot{DENSE ? At{0, 0} : place_of(row, a), offset}; };
+    const int begin = blockIdx.x * a.stretch, end = min(a.rows, begin + a.stretch);
+    const int64_t begin_at = (int64_t)begin * a.C;
+    const auto spot_of = [&](int row, uint32_t offset) { return Spot{DENSE ? At{0, 0} : place_of(row, a), begin_at, offset}; };
     const auto h_in = [&](const Spot& s) { return spot_in<DENSE, TX>(a.x, s, a.x_pixel, a.x_sample, lane * V); };
     const auto b_in = [&](const Spot& s) { return spot_in<DENSE, TB>(a.b, s, a.b_pixel, a.b_sample, lane * V); };
     const auto d_in = [&](const Spot& s) { return spot_in<DENSE, TX>(a.dh, s, a.dh_pixel, a.dh_sample, lane * V); };
@@ -463,33 +548,32 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
         return [=, &a](int k) { return there && (V == 8 ? in_row : lane + k * threads < a.vectors); };
     };
     // asks for a round of rows, `last` the end of their sample's
-    const auto ask = [&](int base, int last, int64_t offset, int slot) {
+    const auto ask = [&](int base, int last, uint32_t offset, int slot) {
         if (base < last) {
             const bool there = base + mine < last;
-            const Spot s = spot_of(there ? base + mine : base, there ? offset : 0);
+            const Spot s = spot_of(there ? base + mine : base, offset);
             const auto live = live_if(there);
             const uint32_t place = ring_at + slot * round;
             if (pre) X::ask(place + h_at, h_in(s), threads, live);
-            if (a.b) B::ask(place + b_at, b_in(s), threads, live);
+            if (has_b) B::ask(place + b_at, b_in(s), threads, live);
             if (pre) B::ask(place + y_at, y_in(s), threads, live);
-            if (a.dh) X::ask(place + d_at, d_in(s), threads, live);
+            if (has_dh) X::ask(place + d_at, d_in(s), threads, live);
         }
         copies_end();
     };
 
-    const int begin = blockIdx.x * a.stretch, end = min(a.rows, begin + a.stretch);
     for (int from = begin; from < end;) {
         const At start = at_row(from, a);
         const int to = a.gate ? min(end, from + (int)a.pixels - start.pixel) : end;
         const float* gate = a.gate ? a.gate + (int64_t)start.sample * a.C : nullptr;
         // what dh is multiplied with on its way to the normalised block
-        Eight k = parameter<V>(a.post_weight, 1.0f, lane, a);
-        const Eight sc = parameter<V>(a.scale, 1.0f, lane, a), ga = parameter<V>(gate, 1.0f, lane, a);
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) k.v[i] = mul(k.v[i], mul(sc.v[i], ga.v[i]));
+        if (!WIDE) __syncthreads();                   // (the sample before has been summed)
+        k_held.set(times<V>(parameter<V>(a.post_weight, 1.0f, lane, a), times<V>(parameter<V>(a.scale, 1.0f, lane, a), parameter<V>(gate, 1.0f, lane, a))),
+                   threads, mine == 0);
+        if (!WIDE) __syncthreads();
 
-        const int64_t stride = (int64_t)here * a.C;
-        int64_t offset = (int64_t)(from + mine) * a.C + lane * V;
+        const uint32_t stride = (uint32_t)(here * a.C);
+        uint32_t offset = (uint32_t)((from - begin + mine) * a.C + lane * V);
         for (int k = 0; k < R - 1; ++k) ask(from + k * here, to, offset + k * stride, k);
         int slot = 0;
         for (int base = from; base < to; base += here, offset += stride) {
@@ -503,31 +587,33 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
             const Spot at = spot_of(there ? row : base, offset);
             Eight h = zero, b = zero;
             if (pre) h = widened(X::get(place + h_at, h_in(at), threads, live));
-            if (a.b) b = widened(B::get(place + b_at, b_in(at), threads, live));
+            if (has_b) b = widened(B::get(place + b_at, b_in(at), threads, live));
             // both norms
             float centres[2] = {0, 0};
-            if (a.pre == PP_NORM_LAYER || a.post == PP_NORM_LAYER) {
+            if (pre_kind == PP_NORM_LAYER || post_kind == PP_NORM_LAYER) {
                 centres[0] = across(sum_of(h)), centres[1] = across(sum_of(b));
                 sum.near(centres, inv_own, a.inv_c);
             }
-            if (a.pre == PP_NORM_LAYER) centre<V>(h, centres[0], lane, a);
-            if (a.post == PP_NORM_LAYER) centre<V>(b, centres[1], lane, a);
-            float moments[4] = {a.pre == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, a.post == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f, dot(h, h), dot(b, b)};
+            if (pre_kind == PP_NORM_LAYER) centre<V>(h, centres[0], lane, a);
+            if (post_kind == PP_NORM_LAYER) centre<V>(b, centres[1], lane, a);
+            float moments[4] = {pre_kind == PP_NORM_LAYER ? across(sum_of(h)) : 0.0f, post_kind == PP_NORM_LAYER ? across(sum_of(b)) : 0.0f, dot(h, h), dot(b, b)};
             if (pre || post) sum.all(moments);
-            const Scaling sh(a.pre, moments[0], moments[2], a), sb(a.post, moments[1], moments[3], a);
+            const Scaling sh(pre_kind, moments[0], moments[2], a), sb(post_kind, moments[1], moments[3], a);
             const float2 r = there ? make_float2(sh.root, sb.root) : make_float2(0.0f, 0.0f);
             const float2 shift = there ? make_float2(sh.shift, sb.shift) : make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i)
                 h.v[i] = fma(h.v[i], both(r.x), both(shift.x)), b.v[i] = fma(b.v[i], both(r.y), both(shift.y));
             Eight d = zero;
-            if (!pre && a.dh) d = widened(X::get(place + d_at, d_in(at), threads, live));
+            if (!pre && has_dh) d = widened(X::get(place + d_at, d_in(at), threads, live));
             if (pre) {
+                const Eight w = w_held.get(threads);
                 Eight dz = widened(B::get(place + y_at, y_in(at), threads, live));
                 if (a.act == PP_ACT_RELU) {
                     // fp32's z is off by less than 2^-18 of its terms' sizes (each value, the mean, and the root by some 16 roundings
                     // of the row's sums), |h^| is at most the root of C: where the smallest z is nearer to 0 than that the
                     // signs are taken in 64 bits
+                    const Eight bias = bias_held.get(threads);
                     float2 z[E / 2];
                     float least = INFINITY;
 #pragma unroll
@@ -535,10 +621,10 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
                         z[i] = fma(h.v[i], w.v[i], bias.v[i]);
                         least = fminf(least, fminf(fabsf(z[i].x), fabsf(z[i].y)));
                     }
-                    const float spread = 1.0f + 2.0f * fabsf(a.pre == PP_NORM_LAYER ? centres[0] * r.x : 0.0f);
+                    const float spread = 1.0f + 2.0f * fabsf(pre_kind == PP_NORM_LAYER ? centres[0] * r.x : 0.0f);
                     const bool close = there && least <= reach * spread;
                     if (WIDE ? __syncthreads_or(close) : __any_sync(0xffffffffu, close)) {
-                        const unsigned above = above_zero<TX, V, FORM>(place + h_at, h_in(at), there, a, lane, sum);
+                        const unsigned above = above_zero<V, FORM>([&](int k) { return there && inside<V>(lane, a, k) ? X::one(place + h_at, h_in(at), threads, k) : 0.0f; }, a, lane, sum);
 #pragma unroll
                         for (int i = 0; i < E / 2; ++i) {
                             if (!(above >> (2 * i) & 1)) dz.v[i].x = 0.0f;
@@ -552,6 +638,7 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
                         }
                     }
                 } else if (a.act == PP_ACT_SILU) {
+                    const Eight bias = bias_held.get(threads);
 #pragma unroll
                     for (int i = 0; i < E / 2; ++i) {
                         const float2 z = fma(h.v[i], w.v[i], bias.v[i]);
@@ -567,14 +654,15 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
                     s_b.v[i] = add(dz.v[i], s_b.v[i]);
                     t.v[i] = mul(dz.v[i], w.v[i]);
                 }
-                const float2 q = means(a.pre, t, h);
-                if (a.dh) d = widened(X::get(place + d_at, d_in(at), threads, live));
+                const float2 q = means(pre_kind, t, h);
+                if (has_dh) d = widened(X::get(place + d_at, d_in(at), threads, live));
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i)
                     d.v[i] = fma(fma(h.v[i], both(-q.y), add(t.v[i], both(-q.x))), both(r.x), d.v[i]);
             }
-            if (a.dx) put(static_cast<TX*>(a.dx) + offset, narrowed<TX, V>(d), threads, live);
-            if (!a.b) continue;
+            put(static_cast<TX*>(a.dx) + begin_at + offset, narrowed<TX, V>(d), threads, live);
+            if (!has_b) continue;
+            const Eight k = k_held.get(threads);
             Eight t;
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
@@ -583,17 +671,17 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
                 t.v[i] = mul(d.v[i], k.v[i]);
             }
             if (post) {
-                const float2 q = means(a.post, t, b);
+                const float2 q = means(post_kind, t, b);
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) t.v[i] = mul(fma(b.v[i], both(-q.y), add(t.v[i], both(-q.x))), both(r.y));
             }
-            put(static_cast<TB*>(a.db) + offset, narrowed<TB, V>(t), threads, live);
+            put(static_cast<TB*>(a.db) + begin_at + offset, narrowed<TB, V>(t), threads, live);
         }
 
         // the sample's sums: of the block's norm, the gate and the scale
-        if (a.b) {
+        if (has_b) {
             float* e_all = lanes_sum;
-            float* f_all = lanes_sum + kBlockThreads * E;
+            float* f_all = lanes_sum + kBlockBackThreads * E;
             if (!WIDE) {
                 __syncthreads();
                 const float* pe = reinterpret_cast<const float*>(s_e.v);
@@ -609,7 +697,7 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
             const bool first = from == begin, whole = (first ? start.pixel == 0 : true) && (to < end || at_row(end - 1, a).pixel == a.pixels - 1);
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-                const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x;
+                const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x + i * kBlockBackThreads;
                 if (c >= a.C) continue;
                 float e = 0, f = 0;
                 if (WIDE) {
@@ -645,20 +733,20 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
         for (int i = 0; i < E; ++i) {
             const int c = channel<V>(lane, threads, i);
             lanes_sum[mine * threads * E + c] = pw[i];
-            lanes_sum[kBlockThreads * E + mine * threads * E + c] = pb[i];
+            lanes_sum[kBlockBackThreads * E + mine * threads * E + c] = pb[i];
         }
         __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
-        const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x;
+        const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x + i * kBlockBackThreads;
         if (c >= a.C) continue;
         float e = 0, f = 0;
         if (WIDE) {
             e = reinterpret_cast<const float*>(s_w.v)[i];
             f = reinterpret_cast<const float*>(s_b.v)[i];
         } else {
-            for (int g = 0; g < here; ++g) e += lanes_sum[g * threads * E + c], f += lanes_sum[kBlockThreads * E + g * threads * E + c];
+            for (int g = 0; g < here; ++g) e += lanes_sum[g * threads * E + c], f += lanes_sum[kBlockBackThreads * E + g * threads * E + c];
         }
         out[c] = e;
         out[a.C + c] = f;
@@ -679,46 +767,51 @@ cudaError_t allow_shared(K* kernel, std::atomic<uint64_t>& done, size_t bytes) {
     if (e != cudaSuccess) cudaGetLastError();
     return e;
 }
-template <typename TX, typename TB, int V, int FORM>
+template <typename TX, typename TB, int V, int FORM, int KIND>
 cudaError_t forward_rows(const BlockArgs& a, cudaStream_t st) {
     constexpr int kRound = Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes, kMost = FORM == kLong ? 512 : kBlockThreads;
     static std::atomic<uint64_t> allowed{0};
-    if (const cudaError_t e = allow_shared(block_rows<TX, TB, V, FORM>, allowed, kRounds * kRound * kMost)) return e;
+    if (const cudaError_t e = allow_shared(block_rows<TX, TB, V, FORM, KIND>, allowed, kRounds * kRound * kMost)) return e;
     const int threads = FORM == kLong ? a.threads : kBlockThreads, here = threads / a.threads;
-    const int most = 152 * (FORM == kLong ? std::max(1, 768 / threads) : 3);
-    block_rows<TX, TB, V, FORM><<<std::min((a.rows + here - 1) / here, most), threads, kRounds * kRound * threads, st>>>(a);
+    const int most = 152 * (FORM == kLong ? std::max(1, 768 / threads) : 4), rounds = (a.rows + here - 1) / here;
+    BlockArgs b = a;
+    b.stretch = (rounds + most - 1) / most * here;
+    block_rows<TX, TB, V, FORM, KIND><<<(a.rows + b.stretch - 1) / b.stretch, threads, kRounds * kRound * threads, st>>>(b);
     return cudaGetLastError();
 }
-template <typename TX, typename TB, int V, int FORM>
+template <typename TX, typename TB, int V, int FORM, int KIND>
 cudaError_t backward_rows(const BlockArgs& a, cudaStream_t st) {
     constexpr int kEach = kRoundsBack<TX, TB, FORM == kLong> * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) +
-                          3 * (FORM == kLong ? E : 1) * (int)sizeof(float);      // of a thread
+                          3 * (FORM == kLong ? E : 32 * E / kBlockBackThreads) * (int)sizeof(float);      // of a thread
     static std::atomic<uint64_t> allowed{0};
-    if (const cudaError_t e = allow_shared(block_back_rows<TX, TB, V, FORM>, allowed, kEach * (FORM == kLong ? 512 : kBlockThreads))) return e;
-    const int threads = FORM == kLong ? a.threads : kBlockThreads;
-    block_back_rows<TX, TB, V, FORM><<<a.ctas, threads, kEach * threads, st>>>(a);
+    if (const cudaError_t e = allow_shared(block_back_rows<TX, TB, V, FORM, KIND>, allowed, kEach * (FORM == kLong ? 512 : kBlockBackThreads))) return e;
+    const int threads = FORM == kLong ? a.threads : kBlockBackThreads;
+    block_back_rows<TX, TB, V, FORM, KIND><<<a.ctas, threads, kEach * threads, st>>>(a);
     if (const cudaError_t e = cudaGetLastError()) return e;
     return block_join(a, st);
 }
-// f with the form of the kernels that a call takes
+// f with the form of the kernels that a call takes, and with the kind of its norms where that goes with it
 template <int V, typename F>
 cudaError_t by_form(const BlockArgs& a, F&& f) {
-    if (a.threads > 32) return f(std::integral_constant<int, kLong>());
+    const auto as = [&](auto form, auto kind) { return f(form, kind); };
+    using std::integral_constant;
+    if (a.threads > 32) return as(integral_constant<int, kLong>(), integral_constant<int, 0>());
     if constexpr (V == 8)
-        if (a.dense) {
-            if (a.threads == 32) return f(std::integral_constant<int, 32>());
-            if (a.threads == 16) return f(std::integral_constant<int, 16>());
-            if (a.threads == 8) return f(std::integral_constant<int, 8>());
+        if (a.dense && a.post == a.pre && a.pre != PP_NORM_NONE && a.threads >= 8) {
+            const auto with = [&](auto form) {
+                return a.pre == PP_NORM_RMS ? as(form, integral_constant<int, PP_NORM_RMS>()) : as(form, integral_constant<int, PP_NORM_LAYER>());
+            };
+            return a.threads == 32 ? with(integral_constant<int, 32>()) : a.threads == 16 ? with(integral_constant<int, 16>()) : with(integral_constant<int, 8>());
         }
-    return f(std::integral_constant<int, kShort>());
+    return as(integral_constant<int, kShort>(), integral_constant<int, 0>());
 }
 template <typename TX, typename TB, int V>
 cudaError_t forward_as(const BlockArgs& a, cudaStream_t st) {
-    return by_form<V>(a, [&](auto form) { return forward_rows<TX, TB, V, decltype(form)::value>(a, st); });
+    return by_form<V>(a, [&](auto form, auto kind) { return forward_rows<TX, TB, V, decltype(form)::value, decltype(kind)::value>(a, st); });
 }
 template <typename TX, typename TB, int V>
 cudaError_t backward_as(const BlockArgs& a, cudaStream_t st) {
-    return by_form<V>(a, [&](auto form) { return backward_rows<TX, TB, V, decltype(form)::value>(a, st); });
+    return by_form<V>(a, [&](auto form, auto kind) { return backward_rows<TX, TB, V, decltype(form)::value, decltype(kind)::value>(a, st); });
 }
 
 }  // namespace

@@ -67,7 +67,7 @@ struct Running {
 // the reading of the seven other rows on the SM, and cost four warps and not eight.
 template <typename T, bool REST, int HARD, int N>
 __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8) distill_rows(DistillArgs a) {
-    constexpr int W = 16 / sizeof(T), U = 4, kWarps = N / 32, kEntries = N == 32 ? 32 : kMostKept;
+    constexpr int W = 16 / sizeof(T), U = N == 32 ? 4 : 2, kWarps = N / 32, kEntries = N == 32 ? 32 : kMostKept;
     extern __shared__ uint4 dynamic[];
     __shared__ float parts[16][3];                    // of a cluster's CTAs, in the first one
     __shared__ float sums[kRowsOfCta][kWarps][3];
@@ -90,7 +90,8 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     // the ends of a row that are no whole vectors are taken by themselves
     const int from = first < last && !r.whole(first) ? first + 1 : first;
     const int to = last > from && !r.whole(last - 1) ? last - 1 : last;
-    // the first logits are asked for at once, whatever the teacher's entries then say
+    // the logits are asked for at once, whatever the teacher's entries then say: all on their way to L2, the first ones here
+    if (N > 32 && threadIdx.x == 0) r.prefetch(first, last);
     int v = from + g.lane;
     Vec<T, W> batch[U];
     const bool early = v + (U - 1) * N < to;
@@ -172,14 +173,21 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
             if (HARD) sum.z1.x += power(y, sum.ref, a.c1);
         }
     };
-    for (bool ready = early; ready; ready = v + (U - 1) * N < to) {
-        if (!(early && v == from + g.lane))
-#pragma unroll
-            for (int k = 0; k < U; ++k) batch[k] = r.at(v + k * N);
+    const auto ready = [&](Vec<T, W> (&b)[U], int v) {
         if (REST)
 #pragma unroll
-            for (int k = 0; k < U; ++k) clear(batch[k], left_out(v + k * N));
+            for (int k = 0; k < U; ++k) clear(b[k], left_out(v + k * N));
+    };
+    for (bool have = early; have;) {                  // the next ones are asked for before these are taken
+        Vec<T, W> next[U];
+        have = v + (2 * U - 1) * N < to;
+        if (have)
+#pragma unroll
+            for (int k = 0; k < U; ++k) next[k] = r.at(v + (U + k) * N);
+        ready(batch, v);
         take(batch);
+#pragma unroll
+        for (int k = 0; k < U; ++k) batch[k] = next[k];
         v += U * N;
     }
     for (; v < to; v += N) {
@@ -201,16 +209,20 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
             if (REST) {
                 unsigned inside = 0;
                 bool keeper = home >= first && home < last;
-                for (int j = 0; j < a.kept; j += 4) {
-                    const int4 four = *reinterpret_cast<const int4*>(kept + j);
-                    const int others[4] = {four.x, four.y, four.z, four.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if ((unsigned)(others[i] ^ place) < (unsigned)W) {     // (-1 is far from every place)
-                            inside |= 1u << (others[i] % W);
-                            if (j + i < k) keeper = false;
-                            again = again || (others[i] == place && j + i < k);
-                        }
+                for (int j = 0; j < a.kept; j += 32) {
+                    unsigned same = 0;                // which of 32 entries are of this vector (an empty place is far from every one)
+#pragma unroll 4
+                    for (int i = 0; i < min(32, a.kept - j); i += 4) {
+                        const int4 four = *reinterpret_cast<const int4*>(kept + j + i);
+                        same |= ((unsigned)((unsigned)(four.x ^ place) < (unsigned)W) | (unsigned)((unsigned)(four.y ^ place) < (unsigned)W) << 1 |
+                                 (unsigned)((unsigned)(four.z ^ place) < (unsigned)W) << 2 | (unsigned)((unsigned)(four.w ^ place) < (unsigned)W) << 3) << i;
+                    }
+                    for (; same; same &= same - 1) {
+                        const int i = j + __ffs(same) - 1, other = kept[i];
+                        inside |= 1u << (other % W);
+                        keeper = keeper && i >= k;
+                        again = again || (other == place && i < k);
+                    }
                 }
                 if (keeper) values_of(r.some(home), inside);
             }

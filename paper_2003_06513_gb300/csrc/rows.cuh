@@ -28,16 +28,39 @@ struct Row {
     __device__ __forceinline__ int vectors() const { return (end + W - 1) / W; }
     __device__ __forceinline__ bool whole(int v) const { return v * W >= pad && v * W + W <= end; }
     __device__ __forceinline__ Vec<T, W> at(int v) const { return load<T, W>(base + (int64_t)v * W); }
-    // a vector that may lie partly outside the row, where it is -inf
+    // a vector that may lie partly outside the row, where it is -inf: as words, so that the whole ones stay as they are read
     __device__ __forceinline__ Vec<T, W> some(int v) const {
-        if (whole(v)) return at(v);
-        Vec<T, W> b;
+        uint4 w;
+        if (whole(v)) {
+            w = *reinterpret_cast<const uint4*>(base + (int64_t)v * W);
+        } else {
+            uint32_t words[4];
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const int place = v * W + i;
-            b.v[i] = place >= pad && place < end ? base[place] : T(kNone);
+            for (int i = 0; i < 4; ++i) {
+                constexpr int A = W / 4;              // values of a word
+                uint32_t bits = 0;
+#pragma unroll
+                for (int k = 0; k < A; ++k) {
+                    const int place = v * W + i * A + k;
+                    const T x = place >= pad && place < end ? base[place] : T(kNone);
+                    uint32_t b = 0;
+                    memcpy(&b, &x, sizeof(T));
+                    bits |= b << (16 * k);
+                }
+                words[i] = bits;
+            }
+            w = make_uint4(words[0], words[1], words[2], words[3]);
         }
+        Vec<T, W> b;
+        memcpy(&b, &w, 16);
         return b;
+    }
+    // the row's vectors from first to last - 1 on their way to L2, all asked for at once
+    __device__ __forceinline__ void prefetch(int first, int last) const {
+        if (first < last && !whole(first)) ++first;
+        if (first < last && !whole(last - 1)) --last;
+        if (first < last)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(base + (int64_t)first * W), "r"((last - first) * 16) : "memory");
     }
 };
 

@@ -25,7 +25,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kClusterMost = 8;
-constexpr size_t kHeld = 96 * 1024;   // bytes of a CTA's slice in shared memory at most: two CTAs on an SM
+constexpr size_t kHeld = 16 * 1024;   // bytes of a CTA's slice in shared memory at most: two CTAs on an SM
 
 struct TopArgs {
     const void* s;
@@ -88,25 +88,28 @@ __global__ void __launch_bounds__(N, N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(T
     // 1. the largest of each thread's values; all of the slice goes to shared memory
     if (threadIdx.x == 0) sh.found = sh.flagged = 0, sh.beside = 0;
     Largest<T> seen;
-    int v = first + threadIdx.x;
-    for (; v + (U - 1) * N < last; v += U * N) {
+    if (threadIdx.x == 0) r.prefetch(first, last);    // all on their way to L2
+    // the ends of a row that are no whole vectors are taken by themselves
+    const int from = first < last && !r.whole(first) ? first + 1 : first;
+    const int to = last > from && !r.whole(last - 1) ? last - 1 : last;
+    const auto first_seen = [&](int v, const Vec<T, W>& b) {
+        seen.take(b);
+        if (a.held) memcpy(held + (v - first), &b, 16);
+    };
+    int v = from + threadIdx.x;
+    for (; v + (U - 1) * N < to; v += U * N) {
         Vec<T, W> b[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) b[k] = r.some(v + k * N);
+        for (int k = 0; k < U; ++k) b[k] = r.at(v + k * N);
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            seen.take(b[k]);
-            if (a.held) held[v + k * N - first] = b[k];
-        }
+        for (int k = 0; k < U; ++k) first_seen(v + k * N, b[k]);
     }
-    for (; v < last; v += N) {
-        const Vec<T, W> b = r.some(v);
-        seen.take(b);
-        if (a.held) held[v - first] = b;
-    }
+    for (; v < to; v += N) first_seen(v, r.at(v));
+    if (from > first && threadIdx.x == 0) first_seen(first, r.some(first));
+    if (to < last && threadIdx.x == N - 1) first_seen(to, r.some(to));
 
     // the bound: this CTA's share of the values wanted reach it here, so that all of them do where the least of the CTAs' does
-    const int share = (wanted + a.parts - 1) / a.parts, own = min(N, last - first);
+    const int share = (wanted + a.parts - 1) / a.parts, own = min(N, to - from);
     const int key = (int)threadIdx.x < own ? key_of(seen.get()) : kLeast;
     int bound = kLeast;
     {
@@ -141,7 +144,13 @@ __global__ void __launch_bounds__(N, N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(T
     unsigned long long* leader_list = a.parts > 1 ? cluster.map_shared_rank(list, 0) : list;
     Group<N> g(scratch);
     const float2 ct = both(a.c);
-    const auto vector_at = [&](int v) { return a.held ? held[v - first] : r.some(v); };
+    const auto middle_at = [&](int v) {               // a whole one
+        const uint4 w = a.held ? *reinterpret_cast<const uint4*>(held + (v - first)) : *reinterpret_cast<const uint4*>(r.base + (int64_t)v * W);
+        Vec<T, W> b;
+        memcpy(&b, &w, 16);
+        return b;
+    };
+    const auto vector_at = [&](int v) { return r.whole(v) ? middle_at(v) : r.some(v); };
     const auto add_vector = [&](float2& sum, const Vec<T, W>& b, float2 far) {
 #pragma unroll
         for (int i = 0; i < W / 2; ++i) {
@@ -164,16 +173,23 @@ __global__ void __launch_bounds__(N, N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(T
         const float limit = of_key(bound), below = reference(limit);
         const float2 far = both(-below);
         float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll 1
-        for (int v = first + threadIdx.x; v < last; v += N) {
-            const Vec<T, W> b = vector_at(v);
+        const auto take = [&](int v, const Vec<T, W>& b) {
             if (bound != kLeast && largest(b) < limit) {               // (places beside the row hold -inf, which adds nothing)
                 add_vector(sum, b, far);
             } else {
                 const int n = atomicAdd(&sh.flagged, 1);
                 if (n < a.list) noted[n] = v;
             }
+        };
+        int v = from + threadIdx.x;
+        for (; v + N < to; v += 2 * N) {
+            const Vec<T, W> b = middle_at(v), c = middle_at(v + N);
+            take(v, b);
+            take(v + N, c);
         }
+        if (v < to) take(v, middle_at(v));
+        if (from > first && threadIdx.x == 0) take(first, r.some(first));
+        if (to < last && threadIdx.x == N - 1) take(to, r.some(to));
         __syncthreads();
         const int flagged = sh.flagged, values = min(flagged, a.list) * W;
         if (flagged > a.list && threadIdx.x == 0) atomicAdd(&leader->found, flagged);     // each has one at least
@@ -314,7 +330,7 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
     const auto slice = [&] { return (size_t)((vectors + a.parts - 1) / a.parts) * 16; };
     a.parts = 1;
     // a cluster where a slice does not fit, or where the rows are too few for the SMs
-    while (N > 128 && a.parts < kClusterMost && (slice() > kHeld || ((int64_t)a.rows * a.parts < kSMs && slice() >= 16384))) a.parts *= 2;
+    while (a.parts < kClusterMost && (slice() > 196608 || ((int64_t)a.rows * a.parts < kSMs && slice() >= 16384))) a.parts *= 2;
     a.held = slice() <= kHeld ? (int)slice() : 0;
     a.list = a.k < 128 ? 512 : 1024;
     constexpr int kLists = 1024 * 12;
@@ -345,8 +361,7 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
 template <typename T>
 cudaError_t top(const TopArgs& a, cudaStream_t st) {
     // a bound takes more threads than values are wanted; beyond that fewer threads have less to do beside reading
-    if (a.classes <= 4096 && a.k < 96) return launch<T, 128>(a, st);
-    return a.k < 192 ? launch<T, 256>(a, st) : launch<T, 512>(a, st);
+    return a.k < 96 ? launch<T, 128>(a, st) : a.k < 192 ? launch<T, 256>(a, st) : launch<T, 512>(a, st);
 }
 
 }  // namespace
