@@ -219,10 +219,10 @@ size_t workspace_of(const Shape& s) {
 
 }  // namespace
 
-// One wave of CTAs: five of 128 threads on an SM, or as many of longer rows' threads; each of four rounds of rows at least.
+// One wave of CTAs: four of 128 threads on an SM, or as many of longer rows' threads; each of four rounds of rows at least.
 int block_ctas(int64_t rows, int C, int64_t* stretch) {
     const int threads = row_threads(C), here = threads > 32 ? 1 : kBlockBackThreads / threads;
-    const int64_t most = threads > 32 ? kSMs * std::max(1, 512 / threads) : kSMs * 5;
+    const int64_t most = threads > 32 ? kSMs * std::max(1, 512 / threads) : kSMs * 4;
     const int64_t n = std::max<int64_t>(1, std::min(most, rows / (4 * here)));
     *stretch = (rows + n - 1) / n;
     return (int)((rows + *stretch - 1) / *stretch);

@@ -20,8 +20,8 @@ namespace {
 constexpr int E = kBlockEight;
 
 // Forms of the kernels.  kLong: a CTA has one row, of whole warps.  kShort: several rows, of a power of two of threads each.
-// 8, 16, 32: the same with so many threads, known beforehand, on dense tensors in vectors of eight channels, with both norms of
-// one kind (KIND) and all inputs there: with loops that unroll, one 32-bit offset for all tensors and no choices left a row takes
+// 8, 16, 32: the same with so many threads, known beforehand.  KIND not 0: dense tensors in vectors of eight or two channels,
+// both norms of this kind and all inputs there: with loops that unroll, one 32-bit offset for all tensors and no choices left a row takes
 // half the instructions, which bound the kernels before memory does.
 enum { kLong = -1, kShort = 0 };
 
@@ -363,8 +363,8 @@ __device__ __forceinline__ float act_of(float z, int act) {
 // -------------------------------------------------------------------------------- forward
 
 template <typename TX, typename TB, int V, int FORM, int KIND>
-__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 4) block_rows(BlockArgs a) {
-    constexpr bool WIDE = FORM == kLong, DENSE = FORM > 0;
+__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 3) block_rows(BlockArgs a) {
+    constexpr bool WIDE = FORM == kLong, DENSE = KIND != 0;
     const int post = KIND ? KIND : a.post, pre = KIND ? KIND : a.pre;
     const bool has_b = KIND || a.b;
     extern __shared__ __align__(16) char ring[];
@@ -373,21 +373,6 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
     const int lane = WIDE ? threadIdx.x : threadIdx.x % threads;
     const int here = WIDE ? 1 : kBlockThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
     RowSum<FORM> sum{threads, scratch};
-    // the block's weight and bias with the residual scale in them, the stream's
-    __shared__ __align__(16) float shared[4][kHeldFloats<FORM>];
-    Held<FORM> wb(shared[0], lane), bb(shared[1], lane), w(shared[2], lane), bias(shared[3], lane);
-    {
-        const Eight sc = parameter<V>(a.scale, 1.0f, lane, a);
-        wb.set(times<V>(parameter<V>(a.post_weight, 1.0f, lane, a), sc), threads, mine == 0);
-        bb.set(times<V>(parameter<V>(a.post_bias, 0.0f, lane, a), sc), threads, mine == 0);
-        w.set(parameter<V>(a.weight, 1.0f, lane, a), threads, mine == 0);
-        bias.set(parameter<V>(a.bias, 0.0f, lane, a), threads, mine == 0);
-        if (!WIDE) __syncthreads();
-    }
-    Eight gate = parameter<V>(nullptr, 1.0f, lane, a);
-    int gate_of = -1;
-    const float inv_own = 1.0f / own_channels<V>(lane, a);
-
     using X = Ahead<TX, V>;
     using B = Ahead<TB, V>;
     // consecutive rows: the gate changes with the sample
@@ -414,6 +399,21 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
     };
     uint32_t offset = (uint32_t)(mine * a.C + lane * V);
     for (int k = 0; k < kRounds - 1; ++k) ask(begin + k * here, offset + k * stride, k);
+
+    // the block's weight and bias with the residual scale in them, the stream's
+    __shared__ __align__(16) float shared[4][kHeldFloats<FORM>];
+    Held<FORM> wb(shared[0], lane), bb(shared[1], lane), w(shared[2], lane), bias(shared[3], lane);
+    {
+        const Eight sc = parameter<V>(a.scale, 1.0f, lane, a);
+        wb.set(times<V>(parameter<V>(a.post_weight, 1.0f, lane, a), sc), threads, mine == 0);
+        bb.set(times<V>(parameter<V>(a.post_bias, 0.0f, lane, a), sc), threads, mine == 0);
+        w.set(parameter<V>(a.weight, 1.0f, lane, a), threads, mine == 0);
+        bias.set(parameter<V>(a.bias, 0.0f, lane, a), threads, mine == 0);
+        if (!WIDE) __syncthreads();
+    }
+    Eight gate = parameter<V>(nullptr, 1.0f, lane, a);
+    int gate_of = -1;
+    const float inv_own = 1.0f / own_channels<V>(lane, a);
     int slot = 0;
     for (int base = begin; base < end; base += here, offset += stride) {
         const int row = base + mine;
@@ -490,8 +490,8 @@ __device__ __forceinline__ unsigned above_zero(F&& value, const BlockArgs& a, in
 }
 
 template <typename TX, typename TB, int V, int FORM, int KIND>
-__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM == kLong ? 1 : 5) block_back_rows(BlockArgs a) {
-    constexpr bool WIDE = FORM == kLong, DENSE = FORM > 0;
+__global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM == kLong ? 1 : 4) block_back_rows(BlockArgs a) {
+    constexpr bool WIDE = FORM == kLong, DENSE = KIND != 0;
     constexpr int R = kRoundsBack<TX, TB, WIDE>;
     extern __shared__ __align__(16) char ring[];
     __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
@@ -504,33 +504,6 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
     const bool pre = pre_kind != PP_NORM_NONE, post = post_kind != PP_NORM_NONE, has_b = KIND || a.b, has_dh = KIND || a.dh;
     __shared__ __align__(16) float shared[3][kHeldFloats<FORM>];
     Held<FORM> w_held(shared[0], lane), bias_held(shared[1], lane), k_held(shared[2], lane);
-    const Eight zero{};
-    const float inv_own = 1.0f / own_channels<V>(lane, a);
-    float reach = 0;                                  // how near to 0 a z of this thread's may be without its sign being sure
-    {
-        const Eight w = parameter<V>(a.weight, 1.0f, lane, a), bias = parameter<V>(a.bias, 0.0f, lane, a);
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i)
-            reach = fmaxf(reach, fmaxf(fmaf(fabsf(w.v[i].x), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].x)),
-                                       fmaf(fabsf(w.v[i].y), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].y))));
-        reach *= 3.8147e-6f;
-        w_held.set(w, threads, mine == 0);
-        bias_held.set(bias, threads, mine == 0);
-    }
-    // the means over a row of t (of a layer norm) and of t v^
-    const auto means = [&](int kind, const Eight& t, const Eight& v) {
-        float q[2] = {kind == PP_NORM_LAYER ? across(sum_of(t)) : 0.0f, dot(t, v)};
-        sum.all(q);
-        return make_float2(q[0] * a.inv_c, q[1] * a.inv_c);
-    };
-    Eight s_w = zero, s_b = zero, s_e = zero, s_f = zero;        // sums of dz h^, dz, and of a sample dh b^, dh
-    // the sums over all samples, in shared memory: of post_weight, post_bias and scale, thread c's, and so on (WIDE: the thread's eight channels')
-    constexpr int OWN = WIDE ? E : 32 * E / kBlockBackThreads;
-    float* totals = reinterpret_cast<float*>(ring + R * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) * blockDim.x) + threadIdx.x;
-    const auto total = [&](int which, int i) -> float& { return totals[(which * OWN + i) * blockDim.x]; };
-#pragma unroll
-    for (int i = 0; i < 3 * OWN; ++i) total(0, i) = 0.0f;
-
     using X = Ahead<TX, V>;
     using B = Ahead<TB, V>;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
@@ -562,9 +535,56 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
         copies_end();
     };
 
+    // a sample's rows of this CTA, the first ones asked for (with a gate; without one all rows are as of one sample)
+    const uint32_t stride = (uint32_t)(here * a.C);
+    At start;
+    int to = end;
+    uint32_t offset;
+    const auto enter = [&](int from) {
+        start = at_row(from, a);
+        if (a.gate) to = min(end, from + (int)a.pixels - start.pixel);
+        offset = (uint32_t)((from - begin + mine) * a.C + lane * V);
+        for (int k = 0; k < R - 1; ++k) ask(from + k * here, to, offset + k * stride, k);
+    };
+    enter(begin);
+
+    const Eight zero{};
+    const float inv_own = 1.0f / own_channels<V>(lane, a);
+    float reach = 0;                                  // how near to 0 a z of this thread's may be without its sign being sure
+    {
+        const Eight w = parameter<V>(a.weight, 1.0f, lane, a);
+        Eight bias = parameter<V>(a.bias, 0.0f, lane, a);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i)
+            reach = fmaxf(reach, fmaxf(fmaf(fabsf(w.v[i].x), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].x)),
+                                       fmaf(fabsf(w.v[i].y), sqrtf((float)a.C) + 1.0f, fabsf(bias.v[i].y))));
+        reach *= 3.8147e-6f;
+        w_held.set(w, threads, mine == 0);
+#pragma unroll
+        for (int i = 0; i < E; ++i)                   // (beyond the row z is 1, and its sign sure)
+            if (!inside<V>(lane, a, i)) reinterpret_cast<float*>(bias.v)[i] = 1.0f;
+        bias_held.set(bias, threads, mine == 0);
+    }
+    // where the rows' threads leave channel c's sums: by the thread's number of it, then by threads
+    const auto place_in_sums = [&](int c) {
+        const int vector = c / V, turn = vector / threads;
+        return (turn * V + c % V) * threads + vector - turn * threads;
+    };
+    // the means over a row of t (of a layer norm) and of t v^
+    const auto means = [&](int kind, const Eight& t, const Eight& v) {
+        float q[2] = {kind == PP_NORM_LAYER ? across(sum_of(t)) : 0.0f, dot(t, v)};
+        sum.all(q);
+        return make_float2(q[0] * a.inv_c, q[1] * a.inv_c);
+    };
+    Eight s_w = zero, s_b = zero, s_e = zero, s_f = zero;        // sums of dz h^, dz, and of a sample dh b^, dh
+    // the sums over all samples, in shared memory: of post_weight, post_bias and scale, thread c's, and so on (WIDE: the thread's eight channels')
+    constexpr int OWN = WIDE ? E : 32 * E / kBlockBackThreads;
+    float* totals = reinterpret_cast<float*>(ring + R * 2 * (Ahead<TX, V>::kBytes + Ahead<TB, V>::kBytes) * blockDim.x) + threadIdx.x;
+    const auto total = [&](int which, int i) -> float& { return totals[(which * OWN + i) * blockDim.x]; };
+#pragma unroll
+    for (int i = 0; i < 3 * OWN; ++i) total(0, i) = 0.0f;
+
     for (int from = begin; from < end;) {
-        const At start = at_row(from, a);
-        const int to = a.gate ? min(end, from + (int)a.pixels - start.pixel) : end;
         const float* gate = a.gate ? a.gate + (int64_t)start.sample * a.C : nullptr;
         // what dh is multiplied with on its way to the normalised block
         if (!WIDE) __syncthreads();                   // (the sample before has been summed)
@@ -572,9 +592,6 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                    threads, mine == 0);
         if (!WIDE) __syncthreads();
 
-        const uint32_t stride = (uint32_t)(here * a.C);
-        uint32_t offset = (uint32_t)((from - begin + mine) * a.C + lane * V);
-        for (int k = 0; k < R - 1; ++k) ask(from + k * here, to, offset + k * stride, k);
         int slot = 0;
         for (int base = from; base < to; base += here, offset += stride) {
             const int row = base + mine;
@@ -611,8 +628,8 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                 Eight dz = widened(B::get(place + y_at, y_in(at), threads, live));
                 if (a.act == PP_ACT_RELU) {
                     // fp32's z is off by less than 2^-18 of its terms' sizes (each value, the mean, and the root by some 16 roundings
-                    // of the row's sums), |h^| is at most the root of C: where the smallest z is nearer to 0 than that the
-                    // signs are taken in 64 bits
+                    // of the row's sums), |h^| is at most the root of C: where the smallest z is nearer to 0 than that, and then
+                    // some z than its own terms allow, the signs are taken in 64 bits
                     const Eight bias = bias_held.get(threads);
                     float2 z[E / 2];
                     float least = INFINITY;
@@ -622,7 +639,17 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                         least = fminf(least, fminf(fabsf(z[i].x), fabsf(z[i].y)));
                     }
                     const float spread = 1.0f + 2.0f * fabsf(pre_kind == PP_NORM_LAYER ? centres[0] * r.x : 0.0f);
-                    const bool close = there && least <= reach * spread;
+                    bool close = there && least <= reach * spread;
+                    if (close) {                      // more closely, of each value by itself
+                        const float* zf = reinterpret_cast<const float*>(z);
+                        const float* hf = reinterpret_cast<const float*>(h.v);
+                        const float* wf = reinterpret_cast<const float*>(w.v);
+                        const float* bf = reinterpret_cast<const float*>(bias.v);
+                        close = false;
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            close = close || fabsf(zf[i]) <= 3.8147e-6f * fmaf(fabsf(wf[i]), fabsf(hf[i]) + spread, fabsf(bf[i]));
+                    }
                     if (WIDE ? __syncthreads_or(close) : __any_sync(0xffffffffu, close)) {
                         const unsigned above = above_zero<V, FORM>([&](int k) { return there && inside<V>(lane, a, k) ? X::one(place + h_at, h_in(at), threads, k) : 0.0f; }, a, lane, sum);
 #pragma unroll
@@ -678,6 +705,12 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
             put(static_cast<TB*>(a.db) + begin_at + offset, narrowed<TB, V>(t), threads, live);
         }
 
+        const bool first = from == begin, last = to == end;
+        const bool whole = (first ? start.pixel == 0 : true) && (last ? at_row(end - 1, a).pixel == a.pixels - 1 : true);
+        const int64_t sample = start.sample;
+        from = to;
+        if (!last) enter(to);
+
         // the sample's sums: of the block's norm, the gate and the scale
         if (has_b) {
             float* e_all = lanes_sum;
@@ -688,13 +721,11 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                 const float* pf = reinterpret_cast<const float*>(s_f.v);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const int c = channel<V>(lane, threads, i);
-                    e_all[mine * threads * E + c] = pe[i];
-                    f_all[mine * threads * E + c] = pf[i];
+                    e_all[(mine * E + i) * threads + lane] = pe[i];
+                    f_all[(mine * E + i) * threads + lane] = pf[i];
                 }
                 __syncthreads();
             }
-            const bool first = from == begin, whole = (first ? start.pixel == 0 : true) && (to < end || at_row(end - 1, a).pixel == a.pixels - 1);
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
                 const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x + i * kBlockBackThreads;
@@ -704,7 +735,8 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                     e = reinterpret_cast<const float*>(s_e.v)[i];
                     f = reinterpret_cast<const float*>(s_f.v)[i];
                 } else {
-                    for (int g = 0; g < here; ++g) e += e_all[g * threads * E + c], f += f_all[g * threads * E + c];
+                    const int at = place_in_sums(c);
+                    for (int g = 0; g < here; ++g) e += e_all[g * threads * E + at], f += f_all[g * threads * E + at];
                 }
                 const float ga_c = gate ? gate[c] : 1.0f, sc_c = a.scale ? a.scale[c] : 1.0f;
                 const float joined = fmaf(a.post_weight ? a.post_weight[c] : 1.0f, e, a.post_bias ? a.post_bias[c] * f : 0.0f);
@@ -713,14 +745,13 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                 total(2, i) = fmaf(ga_c, joined, total(2, i));
                 if (a.dgate) {
                     if (whole)
-                        a.dgate[(int64_t)start.sample * a.C + c] = sc_c * joined;
+                        a.dgate[sample * a.C + c] = sc_c * joined;
                     else
                         a.gates[((int64_t)blockIdx.x * 2 + !first) * a.C + c] = sc_c * joined;
                 }
             }
             s_e = s_f = zero;
         }
-        from = to;
     }
 
     // the CTA's sums
@@ -731,9 +762,8 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
         const float* pb = reinterpret_cast<const float*>(s_b.v);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const int c = channel<V>(lane, threads, i);
-            lanes_sum[mine * threads * E + c] = pw[i];
-            lanes_sum[kBlockBackThreads * E + mine * threads * E + c] = pb[i];
+            lanes_sum[(mine * E + i) * threads + lane] = pw[i];
+            lanes_sum[kBlockBackThreads * E + (mine * E + i) * threads + lane] = pb[i];
         }
         __syncthreads();
     }
@@ -746,7 +776,8 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
             e = reinterpret_cast<const float*>(s_w.v)[i];
             f = reinterpret_cast<const float*>(s_b.v)[i];
         } else {
-            for (int g = 0; g < here; ++g) e += lanes_sum[g * threads * E + c], f += lanes_sum[kBlockBackThreads * E + g * threads * E + c];
+            const int at = place_in_sums(c);
+            for (int g = 0; g < here; ++g) e += lanes_sum[g * threads * E + at], f += lanes_sum[kBlockBackThreads * E + g * threads * E + at];
         }
         out[c] = e;
         out[a.C + c] = f;
@@ -773,7 +804,7 @@ cudaError_t forward_rows(const BlockArgs& a, cudaStream_t st) {
     static std::atomic<uint64_t> allowed{0};
     if (const cudaError_t e = allow_shared(block_rows<TX, TB, V, FORM, KIND>, allowed, kRounds * kRound * kMost)) return e;
     const int threads = FORM == kLong ? a.threads : kBlockThreads, here = threads / a.threads;
-    const int most = 152 * (FORM == kLong ? std::max(1, 768 / threads) : 4), rounds = (a.rows + here - 1) / here;
+    const int most = 152 * (FORM == kLong ? std::max(1, 768 / threads) : 3), rounds = (a.rows + here - 1) / here;
     BlockArgs b = a;
     b.stretch = (rounds + most - 1) / most * here;
     block_rows<TX, TB, V, FORM, KIND><<<(a.rows + b.stretch - 1) / b.stretch, threads, kRounds * kRound * threads, st>>>(b);
@@ -793,17 +824,22 @@ cudaError_t backward_rows(const BlockArgs& a, cudaStream_t st) {
 // f with the form of the kernels that a call takes, and with the kind of its norms where that goes with it
 template <int V, typename F>
 cudaError_t by_form(const BlockArgs& a, F&& f) {
-    const auto as = [&](auto form, auto kind) { return f(form, kind); };
     using std::integral_constant;
-    if (a.threads > 32) return as(integral_constant<int, kLong>(), integral_constant<int, 0>());
-    if constexpr (V == 8)
-        if (a.dense && a.post == a.pre && a.pre != PP_NORM_NONE && a.threads >= 8) {
-            const auto with = [&](auto form) {
-                return a.pre == PP_NORM_RMS ? as(form, integral_constant<int, PP_NORM_RMS>()) : as(form, integral_constant<int, PP_NORM_LAYER>());
-            };
-            return a.threads == 32 ? with(integral_constant<int, 32>()) : a.threads == 16 ? with(integral_constant<int, 16>()) : with(integral_constant<int, 8>());
-        }
-    return as(integral_constant<int, kShort>(), integral_constant<int, 0>());
+    const auto of_kind = [&](auto form) {
+        return a.pre == PP_NORM_RMS ? f(form, integral_constant<int, PP_NORM_RMS>()) : f(form, integral_constant<int, PP_NORM_LAYER>());
+    };
+    const bool known = V > 1 && a.dense && a.post == a.pre && a.pre != PP_NORM_NONE;
+    if (a.threads > 32) {
+        if constexpr (V == 8)
+            if (known) return of_kind(integral_constant<int, kLong>());
+        return f(integral_constant<int, kLong>(), integral_constant<int, 0>());
+    }
+    if constexpr (V > 1)
+        if (known && a.threads >= 8)
+            return a.threads == 32   ? of_kind(integral_constant<int, 32>())
+                   : a.threads == 16 ? of_kind(integral_constant<int, 16>())
+                                     : of_kind(integral_constant<int, 8>());
+    return f(integral_constant<int, kShort>(), integral_constant<int, 0>());
 }
 template <typename TX, typename TB, int V>
 cudaError_t forward_as(const BlockArgs& a, cudaStream_t st) {

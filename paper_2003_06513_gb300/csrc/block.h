@@ -10,7 +10,7 @@ namespace patconv {
 
 constexpr int kBlockEight = 8;                        // channels of a thread
 constexpr int kBlockThreads = 256;                    // of a CTA whose rows are of at most a warp
-constexpr int kBlockBackThreads = 128;                // in the backward pass: five of them, of 102 registers a thread, on an SM
+constexpr int kBlockBackThreads = 128;                // in the backward pass: four of them, of 128 registers a thread, on an SM
 constexpr int kBlockMost = 4096;                      // channels at most
 constexpr int kBlockSums = 5;                         // sums over all rows: weight, bias, post_weight, post_bias, scale
 

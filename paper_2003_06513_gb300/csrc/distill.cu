@@ -163,32 +163,40 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
         w.x = all ? none : w.x, w.y = all ? none : w.y, w.z = all ? none : w.z, w.w = all ? none : w.w;
         memcpy(&b, &w, 16);
     };
-    const auto values_of = [&](const Vec<T, W>& b, unsigned but) {     // a vector's values one by one, but for some
+    const auto values_of = [&](const Vec<T, W>& b, unsigned but) {     // a vector's values but for some
+        float y[W], top = kNone;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            if (but >> i & 1) continue;
-            const float y = widen(b.v[i]);
-            sum.below(y, a.c1, a.ct);
-            sum.zt.x += power(y, sum.ref, a.ct);
-            if (HARD) sum.z1.x += power(y, sum.ref, a.c1);
+            y[i] = but >> i & 1 ? kNone : widen(b.v[i]);
+            top = larger(top, y[i]);
         }
+        sum.below(top, a.c1, a.ct);
+#pragma unroll
+        for (int i = 0; i < W; i += 2) sum.add_pair(make_float2(y[i], y[i + 1]), c1, ct);
     };
     const auto ready = [&](Vec<T, W> (&b)[U], int v) {
         if (REST)
 #pragma unroll
             for (int k = 0; k < U; ++k) clear(b[k], left_out(v + k * N));
     };
-    for (bool have = early; have;) {                  // the next ones are asked for before these are taken
+    // the next ones are asked for before these are taken
+    const int batches = v < to ? ((to - v + N - 1) / N) / U : 0;
+    for (int i = 0; i < batches; i += 2, v += 2 * U * N) {
         Vec<T, W> next[U];
-        have = v + (2 * U - 1) * N < to;
-        if (have)
+        if (i + 1 < batches)
 #pragma unroll
             for (int k = 0; k < U; ++k) next[k] = r.at(v + (U + k) * N);
         ready(batch, v);
         take(batch);
+        if (i + 1 == batches) {
+            v += U * N;
+            break;
+        }
+        if (i + 2 < batches)
 #pragma unroll
-        for (int k = 0; k < U; ++k) batch[k] = next[k];
-        v += U * N;
+            for (int k = 0; k < U; ++k) batch[k] = r.at(v + (2 * U + k) * N);
+        ready(next, v + U * N);
+        take(next);
     }
     for (; v < to; v += N) {
         Vec<T, W> b[1] = {r.at(v)};

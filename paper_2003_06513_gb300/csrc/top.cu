@@ -173,23 +173,51 @@ __global__ void __launch_bounds__(N, N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(T
         const float limit = of_key(bound), below = reference(limit);
         const float2 far = both(-below);
         float2 sum = make_float2(0.0f, 0.0f);
-        const auto take = [&](int v, const Vec<T, W>& b) {
-            if (bound != kLeast && largest(b) < limit) {               // (places beside the row hold -inf, which adds nothing)
+        // a thread remembers which of its vectors reach the bound, 32 at a time, and notes them then
+        unsigned reached = 0;
+        const auto take = [&](const Vec<T, W>& b, int turn) {
+            if (bound != kLeast && largest(b) < limit)                 // (places beside the row hold -inf, which adds nothing)
                 add_vector(sum, b, far);
-            } else {
-                const int n = atomicAdd(&sh.flagged, 1);
-                if (n < a.list) noted[n] = v;
-            }
+            else
+                reached |= 1u << turn;
         };
-        int v = from + threadIdx.x;
-        for (; v + N < to; v += 2 * N) {
-            const Vec<T, W> b = middle_at(v), c = middle_at(v + N);
-            take(v, b);
-            take(v + N, c);
+        const auto noted_from = [&](int v) {          // vectors v, v + N and so on
+            const int mine = __popc(reached);
+            if (!__any_sync(0xffffffffu, mine)) return;
+            int before = mine;                        // of the lanes up to this one
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int y = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += y;
+            }
+            int n = lane == 31 ? atomicAdd(&sh.flagged, before) : 0;
+            n = __shfl_sync(0xffffffffu, n, 31) + before - mine;
+            for (; reached; reached &= reached - 1, ++n)
+                if (n < a.list) noted[n] = v + (__ffs(reached) - 1) * N;
+        };
+        for (int base = from; base < to; base += 32 * N) {             // (the same for all threads)
+            const int v = base + threadIdx.x;
+            int turn = 0;
+#pragma unroll 1
+            for (; turn < 29 && v + (turn + U - 1) * N < to; turn += U) {
+                Vec<T, W> b[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) b[k] = middle_at(v + (turn + k) * N);
+#pragma unroll
+                for (int k = 0; k < U; ++k) take(b[k], turn + k);
+            }
+#pragma unroll 1
+            for (; turn < 32 && v + turn * N < to; ++turn) take(middle_at(v + turn * N), turn);
+            noted_from(v);
         }
-        if (v < to) take(v, middle_at(v));
-        if (from > first && threadIdx.x == 0) take(first, r.some(first));
-        if (to < last && threadIdx.x == N - 1) take(to, r.some(to));
+        if (from > first) {                           // the ends
+            if (threadIdx.x == 0) take(r.some(first), 0);
+            noted_from(first);
+        }
+        if (to < last) {
+            if (threadIdx.x == N - 1) take(r.some(to), 0);
+            noted_from(to);
+        }
         __syncthreads();
         const int flagged = sh.flagged, values = min(flagged, a.list) * W;
         if (flagged > a.list && threadIdx.x == 0) atomicAdd(&leader->found, flagged);     // each has one at least
