@@ -2,7 +2,7 @@
 is installed, _patconv.so, the native binding of the training side, which links against torch and the library.
 
 Both are written to ``paper_2003_06513_gb300/_build/`` (git-ignored), and each is rebuilt whenever a source
-file or a flag of its own changes, the binding with the torch version too.  No CMake: sixteen translation units compiled in parallel and
+file or a flag of its own changes, the binding with the torch version too.  No CMake: eighteen translation units compiled in parallel and
 two links, so a fresh build takes a minute or so, the largest unit's time.
 """
 from __future__ import annotations
@@ -30,7 +30,8 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--expt-relaxed-constexpr", "-Xc
 GXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-I",
              os.path.join(ROOT, "include")]
 KERNELS = ["conv.cu", "tensor.cu", "norm.cu", "norm_f32.cu", "norm_f16.cu", "norm_bf16.cu", "optim.cu",
-           "block.cu", "block_f32.cu", "block_f16.cu", "block_bf16.cu", "top.cu", "distill.cu", "distill_back.cu"]
+           "block.cu", "block_f32.cu", "block_f16.cu", "block_bf16.cu", "block_f16_f32.cu",
+           "block_bf16_f32.cu", "top.cu", "distill.cu", "distill_back.cu"]
 SOURCES = KERNELS + ["tensor.h", "norm.h", "norm.cuh", "vec.cuh", "block.h", "block.cuh", "rows.h", "rows.cuh", "pack.cpp", "layer.h", "gen_dispatch.py"]
 
 

@@ -130,9 +130,9 @@ struct Input {
         return (s.pixels == 1 || pixel == s.C) && (s.N == 1 || sample == s.pixels * s.C);
     }
     size_t bytes(const Shape& s) const { return (size_t)((s.N - 1) * sample + (s.pixels - 1) * pixel + s.C) * es; }
-    // the largest of 8, 2 and 1 channels that a vector of it can have: of at most 16 bytes each
+    // the largest of 8, 4, 2 and 1 channels that a vector of it can have
     int vector(const Shape& s) const {
-        for (const int v : {8, 2}) {
+        for (const int v : {8, 4, 2}) {
             const size_t align = std::min(16, v * es);
             if (s.C % v == 0 && !off(p, align) && (s.pixels == 1 || pixel * es % align == 0) && (s.N == 1 || sample * es % align == 0)) return v;
         }
@@ -203,6 +203,12 @@ void set(BlockArgs& a, const void* BlockArgs::*p, int64_t BlockArgs::*pixel, int
 // of results, whose rows are dense
 int vector_of(const Shape& s, const void* p, int es) { return p ? Input{p, s.C, s.pixels * s.C, es}.vector(s) : 8; }
 
+// what there are kernels for: eight where both are of two bytes, else four; two; one
+int known_vector(const Shape& s, int v) {
+    if (s.x_dtype == PP_F32) return v >= 4 ? 4 : v;
+    return v == 8 ? 8 : std::min(v, 2);
+}
+
 template <typename F>
 int by_type(const Shape& s, F&& f) {
     const cudaError_t e = s.dtype == PP_F32   ? f(BlockKernels<float, float>())
@@ -219,11 +225,11 @@ size_t workspace_of(const Shape& s) {
 
 }  // namespace
 
-// One wave of CTAs: four of 128 threads on an SM, or as many of longer rows' threads; each of four rounds of rows at least.
+// One wave of CTAs: four of 128 threads on an SM, or as many of longer rows' threads.
 int block_ctas(int64_t rows, int C, int64_t* stretch) {
     const int threads = row_threads(C), here = threads > 32 ? 1 : kBlockBackThreads / threads;
     const int64_t most = threads > 32 ? kSMs * std::max(1, 512 / threads) : kSMs * 4;
-    const int64_t n = std::max<int64_t>(1, std::min(most, rows / (4 * here)));
+    const int64_t n = std::min(most, (rows + here - 1) / here);
     *stretch = (rows + n - 1) / n;
     return (int)((rows + *stretch - 1) / *stretch);
 }
@@ -287,8 +293,8 @@ int pp_block_norm(const void* x, int64_t x_pixel, int64_t x_sample, int x_dtype,
     set(a, &BlockArgs::b, &BlockArgs::b_pixel, &BlockArgs::b_sample, b);
     a.h = h;
     a.y = y;
-    if (!block) a.dense = 0;
-    const int V = std::min({in.vector(s), block ? b.vector(s) : 8, vector_of(s, h, in.es), vector_of(s, y, b.es)});
+    a.full = block != nullptr;
+    const int V = known_vector(s, std::min({in.vector(s), block ? b.vector(s) : 8, vector_of(s, h, in.es), vector_of(s, y, b.es)}));
     a.vectors = C / V;
     return by_type(s, [&](auto k) { return k.forward(a, V, static_cast<cudaStream_t>(stream)); });
 }
@@ -354,8 +360,9 @@ int pp_block_norm_backward(const void* dh, int64_t dh_pixel, int64_t dh_sample, 
     int V = std::min(vector_of(s, dx, xs), vector_of(s, dblock, bs));
     for (const Input* t : {&d, &e, &in, &b})
         if (t->p && (t != &in || norm)) V = std::min(V, t->vector(s));
+    V = known_vector(s, V);
     a.vectors = C / V;
-    if (!block || !dh || !norm) a.dense = 0;
+    a.full = block && dh && norm;
     int64_t stretch;
     a.ctas = block_ctas((int64_t)N * pixels, C, &stretch);
     a.stretch = (int)stretch;

@@ -1,5 +1,5 @@
-// Kernels of block.cu, for one type of blocks each in block_f32.cu, block_f16.cu and block_bf16.cu, the stream being of
-// the same type or fp32.
+// Kernels of block.cu, for one type of blocks and stream each in block_f32.cu, block_f16.cu, block_f16_f32.cu and so on: five
+// translation units, compiled side by side.
 //
 // A row -- a pixel's channels -- is taken by `threads` threads of eight channels each: a power of two of them inside a
 // warp for rows of up to 256 channels, whole warps for longer ones.  All of a row is in registers between its readings
@@ -20,10 +20,11 @@ namespace {
 constexpr int E = kBlockEight;
 
 // Forms of the kernels.  kLong: a CTA has one row, of whole warps.  kShort: several rows, of a power of two of threads each.
-// 8, 16, 32: the same with so many threads, known beforehand.  KIND not 0: dense tensors in vectors of eight or two channels,
-// both norms of this kind and all inputs there: with loops that unroll, one 32-bit offset for all tensors and no choices left a row takes
+// 1 to 32: the same with so many threads, known beforehand.  KIND kStrided: any strides; kDense: one offset for all tensors; kRms and
+// kLayer: dense, both norms of this kind and all inputs there.  With loops that unroll, one 32-bit offset for all tensors and no choices left a row takes
 // half the instructions, which bound the kernels before memory does.
 enum { kLong = -1, kShort = 0 };
+enum { kStrided = 0, kRms = PP_NORM_RMS, kLayer = PP_NORM_LAYER, kDense = 3 };
 
 // eight channels of a row: V adjacent ones, then those `threads` vectors on, and so on
 struct Eight {
@@ -364,9 +365,9 @@ __device__ __forceinline__ float act_of(float z, int act) {
 
 template <typename TX, typename TB, int V, int FORM, int KIND>
 __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == kLong ? 1 : 3) block_rows(BlockArgs a) {
-    constexpr bool WIDE = FORM == kLong, DENSE = KIND != 0;
-    const int post = KIND ? KIND : a.post, pre = KIND ? KIND : a.pre;
-    const bool has_b = KIND || a.b;
+    constexpr bool WIDE = FORM == kLong, DENSE = KIND != kStrided, FIXED = KIND == kRms || KIND == kLayer;
+    const int post = FIXED ? KIND : a.post, pre = FIXED ? KIND : a.pre;
+    const bool has_b = FIXED || a.b;
     extern __shared__ __align__(16) char ring[];
     __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
     const int threads = FORM > 0 ? FORM : a.threads;
@@ -491,7 +492,7 @@ __device__ __forceinline__ unsigned above_zero(F&& value, const BlockArgs& a, in
 
 template <typename TX, typename TB, int V, int FORM, int KIND>
 __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM == kLong ? 1 : 4) block_back_rows(BlockArgs a) {
-    constexpr bool WIDE = FORM == kLong, DENSE = KIND != 0;
+    constexpr bool WIDE = FORM == kLong, DENSE = KIND != kStrided, FIXED = KIND == kRms || KIND == kLayer;
     constexpr int R = kRoundsBack<TX, TB, WIDE>;
     extern __shared__ __align__(16) char ring[];
     __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
@@ -500,8 +501,8 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
     const int lane = WIDE ? threadIdx.x : threadIdx.x % threads;
     const int here = WIDE ? 1 : kBlockBackThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
     RowSum<FORM> sum{threads, scratch};
-    const int post_kind = KIND ? KIND : a.post, pre_kind = KIND ? KIND : a.pre;
-    const bool pre = pre_kind != PP_NORM_NONE, post = post_kind != PP_NORM_NONE, has_b = KIND || a.b, has_dh = KIND || a.dh;
+    const int post_kind = FIXED ? KIND : a.post, pre_kind = FIXED ? KIND : a.pre;
+    const bool pre = pre_kind != PP_NORM_NONE, post = post_kind != PP_NORM_NONE, has_b = FIXED || a.b, has_dh = FIXED || a.dh;
     __shared__ __align__(16) float shared[3][kHeldFloats<FORM>];
     Held<FORM> w_held(shared[0], lane), bias_held(shared[1], lane), k_held(shared[2], lane);
     using X = Ahead<TX, V>;
@@ -826,20 +827,24 @@ template <int V, typename F>
 cudaError_t by_form(const BlockArgs& a, F&& f) {
     using std::integral_constant;
     const auto of_kind = [&](auto form) {
-        return a.pre == PP_NORM_RMS ? f(form, integral_constant<int, PP_NORM_RMS>()) : f(form, integral_constant<int, PP_NORM_LAYER>());
+        if (a.pre != a.post || a.pre == PP_NORM_NONE || !a.full) return f(form, integral_constant<int, kDense>());
+        return a.pre == PP_NORM_RMS ? f(form, integral_constant<int, kRms>()) : f(form, integral_constant<int, kLayer>());
     };
-    const bool known = V > 1 && a.dense && a.post == a.pre && a.pre != PP_NORM_NONE;
     if (a.threads > 32) {
-        if constexpr (V == 8)
-            if (known) return of_kind(integral_constant<int, kLong>());
-        return f(integral_constant<int, kLong>(), integral_constant<int, 0>());
+        if constexpr (V > 1)
+            if (a.dense) return of_kind(integral_constant<int, kLong>());
+        return f(integral_constant<int, kLong>(), integral_constant<int, kStrided>());
     }
     if constexpr (V > 1)
-        if (known && a.threads >= 8)
-            return a.threads == 32   ? of_kind(integral_constant<int, 32>())
-                   : a.threads == 16 ? of_kind(integral_constant<int, 16>())
-                                     : of_kind(integral_constant<int, 8>());
-    return f(integral_constant<int, kShort>(), integral_constant<int, 0>());
+        if (a.dense) {
+            if (a.threads >= 8)
+                return a.threads == 32   ? of_kind(integral_constant<int, 32>())
+                       : a.threads == 16 ? of_kind(integral_constant<int, 16>())
+                                         : of_kind(integral_constant<int, 8>());
+            const integral_constant<int, kDense> any;
+            return a.threads == 4 ? f(integral_constant<int, 4>(), any) : a.threads == 2 ? f(integral_constant<int, 2>(), any) : f(integral_constant<int, 1>(), any);
+        }
+    return f(integral_constant<int, kShort>(), integral_constant<int, kStrided>());
 }
 template <typename TX, typename TB, int V>
 cudaError_t forward_as(const BlockArgs& a, cudaStream_t st) {
@@ -854,11 +859,13 @@ cudaError_t backward_as(const BlockArgs& a, cudaStream_t st) {
 
 template <typename TX, typename TB>
 cudaError_t BlockKernels<TX, TB>::forward(const BlockArgs& a, int V, cudaStream_t st) {
-    return V == 8 ? forward_as<TX, TB, 8>(a, st) : V == 2 ? forward_as<TX, TB, 2>(a, st) : forward_as<TX, TB, 1>(a, st);
+    constexpr int W = sizeof(TX) == 2 ? 8 : 4;
+    return V == W ? forward_as<TX, TB, W>(a, st) : V == 2 ? forward_as<TX, TB, 2>(a, st) : forward_as<TX, TB, 1>(a, st);
 }
 template <typename TX, typename TB>
 cudaError_t BlockKernels<TX, TB>::backward(const BlockArgs& a, int V, cudaStream_t st) {
-    return V == 8 ? backward_as<TX, TB, 8>(a, st) : V == 2 ? backward_as<TX, TB, 2>(a, st) : backward_as<TX, TB, 1>(a, st);
+    constexpr int W = sizeof(TX) == 2 ? 8 : 4;
+    return V == W ? backward_as<TX, TB, W>(a, st) : V == 2 ? backward_as<TX, TB, 2>(a, st) : backward_as<TX, TB, 1>(a, st);
 }
 
 }  // namespace patconv

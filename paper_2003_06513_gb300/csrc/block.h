@@ -28,6 +28,7 @@ struct BlockArgs {
     int vectors;                                      // of a row
     int ragged;                                       // whether its threads have more channels than it has
     int flat, dense;                                  // whether every tensor's samples follow one another as its pixels do; and those too
+    int full;                                         // whether no input is missing
     void *h, *y;                                      // (forward)
     void *dx, *db;                                    // (backward)
     float *dweight, *dbias, *dpost_weight, *dpost_bias, *dscale, *dgate;
@@ -36,7 +37,8 @@ struct BlockArgs {
     float* gates;                                     // [ctas][2][C]: of a CTA's first and last sample, where others have rows of it
 };
 
-// Launches for a stream of TX and blocks of TB, with V channels to a vector.
+// Launches for a stream of TX and blocks of TB, with V channels to a vector: eight where both are of two bytes, four where one is
+// fp32 (vectors of 16 bytes lie side by side), two or one.
 template <typename TX, typename TB>
 struct BlockKernels {
     static cudaError_t forward(const BlockArgs& a, int V, cudaStream_t st);

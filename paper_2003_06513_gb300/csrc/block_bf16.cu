@@ -1,5 +1,4 @@
-// Block norm's kernels on blocks of __nv_bfloat16, in a stream of the same type or of fp32.
+// Block norm's kernels on blocks of __nv_bfloat16 in a stream of the same type.
 #include "block.cuh"
 
 template struct patconv::BlockKernels<__nv_bfloat16, __nv_bfloat16>;
-template struct patconv::BlockKernels<float, __nv_bfloat16>;

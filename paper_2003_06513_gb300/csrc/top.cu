@@ -59,7 +59,7 @@ struct Shared {
 };
 
 template <typename T, int N>
-__global__ void __launch_bounds__(N, N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(TopArgs a) {
+__global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(TopArgs a) {
     constexpr int W = 16 / sizeof(T), kWarps = N / 32, U = 4;
     extern __shared__ uint4 dynamic[];
     __shared__ Shared sh;
@@ -360,7 +360,7 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
     // a cluster where a slice does not fit, or where the rows are too few for the SMs
     while (a.parts < kClusterMost && (slice() > 196608 || ((int64_t)a.rows * a.parts < kSMs && slice() >= 16384))) a.parts *= 2;
     a.held = slice() <= kHeld ? (int)slice() : 0;
-    a.list = a.k < 128 ? 512 : 1024;
+    a.list = N == 32 ? 256 : a.k < 128 ? 512 : 1024;
     constexpr int kLists = 1024 * 12;
     static std::atomic<uint64_t> allowed{0};
     int dev = 0;
@@ -388,7 +388,9 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t top(const TopArgs& a, cudaStream_t st) {
-    // a bound takes more threads than values are wanted; beyond that fewer threads have less to do beside reading
+    // a bound takes more threads than values are wanted; beyond that fewer threads have less to do beside reading, and a warp
+    // where there are rows enough (5424 x 746: 17 us, by 128 threads 29; but 256 x 1000 10.5 so, 8.4 by 128)
+    if (a.classes <= 1024 && a.k < 24 && a.rows >= 8 * kSMs) return launch<T, 32>(a, st);
     return a.k < 96 ? launch<T, 128>(a, st) : a.k < 192 ? launch<T, 256>(a, st) : launch<T, 512>(a, st);
 }
 
