@@ -71,7 +71,7 @@ def distill(s, values, indices, rest, labels, t, alpha):
         q = np.concatenate([q, log_q0[:, None]], 1)
     with np.errstate(invalid="ignore"):
         terms = np.where(p > 0, p * (log_p - q), 0.0)
-    loss = np.where(some, alpha * t * t * terms.sum(1), 0.0)
+    loss = np.where(some, alpha * t * t * terms.sum(1), 0.0) if alpha else np.zeros(rows)      # (no weight takes no part, an infinite one neither)
     # gradient: alpha T (q_v - p_v), where a class of the others has its share of q_0 - p_0
     grad = np.exp(log_q)
     reach = grad.copy()
@@ -88,7 +88,7 @@ def distill(s, values, indices, rest, labels, t, alpha):
     with np.errstate(invalid="ignore"):
         parts = np.where(p > 0, p * (np.abs(log_p) + np.abs(q) + 1), 0).sum(1)
     largest = np.where(there & np.isfinite(values), np.abs(values), 0.0).max(1)
-    size = np.abs(loss) + alpha * t * largest + alpha * t * t * parts
+    size = np.abs(loss) + alpha * t * largest + (alpha * t * t * parts if alpha else 0.0)
     z1 = np.zeros(rows)
     useful = some.copy()
     if labels is not None:
@@ -98,8 +98,10 @@ def distill(s, values, indices, rest, labels, t, alpha):
         z1 = np.exp(s - m[:, None]).sum(1)
         yy = np.where(has, y, 0)
         ce = np.log(z1) - (s[np.arange(rows), yy] - m)
-        loss = loss + np.where(has, (1 - alpha) * ce, 0.0)
-        size = size + np.where(has, (1 - alpha) * (np.abs(np.log(z1)) + np.abs(s[np.arange(rows), yy] - m) + 1), 0.0)
+        if alpha < 1:
+            loss = loss + np.where(has, (1 - alpha) * ce, 0.0)
+        if alpha < 1:
+            size = size + np.where(has, (1 - alpha) * (np.abs(np.log(z1)) + np.abs(s[np.arange(rows), yy] - m) + 1), 0.0)
         hard = np.exp(s - m[:, None]) / z1[:, None]
         reach = reach + np.where(has[:, None], (1 - alpha) * hard, 0.0)
         hard[np.arange(rows), yy] -= 1

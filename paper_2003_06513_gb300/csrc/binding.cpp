@@ -300,10 +300,10 @@ PyObject* block_norm(PyObject* const* a, Py_ssize_t n_args) {
     return t;
 }
 
-// dh, dy, h, block, then Parameters' ten, stream, workspace -> (dx, dblock, dpost_weight, dpost_bias, dscale, dgate, dweight, dbias),
+// dh, dy, h, block, then Parameters' ten, out_dx, out_dblock, stream, workspace -> (dx, dblock, dpost_weight, dpost_bias, dscale, dgate, dweight, dbias),
 // None for what is not there
 PyObject* block_norm_backward(PyObject* const* a, Py_ssize_t n_args) {
-    want(n_args, 16);
+    want(n_args, 18);
     const at::Tensor& h = tensor(a[2], "h");
     const Layout l = input(h, "h");
     const at::Tensor *dh = maybe(a[0], "dh"), *dy = maybe(a[1], "dy"), *b = maybe(a[3], "block");
@@ -315,10 +315,10 @@ PyObject* block_norm_backward(PyObject* const* a, Py_ssize_t n_args) {
     const Parameters p(a + 4, h);
     const int n = (int)h.size(0), c = (int)h.size(1), dtype = b ? dtype_of(*b) : dtype_of(h);
     const int64_t pixels = h.size(2) * h.size(3);
-    const Place at(h.device(), a[14]);
+    const Place at(h.device(), a[16]);
     at::Tensor grads[8];                        // in the order of the result
-    grads[0] = result(Py_None, h, h.scalar_type(), "dx");
-    if (b) grads[1] = result(Py_None, h, type, "dblock");
+    grads[0] = result(a[14], h, h.scalar_type(), "dx");
+    if (b) grads[1] = result(a[15], h, type, "dblock");
     const int of[6] = {5, 6, 7, 8, 10, 11};     // the parameters among the arguments
     float* sums[6];
     for (int i = 0; i < 6; ++i) {
@@ -329,7 +329,7 @@ PyObject* block_norm_backward(PyObject* const* a, Py_ssize_t n_args) {
     size_t bytes = 0;
     void* space = nullptr;
     at::Tensor held;
-    if (const at::Tensor* w = maybe(a[15], "workspace")) {
+    if (const at::Tensor* w = maybe(a[17], "workspace")) {
         if (!w->is_contiguous() || w->device() != h.device()) refuse("workspace must be a contiguous CUDA tensor on the stream's device");
         space = w->data_ptr();
         bytes = w->nbytes();
@@ -343,6 +343,8 @@ PyObject* block_norm_backward(PyObject* const* a, Py_ssize_t n_args) {
         p.post_weight, p.post_bias, p.scale, p.gate, p.pre, p.weight, p.bias, p.act, p.eps, grads[0].data_ptr(),
         b ? grads[1].data_ptr() : nullptr, sums[0], sums[1], sums[2], sums[3], sums[4], sums[5], space, bytes, at.stream);
     if (e) return PyLong_FromLong(e);
+    if (a[14] != Py_None) changed(grads[0]);
+    if (b && a[15] != Py_None) changed(grads[1]);
     PyObject* t = PyTuple_New(8);
     if (!t) throw Raised();
     for (int i = 0; i < 8; ++i) {

@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     }
     if (!HARD) sum_1 = sum_t;
     float loss = 0;
-    if (REST && taught) {
+    const bool weighed = taught && a.soft_loss != 0.0f;     // (no weight takes no part, an infinite one neither)
+    if (REST && weighed) {
         // Both sides are whole distributions over the kept classes and the others: sum p (log p - log q) is the sum of
         // q - p - p delta, delta = log q - log p, whose terms are all positive, p delta^2 / 2 for a small delta; summed as they stand
         // the logarithms would cancel where student and teacher agree.
@@ -335,11 +336,11 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
         loss = a.soft_loss * kl[0];
     }
     if (lane) return;
-    if (!REST && taught) {
+    if (!REST && weighed) {
         const float whole = total[0], d = fmaf(whole, (m - mx) * a.inv_t, total[3]);
         loss = a.soft_loss * (d / whole - logf(whole) + logf(sum_t));
     }
-    if (label >= 0) loss += a.hard * (logf(sum_1) - (widen(s[label]) - m));
+    if (label >= 0 && a.hard != 0.0f) loss += a.hard * (logf(sum_1) - (widen(s[label]) - m));
     a.loss[row] = loss;
     float* out = a.stats + (int64_t)row * 5;
     out[0] = m;

@@ -153,12 +153,13 @@ def pp_block_norm_backward(dh: Optional[torch.Tensor], dy: Optional[torch.Tensor
                            block: Optional[torch.Tensor], post: str = "rms", post_weight: Optional[torch.Tensor] = None,
                            post_bias: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                            gate: Optional[torch.Tensor] = None, pre: str = "rms", weight: Optional[torch.Tensor] = None,
-                           bias: Optional[torch.Tensor] = None, act: str = "none", eps: float = 1e-5, stream=None,
+                           bias: Optional[torch.Tensor] = None, act: str = "none", eps: float = 1e-5, out=(None, None), stream=None,
                            workspace: Optional[torch.Tensor] = None) -> BlockGrads:
-    """The gradients from those of h and y (None: zero); h is the forward pass's, the other arguments as they were there."""
+    """The gradients from those of h and y (None: zero); h is the forward pass's, the other arguments as they were there.
+    ``out``: (dx, dblock) to write to, or None: dx may be dh, and dblock dy."""
     return BlockGrads(*_done("pp_block_norm_backward", _lib.binding().block_norm_backward(
         dh, dy, h, block, _norm(post, "post"), post_weight, post_bias, scale, gate, _norm(pre, "pre"), weight, bias, _act(act), eps,
-        None if stream is None else stream.cuda_stream, workspace)))
+        out[0], out[1], None if stream is None else stream.cuda_stream, workspace)))
 
 
 def _ordered(d: Optional[torch.Tensor]) -> Optional[torch.Tensor]:

@@ -271,6 +271,30 @@ def test_in_place(shape, dtype):
     assert tx._version > versions[0] and tb._version > versions[1]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("shape", [(2, 32, 20, 20), (1, 12, 1, 1), (3, 520, 4, 4), (9, 256, 40, 40)], ids=str)
+def test_gradients_in_place(shape, dtype):
+    """dx over dh and dblock over dy, with rows read ahead of those that are written."""
+    rng = np.random.default_rng(16)
+    th, tb, td, ty = (_image(_held(rng, shape, dtype), dtype) for _ in range(4))
+    d = _device(_parameters(rng, shape[0], shape[1], "layer", "rms"))
+    args = ("layer", d["post_weight"], d["post_bias"], d["scale"], d["gate"], "rms", d["weight"], d["bias"], "silu")
+    want = norm.pp_block_norm_backward(td, ty, th, tb, *args)
+    versions = td._version, ty._version
+    got = norm.pp_block_norm_backward(td, ty, th, tb, *args, out=(td, ty))
+    assert got.dx.data_ptr() == td.data_ptr() and got.dblock.data_ptr() == ty.data_ptr()
+    assert td._version > versions[0] and ty._version > versions[1] and all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(PatconvError):
+        norm.pp_block_norm_backward(td, ty, th, tb, *args, out=(th, None))
+
+
+@pytest.mark.parametrize("c", [3, 24, 60, 150, 264])
+@pytest.mark.parametrize("samples,pixels", [(1, 1), (1, 700), (2000, 1), (37, 50), (3, 5000)])
+def test_samples_and_stretches(samples, pixels, c):
+    """Gates' gradients of samples that begin, end and lie inside CTAs' stretches, and of more samples than there are CTAs."""
+    _case((samples, c, pixels, 1), "f16", "f16", 17, "rms", "layer", "silu")
+
+
 def test_nothing_to_do():
     for shape in ((0, 8, 3, 3), (2, 8, 0, 3)):
         x = torch.zeros(shape, device="cuda").contiguous(memory_format=torch.channels_last)
@@ -345,6 +369,47 @@ def test_autograd(wanted):
             _within(_host(leaf.grad), want[name], bound[name], "f32", name)
         else:
             assert not leaf.grad.any()
+
+
+def test_without_a_second_norm_in_autograd():
+    rng = np.random.default_rng(18)
+    x, b, dh = (_held(rng, (2, 24, 6, 7), "f32") for _ in range(3))
+    tx, tb = (_image(a, "f32").detach().requires_grad_(True) for a in (x, b))
+    h, y = norm.block_norm(tx, tb, "rms", pre="none")
+    assert y is None
+    (h * _image(dh, "f32")).sum().backward()
+    want, bound = D.block_backward(dh, None, x, b, "rms", None, None, None, None, "none", None, None, "none", 1e-5)
+    for leaf, name in ((tx, "dx"), (tb, "dblock")):
+        _within(_host(leaf.grad), want[name], bound[name], "f32", name)
+
+
+def test_a_captured_training_step():
+    """Forward, loss and gradients of a block captured into a graph, replayed on other inputs."""
+    rng = np.random.default_rng(19)
+    shape = (2, 40, 8, 8)
+    first, second = ([_image(_held(rng, shape, "f16"), "f16") for _ in range(2)] for _ in range(2))
+    w = torch.rand(40, device="cuda")
+
+    def step(x, b):
+        x, b, leaf = (t.detach().requires_grad_(True) for t in (x, b, w))
+        h, y = norm.block_norm(x, b, "layer", leaf, gate=torch.sigmoid(b.float().mean((2, 3))), pre="rms", act="silu")
+        return torch.autograd.grad((h * y).float().sum(), (x, b, leaf))
+
+    want = step(*second)
+    static = [t.clone(memory_format=torch.preserve_format) for t in first]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*static)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*static)
+    for t, new in zip(static, second):
+        t.copy_(new)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_the_norm_alone_in_autograd():

@@ -258,6 +258,22 @@ def test_rows_of_the_lowest_value(classes, temperature):
 
 
 @pytest.mark.parametrize("rest", [False, True])
+def test_a_part_of_no_weight_takes_no_part(rest):
+    """alpha 0 beside a kept class that the student's mask leaves out, alpha 1 beside such a label: infinite terms of weight 0."""
+    rng = np.random.default_rng(20)
+    for rows, classes in ((6, 50), (6, 5000)):
+        s, t = _rows(rng, rows, classes, "f32")
+        teacher = _teacher(rng, rows, classes, 4, "f32", empty=False)
+        y = teacher[1][:, 1].copy()
+        s[2, y[2]] = -np.inf
+        t[2, y[2]] = -math.inf
+        y[3] = -1
+        _check(s, t, teacher, np.where(np.arange(rows) == 2, teacher[1][:, 0], y), 2.0, 0.0, rest, "f32")
+        loss, stats = distill.pp_distill(t, teacher[3], teacher[4] * 0 - 1, None, torch.from_numpy(y).cuda(), 2.0, 1.0)
+        assert not loss.any()
+
+
+@pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("rows,classes", [(30, 20), (5, 6000)])
 def test_padded_rows_are_not_read(rows, classes, rest):
     """Rows without label and teacher, and rows whose loss has no gradient, hold NaN: zeros come out, and the others do not change."""
@@ -345,6 +361,34 @@ def test_the_same_bits_again_on_another_stream_and_in_a_graph(rows, classes, k):
     torch.cuda.synchronize()
     for a in (again, other, captured, captured2):
         assert all(torch.equal(x, z) for x, z in zip(want, a))
+
+
+def test_a_captured_training_step():
+    """Selection, loss and gradient captured into a graph, replayed on other inputs."""
+    g = torch.Generator("cuda").manual_seed(21)
+    first, second = ([torch.randn(30, 2000, device="cuda", generator=g) * 2 for _ in range(2)] for _ in range(2))
+    y = torch.randint(0, 2000, (30,), device="cuda", generator=g)
+
+    def step(s, teacher):
+        leaf = s.detach().requires_grad_(True)
+        loss = distill.distill_loss(leaf, distill.pp_top_logits(teacher, 20, 2.0), y, 2.0, 0.5)
+        return loss.detach(), torch.autograd.grad(loss.mean(), leaf)[0]
+
+    want = step(*second)
+    static = [t.clone() for t in first]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*static)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*static)
+    for t, new in zip(static, second):
+        t.copy_(new)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_autograd():
