@@ -60,7 +60,7 @@ struct Shared {
 
 template <typename T, int N>
 __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 : 2) top_rows(TopArgs a) {
-    constexpr int W = 16 / sizeof(T), kWarps = N / 32, U = 4;
+    constexpr int W = 16 / sizeof(T), kWarps = N / 32, U = N == 128 ? 8 : 4;
     extern __shared__ uint4 dynamic[];
     __shared__ Shared sh;
     __shared__ float scratch[2 * kWarps * 8];
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 
             const int v = base + threadIdx.x;
             int turn = 0;
 #pragma unroll 1
-            for (; turn < 29 && v + (turn + U - 1) * N < to; turn += U) {
+            for (; turn < 33 - U && v + (turn + U - 1) * N < to; turn += U) {
                 Vec<T, W> b[U];
 #pragma unroll
                 for (int k = 0; k < U; ++k) b[k] = middle_at(v + (turn + k) * N);
