@@ -9,6 +9,7 @@
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
@@ -26,6 +27,9 @@ struct Refused : std::runtime_error {       // becomes ValueError
     using std::runtime_error::runtime_error;
 };
 struct Raised {};                           // a Python error is set already
+struct Status {                             // of a C entry point, where there is no result to return it as
+    int e;
+};
 
 [[noreturn]] void refuse(const std::string& why) { throw Refused(why); }
 
@@ -449,6 +453,55 @@ PyObject* distill_backward(PyObject* const* a, Py_ssize_t n_args) {
     return THPVariable_Wrap(out);
 }
 
+// The loss as one differentiable operation.  Its backward pass runs on a thread of torch's engine: there is no Python in it.
+struct DistillLoss : torch::autograd::Function<DistillLoss> {
+    using Context = torch::autograd::AutogradContext;
+    static at::Tensor forward(Context* ctx, const at::Tensor& s, const at::Tensor& values, const at::Tensor& indices,
+                              const std::optional<at::Tensor>& rest, const std::optional<at::Tensor>& labels, double temperature, double alpha,
+                              int64_t stride) {
+        const c10::cuda::CUDAGuard guard(s.device());
+        const at::Tensor loss = floats({s.size(0)}, s), stats = floats({s.size(0), 5}, s);
+        const int e = pp_distill(s.const_data_ptr(), stride, dtype_of(s), s.size(0), s.size(1), values.const_data_ptr(), dtype_of(values),
+                                 indices.const_data_ptr<int>(), (int)values.size(1), rest ? rest->const_data_ptr<float>() : nullptr,
+                                 labels ? labels->const_data_ptr<int64_t>() : nullptr, temperature, alpha, loss.data_ptr<float>(),
+                                 stats.data_ptr<float>(), c10::cuda::getCurrentCUDAStream(s.get_device()).stream());
+        if (e) throw Status{e};
+        ctx->save_for_backward({s, stats, values, indices, rest.value_or(at::Tensor()), labels.value_or(at::Tensor())});
+        ctx->saved_data["temperature"] = temperature;
+        ctx->saved_data["alpha"] = alpha;
+        return loss;
+    }
+    static torch::autograd::variable_list backward(Context* ctx, torch::autograd::variable_list grads) {
+        TORCH_CHECK(!at::GradMode::is_enabled(), "distill_loss is differentiable once: its gradient has no graph (create_graph)");
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &s = saved[0], &stats = saved[1], &values = saved[2], &indices = saved[3], &rest = saved[4], &labels = saved[5];
+        const c10::cuda::CUDAGuard guard(s.device());
+        const at::Tensor d = grads[0].to(at::kFloat), out = at::empty(s.sizes(), s.options().requires_grad(false));
+        const int64_t n = s.size(0);
+        const int e = pp_distill_backward(d.const_data_ptr<float>(), n > 1 ? d.stride(0) : 0, s.const_data_ptr(), n > 1 ? s.stride(0) : s.size(1),
+                                          dtype_of(s), n, s.size(1), stats.const_data_ptr<float>(), values.const_data_ptr(), dtype_of(values),
+                                          indices.const_data_ptr<int>(), (int)values.size(1),
+                                          rest.defined() ? rest.const_data_ptr<float>() : nullptr,
+                                          labels.defined() ? labels.const_data_ptr<int64_t>() : nullptr, ctx->saved_data["temperature"].toDouble(),
+                                          ctx->saved_data["alpha"].toDouble(), out.data_ptr(),
+                                          c10::cuda::getCurrentCUDAStream(s.get_device()).stream());
+        TORCH_CHECK(e == PP_OK, "pp_distill_backward failed: ", pp_status_string(e));
+        torch::autograd::variable_list r(8);
+        r[0] = out;
+        return r;
+    }
+};
+
+// logits, then Teacher's six -> loss
+PyObject* distill_loss(PyObject* const* a, Py_ssize_t n_args) {
+    want(n_args, 7);
+    const at::Tensor& s = tensor(a[0], "logits");
+    const int64_t stride = row_stride(s, "logits");
+    const Teacher t(a + 1, s);
+    const auto given = [](const at::Tensor* p) { return p ? std::optional<at::Tensor>(*p) : std::nullopt; };
+    return THPVariable_Wrap(DistillLoss::apply(s, *t.values, *t.indices, given(t.rest), given(t.labels), t.temperature, t.alpha, stride));
+}
+
 // ---------------------------------------------------------------------------------- many tensors
 
 struct Wanted {                             // of one tensor's gradient, and of the tensor itself
@@ -658,6 +711,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     try {
         return F(args, n);
     } catch (const Raised&) {
+    } catch (const Status& s) {
+        return PyLong_FromLong(s.e);
     } catch (const Refused& e) {
         PyErr_SetString(PyExc_ValueError, e.what());
     } catch (const std::exception& e) {      // an allocation that failed, for one
@@ -676,6 +731,7 @@ PyMethodDef methods[] = {{"group_norm", fast<group_norm>(), METH_FASTCALL, nullp
                          {"block_norm_backward", fast<block_norm_backward>(), METH_FASTCALL, nullptr},
                          {"top_logits", fast<top_logits>(), METH_FASTCALL, nullptr},
                          {"distill", fast<distill>(), METH_FASTCALL, nullptr},
+                         {"distill_loss", fast<distill_loss>(), METH_FASTCALL, nullptr},
                          {"distill_backward", fast<distill_backward>(), METH_FASTCALL, nullptr},
                          {"layout", fast<layout>(), METH_FASTCALL, nullptr},
                          {"tensors", fast<tensors>(), METH_FASTCALL, nullptr},

@@ -59,22 +59,8 @@ def pp_distill_backward(dloss: torch.Tensor, logits: torch.Tensor, stats: torch.
         dloss, logits, stats, values, indices, rest, labels, temperature, alpha, out, _handle(stream)))
 
 
-class _Distill(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, logits, values, indices, rest, labels, temperature, alpha):
-        loss, stats = pp_distill(logits, values, indices, rest, labels, temperature, alpha)
-        ctx.save_for_backward(logits, stats, values, indices, rest, labels)
-        ctx.numbers = temperature, alpha
-        return loss
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dloss):
-        logits, stats, *teacher = ctx.saved_tensors
-        return (pp_distill_backward(dloss, logits, stats, *teacher, *ctx.numbers),) + (None,) * 6
-
-
 def distill_loss(logits: torch.Tensor, top: TopLogits, labels: Optional[torch.Tensor] = None, temperature: float = 1.0,
                  alpha: float = 0.5) -> torch.Tensor:
-    """Losses of the rows, float32 [rows], as one operation that is differentiable by the logits, on the current stream."""
-    return _Distill.apply(logits, top.values, top.indices, top.rest, labels, temperature, alpha)
+    """Losses of the rows, float32 [rows], as one operation that is differentiable by the logits (once), on the current stream.
+    The operation is native on both sides (csrc/binding.cpp)."""
+    return _done("pp_distill", _lib.binding().distill_loss(logits, top.values, top.indices, top.rest, labels, temperature, alpha))

@@ -415,6 +415,38 @@ def test_autograd():
     _within(_host(x.grad), want[0][2] + want[1][2], (D.roundings(500) + 4 * D.U) * (want[0][4] + want[1][4]), "f32", "gradient of two")
 
 
+def test_autograd_refuses_what_it_cannot_do():
+    x = torch.randn(3, 40, device="cuda", requires_grad=True)
+    top = distill.pp_top_logits(x.detach(), 4)
+    loss = distill.distill_loss(x, top)
+    with pytest.raises(RuntimeError, match="once"):
+        torch.autograd.grad(loss.sum(), x, create_graph=True)
+    with pytest.raises(PatconvError):
+        distill.distill_loss(x, top, temperature=0.0)
+    with pytest.raises(ValueError, match="labels"):
+        distill.distill_loss(x, top, torch.zeros(3, device="cuda"))
+    x.data.add_(1)
+    loss = distill.distill_loss(x, top)
+    with torch.no_grad():
+        x.add_(1)                                       # what the gradient would be of has changed
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.sum().backward()
+
+
+def test_autograd_on_another_stream():
+    x = torch.randn(50, 3000, device="cuda")
+    top = distill.pp_top_logits(x, 9)
+    want = x.clone().requires_grad_(True)
+    distill.distill_loss(want * 0.5, top).sum().backward()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = x.clone().requires_grad_(True)
+        distill.distill_loss(got * 0.5, top).sum().backward()
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got.grad, want.grad)
+
+
 def test_refusals():
     s = torch.zeros(4, 100, device="cuda")
     v, at, rest, y = s[:, :5].contiguous(), torch.zeros(4, 5, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(4, dtype=torch.long, device="cuda")
