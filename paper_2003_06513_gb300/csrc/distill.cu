@@ -25,10 +25,9 @@ namespace cg = cooperative_groups;
 
 constexpr int kWide = 128;            // threads of a CTA that has a row, or a part of one
 constexpr int kRowsOfCta = 4;         // rows of a CTA whose warps have one each
-constexpr int kMostOfWarp = 2048;     // classes of a warp's row at most
+constexpr int kMostOfWarp = 1024;     // 16-byte vectors of a warp's row at most
 
-template <int W>
-constexpr int kBitsOfWarp = ((kMostOfWarp + 2 * W - 2) / W + 31) / 32;       // words of a warp's row: a bit a vector
+constexpr int kBitsOfWarp = kMostOfWarp / 32;        // words of a warp's row: a bit a vector
 
 // what a thread sums of the classes it sees: the largest x, and the sums of 2^((x - m) c) relative to it
 // HARD: how the sum at T = 1 is had beside the one at T.  kNone: there are no labels, or T is 1; kApart: by an exponential of its
@@ -83,7 +82,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     const Row<T, W> r(s, a.classes);
     // this group's vectors
     const int each = (r.vectors() + a.parts - 1) / a.parts, first = part * each, last = min(r.vectors(), first + each);
-    unsigned* bits = reinterpret_cast<unsigned*>(dynamic) + (N == 32 ? slot * kBitsOfWarp<W> : 0);
+    unsigned* bits = reinterpret_cast<unsigned*>(dynamic) + (N == 32 ? slot * kBitsOfWarp : 0);
     int* kept = places[slot];                         // the entries' places in the row, -1: empty
     bool* came = before[slot];                        // whether an entry's class is that of an earlier one
     float *us = teacher[slot], *xs = student[slot];
@@ -353,16 +352,19 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
 template <typename T, bool REST, int HARD>
 cudaError_t launch(DistillArgs a, cudaStream_t st) {
     constexpr int W = 16 / sizeof(T);
-    if (a.classes <= kMostOfWarp && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
-        a.parts = 1;
-        const size_t smem = REST ? kRowsOfCta * kBitsOfWarp<W> * 4 : 0;
+    const int vectors = (a.classes + 2 * W - 2) / W;  // of a row, wherever it begins
+    a.parts = 1;
+    // a warp where there are rows enough, or hardly any classes (8192 x 1000 fp32: 18.5 us, by a CTA 33; 8192 x 4000 39 and 47; 1216 x
+    // 4000 8.5 and 8.2; 512 x 1000 6.4 and 6.0)
+    if (vectors <= kMostOfWarp && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
+        const size_t smem = REST ? kRowsOfCta * kBitsOfWarp * 4 : 0;
         distill_rows<T, REST, HARD, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, smem, st>>>(a);
         return cudaGetLastError();
     }
-    // few long rows: a cluster of CTAs has one
-    a.parts = 1;
-    while (a.parts < 8 && (int64_t)a.rows * a.parts < 2 * kSMs && a.classes / a.parts >= 4096 * 2) a.parts *= 2;
-    const int vectors = (a.classes + 2 * W - 2) / W, each = (vectors + a.parts - 1) / a.parts;
+    // few long rows: a cluster of CTAs has one (6 x 200001 fp32: 42 us by one CTA, 12.9 by eight; 160 x 100000 26 by one, 20 by two,
+    // 16 by four; but 400 x 65536 bf16 15.9 by one, 16.9 by two, 20.8 by four)
+    while (a.parts < 8 && (int64_t)a.rows * a.parts < 3 * kSMs && a.classes / a.parts >= 4096 * 2) a.parts *= 2;
+    const int each = (vectors + a.parts - 1) / a.parts;
     const size_t smem = REST ? ((size_t)each + 31) / 32 * 4 : 0;    // at most 32 KB
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.rows * (unsigned)a.parts);

@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kWide = 256;
 constexpr int kRowsOfCta = 4;
-constexpr int kMostOfWarp = 2048;
+constexpr int kMostOfWarp = 16384;    // bytes of a warp's row at most
 
 // VEC: the logits and their gradient have their 16-byte boundaries at the same places, and are read and written in such
 // vectors; else value by value.  TWO: both exponentials, else the one at T alone, its factor standing for both.
@@ -160,10 +160,17 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
 template <typename T, bool REST, bool TWO, bool VEC>
 cudaError_t launch(DistillArgs a, cudaStream_t st) {
     a.parts = 1;
-    if (a.classes <= kMostOfWarp && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
+    // a warp where there are rows enough, or hardly any classes (8192 x 1000 fp32: 10.6 us, by a CTA 29; 8192 x 4000 52 and 54, of bf16 28
+    // and 51; 1216 x 4000 fp32 8.5 and 7.8; 512 x 1000 4.6 and 4.7)
+    if (a.classes <= kMostOfWarp / (int)sizeof(T) && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
         distill_slopes<T, REST, TWO, VEC, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, 0, st>>>(a);
     } else {
-        while (a.parts < 64 && (int64_t)a.rows * a.parts < 4 * kSMs && a.classes / a.parts >= 4096) a.parts *= 2;
+        // few long rows: several CTAs have one, each its stretch, with nothing to join (6 x 200001 fp32: 32 us by one, 4.9 by 32;
+        // 400 x 65536 bf16 16.4 by one, 14.9 by two, 16.2 by four); of very long ones more, as the last CTAs end alone (300 x 1048576
+        // bf16: 218 us by four, 196 by eight; 1000 x 21841 14.1 by one, 16.6 by two)
+        while (a.parts < 64 && (((int64_t)a.rows * a.parts < 4 * kSMs && a.classes / a.parts >= 4096) ||
+                                ((int64_t)a.rows * a.parts < 16 * kSMs && a.classes / a.parts >= 65536)))
+            a.parts *= 2;
         distill_slopes<T, REST, TWO, VEC, kWide><<<(unsigned)a.rows * (unsigned)a.parts, kWide, 0, st>>>(a);
     }
     return cudaGetLastError();

@@ -52,7 +52,7 @@ constexpr int kLeast = INT_MIN;       // below every key
 struct Shared {
     int found;                        // how many values are listed (the first CTA's)
     int flagged;                      // how many vectors of this CTA are noted
-    unsigned long long beside;        // the sum of their other values' exponentials, in units of 2^-52
+    unsigned long long beside;        // the sum of their other values' exponentials, in units of 2^-46
     int bounds[kClusterMost];
     int counted[2][kClusterMost];
     float sums[kClusterMost];         // of the values that are not listed (the first CTA's)
@@ -118,17 +118,41 @@ __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 
         __syncthreads();
         long long low = INT_MAX, high = INT_MIN;
         for (int w = 0; w < kWarps; ++w) low = min(low, (long long)warp_ends[0][w]), high = max(high, (long long)warp_ends[1][w]);
-        ++high;                                       // `share` of them reach low, and not high
-        if (own >= share) {
+        ++high;
+        // the range's halves until `counted` says that `share` or few more reach it
+        const auto halve = [&](int slack, const auto& counted) {       // `share` reach low, and not high
             for (int k = 0; k < 20 && high - low > 1; ++k) {
-                const int middle = (int)((low + high) >> 1), n = __syncthreads_count(key >= middle);
+                const int middle = (int)((low + high) >> 1), n = counted(middle);
                 if (n >= share)
                     low = middle;
                 else
                     high = middle;
-                if (n >= share && n <= share + max(2, share / 4)) break;
+                if (n >= share && n <= share + slack) break;
             }
             bound = (int)low;
+        };
+        // a short row has as many vectors as values are wanted, or fewer: its values themselves are counted
+        if (4 * own >= 5 * share) {
+            // (where nearly all of the threads' reach it, of their other values many do)
+            halve(max(2, min(share / 4, (own - share) / 8)), [&](int middle) { return __syncthreads_count(key >= middle); });
+        } else if (a.parts == 1 && a.held && a.classes > 2 * share) {
+            int turn = 0;
+            low = kLeast;
+            halve(max(2, share / 4), [&](int middle) {
+                int n = 0;
+                for (int v = first + threadIdx.x; v < last; v += N) {
+                    const Vec<T, W> b = held[v - first];
+#pragma unroll
+                    for (int i = 0; i < W; ++i) n += key_of(widen(b.v[i])) >= middle && v * W + i >= r.pad && v * W + i < r.end;
+                }
+                n = __reduce_add_sync(0xffffffffu, n);
+                turn ^= 1;
+                if (lane == 0) warp_counts[turn][warp] = n;
+                __syncthreads();
+                n = 0;
+                for (int w = 0; w < kWarps; ++w) n += warp_counts[turn][w];
+                return n;
+            });
         }
     }
     if (a.parts > 1) {
@@ -158,14 +182,11 @@ __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 
             sum = add(sum, make_float2(approx_exp2(e.x), approx_exp2(e.y)));
         }
     };
-    const auto note = [&](int key, int place) {
-        const int n = atomicAdd(&leader->found, 1);
-        if (n < a.list) leader_list[n] = (unsigned long long)((unsigned)key ^ 0x80000000u) << 32 | (unsigned)~place;
-    };
+    const auto entry = [](int key, int place) { return (unsigned long long)((unsigned)key ^ 0x80000000u) << 32 | (unsigned)~place; };
     const auto tell = [&](float2 sum) {               // every thread's sum, to the first CTA; how many values are listed
         float total[1] = {sum.x + sum.y};
         g.sum(total);
-        if (threadIdx.x == 0) leader->sums[part] = total[0] + (float)sh.beside * 2.220446e-16f;
+        if (threadIdx.x == 0) leader->sums[part] = total[0] + (float)sh.beside * 0x1p-46f;
         everyone();
         return leader->found;
     };
@@ -219,26 +240,59 @@ __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 
             noted_from(to);
         }
         __syncthreads();
-        const int flagged = sh.flagged, values = min(flagged, a.list) * W;
+        const int flagged = sh.flagged, vectors = min(flagged, a.list);
         if (flagged > a.list && threadIdx.x == 0) atomicAdd(&leader->found, flagged);     // each has one at least
-        for (int i = threadIdx.x; i - lane < values; i += N) {         // (whole warps)
-            const int v = i < values ? noted[i / W] : 0, place = v * W + i % W - r.pad;
-            unsigned high = 0, low = 0;
-            if (i < values && place >= 0 && place < a.classes) {
-                const float x = widen(a.held ? held[v - first].v[i % W] : s[place]);
-                const int key = key_of(x);
-                if (key >= bound) {
-                    note(key, place);
-                } else {                              // integers: the vectors are noted in no order
-                    const float e = power(x, below, a.c) * 67108864.0f;
-                    high = (unsigned)e;
-                    low = (unsigned)((e - (float)high) * 67108864.0f);
+        // the noted vectors' values, M of them a thread
+        const auto examine = [&](auto m) {
+            constexpr int M = decltype(m)::value;
+            for (int i = threadIdx.x; i - lane < vectors * (W / M); i += N) {      // (whole warps)
+                const bool here = i < vectors * (W / M);
+                const int v = here ? noted[i / (W / M)] : first, k0 = M == 1 ? i % W : 0;
+                Vec<T, M> b;
+                if constexpr (M == W) {
+                    b = vector_at(v);
+                } else {
+                    const int place = v * W + k0;
+                    b.v[0] = a.held ? held[v - first].v[k0] : place >= r.pad && place < r.end ? r.base[place] : T(kNone);
                 }
+                // integers: the vectors are noted in no order.  22 bits and 24 more: 256 values are below 2^32, 8192 of both below 2^60
+                unsigned high = 0, low = 0, those = 0;
+#pragma unroll
+                for (int k = 0; k < M; ++k) {
+                    const int place = v * W + k0 + k;
+                    const float x = widen(b.v[k]);
+                    if (!here || place < r.pad || place >= r.end) continue;
+                    if (key_of(x) >= bound) {
+                        those |= 1u << k;
+                    } else {
+                        const float e = power(x, below, a.c) * 4194304.0f, whole = truncf(e);
+                        high += (unsigned)whole;
+                        low += (unsigned)((e - whole) * 16777216.0f);
+                    }
+                }
+                int up_to = __popc(those);            // of the lanes up to this one
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) {
+                    const int y = __shfl_up_sync(0xffffffffu, up_to, o);
+                    if (lane >= o) up_to += y;
+                }
+                int n = lane == 31 && up_to ? atomicAdd(&leader->found, up_to) : 0;
+                n = __shfl_sync(0xffffffffu, n, 31) + up_to - __popc(those);
+                for (; those; those &= those - 1, ++n) {
+                    const int k = __ffs(those) - 1;
+                    if (n < a.list) leader_list[n] = entry(key_of(widen(b.v[k])), v * W + k0 + k - r.pad);
+                }
+                high = __reduce_add_sync(0xffffffffu, high);
+                low = __reduce_add_sync(0xffffffffu, low);
+                if (lane == 0 && (high | low)) atomicAdd(&sh.beside, ((unsigned long long)high << 24) + low);
             }
-            high = __reduce_add_sync(0xffffffffu, high);
-            low = __reduce_add_sync(0xffffffffu, low);
-            if (lane == 0 && (high | low)) atomicAdd(&sh.beside, ((unsigned long long)high << 26) + low);
-        }
+        };
+        // a thread has one where that takes two turns at most, else a vector (4096 x 32768 bf16 with 10 kept: 65 us, by vectors 71;
+        // with 64 92 and 80, with 250 273 and 218)
+        if (vectors * W <= 2 * N)
+            examine(std::integral_constant<int, 1>());
+        else
+            examine(std::integral_constant<int, W>());
         __syncthreads();
         return tell(sum);
     };
@@ -255,10 +309,12 @@ __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 
                 if (place < 0 || place >= a.classes) continue;
                 const float x = widen(b.v[i]);
                 const int key = key_of(x);
-                if (key > bound || (key == bound && place <= until))
-                    note(key, place);
-                else
+                if (key > bound || (key == bound && place <= until)) {
+                    const int n = atomicAdd(&leader->found, 1);
+                    if (n < a.list) leader_list[n] = entry(key, place);
+                } else {
                     sum.x += power(x, below, a.c);
+                }
             }
         }
         return tell(sum);
@@ -319,11 +375,16 @@ __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 
     if (part == 0) {
         T* values = static_cast<T*>(a.values) + (int64_t)row * a.k;
         int* indices = a.indices + (int64_t)row * a.k;
+        if (threadIdx.x == 0 && all % 2) list[all] = 0;                // (the list's room is even) above no value
+        __syncthreads();
         for (int i = threadIdx.x; i < all; i += N) {
             const unsigned long long mine = list[i];
             int rank = 0;
-#pragma unroll 8
-            for (int n = 0; n < all; ++n) rank += list[n] > mine;
+#pragma unroll 4
+            for (int n = 0; n < all; n += 2) {
+                const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(list + n);
+                rank += (two.x > mine) + (two.y > mine);
+            }
             if (rank < a.k) {
                 const int place = (int)~(unsigned)mine;
                 values[rank] = s[place];
@@ -351,16 +412,16 @@ __global__ void __launch_bounds__(N, N == 32 ? 24 : N == 128 ? 8 : N == 256 ? 4 
     if (a.parts > 1) cluster.sync();                  // the first CTA's memory has been read by the others
 }
 
+template <typename T>
+int vectors_of(const TopArgs& a) {                    // of a row, wherever it begins
+    constexpr int W = 16 / sizeof(T);
+    return (a.classes + 2 * W - 2) / W;
+}
 template <typename T, int N>
 cudaError_t launch(TopArgs a, cudaStream_t st) {
-    constexpr int W = 16 / sizeof(T);
-    const int vectors = (a.classes + 2 * W - 2) / W;
-    const auto slice = [&] { return (size_t)((vectors + a.parts - 1) / a.parts) * 16; };
-    a.parts = 1;
-    // a cluster where a slice does not fit, or where the rows are too few for the SMs
-    while (a.parts < kClusterMost && (slice() > 196608 || ((int64_t)a.rows * a.parts < kSMs && slice() >= 16384))) a.parts *= 2;
-    a.held = slice() <= kHeld ? (int)slice() : 0;
-    a.list = N == 32 ? 256 : a.k < 128 ? 512 : 1024;
+    const size_t slice = (size_t)((vectors_of<T>(a) + a.parts - 1) / a.parts) * 16;
+    a.held = slice <= kHeld ? (int)slice : 0;
+    a.list = N == 32 ? 256 : N < 512 ? 512 : 1024;
     constexpr int kLists = 1024 * 12;
     static std::atomic<uint64_t> allowed{0};
     int dev = 0;
@@ -387,11 +448,36 @@ cudaError_t launch(TopArgs a, cudaStream_t st) {
     return e != cudaSuccess ? e : l;
 }
 template <typename T>
-cudaError_t top(const TopArgs& a, cudaStream_t st) {
-    // a bound takes more threads than values are wanted; beyond that fewer threads have less to do beside reading, and a warp
-    // where there are rows enough (5424 x 746: 17 us, by 128 threads 29; but 256 x 1000 10.5 so, 8.4 by 128)
-    if (a.classes <= 1024 && a.k < 24 && a.rows >= 8 * kSMs) return launch<T, 32>(a, st);
-    return a.k < 96 ? launch<T, 128>(a, st) : a.k < 192 ? launch<T, 256>(a, st) : launch<T, 512>(a, st);
+cudaError_t top(TopArgs a, cudaStream_t st) {
+    constexpr int kThreads = 1024, kMost = 512;       // threads of an SM, and of a CTA at most
+    a.parts = 1;
+    // A warp where there are rows enough: 5424 x 746 takes 17 us, by 128 threads 29; 8192 x 2000 fp32 26 and 38, of bf16 22 and 37.
+    // But 8192 x 4000 fp32 takes 59 and 56, and 256 x 1000 takes 10.5 and 8.4.
+    if ((int64_t)vectors_of<T>(a) <= 512 && a.k < 24 && a.rows >= 8 * kSMs) return launch<T, 32>(a, st);
+    // The bound is found among the threads' largest values, so there are half as many threads again as values are wanted: 256 x
+    // 1000 with 95 kept takes 19 us by 128 threads and 7.7 by 256.  No more than that, as a row has its fixed work: 4096 x
+    // 32768 bf16 with 60 kept takes 80 us by 128 threads and 89 by 256, with 10 65, 74 and by 512 107; but
+    int n = a.k < 80 ? 128 : a.k < 160 ? 256 : kMost;
+    const int64_t row = (int64_t)vectors_of<T>(a) * 16;
+    // where the threads of all rows fit on the GPU, a row has more of them, eight vectors each: 64 x 32768 bf16 takes 9.6 us with 128
+    // threads, 7.4 with 512,
+    while (n < kMost && 2 * n * (int64_t)a.rows <= kSMs * kThreads && row >= 2 * n * 128) n *= 2;
+    // and then a cluster of CTAs: 6 x 200001 takes 21.9 us by one CTA and 10.4 by eight (its barriers cost 2 us: 150 x 32768 fp32 takes
+    // 8.2 us by one, 10.8 by two);
+    while (a.parts < kClusterMost && n == kMost &&
+           ((2 * a.parts * (int64_t)a.rows <= kSMs && row >= a.parts * (128 << 10)) ||
+            (2 * a.parts * (int64_t)a.rows * n <= kSMs * kThreads && row >= a.parts * (512 << 10))))
+        a.parts *= 2;
+    // and the rows that are under way together stay in L2 for the second reading: 2000 x 65536 bf16 takes 94 us by 128 threads,
+    // 75 by 256; 1000 x 100000 fp32 136 by 128, 130 by 512 and 120 by two CTAs of 512
+    while ((n < kMost || a.parts < kClusterMost) &&
+           std::min((int64_t)a.rows, kSMs * (int64_t)kThreads / n / a.parts) * row > (80 << 20)) {
+        if (n < kMost)
+            n *= 2;
+        else
+            a.parts *= 2;
+    }
+    return n == 128 ? launch<T, 128>(a, st) : n == 256 ? launch<T, 256>(a, st) : launch<T, kMost>(a, st);
 }
 
 }  // namespace

@@ -110,6 +110,43 @@ def test_top_of_what_is_not_finite():
     assert float(got.rest[2]) == -math.inf and float(got.rest[4]) == math.inf and math.isnan(float(got.rest[5]))
 
 
+# rows of few vectors with many kept, whose values themselves are counted; warps; one CTA of 128 to 512 threads; clusters for few rows
+# and for many that would not stay in L2
+FORMS = [(40, 200, 60), (40, 300, 128), (9, 520, 250), (300, 1000, 250), (5, 1500, 256), (7, 2047, 200), (1300, 60, 23), (1300, 130, 20),
+         (1250, 2000, 23), (1250, 4000, 10), (64, 32768, 20), (3, 90000, 63), (20, 65536, 64), (330, 70001, 20), (160, 270001, 5)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", FORMS, ids=str)
+def test_top_in_every_form(shape, dtype):
+    rows, classes, k = shape
+    rng = np.random.default_rng(classes + k)
+    s, t = _rows(rng, rows, classes, dtype, wide=3, at=2)
+    _check_top(s, t, k, (1.0, 2.0, 3.5)[k % 3])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,classes,k", [(8, 300, 100), (8, 1000, 250), (1300, 100, 23), (8, 1500, 256)])
+def test_top_of_short_rows_of_odd_values(rows, classes, k, dtype):
+    """Equal values, hardly any that are not -inf, ones of very different size, rows of NaN but for few."""
+    rng = np.random.default_rng(5)
+    normal = rng.standard_normal((rows, classes))
+    for s in (np.zeros((rows, classes)), rng.integers(-2, 2, (rows, classes)).astype(float), np.full((rows, classes), -np.inf),
+              np.where(rng.random((rows, classes)) < 0.01, normal, -np.inf), normal * 10.0 ** rng.integers(-30, 30, (rows, classes)),
+              -np.abs(normal), np.where(np.arange(classes) < k // 2, np.nan, normal)):
+        t = torch.from_numpy(s).to(DT[dtype])
+        _check_top(t.double().numpy(), t.cuda(), k, 1.0 if np.abs(np.nan_to_num(s, neginf=0.0)).max() < 10 else 1e3)
+
+
+@pytest.mark.parametrize("classes,k", [(4800, 256), (8000, 250), (6000, 100)])
+def test_top_of_rows_whose_others_are_hardly_less(classes, k):
+    """One value in eight is 1, the seven beside it 0.9995: thousands of exponentials near 1."""
+    s = torch.full((3, classes), 1 - 2.0 ** -11, dtype=torch.float16)
+    s[:, ::8] = 1
+    s[1] = s[1].flip(0)
+    _check_top(s.double().numpy(), s.cuda(), k)
+
+
 # ------------------------------------------------------------------------------------- the loss
 
 # rows, classes, kept: a warp a row, a CTA, a cluster; kept 1, all, the most; odd sizes
@@ -180,6 +217,15 @@ def test_loss_and_gradient(shape, dtype):
         labels[0] = max(0, min(classes - 1, int(teacher[1][0, 0])))         # the label among the kept
     for rest in (False, True):
         _check(s, t, teacher, labels, (1.0, 2.0, 3.5)[classes % 3], (0.5, 0.9, 1.0)[rows % 3], rest, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1250, 4093, 20), (1250, 4096, 32), (1220, 8189, 9), (200, 66001, 30), (400, 65536, 5)], ids=str)
+def test_loss_and_gradient_of_many_long_rows(shape, dtype):
+    rows, classes, k = shape
+    rng = np.random.default_rng(classes + k)
+    s, t = _rows(rng, rows, classes, dtype, wide=1)
+    _check(s, t, _teacher(rng, rows, classes, k, dtype), _labels(rng, rows, classes), 2.0, 0.7, True, dtype)
 
 
 @pytest.mark.parametrize("labels", [False, True])
