@@ -31,8 +31,8 @@
  * pp_adamw_step) serves the masked
  * retraining of a pruned network between its convolutions and after its backward pass; its
  * activations are channels last, as training libraries keep them for convolutions.  The first kernel
- * of each of its calls is a plain launch; further kernels of a group norm's call start while the one
- * before them ends, under capture too, unless PATCONV_PDL=0.
+ * of each of its calls is a plain launch; further kernels of a group norm's call, and the second of a
+ * block norm's backward pass, start while the one before them ends, under capture too, unless PATCONV_PDL=0.
  *
  * Thread safety: a handle is immutable after pp_pack/pp_bind_device, so pp_conv on one handle
  * may be called from several host threads and streams at once.
@@ -402,7 +402,7 @@ typedef enum {
  *              the biases zeros), and a norm that is not there has none;
  *   h          DEVICE, dense, of `x_dtype`; may be x itself where that is dense, else must not overlap;
  *   y          DEVICE, dense, of `dtype`; may be block itself where that is dense, else must not overlap.
- * Sums are fp32, in a fixed order; C is at most 4096.  Pointers need element alignment only; vectors of eight channels
+ * Sums are fp32, in a fixed order; C is at most 4096, and N * pixels below 2^31 - 2^24.  Pointers need element alignment only; vectors of eight channels
  * on 16-byte boundaries are fastest.  Never synchronises.  Errors: PP_ERR_NULL, _SHAPE (sizes, strides), _ALIGN,
  * _DTYPE, _BUFFER (overlap), _ARG (kinds, eps, a parameter of a norm that is not there), _CUDA. */
 int pp_block_norm(const void* x, int64_t x_pixel, int64_t x_sample, int x_dtype, const void* block, int64_t block_pixel,
@@ -441,7 +441,8 @@ int pp_block_norm_workspace_size(int N, int64_t pixels, int C, size_t* bytes);
  *   values     DEVICE [rows][k] of `dtype`;   indices  DEVICE [rows][k];
  *   rest       DEVICE fp32 [rows]: the log-sum-exp of the other logits over `temperature`, -infinity where there are none
  *              (k == classes) or all are -infinity; NaN where one of them is.
- * 0.001 <= temperature <= 1000; logits over the temperature have to be in fp32's range.  Pointers need element alignment.
+ * 0.001 <= temperature <= 1000; logits over the temperature have to be in fp32's range.  At most 2^27 rows.  Pointers need
+ * element alignment; rows that begin on 16-byte boundaries are fastest.
  * The same inputs and strides give the same bits.  Outputs overlap nothing.  Never synchronises.
  * Errors: PP_ERR_NULL, _SHAPE (classes above PP_MOST_CLASSES, k, stride), _ALIGN, _DTYPE, _BUFFER, _ARG, _CUDA. */
 int pp_top_logits(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t classes, int k, double temperature,

@@ -23,6 +23,8 @@ inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return an && bn && x < y + bn && y < x + an;
 }
+// whether rows may be so far apart
+inline bool apart(int64_t rows, int64_t stride, int64_t classes) { return rows <= 1 || (stride >= classes && stride <= (int64_t(1) << 50) / rows); }
 // elements from a row's first to the last row's last
 inline int64_t row_extent(int64_t rows, int64_t stride, int64_t classes) { return rows ? (rows - 1) * stride + classes : 0; }
 

@@ -195,6 +195,19 @@ def test_block_refusals(lib):
     assert bwd(dx=1 << 20) == BUFFER and bwd(dx=1 << 19) == BUFFER and bwd(db=1 << 21) == BUFFER and bwd(db=1 << 18) == BUFFER and bwd(db=1 << 22) == BUFFER
 
 
+def test_sizes_and_strides_that_no_index_reaches(lib):
+    """A CTA's last row, counted in 32 bits, and a tensor's last byte, in 64, have to exist."""
+    size = ctypes.c_size_t()
+    assert lib.pp_block_norm_workspace_size(1, (1 << 31) - (1 << 23), 1, ctypes.byref(size)) == SHAPE
+    assert lib.pp_block_norm_workspace_size(3, (1 << 31) // 3 - (1 << 20), 1, ctypes.byref(size)) == SHAPE
+    assert lib.pp_block_norm_workspace_size(1, (1 << 31) - (1 << 24) - 1, 1, ctypes.byref(size)) == 0
+    big, out = p(1 << 20), p(1 << 40)
+    assert lib.pp_block_norm(big, 8, 1 << 48, 0, big, 8, 32, 0, 8, 4, 8, 0, None, None, None, None, 0, None, None, 0, 1e-5, out, None, None) == SHAPE
+    assert lib.pp_top_logits(big, 1 << 48, 0, 8, 100, 5, 1.0, out, p(1 << 41), p(1 << 42), None) == SHAPE
+    assert lib.pp_top_logits(big, 100, 0, (1 << 27) + 1, 100, 5, 1.0, out, p(1 << 41), p(1 << 42), None) == SHAPE
+    assert lib.pp_distill_backward(p(256), 1 << 48, big, 100, 0, 8, 100, p(1 << 41), p(1 << 42), 0, p(1 << 43), 5, None, None, 1.0, 0.5, out, None) == SHAPE
+
+
 def test_bindings_refuse_what_is_not_on_the_gpu():
     s, at = torch.zeros(3, 10), torch.zeros(3, 2, dtype=torch.int32)
     for call in (lambda: distill.pp_top_logits(s, 2), lambda: distill.pp_distill(s, s[:, :2], at), lambda: distill.pp_distill_backward(s[:, 0], s, s, s, at),
