@@ -129,7 +129,7 @@ def build(force: bool = False, verbose: bool = False, extra_nvcc=(), binding: Op
             glue.result()
             lib = os.path.join(torch_dir, "lib")
             parts[1].link(run, ["g++", "-shared", "-o", None, _obj("binding.cpp"), "-L", BUILD, "-l:libpatconv.so", "-L", lib, "-lc10",
-                                "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN:" + lib])
+                                "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", "-Wl,-rpath,$ORIGIN:" + lib])
     return LIB
 
 

@@ -7,6 +7,7 @@
 // documentation, and return the entry point's status where that is not 0; arguments that are no fit raise
 // ValueError.  Tensors are only looked at and allocated: no operator of torch runs here.
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/custom_function.h>
@@ -48,6 +49,11 @@ double real(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) throw Raised();
     return v;
+}
+
+// A new tensor on x's device, by the allocator without the dispatcher: a backward pass of block norm makes nine.
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& x, at::MemoryFormat order = at::MemoryFormat::Contiguous) {
+    return at::Tensor(at::detail::empty_cuda(shape, type, x.device(), order));
 }
 
 int dtype_of(const at::Tensor& t) {         // pp_dtype, or -1
@@ -122,7 +128,7 @@ const float* values(PyObject* o, int64_t count, const at::Tensor& x, const char*
 
 at::Tensor like(const at::Tensor& x, PyObject* o) {
     const at::Tensor* out = maybe(o, "out");
-    if (!out) return at::empty(x.sizes(), x.options().requires_grad(false), at::MemoryFormat::ChannelsLast);
+    if (!out) return fresh(x.sizes(), x.scalar_type(), x, at::MemoryFormat::ChannelsLast);
     if (out->sizes() != x.sizes() || out->scalar_type() != x.scalar_type() || out->device() != x.device() ||
         !out->is_contiguous(at::MemoryFormat::ChannelsLast))
         refuse("out must be a dense channels-last tensor of x's shape, type and device");
@@ -144,14 +150,14 @@ struct Workspace {
         if (pp_group_norm_workspace_size(dtype, (int)x.size(0), pixels, (int)x.size(1), groups, backward, &bytes) != PP_OK)
             return;                          // the call says what is wrong
         if (bytes) {
-            held = at::empty({(int64_t)bytes}, x.options().dtype(at::kByte).requires_grad(false));
+            held = fresh({(int64_t)bytes}, at::kByte, x);
             p = held.data_ptr();
         }
     }
 };
 
 at::Tensor floats(at::IntArrayRef shape, const at::Tensor& x) {
-    return at::empty(shape, x.options().dtype(at::kFloat).requires_grad(false));
+    return fresh(shape, at::kFloat, x);
 }
 
 PyObject* triple(const at::Tensor& a, const at::Tensor& b, const at::Tensor& c) {
@@ -238,7 +244,7 @@ Layout alike(const at::Tensor& t, const at::Tensor& x, at::ScalarType type, cons
 // a dense channels-last result like x, of a type: the one that is given, or a new one
 at::Tensor result(PyObject* o, const at::Tensor& x, at::ScalarType type, const char* what) {
     const at::Tensor* out = maybe(o, what);
-    if (!out) return at::empty(x.sizes(), x.options().dtype(type).requires_grad(false), at::MemoryFormat::ChannelsLast);
+    if (!out) return fresh(x.sizes(), type, x, at::MemoryFormat::ChannelsLast);
     if (out->sizes() != x.sizes() || out->scalar_type() != type || out->device() != x.device() ||
         !out->is_contiguous(at::MemoryFormat::ChannelsLast))
         refuse(std::string(what) + " must be a dense channels-last tensor of the stream's shape and device, " + c10::toString(type));
@@ -338,7 +344,7 @@ PyObject* block_norm_backward(PyObject* const* a, Py_ssize_t n_args) {
         space = w->data_ptr();
         bytes = w->nbytes();
     } else if (pp_block_norm_workspace_size(n, pixels, c, &bytes) == PP_OK && bytes) {
-        held = at::empty({(int64_t)bytes}, h.options().dtype(at::kByte).requires_grad(false));
+        held = fresh({(int64_t)bytes}, at::kByte, h);
         space = held.data_ptr();
     }
     const int e = pp_block_norm_backward(
@@ -378,8 +384,8 @@ PyObject* top_logits(PyObject* const* a, Py_ssize_t n_args) {
     if (k < 1 || k > PP_MOST_KEPT || k > s.size(1))
         refuse("k must be 1 to " + std::to_string(PP_MOST_KEPT) + " and no more than the classes");
     const Place at(s.device(), a[3]);
-    const at::Tensor values = at::empty({s.size(0), k}, s.options().requires_grad(false)), rest = floats({s.size(0)}, s);
-    const at::Tensor indices = at::empty({s.size(0), k}, s.options().dtype(at::kInt).requires_grad(false));
+    const at::Tensor values = fresh({s.size(0), k}, s.scalar_type(), s), rest = floats({s.size(0)}, s);
+    const at::Tensor indices = fresh({s.size(0), k}, at::kInt, s);
     const int e = pp_top_logits(s.const_data_ptr(), stride, dtype_of(s), s.size(0), s.size(1), (int)k, temperature, values.data_ptr(),
                                 indices.data_ptr<int>(), rest.data_ptr<float>(), at.stream);
     return e ? PyLong_FromLong(e) : triple(values, indices, rest);
@@ -443,7 +449,7 @@ PyObject* distill_backward(PyObject* const* a, Py_ssize_t n_args) {
     const at::Tensor* given = maybe(a[9], "out");
     if (given && (given->sizes() != s.sizes() || given->scalar_type() != s.scalar_type() || given->device() != s.device() || !given->is_contiguous()))
         refuse("out must be a contiguous tensor of the logits' shape, type and device");
-    const at::Tensor out = given ? *given : at::empty(s.sizes(), s.options().requires_grad(false));
+    const at::Tensor out = given ? *given : fresh(s.sizes(), s.scalar_type(), s);
     const int e = pp_distill_backward(d.const_data_ptr<float>(), n > 1 ? d.stride(0) : 0, s.const_data_ptr(), stride, dtype_of(s), n, s.size(1),
                                       stats.const_data_ptr<float>(), t.values->const_data_ptr(), dtype_of(*t.values),
                                       t.indices->const_data_ptr<int>(), t.kept(), t.rest_ptr(), t.labels_ptr(), t.temperature, t.alpha,
@@ -476,7 +482,7 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
         const auto saved = ctx->get_saved_variables();
         const at::Tensor &s = saved[0], &stats = saved[1], &values = saved[2], &indices = saved[3], &rest = saved[4], &labels = saved[5];
         const c10::cuda::CUDAGuard guard(s.device());
-        const at::Tensor d = grads[0].to(at::kFloat), out = at::empty(s.sizes(), s.options().requires_grad(false));
+        const at::Tensor d = grads[0].to(at::kFloat), out = fresh(s.sizes(), s.scalar_type(), s);
         const int64_t n = s.size(0);
         const int e = pp_distill_backward(d.const_data_ptr<float>(), n > 1 ? d.stride(0) : 0, s.const_data_ptr(), n > 1 ? s.stride(0) : s.size(1),
                                           dtype_of(s), n, s.size(1), stats.const_data_ptr<float>(), values.const_data_ptr(), dtype_of(values),
