@@ -27,6 +27,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kWide = 128;            // threads of a CTA that has a row, or a part of one
 constexpr int kRowsOfCta = 4;         // rows of a CTA whose warps have one each
+constexpr int kStep = 1024;           // vectors that a CTA asks for ahead of its reading where it does not ask for its whole row
 constexpr int kMostOfWarp = 1024;     // 16-byte vectors of a warp's row at most
 
 constexpr int kBitsOfWarp = kMostOfWarp / 32;        // words of a warp's row: a bit a vector
@@ -91,8 +92,8 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     // the ends of a row that are no whole vectors are taken by themselves
     const int from = first < last && !r.whole(first) ? first + 1 : first;
     const int to = last > from && !r.whole(last - 1) ? last - 1 : last;
-    // the logits are asked for at once, whatever the teacher's entries then say: all on their way to L2, the first ones here
-    if (N > 32 && threadIdx.x == 0) r.prefetch(first, last);
+    // the logits are asked for at once, whatever the teacher's entries then say: on their way to L2, the first ones here
+    if (N > 32 && threadIdx.x == 0) r.prefetch(first, a.stepwise ? min(last, first + kStep) : last);
     int v = from + g.lane;
     Vec<T, W> batch[U];
     const bool early = v + (U - 1) * N < to;
@@ -183,6 +184,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     // the next ones are asked for before these are taken
     const int batches = v < to ? ((to - v + N - 1) / N) / U : 0;
     for (int i = 0; i < batches; i += 2, v += 2 * U * N) {
+        if (N > 32 && threadIdx.x == 0 && a.stepwise && i * U * N % kStep == 0 && v + kStep < last) r.prefetch(v + kStep, min(last, v + 2 * kStep));
         Vec<T, W> next[U];
         if (i + 1 < batches)
 #pragma unroll
@@ -367,6 +369,9 @@ cudaError_t launch(DistillArgs a, cudaStream_t st) {
     // 16 by four; but 400 x 65536 bf16 15.9 by one, 16.9 by two, 20.8 by four)
     while (a.parts < 8 && (int64_t)a.rows * a.parts < 3 * kSMs && a.classes / a.parts >= 4096 * 2) a.parts *= 2;
     const int each = (vectors + a.parts - 1) / a.parts;
+    // Whole rows on their way to L2 are good as long as L2 holds those of all CTAs under way (8192 x 10000 fp32: 73 us, step by step 75; 6 x
+    // 200001 18.2 and 19.5), and crowd one another out beyond that (2000 x 131072 bf16: 130 and 93; 4096 x 32768 65 and 61).
+    a.stepwise = std::min((int64_t)a.rows, 8 * (int64_t)kSMs / a.parts) * vectors * 16 > (64 << 20);
     const size_t smem = REST ? ((size_t)each + 31) / 32 * 4 : 0;    // at most 32 KB
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.rows * (unsigned)a.parts);

@@ -44,6 +44,7 @@ struct DistillArgs {
     int64_t dloss_stride;
     void* ds;                         // dense [rows][classes]
     int parts;                        // CTAs of a row
+    bool stepwise;                    // whether a row is asked for step by step, not whole
 };
 
 cudaError_t distill_forward(const DistillArgs& a, int dtype, cudaStream_t st);
