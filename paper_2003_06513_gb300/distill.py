@@ -62,5 +62,6 @@ def pp_distill_backward(dloss: torch.Tensor, logits: torch.Tensor, stats: torch.
 def distill_loss(logits: torch.Tensor, top: TopLogits, labels: Optional[torch.Tensor] = None, temperature: float = 1.0,
                  alpha: float = 0.5) -> torch.Tensor:
     """Losses of the rows, float32 [rows], as one operation that is differentiable by the logits (once), on the current stream.
-    The operation is native on both sides (csrc/binding.cpp)."""
+    The operation is native on both sides (csrc/binding.cpp).  Captured into a graph, its leaves are such that no living eager
+    graph was built from."""
     return _done("pp_distill", _lib.binding().distill_loss(logits, top.values, top.indices, top.rest, labels, temperature, alpha))

@@ -194,6 +194,7 @@ def block_norm(x: torch.Tensor, block: Optional[torch.Tensor], post: str = "rms"
                post_bias: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                gate: Optional[torch.Tensor] = None, pre: str = "rms", weight: Optional[torch.Tensor] = None,
                bias: Optional[torch.Tensor] = None, act: str = "none", eps: float = 1e-5):
-    """(h, y) of ``pp_block_norm`` as one differentiable operation, on the current stream."""
+    """(h, y) of ``pp_block_norm`` as one differentiable operation, on the current stream.  Captured into a graph, its leaves
+    are such that no living eager graph was built from."""
     got = _BlockNorm.apply(x, block, post_weight, post_bias, scale, gate, weight, bias, post, pre, act, eps)
     return got if block is not None else (x, got)
