@@ -53,65 +53,67 @@ int row_threads(int C) {
 
 constexpr int kJoinChannels = 32, kJoinParts = 32;
 
-// Sums of the CTAs' parts: blockIdx.y below kBlockSums one of the sums over all rows, else the gate's gradient of a
-// sample that several CTAs have parts of.
+// The gate's gradient of sample y has parts of several CTAs: adds those from part `k0` on, every step-th, of channel c.  With more
+// samples than CTAs y is a CTA, and the sample the one that begins in it and ends in another.  Whether there is one.
+struct GateParts {
+    const float* own;                                 // the first part: the CTA's only, or the second of its two places
+    const float* from;                                // and the others
+    float* to;
+    int n;
+    __device__ __forceinline__ bool find(const BlockArgs& a, int64_t y) {
+        const int64_t i = a.N <= a.ctas ? y * a.pixels / a.stretch : y;
+        const int64_t begin = i * a.stretch, end = begin + a.stretch;
+        if (end >= a.rows) return false;              // the last CTA's samples end there
+        const int64_t sample = a.N <= a.ctas ? y : (end - 1) / a.pixels, first = sample * a.pixels, last = first + a.pixels;
+        if (last <= end || first < begin) return false;       // it ends with this CTA, or began in an earlier one
+        own = a.gates + (i * 2 + (first > begin)) * a.C;
+        from = a.gates + (i + 1) * 2 * a.C;           // of those the sample is the first
+        to = a.dgate + sample * a.C;
+        n = (int)((last - 1) / a.stretch - i);
+        return true;
+    }
+};
+// samples of a CTA of the join: one, whose parts its threads share, or, where a sample has few parts, one for each of its rows of
+// threads (32 x 2048 x 7 x 7, eight parts: 23 us by CTAs of their own; but 32 x 24 x 112 x 112, 19 parts, takes 4 us more so)
+constexpr int kFewParts = 10;
+__host__ __device__ inline int samples_of_join(const BlockArgs& a) { return a.pixels <= (int64_t)kFewParts * a.stretch ? kJoinParts : 1; }
+
+// Sums of the CTAs' parts: blockIdx.y below kBlockSums one of the sums over all rows, else the gate's gradients of samples that
+// several CTAs have parts of.
 __global__ void __launch_bounds__(kJoinChannels* kJoinParts) block_sums(BlockArgs a) {
     asm volatile("griddepcontrol.wait;" ::: "memory");        // its launch overlaps the end of the kernel before it
     __shared__ float parts[kJoinParts][kJoinChannels + 1];
     const int c = blockIdx.x * kJoinChannels + threadIdx.x % kJoinChannels, part = threadIdx.x / kJoinChannels;
-    const float* from;
-    float* to;
-    int64_t step;
-    int n;
+    const int64_t step = (blockIdx.y < kBlockSums ? kBlockSums : 2) * (int64_t)a.C;
+    GateParts gate;
+    float s = 0;
     if (blockIdx.y < kBlockSums) {
         float* const all[kBlockSums] = {a.dweight, a.dbias, a.dpost_weight, a.dpost_bias, a.dscale};
-        to = all[blockIdx.y];
-        if (!to) return;
-        from = a.sums + (int64_t)blockIdx.y * a.C;
-        step = (int64_t)kBlockSums * a.C;
-        n = a.ctas;
-    } else {
-        // of N samples, or of the last one of each CTA where those are fewer: the one that begins in CTA i and ends in another
-        const int64_t y = blockIdx.y - kBlockSums, i = a.N <= a.ctas ? y * a.pixels / a.stretch : y;
-        const int64_t begin = i * a.stretch, end = begin + a.stretch;
-        if (end >= a.rows) return;                    // the last CTA's samples end there
-        const int64_t sample = a.N <= a.ctas ? y : (end - 1) / a.pixels, first = sample * a.pixels, last = first + a.pixels;
-        if (last <= end || first < begin) return;     // it ends with this CTA, or began in an earlier one
-        const int64_t until = (last - 1) / a.stretch;
-        // its first part is the CTA's last, or its only, segment; in the others it is the first one
-        to = a.dgate + sample * a.C;
-        from = a.gates + i * 2 * a.C;
-        step = 2 * (int64_t)a.C;
-        n = (int)(until - i) + 1;
-        float own = 0;
-        if (c < a.C && first > begin) {               // (part 0 of the second of its two places)
-            if (part == 0) own = from[a.C + c];
-        } else if (c < a.C && part == 0) {
-            own = from[c];
-        }
-        from += step;
-        --n;
-        float s = own;
-        if (c < a.C)
-            for (int k = part; k < n; k += kJoinParts) s += from[k * step + c];
-        parts[part][threadIdx.x % kJoinChannels] = s;
-        __syncthreads();
-        if (part || c >= a.C) return;
-        s = 0;
-        for (int p = 0; p < kJoinParts; ++p) s += parts[p][threadIdx.x];
-        to[c] = s;
+        gate.to = all[blockIdx.y];
+        if (!gate.to) return;
+        gate.from = a.sums + (int64_t)blockIdx.y * a.C;
+        gate.n = a.ctas;
+    } else if (samples_of_join(a) > 1) {
+        const int64_t y = (int64_t)(blockIdx.y - kBlockSums) * kJoinParts + part;
+        if (y >= min(a.N, a.ctas) || c >= a.C || !gate.find(a, y)) return;
+        s = gate.own[c];
+#pragma unroll 8
+        for (int k = 0; k < gate.n; ++k) s += gate.from[k * step + c];
+        gate.to[c] = s;
         return;
+    } else {
+        if (!gate.find(a, blockIdx.y - kBlockSums)) return;
+        if (c < a.C && part == 0) s = gate.own[c];
     }
-    float s = 0;
     if (c < a.C)
 #pragma unroll 8
-        for (int k = part; k < n; k += kJoinParts) s += from[k * step + c];
+        for (int k = part; k < gate.n; k += kJoinParts) s += gate.from[k * step + c];
     parts[part][threadIdx.x % kJoinChannels] = s;
     __syncthreads();
     if (part || c >= a.C) return;
     s = 0;
     for (int p = 0; p < kJoinParts; ++p) s += parts[p][threadIdx.x];
-    to[c] = s;
+    gate.to[c] = s;
 }
 
 int size_of(int dtype) { return dtype == PP_F32 ? 4 : 2; }
@@ -241,7 +243,7 @@ int block_ctas(int64_t rows, int C, int64_t* stretch) {
 
 cudaError_t block_join(const BlockArgs& a, cudaStream_t st) {
     if (!a.dweight && !a.dbias && !a.dpost_weight && !a.dpost_bias && !a.dscale && !a.dgate) return cudaSuccess;
-    const dim3 grid((a.C + kJoinChannels - 1) / kJoinChannels, kBlockSums + (a.dgate ? std::min(a.N, a.ctas) : 0));
+    const dim3 grid((a.C + kJoinChannels - 1) / kJoinChannels, kBlockSums + (a.dgate ? (std::min(a.N, a.ctas) + samples_of_join(a) - 1) / samples_of_join(a) : 0));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(kJoinChannels * kJoinParts);

@@ -260,11 +260,14 @@ struct RowSum {
 #pragma unroll
                 for (int k = 0; k < K; ++k) mine[threadIdx.x / 32 * K + k] = s[k];
             __syncthreads();
+            Vec<float, K> of = load<float, K>(mine);
 #pragma unroll
-            for (int k = 0; k < K; ++k) s[k] = mine[k];
-            for (int w = 1; w < threads / 32; ++w)
+            for (int k = 0; k < K; ++k) s[k] = of.v[k];
+            for (int w = 1; w < threads / 32; ++w) {
+                of = load<float, K>(mine + w * K);
 #pragma unroll
-                for (int k = 0; k < K; ++k) s[k] += mine[w * K + k];
+                for (int k = 0; k < K; ++k) s[k] += of.v[k];
+            }
         }
     }
     // near the mean of a row: of a short row the mean of its first thread's values, of a long one the mean but for its rounding
@@ -372,7 +375,7 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockThreads, FORM == k
     const int post = FIXED ? KIND : a.post, pre = FIXED ? KIND : a.pre;
     const bool has_b = FIXED || a.b;
     extern __shared__ __align__(16) char ring[];
-    __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
+    __shared__ __align__(16) float scratch[WIDE ? 128 : 1];
     const int threads = FORM > 0 ? FORM : a.threads;
     const int lane = WIDE ? threadIdx.x : threadIdx.x % threads;
     const int here = WIDE ? 1 : kBlockThreads / threads, mine = WIDE ? 0 : threadIdx.x / threads;
@@ -498,7 +501,7 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
     constexpr bool WIDE = FORM == kLong, DENSE = KIND != kStrided, FIXED = KIND == kRms || KIND == kLayer;
     constexpr int R = kRoundsBack<TX, TB, WIDE>;
     extern __shared__ __align__(16) char ring[];
-    __shared__ __align__(8) float scratch[WIDE ? 128 : 1];
+    __shared__ __align__(16) float scratch[WIDE ? 128 : 1];
     __shared__ float lanes_sum[WIDE ? 1 : 2 * kBlockBackThreads * E];
     const int threads = FORM > 0 ? FORM : a.threads;
     const int lane = WIDE ? threadIdx.x : threadIdx.x % threads;
@@ -730,6 +733,15 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                 }
                 __syncthreads();
             }
+            // (all asked for before the first result is stored: the compiler cannot know that they are not the same)
+            float ga[OWN], sc[OWN], pw[OWN], pb[OWN];
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) {
+                const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x + i * kBlockBackThreads;
+                const bool is = c < a.C;
+                ga[i] = gate && is ? gate[c] : 1.0f, sc[i] = a.scale && is ? a.scale[c] : 1.0f;
+                pw[i] = a.post_weight && is ? a.post_weight[c] : 1.0f, pb[i] = a.post_bias && is ? a.post_bias[c] : 0.0f;
+            }
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
                 const int c = WIDE ? channel<V>(lane, threads, i) : threadIdx.x + i * kBlockBackThreads;
@@ -742,16 +754,15 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
                     const int at = place_in_sums(c);
                     for (int g = 0; g < here; ++g) e += e_all[g * threads * E + at], f += f_all[g * threads * E + at];
                 }
-                const float ga_c = gate ? gate[c] : 1.0f, sc_c = a.scale ? a.scale[c] : 1.0f;
-                const float joined = fmaf(a.post_weight ? a.post_weight[c] : 1.0f, e, a.post_bias ? a.post_bias[c] * f : 0.0f);
-                total(0, i) = fmaf(sc_c * ga_c, e, total(0, i));
-                total(1, i) = fmaf(sc_c * ga_c, f, total(1, i));
-                total(2, i) = fmaf(ga_c, joined, total(2, i));
+                const float joined = fmaf(pw[i], e, a.post_bias ? pb[i] * f : 0.0f);
+                total(0, i) = fmaf(sc[i] * ga[i], e, total(0, i));
+                total(1, i) = fmaf(sc[i] * ga[i], f, total(1, i));
+                total(2, i) = fmaf(ga[i], joined, total(2, i));
                 if (a.dgate) {
                     if (whole)
-                        a.dgate[sample * a.C + c] = sc_c * joined;
+                        a.dgate[sample * a.C + c] = sc[i] * joined;
                     else
-                        a.gates[((int64_t)blockIdx.x * 2 + !first) * a.C + c] = sc_c * joined;
+                        a.gates[((int64_t)blockIdx.x * 2 + !first) * a.C + c] = sc[i] * joined;
                 }
             }
             s_e = s_f = zero;
@@ -808,7 +819,19 @@ cudaError_t forward_rows(const BlockArgs& a, cudaStream_t st) {
     static std::atomic<uint64_t> allowed{0};
     if (const cudaError_t e = allow_shared(block_rows<TX, TB, V, FORM, KIND>, allowed, kRounds * kRound * kMost)) return e;
     const int threads = FORM == kLong ? a.threads : kBlockThreads, here = threads / a.threads;
-    const int most = 152 * (FORM == kLong ? std::max(1, 768 / threads) : 3), rounds = (a.rows + here - 1) / here;
+    int each = 3;                                     // CTAs of an SM: one wave, so of long rows what fits (32 x 512 x 28 x 28 takes 29 us, 40 with a
+    if (FORM == kLong) {                              // sixth of the CTAs left for a second one)
+        static std::atomic<int> fit[16];
+        std::atomic<int>& f = fit[threads / 32 - 1];
+        if (!(each = f.load(std::memory_order_relaxed))) {
+            if (const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, block_rows<TX, TB, V, FORM, KIND>, threads, kRounds * kRound * threads)) {
+                cudaGetLastError();
+                return e;
+            }
+            f = each = std::max(1, each);
+        }
+    }
+    const int most = 152 * each, rounds = (a.rows + here - 1) / here;
     BlockArgs b = a;
     b.stretch = (rounds + most - 1) / most * here;
     block_rows<TX, TB, V, FORM, KIND><<<(a.rows + b.stretch - 1) / b.stretch, threads, kRounds * kRound * threads, st>>>(b);
