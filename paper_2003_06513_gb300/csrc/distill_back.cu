@@ -19,11 +19,23 @@ constexpr int kWide = 256;
 constexpr int kRowsOfCta = 4;
 constexpr int kMostOfWarp = 16384;    // bytes of a warp's row at most
 
-// VEC: the logits and their gradient have their 16-byte boundaries at the same places, and are read and written in such
-// vectors; else value by value.  TWO: both exponentials, else the one at T alone, its factor standing for both.
-template <typename T, bool REST, bool TWO, bool VEC, int N>
+// The 16 bytes at a place `off` bytes beyond a 16-byte boundary, from the two vectors that hold them.
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int off) {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = off & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = off & 4 ? w[i + 1] : w[i];
+    const int bits = off % 4 * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                      __funnelshift_r(w[3], w[4], bits));
+}
+
+// Both are read and written in 16-byte vectors, which begin at the gradient's boundaries.  SHIFT: the logits' boundaries are, or may be,
+// at other places, and a vector is put together from two (1000 x 21841 fp16, rows 21844 apart: 17 us, value by value 31).  TWO: both exponentials, else the one at T alone, its factor standing for both.
+template <typename T, bool REST, bool TWO, bool SHIFT, int N>
 __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(DistillArgs a) {
-    constexpr int W = VEC ? 16 / sizeof(T) : 1, U = VEC ? 2 : 8, P = kPairs<W>;
+    constexpr int W = 16 / sizeof(T), U = 2, P = kPairs<W>;
     __shared__ float scratch[N == 32 ? 1 : 2 * (N / 32) * 8];
     __shared__ int kept_of[N == 32 ? kRowsOfCta : 1][N == 32 ? 32 : kMostKept];
     __shared__ float p_of[N == 32 ? kRowsOfCta : 1][N == 32 ? 32 : kMostKept];
@@ -34,8 +46,10 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
     Group<N> g(scratch);
     const T* s = static_cast<const T*>(a.s) + row * a.stride;
     T* ds = static_cast<T*>(a.ds) + (int64_t)row * a.classes;
-    const Row<T, W> r(s, a.classes);
+    const Row<T, W> r(ds, a.classes);                 // (its places; it is not read)
     T* out = ds - r.pad;                              // place 0 of the gradient
+    const T* in = s - r.pad;                          // and of the logits
+    const int off = SHIFT ? (int)(reinterpret_cast<uintptr_t>(in) % 16) : 0, before = off / (int)sizeof(T);
     const int each = (r.vectors() + a.parts - 1) / a.parts, first = part * each, last = min(r.vectors(), first + each);
     const int from = max(r.pad, first * W), to = min(r.end, last * W);    // this group's places
     int *kept = kept_of[slot];
@@ -118,28 +132,33 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
         for (int i = 0; i < P; ++i) set_pair(y, i, value(pair(v, i)));
         return y;
     };
-    int begin = first, end = last;
-    if (W > 1) {                                      // the ends of a row that are no whole vectors
-        for (int k = 0; k < 2; ++k) {
-            const int v = k ? last - 1 : first;
-            if (last <= first || r.whole(v) || (k && v == first)) continue;
-            if (k)
-                --end;
-            else
-                ++begin;
-            const int place = v * W + g.lane;
-            if (g.lane < W && place >= r.pad && place < r.end) narrow(single(widen(r.base[place])), out[place]);
+    // the ends of a row that are no whole vectors, or whose logits are not in two of them, value by value
+    const auto in_vectors = [&](int v) { return SHIFT ? v * W - before >= r.pad && v * W - before + 2 * W <= r.end : r.whole(v); };
+    const auto vector_at = [&](int v) {
+        if constexpr (SHIFT) {
+            const uint4* p = reinterpret_cast<const uint4*>(in + (int64_t)v * W - before);
+            const uint4 w = shifted(p[0], p[1], off);
+            Vec<T, W> b;
+            memcpy(&b, &w, 16);
+            return b;
+        } else {
+            return load<T, W>(in + (int64_t)v * W);
         }
-    }
+    };
+    int begin = min(first, last), end = last;
+    while (begin < end && !in_vectors(begin)) ++begin;
+    while (end > begin && !in_vectors(end - 1)) --end;
+    for (int place = max(r.pad, first * W) + g.lane; place < min(r.end, begin * W); place += N) narrow(single(widen(in[place])), out[place]);
+    for (int place = max(r.pad, end * W) + g.lane; place < min(r.end, last * W); place += N) narrow(single(widen(in[place])), out[place]);
     int v = begin + g.lane;
     for (; v + (U - 1) * N < end; v += U * N) {
         Vec<T, W> b[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) b[k] = r.at(v + k * N);
+        for (int k = 0; k < U; ++k) b[k] = vector_at(v + k * N);
 #pragma unroll
         for (int k = 0; k < U; ++k) store<T, W>(out + (int64_t)(v + k * N) * W, turn(b[k]));
     }
-    for (; v < end; v += N) store<T, W>(out + (int64_t)v * W, turn(r.at(v)));
+    for (; v < end; v += N) store<T, W>(out + (int64_t)v * W, turn(vector_at(v)));
 
     // the classes with a term of their own
     const bool among = g.any(once && at == label);
@@ -158,13 +177,13 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
     if (labelled && !among && g.lane == 0) narrow(single(x_label) - slope * a.hard, ds[label]);
 }
 
-template <typename T, bool REST, bool TWO, bool VEC>
+template <typename T, bool REST, bool TWO, bool SHIFT>
 cudaError_t launch(DistillArgs a, cudaStream_t st) {
     a.parts = 1;
     // a warp where there are rows enough, or hardly any classes (8192 x 1000 fp32: 10.6 us, by a CTA 29; 8192 x 4000 52 and 54, of bf16 28
     // and 51; 1216 x 4000 fp32 8.5 and 7.8; 512 x 1000 4.6 and 4.7)
     if (a.classes <= kMostOfWarp / (int)sizeof(T) && a.kept <= 32 && (a.rows >= 8 * kSMs || a.classes <= 256)) {
-        distill_slopes<T, REST, TWO, VEC, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, 0, st>>>(a);
+        distill_slopes<T, REST, TWO, SHIFT, 32><<<(a.rows + kRowsOfCta - 1) / kRowsOfCta, 32 * kRowsOfCta, 0, st>>>(a);
     } else {
         // few long rows: several CTAs have one, each its stretch, with nothing to join (6 x 200001 fp32: 32 us by one, 4.9 by 32;
         // 400 x 65536 bf16 16.4 by one, 14.9 by two, 16.2 by four); of very long ones more, as the last CTAs end alone (300 x 1048576
@@ -172,23 +191,23 @@ cudaError_t launch(DistillArgs a, cudaStream_t st) {
         while (a.parts < 64 && (((int64_t)a.rows * a.parts < 4 * kSMs && a.classes / a.parts >= 4096) ||
                                 ((int64_t)a.rows * a.parts < 16 * kSMs && a.classes / a.parts >= 65536)))
             a.parts *= 2;
-        distill_slopes<T, REST, TWO, VEC, kWide><<<(unsigned)a.rows * (unsigned)a.parts, kWide, 0, st>>>(a);
+        distill_slopes<T, REST, TWO, SHIFT, kWide><<<(unsigned)a.rows * (unsigned)a.parts, kWide, 0, st>>>(a);
     }
     return cudaGetLastError();
 }
 
-template <typename T, bool VEC>
+template <typename T, bool SHIFT>
 cudaError_t backward(const DistillArgs& a, cudaStream_t st) {
-    if (a.rest) return a.labels ? launch<T, true, true, VEC>(a, st) : launch<T, true, false, VEC>(a, st);
+    if (a.rest) return a.labels ? launch<T, true, true, SHIFT>(a, st) : launch<T, true, false, SHIFT>(a, st);
     const bool two = a.labels && a.ct != a.c1;
-    return two ? launch<T, false, true, VEC>(a, st) : launch<T, false, false, VEC>(a, st);
+    return two ? launch<T, false, true, SHIFT>(a, st) : launch<T, false, false, SHIFT>(a, st);
 }
 template <typename T>
 cudaError_t backward(const DistillArgs& a, cudaStream_t st) {
     // rows of both lie alike where the first ones and, with more rows, the strides do
     const uintptr_t apart = reinterpret_cast<uintptr_t>(a.s) - reinterpret_cast<uintptr_t>(a.ds);
     const bool alike = apart % 16 == 0 && (a.rows == 1 || (a.stride - a.classes) * (int64_t)sizeof(T) % 16 == 0);
-    return alike ? backward<T, true>(a, st) : backward<T, false>(a, st);
+    return alike ? backward<T, false>(a, st) : backward<T, true>(a, st);
 }
 
 }  // namespace
