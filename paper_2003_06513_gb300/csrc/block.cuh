@@ -326,12 +326,13 @@ __device__ __forceinline__ void centre(Eight& e, float mean, int lane, const Blo
 // From the sums over a row of its values and of their squares -- of a layer norm, of their distances from a value near the
 // mean: v^ = root v + shift.  The first thread's mean is near enough: its square from the mean is at most a thread's
 // share of the row's sum of squares, so that the difference loses at most five bits in rows of 256 channels, and with
-// values in no special order none.  A row of equal values is 0, and one far from zero keeps its spread.
+// values in no special order none.  A row of equal values is 0, and one far from zero keeps its spread.  A row with a NaN is
+// NaN throughout, and so is a layer norm's with an infinity; by its root mean square the rest of that row is 0.
 struct Scaling {
     float root, shift;
     __device__ __forceinline__ Scaling(int kind, float total, float square, const BlockArgs& a) {
         const float left = kind == PP_NORM_LAYER ? total * a.inv_c : 0.0f;
-        root = kind == PP_NORM_NONE ? 1.0f : rsqrtf(fmaxf(fmaf(-left, left, square * a.inv_c), 0.0f) + a.eps);
+        root = kind == PP_NORM_NONE ? 1.0f : rsqrtf(larger(fmaf(-left, left, square * a.inv_c), 0.0f) + a.eps);
         shift = -left * root;
     }
 };
@@ -358,11 +359,7 @@ __device__ __forceinline__ const T* spot_in(const void* p, const Spot& s, int64_
 }
 
 __device__ __forceinline__ float act_of(float z, int act) {
-    if (act == PP_ACT_RELU) {
-        float y;
-        asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(z));
-        return y;
-    }
+    if (act == PP_ACT_RELU) return larger(z, 0.0f);
     if (act == PP_ACT_SILU) return z * approx_rcp(1.0f + approx_exp2(-1.4426950408889634f * z));
     return z;
 }

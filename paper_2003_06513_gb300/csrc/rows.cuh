@@ -124,11 +124,6 @@ __device__ __forceinline__ float power(float x, float m, float c) { return appro
 __device__ __forceinline__ float factor(float a, float m, float c) { return a == kNone ? 0.0f : approx_exp2((a - m) * c); }
 
 // The largest of values as they come, a NaN above all: packed where two share a register.
-__device__ __forceinline__ float larger(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
 template <typename T>
 struct Largest;
 template <>
