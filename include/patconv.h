@@ -461,7 +461,8 @@ int pp_top_logits(const void* logits, int64_t stride, int dtype, int64_t rows, i
  *              labels), the sum of exp((s - m) / T), and, of the classes that are not kept (without `rest`: of all), the
  *              largest logit and the sum of exp((s - it) / T).
  * A row that has neither a label nor a kept logit or rest above -infinity (a padded row) is not read: its loss and stats
- * are 0.  NaN and +infinity in a row that counts give NaN.  0 <= alpha <= 1.  Otherwise as pp_top_logits. */
+ * are 0.  NaN and +infinity in a row that counts give NaN; a part of weight 0 (with alpha 0 the teacher's, with alpha 1 the
+ * label's) takes no part in loss and gradient, whatever it holds.  0 <= alpha <= 1.  Otherwise as pp_top_logits. */
 int pp_distill(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t classes, const void* values,
                int value_type, const int* indices, int kept, const float* rest, const int64_t* labels, double temperature,
                double alpha, float* loss, float* stats, void* stream);

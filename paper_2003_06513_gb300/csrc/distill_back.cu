@@ -80,7 +80,9 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
     const float m = stats[0], z1 = stats[1], zt = stats[2], mo = stats[3], zo = stats[4];
 
     const bool taught = g.any((at >= 0 && u != kNone) || (REST && rest != kNone));
-    if (slope == 0.0f || (!taught && label < 0)) {
+    // a part of weight 0 takes no part, whatever it holds, as in the loss
+    const bool soft = taught && a.soft_slope != 0.0f, hard = label >= 0 && a.hard != 0.0f;
+    if (slope == 0.0f || (!soft && !hard)) {
         for (int i = from + g.lane; i < to; i += N) narrow(0.0f, out[i]);
         return;
     }
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
     float whole[1] = {e};
     g.sum(whole);
     const float e0 = REST ? factor(rest, mu, a.c1) : 0.0f;
-    const float per = taught ? 1.0f / (whole[0] + e0) : 0.0f;
+    const float per = soft ? 1.0f / (whole[0] + e0) : 0.0f;
     if (g.lane < a.kept) p_at[g.lane] = e * per;
     g.sync();
     bool once = owned;
@@ -105,10 +107,10 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
             }
 
     // ds = A 2^((x - m) c1) + B 2^((x - r) ct)
-    const float weight = taught ? slope * a.soft_slope : 0.0f;
-    const float A = label >= 0 ? slope * a.hard / z1 : 0.0f;
+    const float weight = soft ? slope * a.soft_slope : 0.0f;
+    const float A = hard ? slope * a.hard / z1 : 0.0f;
     float B = 0.0f;
-    if (taught) {
+    if (soft) {
         if (REST)
             B = zo == 0.0f ? 0.0f : weight * (factor(mo, m, a.ct) * (zo / zt) - e0 * per) / zo;
         else
@@ -166,10 +168,10 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N) distill_slopes(
     if (once) {
         float y;
         if (REST) {
-            y = taught ? weight * (power(x, m, a.ct) / zt - p) : 0.0f;
-            if (label >= 0) y += A * power(x, m, a.c1);
+            y = soft ? weight * (power(x, m, a.ct) / zt - p) : 0.0f;
+            if (hard) y += A * power(x, m, a.c1);
         } else {
-            y = single(x) - weight * p;
+            y = single(x) - (soft ? weight * p : 0.0f);
         }
         if (at == label) y -= slope * a.hard;
         narrow(y, ds[at]);
