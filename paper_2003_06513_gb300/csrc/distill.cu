@@ -11,6 +11,11 @@
 // to the thread that has that class of the teacher's.  A thread keeps a running maximum and the sums below it, so that the
 // row is read once; the kept logits themselves join at the end.
 //
+// The divergence is summed as sum of p f(delta), f(delta) = e^delta - 1 - delta and delta = log q - log p, whose terms are all positive and
+// exact where student and teacher agree; its logarithms by themselves would cancel there.  Without `rest` that also takes
+// 1 - sum q_k, the mass of the classes that are not kept: rows whose divergence is small beside its logarithms are read a
+// second time for it, the others' logarithms are summed as they stand (8192 x 32768 bf16: 89 us, 87.5 without the choice).
+//
 // What bounds it is memory, a row is read and next to nothing written, and issued instructions (68 % of the slots).  8192 x 32768 bf16 with 64 kept, labels and T = 2 takes 109
 // us, 4.9 TB/s, of 80 at a copy's rate; what is left is the rows' fixed work, the teacher's entries and the join.  The kept logits
 // gathered before the row took 118 us; without the exponential's square, the prefetch and the batches a thread has under way 153.
@@ -76,6 +81,8 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     __shared__ __align__(16) int places[N == 32 ? kRowsOfCta : 1][kEntries];
     __shared__ float teacher[N == 32 ? kRowsOfCta : 1][kEntries], student[N == 32 ? kRowsOfCta : 1][kEntries];
     __shared__ bool before[N == 32 ? kRowsOfCta : 1][kEntries];
+    __shared__ unsigned long long whole_of[kWarps];   // the warps' shares of a second reading
+    __shared__ float again_from;                      // what it is relative to, NaN: there is none
     const int slot = N == 32 ? threadIdx.x / 32 : 0;
     const int part = N == 32 ? 0 : blockIdx.x % a.parts;
     const int row = N == 32 ? blockIdx.x * kRowsOfCta + slot : blockIdx.x / a.parts;
@@ -242,6 +249,33 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
         came[k] = again;
     }
 
+    // A second reading of the whole row by this CTA's threads: a warp's sum of exp((s - m) / T) in units of 2^-52.  Of integers the kept
+    // classes' can be subtracted, and nothing is lost; a row has 2^20 classes of 2^-53 each to lose by rounding, 1e-10.
+    const auto unit = [&](float x, float m) { return __float2ull_rn(power(x, m, a.ct) * 0x1p52f); };
+    const auto read_again = [&](float m) {
+        unsigned long long n = 0;
+        for (int v = g.lane; v < r.vectors(); v += N) {
+            const Vec<T, W> b = r.some(v);
+#pragma unroll
+            for (int i = 0; i < W; ++i) n += unit(widen(b.v[i]), m);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+        return n;
+    };
+    // the first warp and the others come to it from different places
+    const auto meet = [] { asm volatile("barrier.sync 1, %0;" ::"n"(N) : "memory"); };
+    const auto help = [&] {
+        if constexpr (!REST && N > 32) {
+            meet();
+            const float from = again_from;
+            if (from != from) return;
+            const unsigned long long n = read_again(from);
+            if (threadIdx.x % 32 == 0) whole_of[threadIdx.x / 32] = n;
+            meet();
+        }
+    };
+
     // the warps' sums, and from here on one warp
     const int lane = threadIdx.x % 32, warp = N == 32 ? 0 : threadIdx.x / 32;
     Group<32> one(nullptr);
@@ -268,7 +302,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     } else {
         if (lane == 0) sums[0][warp][0] = m, sums[0][warp][1] = sum_t, sums[0][warp][2] = sum_1;
         __syncthreads();
-        if (a.parts == 1 && warp) return;
+        if (a.parts == 1 && warp) return help();
         joined(sums[0], kWarps);
         if (a.parts > 1) {                            // the parts' sums, in the first CTA of the cluster
             cg::cluster_group cluster = cg::this_cluster();
@@ -278,7 +312,8 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
                 to0[0] = m, to0[1] = sum_t, to0[2] = sum_1;
             }
             cluster.sync();
-            if (part || warp) return;
+            if (part) return;
+            if (warp) return help();
             joined(parts, a.parts);
         }
     }
@@ -286,7 +321,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     for (int k = lane; k < a.kept; k += 32) top[0] = fmaxf(top[0], us[k]), top[1] = fmaxf(top[1], xs[k]);
     one.max(top);
     const float mu = reference(top[0]), mx = reference(top[1]);
-    float total[4] = {0, 0, 0, 0};                    // of the teacher's masses; of the kept classes' at T and at 1; of p (log p - log q)
+    float total[4] = {0, 0, 0, 0};                    // of the teacher's masses; of the kept classes' at T and at 1, or of the logarithms' sizes; of p (log p - log q)
     for (int k = lane; k < a.kept; k += 32) {
         if (kept[k] < 0) continue;
         const float u = us[k], x = xs[k], e = power(u, mu, a.c1);
@@ -295,7 +330,11 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
             total[1] += power(x, mx, a.ct);
             if (HARD) total[2] += power(x, mx, a.c1);
         }
-        if (!REST && e != 0.0f) total[3] += e * ((u - mu) - (x - mx) * a.inv_t);
+        if (!REST && e != 0.0f) {
+            const float log_p = u - mu, log_q = (x - mx) * a.inv_t;
+            total[1] -= e * (log_p + log_q);
+            total[3] += e * (log_p - log_q);
+        }
     }
     one.sum(total);
     const float other = m, other_t = sum_t;           // without `rest` the classes seen are all there are
@@ -309,18 +348,16 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     if (!HARD) sum_1 = sum_t;
     float loss = 0;
     const bool weighed = taught && a.soft_loss != 0.0f;     // (no weight takes no part, an infinite one neither)
+    const auto term = [](float p, float q, float delta, bool with_q) {     // p f(delta) = q - p - p delta
+        if (p == 0.0f) return with_q ? q : 0.0f;
+        if (with_q && fabsf(delta) < 0.25f)           // (e^delta - 1 - delta) / (delta^2 / 2) by its series, to delta^7 / 181440
+            return p * delta * delta * fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, 1.0f / 40320, 1.0f / 5040), 1.0f / 720),
+                                                                               1.0f / 120), 1.0f / 24), 1.0f / 6), 0.5f);
+        return (with_q ? q : 0.0f) - fmaf(p, delta, p);
+    };
     if (REST && weighed) {
-        // Both sides are whole distributions over the kept classes and the others: sum p (log p - log q) is the sum of
-        // q - p - p delta, delta = log q - log p, whose terms are all positive, p delta^2 / 2 for a small delta; summed as they stand
-        // the logarithms would cancel where student and teacher agree.
+        // both sides are whole distributions over the kept classes and the others
         const float e0 = factor(rest, mu, a.c1), whole = total[0] + e0, per_t = 1.0f / sum_t, level = logf(sum_t / whole);
-        const auto term = [](float p, float q, float delta, bool with_q) {
-            if (p == 0.0f) return with_q ? q : 0.0f;
-            if (with_q && fabsf(delta) < 0.25f)       // (e^delta - 1 - delta) / (delta^2 / 2) by its series, to delta^7 / 181440
-                return p * delta * delta * fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, fmaf(delta, 1.0f / 40320, 1.0f / 5040), 1.0f / 720),
-                                                                                   1.0f / 120), 1.0f / 24), 1.0f / 6), 0.5f);
-            return (with_q ? q : 0.0f) - fmaf(p, delta, p);
-        };
         float kl[1] = {0};
         for (int k = lane; k < a.kept; k += 32)
             if (kept[k] >= 0) {
@@ -338,11 +375,42 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
         one.sum(kl);
         loss = a.soft_loss * kl[0];
     }
-    if (lane) return;
-    if (!REST && weighed) {
-        const float whole = total[0], d = fmaf(whole, (m - mx) * a.inv_t, total[3]);
-        loss = a.soft_loss * (d / whole - logf(whole) + logf(sum_t));
+    if constexpr (!REST) {
+        // As its logarithms stand the divergence is off by some 64 roundings, 2^-18, of 1 and their size; where it is below 2^-6 of that it is
+        // summed by its positive terms, sum p f(delta) + 1 - sum q over the teacher's entries.  (Where Z_T is above 1024 the kept
+        // classes have a quarter at most, and the divergence is no less than log 4: the integers' sums stay below 2^63.)
+        bool again = false;
+        if (weighed) {
+            const float whole = total[0], kl = fmaf(whole, (m - mx) * a.inv_t, total[3]) / whole - logf(whole) + logf(sum_t);
+            again = sum_t <= 1024.0f && kl < 0x1p-6f * (1.0f + total[1] / whole);
+            loss = a.soft_loss * kl;
+        }
+        if constexpr (N > 32) {
+            if (lane == 0) again_from = again ? m : NAN;
+            meet();
+        }
+        if (again) {
+            unsigned long long left = read_again(m);
+            if constexpr (N > 32) {
+                meet();
+                for (int w = 1; w < kWarps; ++w) left += whole_of[w];
+            }
+            const float whole = total[0], per_t = 1.0f / sum_t, level = logf(sum_t / whole);
+            float kl[1] = {0};
+            unsigned long long own = 0;
+            for (int k = lane; k < a.kept; k += 32) {
+                const float u = us[k], x = xs[k], p = kept[k] < 0 ? 0.0f : power(u, mu, a.c1) / whole;
+                if (p == 0.0f) continue;
+                kl[0] += term(p, power(x, m, a.ct) * per_t, (x - m) * a.inv_t - (u - mu) - level, true);
+                own += unit(x, m);
+            }
+            one.sum(kl);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
+            loss = a.soft_loss * fmaf((float)(long long)(left - own) * 0x1p-52f, per_t, kl[0]);
+        }
     }
+    if (lane) return;
     if (label >= 0 && a.hard != 0.0f) loss += a.hard * (logf(sum_1) - (widen(s[label]) - m));
     a.loss[row] = loss;
     float* out = a.stats + (int64_t)row * 5;
