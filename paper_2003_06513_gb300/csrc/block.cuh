@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(FORM == kLong ? 512 : kBlockBackThreads, FORM 
     uint32_t offset;
     const auto enter = [&](int from) {
         start = at_row(from, a);
-        if (a.gate) to = min(end, from + (int)a.pixels - start.pixel);
+        if (a.gate) to = min(end, from - start.pixel + (int)a.pixels);     // (a row of the sample plus its pixels may pass 2^31)
         offset = (uint32_t)((from - begin + mine) * a.C + lane * V);
         for (int k = 0; k < R - 1; ++k) ask(from + k * here, to, offset + k * stride, k);
     };

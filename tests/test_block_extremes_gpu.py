@@ -81,3 +81,28 @@ def test_a_value_that_is_not_finite(c, post, pre, bad):
                 for a in spoilt[1:2] if where == "block" else spoilt[::2]:
                     a[1, channel, 2, 1] = BAD[bad]
                 _check(shape, dtype, stream, post, pre, act, *spoilt, dh, dy, par)
+
+
+def test_rows_up_to_the_limit():
+    """2.13e9 pixels of one channel in two samples with a gate: the second one's rows plus its pixels pass 2^31.  Compared with itself alone;
+    its sums, of some 27 thousand positive terms a thread, are off by as many roundings at most on either side."""
+    n, h, w = 2, 35500, 30000
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    assert n * h * w < 2 ** 31 - 2 ** 24 < n * h * w + h * w
+
+    def values(seed):
+        t = torch.empty((n, h, w, 1), dtype=torch.float16, device="cuda")
+        return t.uniform_(0.5, 2.0, generator=torch.Generator("cuda").manual_seed(seed)).permute(0, 3, 1, 2)
+
+    x, b, dh, dy = (values(seed) for seed in range(4))
+    gate, scale = torch.tensor([[0.7], [0.4]], device="cuda"), torch.ones(1, device="cuda")
+    kinds = {"post": "rms", "pre": "rms", "scale": scale, "act": "relu"}
+    out_h, y = norm.pp_block_norm(x, b, gate=gate, **kinds)
+    h1, y1 = norm.pp_block_norm(x[1:], b[1:], gate=gate[1:], **kinds)
+    assert torch.equal(out_h[1:], h1) and torch.equal(y[1:], y1)
+    del y, y1, x
+    g = norm.pp_block_norm_backward(dh, dy, out_h, b, gate=gate, **kinds)
+    g1 = norm.pp_block_norm_backward(dh[1:], dy[1:], h1, b[1:], gate=gate[1:], **kinds)
+    assert torch.equal(g.dx[1:], g1.dx) and torch.equal(g.dblock[1:], g1.dblock)
+    assert abs(float(g.dgate[1]) - float(g1.dgate[0])) <= 2 * 27000 * 2.0 ** -24 * float(g1.dgate[0])
