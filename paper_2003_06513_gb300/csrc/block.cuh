@@ -44,18 +44,19 @@ struct Raw {                                          // as it is read
 // is under way costs no registers.  There is no copy of two bytes: single halves are read when they are used.
 template <typename T, int V>
 struct Ahead {
-    static constexpr int S = sizeof(T) * V > 16 ? 16 : sizeof(T) * V, P = E * (int)sizeof(T) / S;
+    static_assert(sizeof(T) * V <= 16);
+    static constexpr int S = sizeof(T) * V, P = E / V;
     static constexpr bool kAsync = S >= 4;
     static constexpr int kBytes = kAsync ? E * (int)sizeof(T) : 0;       // of a thread and round
     // channels from the thread's first one to piece k
-    static __device__ __forceinline__ int apart(int threads, int k) { return sizeof(T) * V > 16 ? k * (S / (int)sizeof(T)) : k * threads * V; }
+    static __device__ __forceinline__ int apart(int threads, int k) { return k * threads * V; }
     // the thread's own channels from `mine` on, those that `live(k)` says are there; what is not copied becomes 0
     template <typename Live>
     static __device__ __forceinline__ void ask(uint32_t place, const T* mine, int threads, Live&& live) {
         if constexpr (kAsync) {
 #pragma unroll
             for (int k = 0; k < P; ++k) {
-                const bool wanted = live(sizeof(T) * V > 16 ? 0 : k);
+                const bool wanted = live(k);
                 const T* from = wanted ? mine + apart(threads, k) : mine;
                 const uint32_t to = place + (k * blockDim.x + threadIdx.x) * S;
                 const int n = wanted ? S : 0;
@@ -154,16 +155,7 @@ __device__ __forceinline__ void put(T* mine, const Raw<T, V>& r, int threads, Li
 #pragma unroll
     for (int j = 0; j < E / V; ++j) {
         if (!live(j)) continue;
-        T* p = mine + j * threads * V;
-        if constexpr (sizeof(T) * V > 16) {
-            float4 lo, hi;
-            memcpy(&lo, &r.v[j], 16);
-            memcpy(&hi, &r.v[j].v[4], 16);
-            __stcs(reinterpret_cast<float4*>(p), lo);
-            __stcs(reinterpret_cast<float4*>(p) + 1, hi);
-        } else {
-            store<T, V>(p, r.v[j]);
-        }
+        store<T, V>(mine + j * threads * V, r.v[j]);
     }
 }
 // a parameter's values, `otherwise` where there is none, and beyond the row 0
