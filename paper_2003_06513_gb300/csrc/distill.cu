@@ -14,7 +14,8 @@
 // The divergence is summed as sum of p f(delta), f(delta) = e^delta - 1 - delta and delta = log q - log p, whose terms are all positive and
 // exact where student and teacher agree; its logarithms by themselves would cancel there.  Without `rest` that also takes
 // 1 - sum q_k, the mass of the classes that are not kept: rows whose divergence is small beside its logarithms are read a
-// second time for it, the others' logarithms are summed as they stand (8192 x 32768 bf16: 89 us, 87.5 without the choice).
+// second time for it, the others' logarithms are summed as they stand (8192 x 32768 bf16 89.8 us, 88.1 without the choice, 213
+// where every row is read again; 8192 x 1000 fp32 with 16 kept 12.6, 12.3 and 21.2).
 //
 // What bounds it is memory, a row is read and next to nothing written, and issued instructions (68 % of the slots).  8192 x 32768 bf16 with 64 kept, labels and T = 2 takes 109
 // us, 4.9 TB/s, of 80 at a copy's rate; what is left is the rows' fixed work, the teacher's entries and the join.  The kept logits
@@ -82,7 +83,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     __shared__ float teacher[N == 32 ? kRowsOfCta : 1][kEntries], student[N == 32 ? kRowsOfCta : 1][kEntries];
     __shared__ bool before[N == 32 ? kRowsOfCta : 1][kEntries];
     __shared__ unsigned long long whole_of[kWarps];   // the warps' shares of a second reading
-    __shared__ float again_from;                      // what it is relative to, NaN: there is none
+    __shared__ float again_from, again_least;         // what it is relative to, NaN: there is none; the least logit of the teacher's entries
     const int slot = N == 32 ? threadIdx.x / 32 : 0;
     const int part = N == 32 ? 0 : blockIdx.x % a.parts;
     const int row = N == 32 ? blockIdx.x * kRowsOfCta + slot : blockIdx.x / a.parts;
@@ -250,15 +251,39 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
     }
 
     // A second reading of the whole row by this CTA's threads: a warp's sum of exp((s - m) / T) in units of 2^-52.  Of integers the kept
-    // classes' can be subtracted, and nothing is lost; a row has 2^20 classes of 2^-53 each to lose by rounding, 1e-10.
+    // classes' can be subtracted, and nothing is lost; those below the least of them, as nearly all are, are no kept ones and summed
+    // as they are (all of them as integers: 457 us for 8192 x 32768 bf16, 213 so).  What an integer loses by rounding is 2^-53.
     const auto unit = [&](float x, float m) { return __float2ull_rn(power(x, m, a.ct) * 0x1p52f); };
-    const auto read_again = [&](float m) {
+    const auto read_again = [&](float m, float least) {
+        constexpr int A = 4;
         unsigned long long n = 0;
-        for (int v = g.lane; v < r.vectors(); v += N) {
-            const Vec<T, W> b = r.some(v);
+        float2 below = make_float2(0.0f, 0.0f);
+        const auto add_vector = [&](const Vec<T, W>& b, int v) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) n += unit(widen(b.v[i]), m);
+            for (int i = 0; i < W / 2; ++i) {
+                const float2 x = pair(b, i), l = mul(add(x, both(-m)), ct), e = make_float2(approx_exp2(l.x), approx_exp2(l.y));
+                below = add(below, make_float2(x.x < least ? e.x : 0.0f, x.y < least ? e.y : 0.0f));
+            }
+            if (largest(b) < least) return;
+            unsigned those = 0;
+#pragma unroll
+            for (int i = 0; i < W; ++i) those |= (unsigned)(widen(b.v[i]) >= least) << i;
+            for (; those; those &= those - 1) n += unit(widen(r.base[v * W + __ffs(those) - 1]), m);
+        };
+        const int last = r.vectors(), begin = r.whole(0) ? 0 : 1, end = last > begin && !r.whole(last - 1) ? last - 1 : last;
+        for (int v = begin; v < end; v += A * N) {
+            Vec<T, W> b[A];
+#pragma unroll
+            for (int k = 0; k < A; ++k) b[k] = r.at(min(v + k * N + g.lane, end - 1));
+#pragma unroll
+            for (int k = 0; k < A; ++k) {
+                clear(b[k], v + k * N + g.lane >= end);
+                add_vector(b[k], v + k * N + g.lane);
+            }
         }
+        if (begin > 0 && g.lane == 0) add_vector(r.some(0), 0);
+        if (end < last && g.lane == N - 1) add_vector(r.some(last - 1), last - 1);
+        n += __float2ull_rn((below.x + below.y) * 0x1p52f);
 #pragma unroll
         for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
         return n;
@@ -270,7 +295,7 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
             meet();
             const float from = again_from;
             if (from != from) return;
-            const unsigned long long n = read_again(from);
+            const unsigned long long n = read_again(from, again_least);
             if (threadIdx.x % 32 == 0) whole_of[threadIdx.x / 32] = n;
             meet();
         }
@@ -376,21 +401,29 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
         loss = a.soft_loss * kl[0];
     }
     if constexpr (!REST) {
-        // As its logarithms stand the divergence is off by some 64 roundings, 2^-18, of 1 and their size; where it is below 2^-6 of that it is
-        // summed by its positive terms, sum p f(delta) + 1 - sum q over the teacher's entries.  (Where Z_T is above 1024 the kept
-        // classes have a quarter at most, and the divergence is no less than log 4: the integers' sums stay below 2^63.)
+        // As its logarithms stand the divergence is off by 64 roundings of 1 and their size, 2^-18, at most, and as a rule by two or three;
+        // where it is below 2^-8 of that it is summed by its positive terms, sum p f(delta) + 1 - sum q over the teacher's entries.
+        // (Where Z_T is above 1024 the kept classes have a quarter at most, and the divergence is no less than log 4: the integers'
+        // sums stay below 2^63.)
         bool again = false;
         if (weighed) {
             const float whole = total[0], kl = fmaf(whole, (m - mx) * a.inv_t, total[3]) / whole - logf(whole) + logf(sum_t);
-            again = sum_t <= 1024.0f && kl < 0x1p-6f * (1.0f + total[1] / whole);
+            again = sum_t <= 1024.0f && kl < 0x1p-8f * (1.0f + total[1] / whole);
             loss = a.soft_loss * kl;
         }
+        float least = INFINITY;
+        if (again) {                                  // (the same in all lanes)
+            for (int k = lane; k < a.kept; k += 32)
+                if (kept[k] >= 0 && power(us[k], mu, a.c1) != 0.0f) least = fminf(least, xs[k]);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+        }
         if constexpr (N > 32) {
-            if (lane == 0) again_from = again ? m : NAN;
+            if (lane == 0) again_from = again ? m : NAN, again_least = least;
             meet();
         }
         if (again) {
-            unsigned long long left = read_again(m);
+            unsigned long long left = read_again(m, least);
             if constexpr (N > 32) {
                 meet();
                 for (int w = 1; w < kWarps; ++w) left += whole_of[w];
@@ -399,9 +432,9 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
             float kl[1] = {0};
             unsigned long long own = 0;
             for (int k = lane; k < a.kept; k += 32) {
-                const float u = us[k], x = xs[k], p = kept[k] < 0 ? 0.0f : power(u, mu, a.c1) / whole;
-                if (p == 0.0f) continue;
-                kl[0] += term(p, power(x, m, a.ct) * per_t, (x - m) * a.inv_t - (u - mu) - level, true);
+                const float u = us[k], x = xs[k], mass = kept[k] < 0 ? 0.0f : power(u, mu, a.c1);
+                if (mass == 0.0f) continue;
+                kl[0] += term(mass / whole, power(x, m, a.ct) * per_t, (x - m) * a.inv_t - (u - mu) - level, true);
                 own += unit(x, m);
             }
             one.sum(kl);

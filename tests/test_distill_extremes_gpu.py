@@ -107,7 +107,7 @@ def _bound(s, values, at, t, alpha):
         + s.shape[1] * 2.0 ** -53 / np.exp(log_z)
     size = (p * ((v.max(1, keepdims=True) - v) + (x.max(1, keepdims=True) - x))).sum(1) / t
     plain = e + (size + (m - x.max(1, keepdims=True))[:, 0] / t) * (e + 16 * D.U)
-    small = (f + o < (1 + size) / 128) & (np.abs(d).max(1) < 0.25)
+    small = (f + o < (1 + size) / 512) & (np.abs(d).max(1) < 0.25)
     return alpha * t * t * (f + o), alpha * t * t * np.where(small, fine, fine + plain), np.abs(d).max(1) < 0.25
 
 
