@@ -402,7 +402,9 @@ typedef enum {
  *              the biases zeros), and a norm that is not there has none;
  *   h          DEVICE, dense, of `x_dtype`; may be x itself where that is dense, else must not overlap;
  *   y          DEVICE, dense, of `dtype`; may be block itself where that is dense, else must not overlap.
- * Sums are fp32, in a fixed order; C is at most 4096, and N * pixels below 2^31 - 2^24.  Pointers need element alignment only; vectors of eight channels
+ * Sums are fp32, in a fixed order; C is at most 4096, and N * pixels below 2^31 - 2^24.  The sum of a pixel's squares has to be in fp32's
+ * range.  With a NaN among a norm's values all of the pixel is NaN, and with an infinity in a layer norm's; in an RMS norm that value is
+ * normalised to NaN and the others to 0, as the formula has it.  Pointers need element alignment only; vectors of eight channels
  * on 16-byte boundaries are fastest.  Never synchronises.  Errors: PP_ERR_NULL, _SHAPE (sizes, strides), _ALIGN,
  * _DTYPE, _BUFFER (overlap), _ARG (kinds, eps, a parameter of a norm that is not there), _CUDA. */
 int pp_block_norm(const void* x, int64_t x_pixel, int64_t x_sample, int x_dtype, const void* block, int64_t block_pixel,
@@ -441,7 +443,8 @@ int pp_block_norm_workspace_size(int N, int64_t pixels, int C, size_t* bytes);
  *   values     DEVICE [rows][k] of `dtype`;   indices  DEVICE [rows][k];
  *   rest       DEVICE fp32 [rows]: the log-sum-exp of the other logits over `temperature`, -infinity where there are none
  *              (k == classes) or all are -infinity; NaN where one of them is.
- * 0.001 <= temperature <= 1000; logits over the temperature have to be in fp32's range.  At most 2^27 rows.  Pointers need
+ * 0.001 <= temperature <= 1000; logits over the temperature have to be in fp32's range.  `rest` is good for losses at the same temperature
+ * alone, which nothing checks.  At most 2^27 rows.  Pointers need
  * element alignment; rows that begin on 16-byte boundaries are fastest.
  * The same inputs and strides give the same bits.  Outputs overlap nothing.  Never synchronises.
  * Errors: PP_ERR_NULL, _SHAPE (classes above PP_MOST_CLASSES, k, stride), _ALIGN, _DTYPE, _BUFFER, _ARG, _CUDA. */
@@ -460,8 +463,8 @@ int pp_top_logits(const void* logits, int64_t stride, int dtype, int64_t rows, i
  *   stats      DEVICE fp32 [rows][5], for the backward pass: the largest logit m, the sum of exp(s - m) (0 without
  *              labels), the sum of exp((s - m) / T), and, of the classes that are not kept (without `rest`: of all), the
  *              largest logit and the sum of exp((s - it) / T).
- * A row that has neither a label nor a kept logit or rest above -infinity (a padded row) is not read: its loss and stats
- * are 0.  NaN and +infinity in a row that counts give NaN; a part of weight 0 (with alpha 0 the teacher's, with alpha 1 the
+ * Of a row that has neither a label nor a kept logit or rest above -infinity (a padded row) the values do not matter, although they may be
+ * read: its loss and stats are 0.  NaN and +infinity in a row that counts give NaN; a part of weight 0 (with alpha 0 the teacher's, with alpha 1 the
  * label's) takes no part in loss and gradient, whatever it holds.  0 <= alpha <= 1.  Otherwise as pp_top_logits. */
 int pp_distill(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t classes, const void* values,
                int value_type, const int* indices, int kept, const float* rest, const int64_t* labels, double temperature,

@@ -13,9 +13,11 @@
 //     dgate_n = scale joined_n,  dscale = sum_n gate_n joined_n,  dpost_weight = sum_n scale gate_n e,  dpost_bias with f,
 //     dweight = sum dz h^,  dbias = sum dz.
 //
-// Memory would bound it: four arrays forward, six backward; but for 20 to 60 operations a value the instructions that are
-// issued bound it as much.  Forward 32 x 256 x 56 x 56 fp16, layer norms, ReLU and a gate, takes 41 us, 5.0 TB/s, 0.73 of a
-// copy's rate; backward 32 x 128 x 112 x 112 125 us, 4.9 TB/s, 0.72.  Mean and root are not kept for the backward pass, which
+// Memory would bound it: four arrays forward, six backward.  What does is latency: a row's chain of readings, shuffles and 20 to 60
+// operations a value, each of which waits for the one before, at the 24 (forward) and 16 (backward) warps of an SM that the
+// registers allow; 52 to 55 % of the issue slots are used, and no single wait stands out.  Forward 32 x 256 x 56 x 56 fp16, layer
+// norms, ReLU and a gate, takes 41 us, 5.1 TB/s, 0.75 of a copy's rate; backward 32 x 128 x 112 x 112 124 us, 5.0 TB/s, 0.73; RMS
+// norms 41 and 109, of fp32 backward 204 (0.89).  (GPU time, calls one after another in one graph.)  Mean and root are not kept for the backward pass, which
 // has h and b in registers anyway.  A CTA takes a stretch of consecutive pixels (the gate is read when the sample changes,
 // not with each row) and in the backward pass keeps its channels' sums in registers; the CTAs' sums are joined by a second
 // launch, in order, which is started before the first one's end (norm_starts_early).  By loads that are waited for, with any

@@ -22,8 +22,8 @@ constexpr int E = kBlockEight;
 // Forms of the kernels.  kLong: a CTA has one row, of whole warps.  kShort: several rows, of a power of two of threads each.
 // 1 to 32: the same with so many threads, known beforehand.  KIND kStrided: any strides; kDense: one offset for all tensors; kRms and
 // kLayer: dense, both norms of this kind and all inputs there.  With loops that unroll, one 32-bit offset for all tensors and no
-// choices left a row takes half the instructions, which bound the kernels before memory does (32 x 256 x 56 x 56 forward: 58 us to
-// 44 with known forms and the parameters in shared memory).
+// choices left a row takes half the instructions, and its chain of dependent ones, which bounds the kernels, is shorter (32 x 256 x
+// 56 x 56 forward: 58 us to 44 with known forms and the parameters in shared memory).
 enum { kLong = -1, kShort = 0 };
 enum { kStrided = 0, kRms = PP_NORM_RMS, kLayer = PP_NORM_LAYER, kDense = 3 };
 

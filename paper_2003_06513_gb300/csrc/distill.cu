@@ -17,8 +17,8 @@
 // second time for it, the others' logarithms are summed as they stand (8192 x 32768 bf16 89.8 us, 88.1 without the choice, 213
 // where every row is read again; 8192 x 1000 fp32 with 16 kept 12.6, 12.3 and 21.2).
 //
-// What bounds it is memory, a row is read and next to nothing written, and issued instructions (68 % of the slots).  8192 x 32768 bf16 with 64 kept, labels and T = 2 takes 109
-// us, 4.9 TB/s, of 80 at a copy's rate; what is left is the rows' fixed work, the teacher's entries and the join.  The kept logits
+// What bounds it is memory, a row is read and next to nothing written, and issued instructions (69 % of the slots).  8192 x 32768 bf16 with 64 kept, labels and T = 2 takes 107
+// us, 5.0 TB/s, of 80 at a copy's rate (GPU time, calls one after another in one graph); what is left is the rows' fixed work, the teacher's entries and the join.  The kept logits
 // gathered before the row took 118 us; without the exponential's square, the prefetch and the batches a thread has under way 153.
 #include <cooperative_groups.h>
 
@@ -401,8 +401,8 @@ __global__ void __launch_bounds__(N == 32 ? 32 * kRowsOfCta : N, N == 32 ? 6 : 8
         loss = a.soft_loss * kl[0];
     }
     if constexpr (!REST) {
-        // As its logarithms stand the divergence is off by 64 roundings of 1 and their size, 2^-18, at most, and as a rule by two or three;
-        // where it is below 2^-8 of that it is summed by its positive terms, sum p f(delta) + 1 - sum q over the teacher's entries.
+        // As its logarithms stand the divergence is off by two or three roundings of 1 and their size as a rule; where it is below 2^-8 of
+        // that it is summed by its positive terms, sum p f(delta) + 1 - sum q over the teacher's entries.
         // (Where Z_T is above 1024 the kept classes have a quarter at most, and the divergence is no less than log 4: the integers'
         // sums stay below 2^63.)
         bool again = false;

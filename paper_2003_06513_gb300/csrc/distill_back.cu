@@ -6,8 +6,8 @@
 // and without them q_v.  So every value is two exponentials times two numbers of the row; the kept classes and the
 // label, which have a term of their own, are written again after their CTA's others, at a barrier.
 //
-// What bounds it is memory: a row is read and one of the same size written.  8192 x 65536 bf16 with 64 kept takes 335 us, 6.4 TB/s,
-// 0.95 of a copy's rate; 512 x 1000 fp32 with 16 kept 4.7 us.
+// What bounds it is memory: a row is read and one of the same size written.  8192 x 65536 bf16 with 64 kept takes 334 us, 6.4 TB/s,
+// 0.95 of a copy's rate; 512 x 1000 fp32 with 16 kept 4.5 us (GPU time, calls one after another in one graph).
 #include <algorithm>
 
 #include "rows.cuh"

@@ -13,8 +13,8 @@
 // most 20 countings, which any row ends after.
 //
 // What bounds it: of many rows the two readings and the exponentials, about five instructions a value, beside memory; of few the
-// chain of barriers.  4096 x 32768 bf16 with 64 kept takes 80 us, 3.4 TB/s of the 268 MB that have to be read (40 us at a copy's
-// rate), 256 x 1000 fp32 5.7 us, 6 x 200001 fp32 10.  Rows of 64 KB held in shared memory, one reading but fewer rows under way, took
+// chain of barriers.  4096 x 32768 bf16 with 64 kept takes 79 us, 3.4 TB/s of the 268 MB that have to be read (40 us at a copy's
+// rate), 256 x 1000 fp32 with 16 kept 5.7 us, 6 x 200001 fp32 with 200 kept 12.4 (GPU time, calls one after another in one graph).  Rows of 64 KB held in shared memory, one reading but fewer rows under way, took
 // 114 us where this took 94.
 #include <cooperative_groups.h>
 

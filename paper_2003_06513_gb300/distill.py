@@ -24,7 +24,9 @@ MOST_KEPT, MOST_CLASSES = 256, 1 << 20
 
 class TopLogits(NamedTuple):
     """What is kept of a teacher's rows: ``values`` [rows, k] in order, ``indices`` int32 [rows, k], and ``rest`` float32
-    [rows], the log-sum-exp of the other logits over the temperature (None: the others are left out of the loss)."""
+    [rows], the log-sum-exp of the other logits over the temperature (None: the others are left out of the loss).  ``rest`` is at the
+    temperature that ``pp_top_logits`` was called with, which is not held here: a loss at another one is silently another loss.
+    Whoever stores top logits stores their temperature too."""
     values: torch.Tensor
     indices: torch.Tensor
     rest: Optional[torch.Tensor]
@@ -47,7 +49,8 @@ def pp_distill(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor
 
     ``rest``     None: the teacher's probabilities are of the kept classes alone; else the others are one more class;
     ``labels``   int64 [rows], one outside the classes (-100) leaves a row to the teacher; None: no label's part.
-    An index outside the classes (-1) is an empty place; a row with neither labels nor kept logits has loss 0."""
+    An index outside the classes (-1) is an empty place; a row with neither labels nor kept logits has loss 0, whatever its logits are.  With
+    alpha 0 the teacher, with 1 the label takes no part, whatever it holds."""
     return _done("pp_distill", _lib.binding().distill(logits, values, indices, rest, labels, temperature, alpha, _handle(stream)))
 
 

@@ -121,7 +121,8 @@ class Retrainer:
     def step(self, x: torch.Tensor, labels: Optional[torch.Tensor],
              top: Optional[distill.TopLogits] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """One step on a batch: (loss, norm of the gradients before clipping), on the device.  ``top``: a teacher's top logits for
-        it, at the net's temperature; with them ``labels`` may be None, or hold -100 where there is none."""
+        it, selected at the net's ``temperature`` (nothing checks that); with them ``labels`` may be None, or hold -100 where there is
+        none.  The loss is the mean over all rows with a teacher, and over those that have a label (cross entropy's mean) without."""
         if top is None:
             loss = F.cross_entropy(self.logits(x), labels)
         else:
